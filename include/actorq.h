@@ -390,6 +390,91 @@ aq_status aq_convert_params_fp16(aq_policy* p, const float* const* h_d_w, const 
 aq_status aq_policy_forward_fp16(aq_policy* p, const void* d_obs, int64_t batch, void* d_actions,
                                  void* const* taps_out, void* stream);
 
+/* ---- The learner's operators: the layers of the policy that the actors run, while it trains.  LayerNorm with its
+ * gradients; activations kept in 8 bits between the forward and the backward pass (checkpoints) and the gradients that
+ * read them; fully connected layers whose products run on microscaled 4-bit floats, for training and for serving.
+ * None of them needs a handle, allocates or waits: scratch is the caller's (d_workspace, of the size that the matching
+ * *_workspace call gives; it may be used again behind the call on the same stream, needs no particular contents, and
+ * calls in flight at once need one each), so all may be captured into graphs.  Results do not depend on timing: sums
+ * are formed in a fixed order, in fp32.
+ *
+ * Matrices are row-major, with rows that start `ld` elements apart (ld >= cols) at any multiple of the element's size.
+ * A value is fp32, binary16 or bfloat16; what a call computes is formed in fp32 and rounded once, to nearest even.
+ * Vectors (gains, offsets, biases, statistics and their gradients) are fp32 and contiguous.  An operand without rows
+ * has no effect, and gradients over no rows are zeros.  Outputs overlap neither inputs nor each other.
+ * AQ_EINVAL: a NULL argument that is not said to be optional, a negative size, ld < cols, an unknown type, an
+ * address that is no multiple of its element's size, a workspace that is too small.  AQ_ESHAPE: operands
+ * whose sizes or types do not go together, or beyond a call's limits; rows are below 2^31 everywhere. */
+typedef enum { AQ_F32 = 0, AQ_F16 = 1, AQ_BF16 = 2 } aq_dtype;
+typedef struct {
+    void* d;
+    int64_t rows, cols, ld;
+    int32_t dtype; /* aq_dtype */
+} aq_matrix;
+
+/* Blocks of 32 values along a row share one scale byte (the last block of a row may be short; its codes are padded
+ * with zeros).  B = ceil(cols / 32): d_scales is uint8 [rows][B] (any address), d_codes is 16-byte aligned.
+ *   aq_ckpt8: d_codes int8 [rows][32 B]; value = code * 2^(scale - 133).  scale = the biased fp32 exponent of the
+ *     block's largest magnitude, codes round to nearest even and stay within [-127, 127]: the error is at most half a
+ *     step (one step for the codes that saturate), 2^-7 (2^-6) of that power of two.
+ *   aq_mx4: d_codes uint8 [rows][16 B], two codes a byte, the even value in the low half; a code is a sign, two exponent
+ *     bits and one mantissa bit (0, .5, 1, 1.5, 2, 3, 4, 6), value = element * 2^(scale - 127).  scale = max(0, the
+ *     biased exponent of the block's largest magnitude - 2); elements round to nearest even and saturate at 6.  (The
+ *     OCP microscaling formats' E2M1 with E8M0 scales, and their conversion.)
+ * A block that holds a NaN or an infinity has scale 255 and stands for NaNs: nothing of it is lost silently. */
+typedef struct {
+    void* d_codes;
+    uint8_t* d_scales;
+    int64_t rows, cols;
+} aq_ckpt8;
+typedef struct {
+    void* d_codes;
+    uint8_t* d_scales;
+    int64_t rows, cols;
+} aq_mx4;
+
+/* LayerNorm over rows of 1 .. AQ_LAYERNORM_MAX_COLS values: y = (x - mean) * rstd * gamma + beta, mean and biased
+ * variance of the row, rstd = 1 / sqrt(variance + eps).  x and y have one type.  d_gamma and d_beta may be NULL (1 and
+ * 0).  d_mean and d_rstd (fp32 [rows], for the backward pass) may be NULL.  `kept` (may be NULL) receives the
+ * checkpoint of x in the same pass over it.
+ *
+ * The backward pass, with g = dy * gamma and h = (x - mean) * rstd:
+ *   dx = rstd * (g - mean_of_row(g) - h * mean_of_row(g * h)),  dgamma = sum over rows of dy * h,  dbeta = of dy.
+ * Of x and kept exactly one is given: the input itself or its checkpoint, with mean and rstd as the forward pass left
+ * them.  dy, dx and x have one type.  dgamma and dbeta may be NULL. */
+#define AQ_LAYERNORM_MAX_COLS 16384
+aq_status aq_layernorm_forward(const aq_matrix* x, const float* d_gamma, const float* d_beta, float eps,
+                               const aq_matrix* y, float* d_mean, float* d_rstd, const aq_ckpt8* kept, void* stream);
+aq_status aq_layernorm_backward_workspace(int64_t rows, int64_t cols, uint64_t* bytes);
+aq_status aq_layernorm_backward(const aq_matrix* dy, const aq_matrix* x, const aq_ckpt8* kept, const float* d_gamma,
+                                const float* d_mean, const float* d_rstd, const aq_matrix* dx, float* d_dgamma,
+                                float* d_dbeta, void* d_workspace, uint64_t workspace_bytes, void* stream);
+
+/* Checkpoints of activations, and what they stand for. */
+aq_status aq_ckpt8_pack(const aq_matrix* x, const aq_ckpt8* kept, void* stream);
+aq_status aq_ckpt8_unpack(const aq_ckpt8* kept, const aq_matrix* x, void* stream);
+/* The gradients of a fully connected layer y = x W^T + b from its checkpointed input: dw[n][k] = sum over rows of
+ * dy[row][n] * x[row][k] (fp32, n = dy's columns, k = kept's), d_db[n] = sum over rows of dy[row][n] (may be NULL).
+ * The products are exact and their sums are fp32, whatever dy's type.  At most 2^20 columns each. */
+aq_status aq_ckpt8_weight_grad_workspace(int64_t rows, int64_t n, int64_t k, uint64_t* bytes);
+aq_status aq_ckpt8_weight_grad(const aq_matrix* dy, const aq_ckpt8* kept, const aq_matrix* dw, float* d_db,
+                               void* d_workspace, uint64_t workspace_bytes, void* stream);
+
+/* Microscaled 4-bit tensors, and what they stand for. */
+aq_status aq_mx4_quantize(const aq_matrix* x, const aq_mx4* q, void* stream);
+aq_status aq_mx4_dequantize(const aq_mx4* q, const aq_matrix* x, void* stream);
+/* A fully connected layer in 4 bits: y = Q(x) w^T + bias, Q the conversion above (w: n rows of k values; bias fp32 [n],
+ * may be NULL).  The products are those of the 4-bit values, exact, and their sums are fp32.  x and y have
+ * one type.  aq_mx4_matmul takes an input that is quantized already and any type of y.  At most 2^20 columns each. */
+aq_status aq_mx4_linear_workspace(int64_t rows, int64_t n, int64_t k, uint64_t* bytes);
+aq_status aq_mx4_linear(const aq_matrix* x, const aq_mx4* w, const float* d_bias, const aq_matrix* y,
+                        void* d_workspace, uint64_t workspace_bytes, void* stream);
+aq_status aq_mx4_matmul(const aq_mx4* x, const aq_mx4* w, const float* d_bias, const aq_matrix* y, void* stream);
+/* Its gradient with respect to the input, the conversion taken for the identity: dx = dy w, dy and dx of one type. */
+aq_status aq_mx4_input_grad_workspace(int64_t rows, int64_t n, int64_t k, uint64_t* bytes);
+aq_status aq_mx4_input_grad(const aq_matrix* dy, const aq_mx4* w, const aq_matrix* dx, void* d_workspace,
+                            uint64_t workspace_bytes, void* stream);
+
 const char* aq_status_string(aq_status s);
 
 #ifdef __cplusplus

@@ -29,7 +29,10 @@ EXPORTS = ["aq_policy_create", "aq_policy_destroy", "aq_policy_reserve", "aq_pol
            "aq_policy_packed_blob_size", "aq_policy_export_packed_blob", "aq_policy_import_packed_blob",
            "aq_policy_conv_stack_layers", "aq_policy_fp16_conv_stack_layers", "aq_policy_fused_plan", "aq_policy_forward_int8_static",
            "aq_policy_set_params_fp32", "aq_calibrate_fp32", "aq_policy_forward_fp32_params", "aq_stream_reference",
-           "aq_mfma_loop_reference", "aq_policy_subbyte_layers", "aq_policy_fp32_plan", "aq_policy_fp16_plan"]
+           "aq_mfma_loop_reference", "aq_policy_subbyte_layers", "aq_policy_fp32_plan", "aq_policy_fp16_plan",
+           "aq_layernorm_forward", "aq_layernorm_backward", "aq_layernorm_backward_workspace", "aq_ckpt8_pack", "aq_ckpt8_unpack",
+           "aq_ckpt8_weight_grad", "aq_ckpt8_weight_grad_workspace", "aq_mx4_quantize", "aq_mx4_dequantize", "aq_mx4_linear",
+           "aq_mx4_linear_workspace", "aq_mx4_matmul", "aq_mx4_input_grad", "aq_mx4_input_grad_workspace"]
 
 
 class AqLayer(C.Structure):
@@ -55,6 +58,15 @@ class AqExplore(C.Structure):
 class AqTaps(C.Structure):
     _fields_ = [("acc", C.POINTER(C.c_void_p)), ("act", C.POINTER(C.c_void_p)), ("ln_t", C.POINTER(C.c_void_p)),
                 ("a0", C.c_void_p), ("y", C.c_void_p)]
+
+
+class AqMatrix(C.Structure):
+    _fields_ = [("d", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("dtype", C.c_int32)]
+
+
+class AqBlocks(C.Structure):
+    """aq_ckpt8 and aq_mx4, which are laid out alike."""
+    _fields_ = [("d_codes", C.c_void_p), ("d_scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64)]
 
 
 class AqError(RuntimeError):
@@ -112,6 +124,18 @@ def load():
     lib.aq_policy_import_packed_blob.argtypes = [vp, vp, C.c_uint64, vp]
     lib.aq_convert_params_fp16.argtypes = [vp, pp, pp, pp, pp, vp]
     lib.aq_policy_forward_fp16.argtypes = [vp, vp, i64, vp, pp, vp]
+    mat, blk, u64, f32 = C.POINTER(AqMatrix), C.POINTER(AqBlocks), C.c_uint64, C.c_float
+    lib.aq_layernorm_forward.argtypes = [mat, vp, vp, f32, mat, vp, vp, blk, vp]
+    lib.aq_layernorm_backward.argtypes = [mat, mat, blk, vp, vp, vp, mat, vp, vp, vp, u64, vp]
+    lib.aq_layernorm_backward_workspace.argtypes = [i64, i64, C.POINTER(u64)]
+    lib.aq_ckpt8_pack.argtypes = lib.aq_mx4_quantize.argtypes = [mat, blk, vp]
+    lib.aq_ckpt8_unpack.argtypes = lib.aq_mx4_dequantize.argtypes = [blk, mat, vp]
+    lib.aq_ckpt8_weight_grad.argtypes = [mat, blk, mat, vp, vp, u64, vp]
+    lib.aq_mx4_linear.argtypes = [mat, blk, vp, mat, vp, u64, vp]
+    lib.aq_mx4_matmul.argtypes = [blk, blk, vp, mat, vp]
+    lib.aq_mx4_input_grad.argtypes = [mat, blk, mat, vp, u64, vp]
+    for name in ("aq_ckpt8_weight_grad_workspace", "aq_mx4_linear_workspace", "aq_mx4_input_grad_workspace"):
+        getattr(lib, name).argtypes = [i64, i64, i64, C.POINTER(u64)]
     for name in EXPORTS:
         fn = getattr(lib, name)
         # (addresses travel as plain integers, which ctypes cuts to 32 bits where no argument types are declared)
@@ -382,3 +406,157 @@ def mfma_loop_reference(weights, acts, ksteps, stream_weights, workgroups, acc):
 def quantize_tensor(w, rows, cols, wscheme, qdenom, codes, scale, zp, workspace):
     _check(load().aq_quantize_tensor(_ptr(w), int(rows), int(cols), WSCHEME[wscheme], int(qdenom), _ptr(codes),
                                      _ptr(scale), _ptr(zp), _ptr(workspace), _stream()), "aq_quantize_tensor")
+
+
+# ---- the learner's operators.  Matrices are two-dimensional device tensors whose rows are contiguous (any distance between rows);
+# vectors are contiguous fp32 tensors; `workspace` is a uint8 tensor of the size that the matching *_workspace call gives (None for 0).
+
+_DTYPES = {}
+
+
+def _matrix(t):
+    """A tensor as an aq_matrix; None stays None."""
+    if t is None:
+        return None
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    if t.dim() != 2 or t.dtype not in _DTYPES:
+        raise ValueError("a matrix is a two-dimensional tensor of float32, float16 or bfloat16")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("the values of a row are contiguous")
+    return AqMatrix(t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols, _DTYPES[t.dtype])
+
+
+def _vector(t, n, what):
+    """A contiguous fp32 vector of n values as a pointer; None stays None."""
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} is a contiguous float32 tensor of {n} values")
+    return t.data_ptr()
+
+
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+class _Blocks:
+    """Codes and scales of a [rows][cols] tensor in blocks of 32 values along a row."""
+    CODE_BYTES = 0  # of a block
+
+    def __init__(self, codes, scales, cols):
+        import torch
+        rows, blocks = scales.shape
+        if blocks != (cols + 31) // 32 or tuple(codes.shape) != (rows, self.CODE_BYTES * blocks):
+            raise ValueError(f"codes are [rows][{self.CODE_BYTES} B] and scales [rows][B], B = ceil(cols / 32)")
+        if scales.dtype != torch.uint8 or codes.element_size() != 1 or not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("codes and scales are contiguous tensors of bytes")
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, int(cols)
+        self._c = AqBlocks(codes.data_ptr(), scales.data_ptr(), rows, int(cols))
+
+
+class Ckpt8(_Blocks):
+    """An 8-bit checkpoint (aq_ckpt8): codes int8 [rows][32 B], scales uint8 [rows][B], B = ceil(cols / 32)."""
+    CODE_BYTES = 32
+
+
+class Mx4(_Blocks):
+    """A microscaled 4-bit tensor (aq_mx4): codes uint8 [rows][16 B], scales uint8 [rows][B], B = ceil(cols / 32)."""
+    CODE_BYTES = 16
+
+
+def _blocks_empty(kind, code_type, rows, cols, device):
+    import torch
+    b = (int(cols) + 31) // 32
+    return kind(torch.empty(int(rows), kind.CODE_BYTES * b, dtype=code_type, device=device),
+                torch.empty(int(rows), b, dtype=torch.uint8, device=device), cols)
+
+
+def ckpt8_empty(rows, cols, device="cuda:0"):
+    import torch
+    return _blocks_empty(Ckpt8, torch.int8, rows, cols, device)
+
+
+def mx4_empty(rows, cols, device="cuda:0"):
+    import torch
+    return _blocks_empty(Mx4, torch.uint8, rows, cols, device)
+
+
+def _size(fn, *sizes):
+    n = C.c_uint64(0)
+    _check(getattr(load(), fn)(*[int(v) for v in sizes], C.byref(n)), fn)
+    return int(n.value)
+
+
+def layernorm_backward_workspace(rows, cols):
+    return _size("aq_layernorm_backward_workspace", rows, cols)
+
+
+def ckpt8_weight_grad_workspace(rows, n, k):
+    return _size("aq_ckpt8_weight_grad_workspace", rows, n, k)
+
+
+def mx4_linear_workspace(rows, n, k):
+    return _size("aq_mx4_linear_workspace", rows, n, k)
+
+
+def mx4_input_grad_workspace(rows, n, k):
+    return _size("aq_mx4_input_grad_workspace", rows, n, k)
+
+
+def layernorm_forward(x, gamma, beta, eps, y, mean=None, rstd=None, kept=None):
+    """y = LayerNorm(x); kept: a Ckpt8 that receives x."""
+    rows, cols = x.shape
+    _check(load().aq_layernorm_forward(_matrix(x), _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), float(eps), _matrix(y),
+                                       _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), kept and kept._c, _stream()),
+           "aq_layernorm_forward")
+
+
+def layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace=None):
+    """x: the forward pass's input, or its Ckpt8."""
+    rows, cols = dy.shape
+    kept = x if isinstance(x, Ckpt8) else None
+    _check(load().aq_layernorm_backward(_matrix(dy), None if kept else _matrix(x), kept and kept._c, _vector(gamma, cols, "gamma"),
+                                        _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), _matrix(dx),
+                                        _vector(dgamma, cols, "dgamma"), _vector(dbeta, cols, "dbeta"), _ptr(workspace),
+                                        _bytes(workspace), _stream()), "aq_layernorm_backward")
+
+
+def ckpt8_pack(x, kept):
+    _check(load().aq_ckpt8_pack(_matrix(x), kept._c, _stream()), "aq_ckpt8_pack")
+
+
+def ckpt8_unpack(kept, x):
+    _check(load().aq_ckpt8_unpack(kept._c, _matrix(x), _stream()), "aq_ckpt8_unpack")
+
+
+def ckpt8_weight_grad(dy, kept, dw, db=None, workspace=None):
+    _check(load().aq_ckpt8_weight_grad(_matrix(dy), kept._c, _matrix(dw), _vector(db, dy.shape[1], "db"), _ptr(workspace),
+                                       _bytes(workspace), _stream()), "aq_ckpt8_weight_grad")
+
+
+def mx4_quantize(x, q):
+    _check(load().aq_mx4_quantize(_matrix(x), q._c, _stream()), "aq_mx4_quantize")
+
+
+def mx4_dequantize(q, x):
+    _check(load().aq_mx4_dequantize(q._c, _matrix(x), _stream()), "aq_mx4_dequantize")
+
+
+def mx4_linear(x, w, bias, y, workspace=None):
+    """y = Q(x) w^T + bias; w: Mx4 [n][k]."""
+    _check(load().aq_mx4_linear(_matrix(x), w._c, _vector(bias, w.rows, "bias"), _matrix(y), _ptr(workspace), _bytes(workspace), _stream()),
+           "aq_mx4_linear")
+
+
+def mx4_matmul(x, w, bias, y):
+    """The same from an Mx4 x."""
+    _check(load().aq_mx4_matmul(x._c, w._c, _vector(bias, w.rows, "bias"), _matrix(y), _stream()), "aq_mx4_matmul")
+
+
+def mx4_input_grad(dy, w, dx, workspace=None):
+    """dx = dy w; w: Mx4 [n][k]."""
+    _check(load().aq_mx4_input_grad(_matrix(dy), w._c, _matrix(dx), _ptr(workspace), _bytes(workspace), _stream()), "aq_mx4_input_grad")

@@ -1,0 +1,124 @@
+// The two block formats to and from rows of values: 8-bit checkpoints and microscaled 4-bit floats.
+//
+// Bound by memory.  A thread holds eight values, four neighbouring threads a block, whose largest magnitude they find by two
+// exchanges within their quad; L = 4 .. 64 threads walk along a row (few, so that short rows share a wavefront), a workgroup
+// takes 256 / L rows at a time.
+#include "learner.hpp"
+#include "learner_device.hpp"
+
+namespace aq {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct Ckpt8 {
+    static constexpr int kBytes = 8;  // of codes to a piece of eight values
+    static __device__ __forceinline__ void pack(const float (&v)[8], uint8_t* codes, uint32_t& scale) {
+        scale = ckpt8_scale(most_of4lanes(most_of8(v)));
+        *(v2u*)codes = ckpt8_codes(v, scale);
+    }
+    static __device__ __forceinline__ void unpack(const uint8_t* codes, uint32_t scale, float (&v)[8]) {
+        ckpt8_values(*(const v2u*)codes, ckpt8_step(scale), v);
+    }
+};
+struct Mx4 {
+    static constexpr int kBytes = 4;
+    static __device__ __forceinline__ void pack(const float (&v)[8], uint8_t* codes, uint32_t& scale) {
+        scale = mx4_scale(most_of4lanes(most_of8(v)));
+        *(uint32_t*)codes = mx4_codes(v, scale);
+    }
+    static __device__ __forceinline__ void unpack(const uint8_t* codes, uint32_t scale, float (&v)[8]) {
+        const uint32_t c = *(const uint32_t*)codes;
+        const float s = mx4_step(scale);
+        v2f32 q[4];
+        q[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0);
+        q[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
+        q[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2);
+        q[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = q[j / 2][j & 1];
+    }
+};
+
+template <class Format, class T, int L>
+__global__ void __launch_bounds__(kThreads)
+    k_to_blocks(const T* __restrict__ x, int64_t ld, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int rows, int cols, int blocks) {
+    const int piece = blockIdx.x * L + threadIdx.x % L;
+    if (piece >= 4 * blocks) return;  // (whole quads)
+    const int64_t step = (int64_t)gridDim.y * (kThreads / L);
+    for (int64_t row = (int64_t)blockIdx.y * (kThreads / L) + threadIdx.x / L; row < rows; row += step) {
+        Piece<T> in;
+        in.load(x + row * ld + 8 * (int64_t)piece, cols - 8 * piece);
+        float v[8];
+        in.get(v);
+        uint32_t scale;
+        Format::pack(v, codes + (row * blocks * 4 + piece) * Format::kBytes, scale);
+        if ((threadIdx.x & 3) == 0) scales[row * blocks + (piece >> 2)] = (uint8_t)scale;
+    }
+}
+
+template <class Format, class T, int L>
+__global__ void __launch_bounds__(kThreads)
+    k_from_blocks(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, int64_t ld, int rows, int cols,
+                  int blocks) {
+    const int piece = blockIdx.x * L + threadIdx.x % L;
+    if (8 * (int64_t)piece >= cols) return;
+    const int64_t step = (int64_t)gridDim.y * (kThreads / L);
+    for (int64_t row = (int64_t)blockIdx.y * (kThreads / L) + threadIdx.x / L; row < rows; row += step) {
+        float v[8];
+        Format::unpack(codes + (row * blocks * 4 + piece) * Format::kBytes, scales[row * blocks + (piece >> 2)], v);
+        Piece<T> out;
+        out.set(v);
+        out.store(x + row * ld + 8 * (int64_t)piece, cols - 8 * piece);
+    }
+}
+
+template <class Go>
+aq_status by_width(int64_t rows, int64_t cols, Go&& go) {
+    const int64_t pieces = 4 * blocks32(cols);
+    auto with = [&](auto l) {
+        constexpr int L = decltype(l)::value;
+        const int64_t y = (rows + kThreads / L - 1) / (kThreads / L);
+        go(l, dim3((unsigned)((pieces + L - 1) / L), (unsigned)(y < 65535 ? y : 65535)));
+        return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+    };
+    if (pieces <= 4) return with(std::integral_constant<int, 4>());
+    if (pieces <= 8) return with(std::integral_constant<int, 8>());
+    if (pieces <= 16) return with(std::integral_constant<int, 16>());
+    if (pieces <= 32) return with(std::integral_constant<int, 32>());
+    return with(std::integral_constant<int, 64>());
+}
+
+template <class Format>
+aq_status to_blocks(const aq_matrix& x, void* codes, uint8_t* scales, hipStream_t st) {
+    return with_dtype(x.dtype, [&](auto t) {
+        using T = decltype(t);
+        return by_width(x.rows, x.cols, [&](auto l, dim3 grid) {
+            k_to_blocks<Format, T, decltype(l)::value><<<grid, kThreads, 0, st>>>((const T*)x.d, x.ld, (uint8_t*)codes, scales, (int)x.rows,
+                                                                                (int)x.cols, (int)blocks32(x.cols));
+        });
+    });
+}
+template <class Format>
+aq_status from_blocks(const void* codes, const uint8_t* scales, const aq_matrix& x, hipStream_t st) {
+    return with_dtype(x.dtype, [&](auto t) {
+        using T = decltype(t);
+        return by_width(x.rows, x.cols, [&](auto l, dim3 grid) {
+            k_from_blocks<Format, T, decltype(l)::value><<<grid, kThreads, 0, st>>>((const uint8_t*)codes, scales, (T*)x.d, x.ld, (int)x.rows,
+                                                                                  (int)x.cols, (int)blocks32(x.cols));
+        });
+    });
+}
+
+}  // namespace
+
+aq_status launch_ckpt8_pack(const aq_matrix& x, const aq_ckpt8& kept, hipStream_t st) {
+    return to_blocks<Ckpt8>(x, kept.d_codes, kept.d_scales, st);
+}
+aq_status launch_ckpt8_unpack(const aq_ckpt8& kept, const aq_matrix& x, hipStream_t st) {
+    return from_blocks<Ckpt8>(kept.d_codes, kept.d_scales, x, st);
+}
+aq_status launch_mx4_quantize(const aq_matrix& x, const aq_mx4& q, hipStream_t st) { return to_blocks<Mx4>(x, q.d_codes, q.d_scales, st); }
+aq_status launch_mx4_dequantize(const aq_mx4& q, const aq_matrix& x, hipStream_t st) { return from_blocks<Mx4>(q.d_codes, q.d_scales, x, st); }
+
+}  // namespace aq

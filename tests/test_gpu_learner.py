@@ -1,0 +1,520 @@
+"""The learner's operators against their definitions in 64 bits: LayerNorm and its gradients, 8-bit checkpoints and the weight
+gradients that read them, microscaled 4-bit tensors, their products and the gradient through them.
+
+Tolerances: U is the rounding of an fp32 operation (2^-24) and OUT that of the output's type.  A sum of n terms is off by at most
+n U times the sum of their magnitudes, in any order; what each test allows is that for the sums it makes.  Quantized values are exact."""
+import math
+import zlib
+
+import pytest
+import torch
+
+from paper_1910_01055_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+OUT = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -133}  # half a step of the smallest values
+SENTINEL = 77.0
+
+
+class Framed:
+    """A [rows][cols] matrix on the GPU whose rows lie `gap` apart and start at element `first`, in a buffer that holds SENTINEL elsewhere."""
+
+    def __init__(self, rows, cols, dtype, gap=0, first=0, values=None):
+        ld = cols + gap
+        self.buf = torch.full((first + rows * ld + 64,), SENTINEL, dtype=dtype, device=DEV)
+        self.m = self.buf[first:first + rows * ld].view(rows, ld)[:, :cols] if rows else self.buf[:0].view(0, cols)
+        self.inside = torch.zeros_like(self.buf, dtype=torch.bool)
+        if rows:
+            self.inside[first:first + rows * ld].view(rows, ld)[:, :cols] = True
+        if values is not None:
+            self.m.copy_(values)
+
+    def get(self):
+        torch.cuda.synchronize()
+        assert bool((self.buf[~self.inside] == SENTINEL).all()), "values outside of the matrix were written"
+        return self.m.cpu().double()
+
+
+def rng(*key):
+    return torch.Generator().manual_seed(zlib.crc32(repr(key).encode()))
+
+
+def normal(g, *shape):
+    return torch.randn(shape, generator=g)
+
+
+def near(got, want, bound):
+    """Each value within its bound; NaNs and infinities in the same places."""
+    assert got.shape == want.shape
+    odd = ~torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(got[odd & ~torch.isnan(want)], want[odd & ~torch.isnan(want)])
+    far = ((got - want).abs() - bound)[~odd]
+    assert far.numel() == 0 or float(far.max()) <= 0.0, f"off by {float(far.max())} more than allowed"
+
+
+# ---- definitions
+
+def blocks_of(x):
+    """x (fp64) in blocks of 32 and the power of two at or below each block's largest magnitude (2^-127 at least)."""
+    rows, cols = x.shape
+    b = (cols + 31) // 32
+    p = torch.zeros(rows, 32 * b, dtype=torch.float64)
+    p[:, :cols] = x
+    p = p.view(rows, b, 32)
+    most = p.abs().amax(2)
+    bad = ~torch.isfinite(most)
+    e = torch.frexp(torch.where(bad, torch.ones_like(most), most))[1].double() - 1
+    e = torch.where(most > 0, e, torch.full_like(e, -127.0)).clamp(min=-127.0)
+    return p, e, bad
+
+
+def ckpt8_ref(x):
+    p, e, bad = blocks_of(x)
+    code = torch.clamp(torch.round(p * torch.exp2(6 - e)[:, :, None]), -127, 127)
+    value = code * torch.exp2(e - 6)[:, :, None]
+    value[bad] = math.nan
+    scale = torch.where(bad, torch.full_like(e, 255), e + 127)
+    return code, scale, bad, value.view(x.shape[0], -1)[:, :x.shape[1]]
+
+
+def mx4_ref(x):
+    p, e, bad = blocks_of(x)
+    e = (e - 2).clamp(min=-127.0)
+    a = (p.abs() * torch.exp2(-e)[:, :, None])
+    levels = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64)
+    far = (torch.where(torch.isfinite(a), a, torch.zeros_like(a))[..., None] - levels).abs()
+    best = far.amin(-1, keepdim=True)
+    # the nearest, of two the one with the even code
+    order = far + torch.where(far == best, torch.arange(8) % 2 * 1e-9, torch.zeros(8, dtype=torch.float64))
+    code = order.argmin(-1)
+    value = torch.where(p < 0, -1.0, 1.0) * levels[code] * torch.exp2(e)[:, :, None]
+    value[bad] = math.nan
+    code = code + 8 * torch.signbit(p).long()
+    scale = torch.where(bad, torch.full_like(e, 255), e + 127)
+    return code, scale, bad, value.view(x.shape[0], -1)[:, :x.shape[1]]
+
+
+def mx4_values(q):
+    levels = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64)
+    c, s = q.codes.cpu().long(), q.scales.cpu().double()
+    c = torch.stack([c & 15, c >> 4], 2).view(q.rows, -1)
+    step = torch.exp2(s - 127)
+    step[s == 255] = math.nan
+    v = levels[c & 7] * torch.where(c >= 8, -1.0, 1.0) * step.repeat_interleave(32, 1)
+    return v[:, :q.cols]
+
+
+def ckpt8_values(k):
+    s = k.scales.cpu().double()
+    step = torch.exp2(s - 133)
+    step[s == 255] = math.nan
+    return (k.codes.cpu().double() * step.repeat_interleave(32, 1))[:, :k.cols]
+
+
+def framed_blocks(kind, rows, cols):
+    """Blocks whose buffers go on behind their ends with bytes that must stay."""
+    b = (cols + 31) // 32
+    codes = torch.full((rows * b * kind.CODE_BYTES + 64,), 0x55, dtype=torch.uint8, device=DEV)
+    scales = torch.full((rows * b + 64,), 0x55, dtype=torch.uint8, device=DEV)
+    q = kind(codes[:rows * b * kind.CODE_BYTES].view(rows, -1).view(torch.int8 if kind is B.Ckpt8 else torch.uint8) if rows else
+             torch.empty(0, b * kind.CODE_BYTES, dtype=torch.uint8, device=DEV), scales[:rows * b].view(rows, b), cols)
+
+    def check():
+        torch.cuda.synchronize()
+        assert bool((codes[rows * b * kind.CODE_BYTES:] == 0x55).all()) and bool((scales[rows * b:] == 0x55).all())
+    return q, check
+
+
+# what the formats meet: values of all sizes, ties, blocks of zeros, of one value, of the smallest and the largest ones
+def awkward(g, rows, cols, kind):
+    x = normal(g, rows, cols) * torch.exp2(torch.randint(-12, 5, (rows, 1), generator=g).float())
+    pick = torch.randint(0, 8, (rows, 1), generator=g).expand(rows, cols)
+    ties = torch.randint(-16, 17, (rows, cols), generator=g).float() / 4
+    x = torch.where(pick == 1, ties, x)
+    x = torch.where(pick == 2, torch.zeros(()), x)
+    x = torch.where(pick == 3, x * (2.0 ** -130 if kind != "f16" else 2.0 ** -20), x)
+    x = torch.where(pick == 4, torch.clamp(x * (2.0 ** 126 if kind != "f16" else 2.0 ** 14), -6e4 if kind == "f16" else -3e38, 6e4 if kind == "f16" else 3e38), x)
+    x = torch.where(pick == 5, torch.randint(-128, 129, (rows, cols), generator=g).float() / 64 * (127.5 / 128), x)
+    return x.to(TYPES[kind])
+
+
+SHAPES = [(1, 1), (1, 31), (3, 32), (2, 33), (5, 64), (7, 100), (64, 67), (33, 129), (4, 255), (1, 4096), (2, 5000), (300, 257), (3, 777)]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_block_formats(rows, cols, kind):
+    print(f"[blocks] {rows}x{cols} {kind}", flush=True)
+    g = rng(rows, cols, kind)
+    x = awkward(g, rows, cols, kind)
+    if rows * cols > 200:  # a NaN and both infinities, each in a block of its own where there are that many
+        x.view(-1)[7], x.view(-1)[rows * cols // 2], x.view(-1)[-1] = math.nan, math.inf, -math.inf
+    for gap, first in ((0, 0), (3, 1)):
+        X = Framed(rows, cols, TYPES[kind], gap, first, x)
+        for make, pack, unpack, ref, values in ((B.Ckpt8, B.ckpt8_pack, B.ckpt8_unpack, ckpt8_ref, ckpt8_values),
+                                                (B.Mx4, B.mx4_quantize, B.mx4_dequantize, mx4_ref, mx4_values)):
+            q, check = framed_blocks(make, rows, cols)
+            pack(X.m, q)
+            check()
+            code, scale, bad, value = ref(x.double())
+            assert torch.equal(q.scales.cpu().double(), scale)
+            if make is B.Ckpt8:
+                got = q.codes.cpu().double().view(rows, -1, 32)
+            else:
+                c = q.codes.cpu().long()
+                got = torch.stack([c & 15, c >> 4], 2).view(rows, -1, 32)
+            assert torch.equal(got[~bad].double(), code[~bad].double())  # the padding's zeros among them
+            assert torch.equal(torch.isnan(values(q)), torch.isnan(value)) and torch.equal(values(q).nan_to_num(0.5), value.nan_to_num(0.5))
+            for out in TYPES:
+                Y = Framed(rows, cols, TYPES[out], gap, first)
+                unpack(q, Y.m)
+                want = value.to(TYPES[out]).double()
+                have = Y.get()
+                assert torch.equal(torch.isnan(have), torch.isnan(want)) and torch.equal(have.nan_to_num(0.5), want.nan_to_num(0.5))
+
+
+# ---- LayerNorm
+
+LN_SHAPES = [(1, 1), (5, 1), (3, 2), (17, 31), (40, 128), (9, 129), (300, 256), (11, 257), (130, 512), (6, 513), (70, 777), (33, 1024), (5, 1025),
+             (9, 2048), (3, 2049), (4, 4097), (2, 8192), (3, 8193), (2, 16384), (1, 256), (3000, 64)]
+
+
+def ln_inputs(rows, cols, kind, *key):
+    g = rng(rows, cols, kind, *key)
+    x = (normal(g, rows, cols) * torch.exp(0.5 * normal(g, rows, 1)) + 2.0 * normal(g, rows, 1)).to(TYPES[kind])
+    dy = (0.1 * normal(g, rows, cols)).to(TYPES[kind])
+    return x, dy, 1.0 + 0.1 * normal(g, cols), 0.1 * normal(g, cols)
+
+
+def ln_check(rows, cols, kind, x, dy, gamma, beta, eps, keep, gap, first):
+    t = TYPES[kind]
+    X, Y = Framed(rows, cols, t, gap, first, x), Framed(rows, cols, t, gap, first)
+    dev = [None if v is None else v.to(DEV) for v in (gamma, beta)]
+    mean, rstd = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    kept, check = framed_blocks(B.Ckpt8, rows, cols) if keep else (None, lambda: None)
+    B.layernorm_forward(X.m, dev[0], dev[1], eps, Y.m, mean, rstd, kept)
+    check()
+    xd = x.double()
+    gd = torch.ones(cols, dtype=torch.float64) if gamma is None else gamma.double()
+    bd = torch.zeros(cols, dtype=torch.float64) if beta is None else beta.double()
+    m = xd.mean(1, keepdim=True)
+    var = ((xd - m) ** 2).mean(1, keepdim=True)
+    r = 1.0 / torch.sqrt(var + eps)
+    top = xd.abs().amax(1, keepdim=True)
+    n = 64 * U  # at most 16 values of a thread, 6 + 4 exchanges, 16 wavefronts and a dozen operations
+    # the mean is off by n top, so a deviation by 2 n top, and rstd by n and by what those deviations make of it
+    mean_off, rstd_off = n * top, r * (n + 2 * n * top * r + (2 * n * top * r) ** 2)
+    near(mean.cpu().double()[:, None], m, mean_off)
+    near(rstd.cpu().double()[:, None], r, rstd_off)
+    y = (xd - m) * r * gd + bd
+    off = gd.abs() * (2 * mean_off * r + (xd - m).abs() * rstd_off) + 8 * U * ((xd - m).abs() * r * gd.abs() + bd.abs())
+    near(Y.get(), y, off + OUT[kind] * (y.abs() + off) + TINY[kind])
+    if keep:
+        _, scale, _, value = ckpt8_ref(xd)
+        assert torch.equal(kept.scales.cpu().double(), scale) and torch.equal(ckpt8_values(kept), value)
+    # backward, from the statistics as they are
+    D, DX = Framed(rows, cols, t, gap, first, dy), Framed(rows, cols, t, gap, first)
+    dgamma, dbeta = torch.full((cols,), SENTINEL, device=DEV), torch.full((cols,), SENTINEL, device=DEV)
+    size = B.layernorm_backward_workspace(rows, cols)
+    ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV) if size else None
+    B.layernorm_backward(D.m, kept if keep else X.m, dev[0], mean, rstd, DX.m, dgamma, dbeta, ws)
+    src = ckpt8_values(kept) if keep else xd
+    m, r, dyd = mean.cpu().double()[:, None], rstd.cpu().double()[:, None], dy.double()
+    h = (src - m) * r
+    g = dyd * gd
+    dx = r * (g - g.mean(1, keepdim=True) - h * (g * h).mean(1, keepdim=True))
+    gm = g.abs().amax(1, keepdim=True)
+    ha, hm = h.abs(), (h.abs().amax(1, keepdim=True))
+    off = n * r * gm * (1 + hm + ha * (1 + hm)) + 4 * U * r * g.abs()
+    near(DX.get(), dx, off + OUT[kind] * (dx.abs() + off) + TINY[kind])
+    # a thread's rows one after the other, then the workgroup's, then 32 slices
+    terms = (rows + 64) * U
+    near(dgamma.cpu().double(), (dyd * h).sum(0), (terms + 4 * U) * (dyd.abs() * (ha + 1e-300)).sum(0) + 1e-45)
+    near(dbeta.cpu().double(), dyd.sum(0), terms * dyd.abs().sum(0) + 1e-45)
+    return Y.get(), DX.get(), dgamma.cpu(), dbeta.cpu()
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows,cols", LN_SHAPES)
+def test_layernorm(rows, cols, kind):
+    print(f"[layernorm] {rows}x{cols} {kind}", flush=True)
+    x, dy, gamma, beta = ln_inputs(rows, cols, kind)
+    for keep in (False, True):
+        first = ln_check(rows, cols, kind, x, dy, gamma, beta, 1e-5, keep, 0, 0)
+        other = ln_check(rows, cols, kind, x, dy, gamma, beta, 1e-5, keep, 5, 3)
+        assert all(torch.equal(a, b) for a, b in zip(first, other))  # the same numbers wherever the rows lie
+
+
+@pytest.mark.parametrize("rows,cols", [(9, 40), (33, 1024)])
+def test_layernorm_without_parameters(rows, cols):
+    x, dy, gamma, beta = ln_inputs(rows, cols, "bf16")
+    ln_check(rows, cols, "bf16", x, dy, None, None, 1e-5, False, 0, 0)
+    ln_check(rows, cols, "bf16", x, dy, gamma, None, 1e-3, True, 0, 0)
+    # rows of one value throughout: no spread, h = 0
+    same = torch.full((rows, cols), 3.0, dtype=torch.bfloat16)
+    ln_check(rows, cols, "bf16", same, dy, gamma, beta, 1e-5, False, 0, 0)
+    # the gradients of the parameters alone may be left out
+    X, D = same.to(DEV), dy.to(DEV)
+    mean, rstd = torch.full((rows,), 3.0, device=DEV), torch.ones(rows, device=DEV)
+    dx, dbeta = torch.empty_like(X), torch.empty(cols, device=DEV)
+    ws = torch.empty(max(16, B.layernorm_backward_workspace(rows, cols)), dtype=torch.uint8, device=DEV)
+    B.layernorm_backward(D, X, None, mean, rstd, dx, None, dbeta, ws)
+    near(dbeta.cpu().double(), dy.double().sum(0), (rows + 64) * U * dy.double().abs().sum(0))
+    B.layernorm_backward(D, X, None, mean, rstd, dx, None, None, ws)
+
+
+def test_layernorm_keeps_what_is_not_finite_in_its_row():
+    x, dy, gamma, beta = ln_inputs(40, 300, "f32")
+    x[3, 17], x[8, 299], x[39, 0] = math.nan, math.inf, -math.inf
+    for keep in (False, True):
+        X, Y = x.to(DEV), torch.empty(40, 300, device=DEV)
+        mean, rstd = torch.empty(40, device=DEV), torch.empty(40, device=DEV)
+        kept = B.ckpt8_empty(40, 300) if keep else None
+        B.layernorm_forward(X, gamma.to(DEV), beta.to(DEV), 1e-5, Y, mean, rstd, kept)
+        bad = torch.zeros(40, dtype=torch.bool)
+        bad[[3, 8, 39]] = True
+        assert bool(torch.isnan(Y.cpu()[bad]).all()) and bool(torch.isfinite(Y.cpu()[~bad]).all())
+        dx, dg, db = torch.empty_like(X), torch.empty(300, device=DEV), torch.empty(300, device=DEV)
+        ws = torch.empty(max(16, B.layernorm_backward_workspace(40, 300)), dtype=torch.uint8, device=DEV)
+        B.layernorm_backward(dy.to(DEV), kept or X, gamma.to(DEV), mean, rstd, dx, dg, db, ws)
+        assert bool(torch.isnan(dx.cpu()[bad]).all()) and bool(torch.isfinite(dx.cpu()[~bad]).all())
+        assert bool(torch.isnan(dg.cpu()).all()) and bool(torch.isfinite(db.cpu()).all())
+
+
+def test_layernorm_gradients_are_differences():
+    """Directional derivatives of a loss by central differences of the forward pass, in fp32."""
+    rows, cols = 6, 48
+    g = rng("differences")
+    x, gamma, beta, dy = normal(g, rows, cols), 1 + 0.1 * normal(g, cols), 0.1 * normal(g, cols), normal(g, rows, cols)
+
+    def forward(x, gamma, beta):
+        y, mean, rstd = torch.empty(rows, cols, device=DEV), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+        B.layernorm_forward(x.to(DEV), gamma.to(DEV), beta.to(DEV), 1e-5, y, mean, rstd)
+        return y, mean, rstd
+
+    y, mean, rstd = forward(x, gamma, beta)
+    dx, dg, db = torch.empty(rows, cols, device=DEV), torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+    ws = torch.empty(max(16, B.layernorm_backward_workspace(rows, cols)), dtype=torch.uint8, device=DEV)
+    B.layernorm_backward(dy.to(DEV), x.to(DEV), gamma.to(DEV), mean, rstd, dx, dg, db, ws)
+    h = 2.0 ** -6
+    for i, grad in enumerate((dx, dg, db)):
+        v = normal(g, *grad.shape)
+        v /= v.norm()
+        a, b = [x, gamma, beta], [x, gamma, beta]
+        a[i], b[i] = a[i] + h * v, b[i] - h * v
+        slope = ((forward(*a)[0].double() - forward(*b)[0].double()) * dy.to(DEV).double()).sum().item() / (2 * h)
+        want = (grad.double().cpu() * v.double()).sum().item()
+        # the third derivative along a unit vector, and rounding: values up to 4 through sums of 8 values, 4 exchanges and four operations
+        allowed = h * h * float(dy.norm()) + 16 * U * 4 * float(dy.abs().sum()) / h
+        assert abs(slope - want) <= allowed and abs(want) > 0
+
+
+# ---- the weight gradient
+
+WG_SHAPES = [(1, 1, 1), (1, 40, 17), (3, 8, 33), (63, 130, 67), (64, 128, 128), (65, 127, 129), (300, 21, 256), (129, 300, 70), (1000, 64, 64),
+             (4097, 40, 200), (2, 5, 1000), (700, 257, 129)]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows,n,k", WG_SHAPES)
+def test_weight_grad(rows, n, k, kind):
+    print(f"[weight grad] {rows} x {n} x {k} {kind}", flush=True)
+    g = rng(rows, n, k, kind)
+    x = (torch.relu(normal(g, rows, k)) * torch.exp(normal(g, k))).to(TYPES[kind])
+    dy = normal(g, rows, n).to(TYPES[kind])
+    kept = B.ckpt8_empty(rows, k)
+    B.ckpt8_pack(x.to(DEV), kept)
+    xv, dyd = ckpt8_values(kept), dy.double()
+    want, total = dyd.t() @ xv, dyd.abs().t() @ xv.abs()
+    size = B.ckpt8_weight_grad_workspace(rows, n, k)
+    results = []
+    for gap, first in ((0, 0), (1, 1), (8, 0)):
+        D, W = Framed(rows, n, TYPES[kind], gap, first, dy), Framed(n, k, torch.float32, gap, first)
+        db = torch.full((n + 8,), SENTINEL, device=DEV)
+        ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV) if size else None
+        B.ckpt8_weight_grad(D.m, kept, W.m, db[:n], ws)
+        near(W.get(), want, (3 * rows + 8) * U * total)
+        near(db[:n].cpu().double(), dyd.sum(0), (rows + 8) * U * dyd.abs().sum(0))
+        assert bool((db[n:] == SENTINEL).all())
+        results.append(W.get())
+        alone = Framed(n, k, torch.float32, gap, first)
+        B.ckpt8_weight_grad(D.m, kept, alone.m, None, ws)
+        assert torch.equal(alone.get(), results[-1])
+    assert all(torch.equal(r, results[0]) for r in results)
+
+
+def test_weight_grad_of_wide_ranges():
+    """fp32 gradients over the whole range of exponents, values whose parts reach its ends, and what is not finite."""
+    rows, n, k = 130, 40, 70
+    g = rng("wide")
+    dy = normal(g, rows, n) * torch.exp2(torch.randint(-60, 60, (1, n), generator=g).float())
+    dy[5, 3] = 3.4e38
+    x = normal(g, rows, k) * 2.0 ** -20
+    kept = B.ckpt8_empty(rows, k)
+    B.ckpt8_pack(x.to(DEV), kept)
+    dw, db = torch.empty(n, k, device=DEV), torch.empty(n, device=DEV)
+    ws = torch.empty(max(16, B.ckpt8_weight_grad_workspace(rows, n, k)), dtype=torch.uint8, device=DEV)
+    B.ckpt8_weight_grad(dy.to(DEV), kept, dw, db, ws)
+    xv, dyd = ckpt8_values(kept), dy.double()
+    near(dw.cpu().double(), dyd.t() @ xv, (3 * rows + 8) * U * (dyd.abs().t() @ xv.abs()) + 2.0 ** -126)
+    dy[7, 9], dy[8, 10] = math.nan, math.inf
+    x[20, 65] = math.nan
+    B.ckpt8_pack(x.to(DEV), kept)
+    B.ckpt8_weight_grad(dy.to(DEV), kept, dw, db, ws)
+    got = dw.cpu()
+    assert bool(torch.isnan(got[9]).all()) and bool((~torch.isfinite(got[10])).all()) and bool(torch.isnan(got[:, 64:]).all())
+    keep = torch.ones(n, dtype=torch.bool)
+    keep[[9, 10]] = False
+    assert bool(torch.isfinite(got[keep][:, :64]).all())
+    d = db.cpu()
+    assert bool(torch.isnan(d[9])) and float(d[10]) == math.inf and bool(torch.isfinite(d[keep]).all())
+
+
+# ---- 4-bit layers
+
+LINEAR_SHAPES = [(1, 1, 1), (1, 256, 67), (1, 17, 2048), (2, 40, 33), (15, 100, 130), (16, 64, 128), (17, 21, 256), (64, 130, 1000), (65, 33, 257),
+                 (128, 128, 256), (129, 257, 300), (300, 403, 1111), (700, 64, 64), (1030, 8, 4096)]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows,n,k", LINEAR_SHAPES)
+def test_mx4_linear(rows, n, k, kind):
+    print(f"[mx4 linear] {rows} x {n} x {k} {kind}", flush=True)
+    g = rng(rows, n, k, kind)
+    x, w, bias = normal(g, rows, k).to(TYPES[kind]), normal(g, n, k) / math.sqrt(k), normal(g, n)
+    q = B.mx4_empty(n, k)
+    B.mx4_quantize(w.to(DEV), q)
+    wv, xv = mx4_values(q), mx4_ref(x.double())[3]
+    total = xv.abs() @ wv.abs().t()
+    size = B.mx4_linear_workspace(rows, n, k)
+    results = []
+    for gap, first, b in ((0, 0, bias), (3, 1, bias), (0, 0, None)):
+        X, Y = Framed(rows, k, TYPES[kind], gap, first, x), Framed(rows, n, TYPES[kind], gap, first)
+        ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV) if size else None
+        B.mx4_linear(X.m, q, None if b is None else b.to(DEV), Y.m, ws)
+        want = xv @ wv.t() + (0 if b is None else b.double())
+        off = (k + 8) * U * total + U * want.abs()
+        near(Y.get(), want, off + OUT[kind] * (want.abs() + off) + TINY[kind])
+        results.append(Y.get())
+        # the same from an input that is quantized already, in every type of output
+        xq = B.mx4_empty(rows, k)
+        B.mx4_quantize(X.m, xq)
+        for out in TYPES:
+            Z = Framed(rows, n, TYPES[out], gap, first)
+            B.mx4_matmul(xq, q, None if b is None else b.to(DEV), Z.m)
+            near(Z.get(), want, off + OUT[out] * (want.abs() + off) + TINY[out])
+            if out == kind:
+                assert torch.equal(Z.get(), results[-1])
+    assert torch.equal(results[0], results[1])
+
+
+@pytest.mark.parametrize("rows", [3, 200])
+def test_mx4_linear_of_what_is_not_finite(rows):
+    n, k = 50, 200
+    g = rng("nonfinite", rows)
+    x, w = normal(g, rows, k), normal(g, n, k)
+    x[1, 60], x[2, 199] = math.nan, math.inf
+    w[7, 3] = math.nan
+    q = B.mx4_empty(n, k)
+    B.mx4_quantize(w.to(DEV), q)
+    y = torch.empty(rows, n, device=DEV)
+    ws = torch.empty(max(16, B.mx4_linear_workspace(rows, n, k)), dtype=torch.uint8, device=DEV)
+    B.mx4_linear(x.to(DEV), q, None, y, ws)
+    bad = torch.zeros(rows, n, dtype=torch.bool)
+    bad[1:3], bad[:, 7] = True, True
+    assert torch.equal(torch.isnan(y.cpu()), bad) and bool(torch.isfinite(y.cpu()[~bad]).all())
+
+
+IG_SHAPES = [(1, 1, 1), (1, 17, 256), (2, 40, 33), (63, 65, 67), (64, 64, 128), (129, 128, 129), (300, 403, 1111), (700, 21, 64), (4100, 33, 40)]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows,n,k", IG_SHAPES)
+def test_mx4_input_grad(rows, n, k, kind):
+    print(f"[mx4 input grad] {rows} x {n} x {k} {kind}", flush=True)
+    g = rng(rows, n, k, kind)
+    dy, w = normal(g, rows, n).to(TYPES[kind]), normal(g, n, k)
+    q = B.mx4_empty(n, k)
+    B.mx4_quantize(w.to(DEV), q)
+    wv, dyd = mx4_values(q), dy.double()
+    want, total = dyd @ wv, dyd.abs() @ wv.abs()
+    size = B.mx4_input_grad_workspace(rows, n, k)
+    results = []
+    for gap, first in ((0, 0), (1, 1), (8, 0)):
+        D, X = Framed(rows, n, TYPES[kind], gap, first, dy), Framed(rows, k, TYPES[kind], gap, first)
+        ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV) if size else None
+        B.mx4_input_grad(D.m, q, X.m, ws)
+        off = (3 * n + 8) * U * total
+        near(X.get(), want, off + OUT[kind] * (want.abs() + off) + TINY[kind])
+        results.append(X.get())
+    assert all(torch.equal(r, results[0]) for r in results)
+
+
+# ---- how they are called
+
+def test_no_rows():
+    """No rows: nothing is written, and gradients over no rows are zeros."""
+    e = torch.empty(0, 40, device=DEV)
+    v = torch.empty(0, device=DEV)
+    dg, db, dw, dbias = (torch.full(s, SENTINEL, device=DEV) for s in ((40,), (40,), (21, 40), (21,)))
+    kept, q = B.ckpt8_empty(0, 40), B.mx4_empty(21, 40)
+    B.mx4_quantize(torch.zeros(21, 40, device=DEV), q)
+    B.layernorm_forward(e, None, None, 1e-5, torch.empty_like(e), v, v, kept)
+    B.layernorm_backward(e, e, None, v, v, torch.empty_like(e), dg, db, None)
+    B.ckpt8_pack(e, kept)
+    B.ckpt8_weight_grad(torch.empty(0, 21, device=DEV), kept, dw, dbias, None)
+    B.mx4_linear(e, q, None, torch.empty(0, 21, device=DEV))
+    B.mx4_input_grad(torch.empty(0, 21, device=DEV), q, e)
+    for t in (dg, db, dw, dbias):
+        assert not bool(t.any())
+
+
+def test_graph_and_stream():
+    """A step of all of them, captured on a stream of its own and replayed between eager work: the eager results each time."""
+    rows, k, n = 300, 200, 130
+    g = rng("graph")
+    x, dy = normal(g, rows, k).to(DEV, torch.bfloat16), normal(g, rows, n).to(DEV, torch.bfloat16)
+    w, gamma, beta = normal(g, n, k).to(DEV), (1 + 0.1 * normal(g, k)).to(DEV), normal(g, k).to(DEV)
+    h, dh, dx = (torch.empty(rows, k, device=DEV, dtype=torch.bfloat16) for _ in range(3))
+    y = torch.empty(rows, n, device=DEV, dtype=torch.bfloat16)
+    mean, rstd = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    dw, db, dg, dbe = torch.empty(n, k, device=DEV), torch.empty(n, device=DEV), torch.empty(k, device=DEV), torch.empty(k, device=DEV)
+    kx, kh, q = B.ckpt8_empty(rows, k), B.ckpt8_empty(rows, k), B.mx4_empty(n, k)
+    sizes = (B.layernorm_backward_workspace(rows, k), B.ckpt8_weight_grad_workspace(rows, n, k), B.mx4_linear_workspace(rows, n, k),
+             B.mx4_input_grad_workspace(rows, n, k))
+    ws = torch.empty(max(16, *sizes), dtype=torch.uint8, device=DEV)
+
+    def step():
+        B.mx4_quantize(w, q)
+        B.layernorm_forward(x, gamma, beta, 1e-5, h, mean, rstd, kx)
+        B.ckpt8_pack(h, kh)
+        B.mx4_linear(h, q, None, y, ws)
+        B.ckpt8_weight_grad(dy, kh, dw, db, ws)
+        B.mx4_input_grad(dy, q, dh, ws)
+        B.layernorm_backward(dh, kx, gamma, mean, rstd, dx, dg, dbe, ws)
+
+    outs = (h, y, dw, db, dh, dx, dg, dbe)
+    step()
+    torch.cuda.synchronize()
+    eager = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for _ in range(3):
+        for o in outs:
+            o.fill_(SENTINEL)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, eager))
