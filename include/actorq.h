@@ -404,7 +404,8 @@ aq_status aq_policy_forward_fp16(aq_policy* p, const void* d_obs, int64_t batch,
  * has no effect, and gradients over no rows are zeros.  Outputs overlap neither inputs nor each other.
  * AQ_EINVAL: a NULL argument that is not said to be optional, a negative size, ld < cols, an unknown type, an
  * address that is no multiple of its element's size, a workspace that is too small.  AQ_ESHAPE: operands
- * whose sizes or types do not go together, or beyond a call's limits; rows are below 2^31 everywhere. */
+ * whose sizes or types do not go together, no columns, or beyond the limits: rows < 2^31, columns <= 2^20, ld <= 2^21
+ * (256 rows lie within 2 GiB), and what a call states. */
 typedef enum { AQ_F32 = 0, AQ_F16 = 1, AQ_BF16 = 2 } aq_dtype;
 typedef struct {
     void* d;
@@ -455,7 +456,7 @@ aq_status aq_ckpt8_pack(const aq_matrix* x, const aq_ckpt8* kept, void* stream);
 aq_status aq_ckpt8_unpack(const aq_ckpt8* kept, const aq_matrix* x, void* stream);
 /* The gradients of a fully connected layer y = x W^T + b from its checkpointed input: dw[n][k] = sum over rows of
  * dy[row][n] * x[row][k] (fp32, n = dy's columns, k = kept's), d_db[n] = sum over rows of dy[row][n] (may be NULL).
- * The products are exact and their sums are fp32, whatever dy's type.  At most 2^20 columns each. */
+ * The products are exact and their sums are fp32, whatever dy's type.  */
 aq_status aq_ckpt8_weight_grad_workspace(int64_t rows, int64_t n, int64_t k, uint64_t* bytes);
 aq_status aq_ckpt8_weight_grad(const aq_matrix* dy, const aq_ckpt8* kept, const aq_matrix* dw, float* d_db,
                                void* d_workspace, uint64_t workspace_bytes, void* stream);
@@ -465,7 +466,7 @@ aq_status aq_mx4_quantize(const aq_matrix* x, const aq_mx4* q, void* stream);
 aq_status aq_mx4_dequantize(const aq_mx4* q, const aq_matrix* x, void* stream);
 /* A fully connected layer in 4 bits: y = Q(x) w^T + bias, Q the conversion above (w: n rows of k values; bias fp32 [n],
  * may be NULL).  The products are those of the 4-bit values, exact, and their sums are fp32.  x and y have
- * one type.  aq_mx4_matmul takes an input that is quantized already and any type of y.  At most 2^20 columns each. */
+ * one type.  aq_mx4_matmul takes an input that is quantized already and any type of y.  */
 aq_status aq_mx4_linear_workspace(int64_t rows, int64_t n, int64_t k, uint64_t* bytes);
 aq_status aq_mx4_linear(const aq_matrix* x, const aq_mx4* w, const float* d_bias, const aq_matrix* y,
                         void* d_workspace, uint64_t workspace_bytes, void* stream);

@@ -5,7 +5,7 @@
 // either format times its power of two has at most seven significant bits, so it is a bf16 value, and a value of dy is the sum of
 // one (bfloat16), two (binary16) or three (fp32) bf16 values.
 //
-// A workgroup's 64 t of both operands go through LDS.  B lies there as it does in memory, t by t (and so does A for the weight
+// A workgroup's 32 t of both operands go through LDS.  B lies there as it does in memory, t by t (and so does A for the weight
 // gradient), and is transposed on its way to the registers: ds_read_b64_tr_b16 hands lane i of 16 the four t of column i out of
 // four rows of 16 columns.
 #include "learner.hpp"
@@ -15,7 +15,10 @@ namespace aq {
 namespace {
 
 typedef short v4s16 __attribute__((ext_vector_type(4)));
-typedef short v8s16 __attribute__((ext_vector_type(8)));
+typedef float v16f32 __attribute__((ext_vector_type(16)));
+
+constexpr int kMostLds = 160 * 1024;
+constexpr int grad_buffers(int bytes) { return 3 * bytes <= kMostLds ? 3 : 2; }
 
 template <class T>
 constexpr int kParts = std::is_same<T, float>::value ? 3 : std::is_same<T, f16_t>::value ? 2 : 1;
@@ -45,281 +48,370 @@ __device__ __forceinline__ void split(const Piece<T>& in, v4u (&out)[P]) {
     }
 }
 
-// ---- LDS tiles
-// [64 t][S columns]: 32-byte pieces of a row, piece p of row t in place p ^ turned(t), so that the 16 rows of a transposing
-// read lie in different banks
-__device__ __forceinline__ int turned(int t) { return (t & 3) | ((t >> 3) & 1) << 2; }
+// ---- LDS tiles of 32 t
+// [t][S columns]: 32-byte pieces of a row, piece p of row t in place p ^ 2 (t mod 4), so that the four rows and two pieces which 32 lanes
+// of a transposing read take lie in different banks
 template <int S>
 __device__ __forceinline__ int t_at(int t, int col) {  // byte address of column col (a multiple of 8) of row t
-    return t * 2 * S + (((col >> 4) ^ (turned(t) & (S / 16 - 1))) << 5) + ((col & 8) << 1);
+    return t * 2 * S + (((col >> 4) ^ ((t & 3) << 1 & (S / 16 - 1))) << 5) + ((col & 8) << 1);
 }
-// 16 columns from col on, 32 t from t0 on, as an MFMA operand: lane l has column l mod 16, t = 8 (l / 16) .. + 7
+// 32 columns from col on, 16 t from t0 on, as an MFMA operand: lane l has column l mod 32, t = 8 (l / 32) .. + 7
 template <int S>
 __device__ __forceinline__ v8bf16 t_operand(const uint8_t* tile, int t0, int col, int lane) {
     typedef __attribute__((address_space(3))) v4s16* lds_ptr;
-    const int g = lane >> 4, i = lane & 15, t = t0 + 8 * g + (i >> 2);
-    const uint8_t* p = tile + t * 2 * S + (((col >> 4) ^ (turned(t) & (S / 16 - 1))) << 5) + (i & 3) * 8;
+    const int i = lane & 15, t = t0 + 8 * (lane >> 5) + (i >> 2);
+    const uint8_t* p = tile + t_at<S>(t, col + (lane & 16)) + (i & 3) * 8;
     const v4s16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
     const v4s16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * 2 * S));
     return __builtin_bit_cast(v8bf16, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
-// [S rows][64 t]: 16-byte pieces, piece p of row m in place p ^ (m / 2 mod 8)
-__device__ __forceinline__ int m_at(int m, int piece) { return m * 128 + ((piece ^ ((m >> 1) & 7)) << 4); }
+// [row m][32 t]: 16-byte pieces, piece p of row m in place p ^ (m / 4 mod 4)
+__device__ __forceinline__ int m_at(int m, int piece) { return m * 64 + ((piece ^ ((m >> 2) & 3)) << 4); }
 
-// ---- the operands.  Each thread fetches its part of 64 t into registers and later puts it into LDS as bf16.
-// dy with t along the rows (weight gradient): [t][m]
-template <class T, int S>
-struct DyRows {
-    static constexpr int P = kParts<T>, kUnits = S / 32, kPlane = 64 * 2 * S;
-    static constexpr bool kTransposed = true;
-    const T* d;
-    int64_t ld;
-    Piece<T> in[kUnits];
-    __device__ __forceinline__ void fetch(int64_t t0, int64_t tn, int64_t m0, int64_t mn) {
+// ---- the operands.  Of 32 t and S columns (or rows) each thread fetches S / 64 units of eight values into registers and later puts them
+// into LDS as bf16.  Loads go through windows on the matrix that begin at the workgroup's first row: what lies behind the
+// matrix's end comes as zeros, without a branch.  Columns of an operand that do not exist only reach results that are not stored.
+struct Window {
+    __amdgpu_buffer_rsrc_t r;
+    // of the bytes from `at` (a multiple of 4) on of `size` bytes at `base`
+    __device__ __forceinline__ void set(const uint8_t* base, int64_t at, int64_t size) {
+        const int64_t left = size - at;
+        r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (left > 0 ? at : 0)), 0, left <= 0 ? 0 : left < kMost ? (int)left : kMost, 0x00020000);
+    }
+    static constexpr int kMost = 0x7ffffff0, kOutside = (int)0x80000000u;
+};
+// A matrix in whole words of memory: from the word of its first element to that of its last.
+struct Words {
+    const uint8_t* base;
+    int64_t size;
+    int skew;  // bytes in front of the first element
+    int64_t ld, rows;
+};
+template <class T>
+Words words_of(const aq_matrix& m) {
+    const uintptr_t first = (uintptr_t)m.d, end = first + (m.rows ? ((m.rows - 1) * m.ld + m.cols) * sizeof(T) : 0);
+    const uintptr_t base = first & ~(uintptr_t)3;
+    return {(const uint8_t*)base, (int64_t)(((end + 3) & ~(uintptr_t)3) - base), (int)(first - base), m.ld, m.rows};
+}
+// Eight values `at` bytes from a window's beginning.  ODD: 16-bit values of which some pieces begin in the middle of a word; they are
+// shifted into place out of five words, so that no load leaves the matrix's words.
+template <class T, bool ODD>
+__device__ __forceinline__ void load_piece(Piece<T>& q, const Window& w, int at) {
+    if constexpr (ODD) {
+        const v4u v = __builtin_amdgcn_raw_buffer_load_b128(w.r, at & ~3, 0, 0);
+        const uint32_t last = __builtin_amdgcn_raw_buffer_load_b32(w.r, (at & ~3) + 16, 0, 0), by = (at & 2) * 8;
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i;
-            const int64_t t = t0 + u / (S / 8), m = m0 + 8 * (u % (S / 8));
-            in[i].zero();
-            if (t < tn) in[i].load(d + t * ld + m, (int)(mn - m < 8 ? mn - m : 8));
+        for (int i = 0; i < 4; ++i) q.w[i] = __builtin_amdgcn_alignbit(i < 3 ? v[i < 3 ? i + 1 : 0] : last, v[i], by);
+    } else {
+#pragma unroll
+        for (int i = 0; i < Piece<T>::kWords; i += 4) {
+            const v4u v = __builtin_amdgcn_raw_buffer_load_b128(w.r, at, 0, 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q.w[i + j] = v[j];
+            at += 16;
         }
     }
-    __device__ __forceinline__ void put(uint8_t* to) const {
+}
+template <class T, bool ANY>
+constexpr bool kOdd = ANY && sizeof(T) == 2;
+// dy with t along the rows (weight gradient): [t][m].  ANY: rows of any alignment.
+template <class T, int S, bool ANY>
+struct DyRows {
+    static constexpr int P = kParts<T>, kUnits = S / 64, kPlane = 32 * 2 * S, kPer = S / 8;
+    static constexpr bool kSums = true;
+    Words d;
+    int64_t m0;
+    int off, left;
+    Window w;
+    Piece<T> in[kUnits];
+    __device__ __forceinline__ void begin(int64_t m, int64_t) { m0 = m; }
+    __device__ __forceinline__ void at(int64_t t0) {
+        const int64_t byte = (t0 * d.ld + m0) * (int64_t)sizeof(T) + d.skew;
+        w.set(d.base, byte & ~(int64_t)3, d.size);
+        off = (int)byte & 3;
+        left = (int)(d.rows - t0 < 32 ? d.rows - t0 : 32);
+    }
+    __device__ __forceinline__ void fetch(int i) {
+        const int u = threadIdx.x + 256 * i;
+        int at = off + ((u / kPer) * (int)d.ld + 8 * (u % kPer)) * (int)sizeof(T);
+        // (the last word may hold what would be the first value of a row behind the last)
+        if (kOdd<T, ANY> && u / kPer >= left) at = Window::kOutside;
+        load_piece<T, kOdd<T, ANY>>(in[i], w, at);
+    }
+    __device__ __forceinline__ void put(int i, uint8_t* to) const {
+        const int u = threadIdx.x + 256 * i;
+        v4u q[P];
+        split<T, P>(in[i], q);
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i;
-            v4u q[P];
-            split<T, P>(in[i], q);
-#pragma unroll
-            for (int p = 0; p < P; ++p) *(v4u*)(to + p * kPlane + t_at<S>(u / (S / 8), 8 * (u % (S / 8)))) = q[p];
-        }
+        for (int p = 0; p < P; ++p) *(v4u*)(to + p * kPlane + t_at<S>(u / kPer, 8 * (u % kPer))) = q[p];
     }
     static __device__ __forceinline__ v8bf16 operand(const uint8_t* tile, int t0, int m, int lane) { return t_operand<S>(tile, t0, m, lane); }
 };
-// dy with t along the columns (input gradient): [m][t]
-template <class T, int S>
+// dy with t along the columns (input gradient): [m][t].  ANY: rows of any alignment, which may end inside a piece whose other
+// values are the next row's.
+template <class T, int S, bool ANY>
 struct DyCols {
-    static constexpr int P = kParts<T>, kUnits = S / 32, kPlane = 64 * 2 * S;
-    static constexpr bool kTransposed = false;
-    const T* d;
-    int64_t ld;
+    static constexpr int P = kParts<T>, kUnits = S / 64, kPlane = 32 * 2 * S;
+    static constexpr bool kSums = false;
+    Words d;
+    int64_t m0;
+    int tn, off, left, held;  // values that exist of the pieces that this thread fetches and of those that it puts
+    Window w;
     Piece<T> in[kUnits];
-    __device__ __forceinline__ void fetch(int64_t t0, int64_t tn, int64_t m0, int64_t mn) {
-#pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i;
-            const int64_t m = m0 + u / 8, t = t0 + 8 * (u % 8);
-            in[i].zero();
-            if (m < mn) in[i].load(d + m * ld + t, (int)(tn - t < 8 ? tn - t : 8));
-        }
+    __device__ __forceinline__ void begin(int64_t m, int64_t t_end) {
+        m0 = m;
+        tn = (int)t_end;
     }
-    __device__ __forceinline__ void put(uint8_t* to) const {
+    __device__ __forceinline__ void at(int64_t t0) {
+        const int64_t byte = (m0 * d.ld + t0) * (int64_t)sizeof(T) + d.skew;
+        w.set(d.base, byte & ~(int64_t)3, d.size);
+        off = (int)byte & 3;
+        held = left;
+        left = tn - (int)t0 - 8 * (threadIdx.x & 3);
+    }
+    __device__ __forceinline__ void fetch(int i) {
+        const int u = threadIdx.x + 256 * i;
+        load_piece<T, kOdd<T, ANY>>(in[i], w, left > 0 ? off + ((u >> 2) * (int)d.ld + 8 * (u & 3)) * (int)sizeof(T) : Window::kOutside);
+    }
+    __device__ __forceinline__ void put(int i, uint8_t* to) const {
+        const int u = threadIdx.x + 256 * i;
+        Piece<T> own = in[i];
+        if constexpr (ANY) {
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i;
-            v4u q[P];
-            split<T, P>(in[i], q);
-#pragma unroll
-            for (int p = 0; p < P; ++p) *(v4u*)(to + p * kPlane + m_at(u / 8, u % 8)) = q[p];
+            for (int k = 0; k < Piece<T>::kWords; ++k) {
+                if constexpr (sizeof(T) == 4) own.w[k] = k < held ? own.w[k] : 0;
+                else own.w[k] &= 2 * k + 1 < held ? 0xffffffffu : 2 * k < held ? 0xffffu : 0u;
+            }
         }
+        v4u q[P];
+        split<T, P>(own, q);
+#pragma unroll
+        for (int p = 0; p < P; ++p) *(v4u*)(to + p * kPlane + m_at(u >> 2, u & 3)) = q[p];
     }
     static __device__ __forceinline__ v8bf16 operand(const uint8_t* tile, int t0, int m, int lane) {
-        return *(const v8bf16*)(tile + m_at(m + (lane & 15), t0 / 8 + (lane >> 4)));
+        return *(const v8bf16*)(tile + m_at(m + (lane & 31), t0 / 8 + (lane >> 5)));
     }
 };
-// checkpoint rows: 16 codes and a scale to a unit
+// rows of the checkpoint
 template <int S>
 struct KeptRows {
-    static constexpr int kUnits = S / 64, kPlane = 64 * 2 * S;
+    static constexpr int kUnits = S / 64, kPlane = 32 * 2 * S, kPer = S / 8;
     const uint8_t* codes;
     const uint8_t* scales;
-    int64_t blocks;
-    v4u c[kUnits];
+    int64_t blocks, rows;
+    int64_t c0;
+    int off;
+    Window wc, ws;
+    v2u c[kUnits];
     uint32_t s[kUnits];
-    __device__ __forceinline__ void fetch(int64_t t0, int64_t tn, int64_t c0) {
-#pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i;
-            const int64_t t = t0 + u / (S / 16), b = (c0 + 16 * (u % (S / 16))) >> 5;
-            c[i] = v4u{0, 0, 0, 0};
-            s[i] = 0;
-            if (t < tn && b < blocks) {
-                c[i] = *(const v4u AQ_GLOBAL*)(codes + t * blocks * 32 + c0 + 16 * (u % (S / 16)));
-                s[i] = ((const uint8_t AQ_GLOBAL*)scales)[t * blocks + b];
-            }
-        }
+    __device__ __forceinline__ void begin(int64_t col) { c0 = col; }
+    __device__ __forceinline__ void at(int64_t t0) {
+        wc.set(codes, t0 * blocks * 32 + c0, rows * blocks * 32);
+        const int64_t byte = t0 * blocks + (c0 >> 5) + ((uintptr_t)scales & 3);
+        ws.set((const uint8_t*)((uintptr_t)scales & ~(uintptr_t)3), byte & ~(int64_t)3, rows * blocks + ((uintptr_t)scales & 3));
+        off = (int)byte & 3;
     }
-    __device__ __forceinline__ void put(uint8_t* to) const {
-#pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i, t = u / (S / 16), col = 16 * (u % (S / 16));
-            const float step = ckpt8_step(s[i]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float v[8];
-                ckpt8_values(v2u{c[i][2 * h], c[i][2 * h + 1]}, step, v);
-                Piece<bf16_t> o;
-                o.set(v);
-                *(v4u*)(to + t_at<S>(t, col + 8 * h)) = v4u{o.w[0], o.w[1], o.w[2], o.w[3]};
-            }
-        }
+    __device__ __forceinline__ void fetch(int i) {
+        const int u = threadIdx.x + 256 * i, t = u / kPer, col = 8 * (u % kPer);
+        c[i] = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(wc.r, t * (int)blocks * 32 + col, 0, 0));
+        s[i] = __builtin_amdgcn_raw_buffer_load_b8(ws.r, off + t * (int)blocks + (col >> 5), 0, 0);
+    }
+    __device__ __forceinline__ void put(int i, uint8_t* to) const {
+        const int u = threadIdx.x + 256 * i;
+        float v[8];
+        ckpt8_values(c[i], ckpt8_step(s[i]), v);
+        Piece<bf16_t> o;
+        o.set(v);
+        *(v4u*)(to + t_at<S>(u / kPer, 8 * (u % kPer))) = v4u{o.w[0], o.w[1], o.w[2], o.w[3]};
     }
 };
-// rows of 4-bit weights: a block of 32 to a unit
+// rows of 4-bit weights
 template <int S>
 struct Mx4Rows {
-    static constexpr int kUnits = S / 128 ? S / 128 : 1, kPlane = 64 * 2 * S;
+    static constexpr int kUnits = S / 64, kPlane = 32 * 2 * S, kPer = S / 8;
     const uint8_t* codes;
     const uint8_t* scales;
-    int64_t blocks;
-    v4u c[kUnits];
-    uint32_t s[kUnits];
-    static __device__ __forceinline__ bool mine(int u) { return u < 64 * (S / 32); }
-    __device__ __forceinline__ void fetch(int64_t t0, int64_t tn, int64_t c0) {
-#pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i;
-            const int64_t t = t0 + u / (S / 32), b = (c0 >> 5) + u % (S / 32);
-            c[i] = v4u{0, 0, 0, 0};
-            s[i] = 0;
-            if (mine(u) && t < tn && b < blocks) {
-                c[i] = *(const v4u AQ_GLOBAL*)(codes + (t * blocks + b) * 16);
-                s[i] = ((const uint8_t AQ_GLOBAL*)scales)[t * blocks + b];
-            }
-        }
+    int64_t blocks, rows;
+    int64_t c0;
+    int off;
+    Window wc, ws;
+    uint32_t c[kUnits], s[kUnits];
+    __device__ __forceinline__ void begin(int64_t col) { c0 = col; }
+    __device__ __forceinline__ void at(int64_t t0) {
+        wc.set(codes, t0 * blocks * 16 + c0 / 2, rows * blocks * 16);
+        const int64_t byte = t0 * blocks + (c0 >> 5) + ((uintptr_t)scales & 3);
+        ws.set((const uint8_t*)((uintptr_t)scales & ~(uintptr_t)3), byte & ~(int64_t)3, rows * blocks + ((uintptr_t)scales & 3));
+        off = (int)byte & 3;
     }
-    __device__ __forceinline__ void put(uint8_t* to) const {
-#pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i, t = u / (S / 32), col = 32 * (u % (S / 32));
-            if (!mine(u)) continue;
-            const float step = mx4_step(s[i]);
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                v4u o;
-                o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i][h], step, 0));
-                o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i][h], step, 1));
-                o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i][h], step, 2));
-                o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i][h], step, 3));
-                *(v4u*)(to + t_at<S>(t, col + 8 * h)) = o;
-            }
-        }
+    __device__ __forceinline__ void fetch(int i) {
+        const int u = threadIdx.x + 256 * i, t = u / kPer, col = 8 * (u % kPer);
+        c[i] = __builtin_amdgcn_raw_buffer_load_b32(wc.r, t * (int)blocks * 16 + col / 2, 0, 0);
+        s[i] = __builtin_amdgcn_raw_buffer_load_b8(ws.r, off + t * (int)blocks + (col >> 5), 0, 0);
+    }
+    __device__ __forceinline__ void put(int i, uint8_t* to) const {
+        const int u = threadIdx.x + 256 * i;
+        const float step = mx4_step(s[i]);
+        v4u o;
+        o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], step, 0));
+        o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], step, 1));
+        o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], step, 2));
+        o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], step, 3));
+        *(v4u*)(to + t_at<S>(u / kPer, 8 * (u % kPer))) = o;
     }
 };
 
-// C tile of S x S, four wavefronts of S/2 x S/2.  blockIdx.z takes chunks [z * chunks, + chunks) of 64 t and writes its own C (and its
-// own sums of A over t, where `sums` is given).
+// every outstanding LDS operation of the wavefront, then the barrier; loads from memory stay in flight
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// C tile of S x S, four wavefronts of S/2 x S/2.  blockIdx.z takes t in [z * chunks * 32, + chunks * 32) and writes its own C (and its
+// own sums of A over t, where `sums` is given).  While the products of one 32 t run, the next 32 t go from registers to LDS and the
+// ones behind those into the registers, unit by unit; with three buffers the barrier lies two groups of products before the
+// end, and the next operands are read behind it.
 template <class A, class B, class T, int S>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 1)
     k_grad(A a, B b, T* __restrict__ out, int64_t ld, int64_t out_stride, float* __restrict__ sums, int64_t mn, int64_t cn, int64_t tn,
            int chunks) {
-    constexpr int P = A::P, H = S / 2, N = H / 16, kBuf = P * A::kPlane + B::kPlane;
+    constexpr int P = A::P, H = S / 2, N = H / 32, kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(kBuf);
+    constexpr int G = 2 * P * N;  // groups of N products: 16 t, part, row tile
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
     const int64_t m0 = (int64_t)blockIdx.x * S, c0 = (int64_t)blockIdx.y * S;
     const int wm = (wave & 1) * H, wc = (wave >> 1) * H;
-    int64_t t = (int64_t)blockIdx.z * chunks * 64;
-    if (t + (int64_t)chunks * 64 < tn) tn = t + (int64_t)chunks * 64;
-    const bool summing = sums && blockIdx.y == 0;
-    float total[8];
-    auto add = [&]() __attribute__((always_inline)) {
-        if constexpr (A::kTransposed) {
-            if (summing) {
-#pragma unroll
-                for (int i = 0; i < A::kUnits; ++i) {
-                    float v[8];
-                    a.in[i].get(v);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) total[j] += v[j];
-                }
-            }
-        }
-    };
-#pragma unroll
-    for (int j = 0; j < 8; ++j) total[j] = 0.0f;
-    v4f32 acc[N][N];
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int j = 0; j < N; ++j) acc[i][j] = v4f32{0, 0, 0, 0};
-    a.fetch(t, tn, m0, mn);
-    b.fetch(t, tn, c0);
-    a.put(lds);
-    b.put(lds + P * A::kPlane);
-    add();
-    __syncthreads();
-    int buf = 0;
-    for (; t < tn; t += 64) {
-        const bool more = t + 64 < tn;
-        if (more) {
-            a.fetch(t + 64, tn, m0, mn);
-            b.fetch(t + 64, tn, c0);
-        }
-        const uint8_t* const ta = lds + buf * kBuf;
-        const uint8_t* const tb = ta + P * A::kPlane;
-#pragma unroll
-        for (int k = 0; k < 64; k += 32) {
-            v8bf16 ob[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) ob[j] = t_operand<S>(tb, k, wc + 16 * j, lane);
-#pragma unroll
-            for (int p = P - 1; p >= 0; --p) {  // the smallest terms first
-                v8bf16 oa[N];
-#pragma unroll
-                for (int i = 0; i < N; ++i) oa[i] = A::operand(ta + p * A::kPlane, k, wm + 16 * i, lane);
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-#pragma unroll
-                    for (int j = 0; j < N; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ob[j], oa[i], acc[i][j], 0, 0, 0);
-            }
-        }
-        buf ^= 1;
-        if (more) {
-            a.put(lds + buf * kBuf);
-            b.put(lds + buf * kBuf + P * A::kPlane);
-            add();
-        }
-        __syncthreads();
-    }
-    out += blockIdx.z * out_stride;
-    const int r = lane & 15, g = lane >> 4;
+    const int64_t t_first = (int64_t)blockIdx.z * chunks * 32;
+    if (t_first + (int64_t)chunks * 32 < tn) tn = t_first + (int64_t)chunks * 32;
+    a.begin(m0, tn);
+    b.begin(c0);
+    v16f32 acc[N][N];
+    float acc_sum[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int64_t m = m0 + wm + 16 * i + r;
-        if (m >= mn) continue;
+        acc_sum[i] = 0.0f;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int64_t c = c0 + wc + 16 * j + 4 * g;
-            float v[4];
+        for (int j = 0; j < N; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e];
-            if (c < cn) store4(out + m * ld, c, cn, v);
-        }
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     }
-    if constexpr (A::kTransposed) {
-        if (summing) {  // 256 / (S / 8) threads have a piece of eight columns each
-            float* const red = (float*)lds;
+    auto at = [&](int64_t t) __attribute__((always_inline)) {  // where the next units are fetched
+        a.at(t);
+        b.at(t);
+    };
+    auto fetch_all = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) red[(threadIdx.x / (S / 8)) * S + 8 * (threadIdx.x % (S / 8)) + j] = total[j];
-            __syncthreads();
-            if (threadIdx.x < S && m0 + threadIdx.x < mn) {
-                float s = 0.0f;
+        for (int i = 0; i < A::kUnits; ++i) a.fetch(i);
 #pragma unroll
-                for (int i = 0; i < 2048 / S; ++i) s += red[i * S + threadIdx.x];
-                sums[blockIdx.z * mn + m0 + threadIdx.x] = s;
+        for (int i = 0; i < B::kUnits; ++i) b.fetch(i);
+    };
+    // group q: 16 t from 16 (q / (P N)), part P - 1 - q / N mod P (the smallest first), row tile q mod N
+    auto read_a = [&](const uint8_t* tile, int q) __attribute__((always_inline)) {
+        return A::operand(tile + (P - 1 - q / N % P) * A::kPlane, 16 * (q / (P * N)), wm + 32 * (q % N), lane);
+    };
+    auto read_b = [&](const uint8_t* tile, int j) __attribute__((always_inline)) {  // j: 16 t from 16 (j / N), column tile j mod N
+        return t_operand<S>(tile + P * A::kPlane, 16 * (j / N), wc + 32 * (j % N), lane);
+    };
+    auto run = [&](auto summing) __attribute__((always_inline)) {
+        constexpr bool kSumming = decltype(summing)::value;
+        const v2bf16 ones = __builtin_bit_cast(v2bf16, 0x3f803f80u);
+        at(t_first);
+        fetch_all();
+        at(t_first + 32);
+#pragma unroll
+        for (int i = 0; i < A::kUnits; ++i) a.put(i, lds);
+#pragma unroll
+        for (int i = 0; i < B::kUnits; ++i) b.put(i, lds + P * A::kPlane);
+        fetch_all();
+        lds_barrier();
+        v8bf16 ob[2 * N], oa;
+#pragma unroll
+        for (int j = 0; j < 2 * N; ++j) ob[j] = read_b(lds, j);
+        oa = read_a(lds, 0);
+        int now = 0;
+        for (int64_t t = t_first; t < tn; t += 32) {
+            const int then = now + 1 == kBufs ? 0 : now + 1;
+            const uint8_t* const tile = lds + now * kBuf;
+            uint8_t* const next = lds + then * kBuf;
+            at(t + 64);
+            v8bf16 ob_next[2 * N], oa_next;
+            constexpr int kTasks = A::kUnits + B::kUnits, kSlots = G > 2 ? G - 2 : 1;
+#pragma unroll
+            for (int q = 0; q < G; ++q) {
+                if (kBufs == 3 && q >= kSlots) {
+                    if (q == kSlots) lds_barrier();
+#pragma unroll
+                    for (int j = (q - kSlots) * 2 * N / (G - kSlots); j < (q - kSlots + 1) * 2 * N / (G - kSlots); ++j) ob_next[j] = read_b(next, j);
+                }
+                if (q + 1 < G) oa_next = read_a(tile, q + 1);
+                else if (kBufs == 3) oa_next = read_a(next, 0);
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    acc[q % N][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ob[q / (P * N) * N + j], oa, acc[q % N][j], 0, 0, 0);
+                if (kSumming) {
+                    const v4u w = __builtin_bit_cast(v4u, oa);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t pair = w[j];  // (a vector's element itself is not cast right: the first one is taken for all)
+                        acc_sum[q % N] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf16, pair), ones, acc_sum[q % N], false);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < kTasks; ++k)
+                    if (k * kSlots / kTasks == q) {
+                        if (k & 1 ? k / 2 < B::kUnits : k / 2 >= A::kUnits) {
+                            b.put(k / 2, next + P * A::kPlane);
+                            b.fetch(k / 2);
+                        } else {
+                            a.put(k / 2, next);
+                            a.fetch(k / 2);
+                        }
+                    }
+                oa = oa_next;
             }
+            if constexpr (kBufs == 3) {
+#pragma unroll
+                for (int j = 0; j < 2 * N; ++j) ob[j] = ob_next[j];
+            } else {
+                lds_barrier();
+#pragma unroll
+                for (int j = 0; j < 2 * N; ++j) ob[j] = read_b(next, j);
+                oa = read_a(next, 0);
+            }
+            now = then;
+        }
+    };
+    if constexpr (A::kSums) {
+        if (sums && blockIdx.y == 0) run(std::true_type());
+        else run(std::false_type());
+    } else {
+        run(std::false_type());
+    }
+    out += blockIdx.z * out_stride;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int64_t m = m0 + wm + 32 * i + r;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t c = c0 + wc + 32 * j + 8 * e + 4 * g;
+                const float v[4] = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+                if (m < mn && c < cn) store4(out + m * ld, c, cn, v);
+                __builtin_amdgcn_sched_barrier(0);  // (not all sums in vector registers at once)
+            }
+        if constexpr (A::kSums) {
+            const float s = acc_sum[i] + __shfl_xor(acc_sum[i], 32, 64);
+            if (sums && blockIdx.y == 0 && wc == 0 && g == 0 && m < mn) sums[blockIdx.z * mn + m] = s;
         }
     }
 }
 
-// the slices' results join, in their order: dw, and dy's sums behind it
-__global__ void __launch_bounds__(256) k_grad_join(const float* __restrict__ part, int slices, int64_t m, int64_t c, float* __restrict__ out,
+// the slices' results join, in their order, and are rounded; dy's sums behind them
+template <class T>
+__global__ void __launch_bounds__(256) k_grad_join(const float* __restrict__ part, int slices, int64_t m, int64_t c, T* __restrict__ out,
                                                    int64_t ld, const float* __restrict__ part_sums, float* __restrict__ sums) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i < m * c) {
         float s = 0.0f;
         for (int k = 0; k < slices; ++k) s += part[k * m * c + i];
-        out[i / c * ld + i % c] = s;
+        out[i / c * ld + i % c] = (T)s;
     } else if (sums && i < m * c + m) {
         float s = 0.0f;
         for (int k = 0; k < slices; ++k) s += part_sums[k * m + (i - m * c)];
@@ -327,23 +419,20 @@ __global__ void __launch_bounds__(256) k_grad_join(const float* __restrict__ par
     }
 }
 
-// how a product of m x c over t runs: tiles of S x S, z slices of t
+// how a product of m x c over t runs: tiles of s x s, z slices of `chunks` times 32 t
 struct Plan {
     int s, z, chunks;
 };
-Plan plan(int64_t m, int64_t c, int64_t t, bool split_t) {
-    auto tiles = [&](int64_t s) { return ((m + s - 1) / s) * ((c + s - 1) / s); };
+Plan plan(int64_t m, int64_t c, int64_t t) {
+    auto tiles = [&](int64_t s) { return ((m < 1 ? 1 : m) + s - 1) / s * ((c + s - 1) / s); };
+    const int64_t all = (t + 31) / 32;
     Plan p;
-    p.s = 128;
-    const int64_t all = (t + 63) / 64;
-    int64_t z = 1;
-    if (split_t) {
-        z = 512 / tiles(p.s);
-        if (z > all / 4) z = all / 4;
-        if (z < 1) z = 1;
-    } else if (tiles(128) < 256) {
-        p.s = 64;
-    }
+    p.s = 256;
+    if (tiles(256) * all < 256 * 16) p.s = 128;
+    if (p.s == 128 && tiles(128) * all < 256 * 8) p.s = 64;
+    int64_t z = 256 / tiles(p.s);
+    if (z > all / 4) z = all / 4;
+    if (z < 1) z = 1;
     p.chunks = (int)((all + z - 1) / z);
     p.z = p.chunks ? (int)((all + p.chunks - 1) / p.chunks) : 1;
     return p;
@@ -352,50 +441,85 @@ Plan plan(int64_t m, int64_t c, int64_t t, bool split_t) {
 template <class A, class B, class T, int S>
 aq_status launch(const A& a, const B& b, T* out, int64_t ld, int64_t stride, float* sums, int64_t m, int64_t c, int64_t t, const Plan& p,
                  hipStream_t st) {
-    constexpr int kLds = 2 * (A::P * A::kPlane + B::kPlane);
+    constexpr int kBuf = A::P * A::kPlane + B::kPlane, kLds = grad_buffers(kBuf) * kBuf;
+    const int64_t x = (m + S - 1) / S, y = (c + S - 1) / S;
+    if (!grid_ok(x, 256)) return AQ_ESHAPE;
     auto* const k = k_grad<A, B, T, S>;
     if (hip_failed(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds))) return AQ_EHIP;
-    k<<<dim3((unsigned)((m + S - 1) / S), (unsigned)((c + S - 1) / S), (unsigned)p.z), 256, kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks);
+    k<<<dim3((unsigned)x, (unsigned)y, (unsigned)p.z), 256, kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks);
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+}
+template <class T>
+aq_status join(const float* part, const Plan& p, int64_t m, int64_t c, T* out, int64_t ld, const float* part_sums, float* sums, hipStream_t st) {
+    const int64_t g = (m * c + m + 255) / 256;
+    if (!grid_ok(g, 256)) return AQ_ESHAPE;
+    k_grad_join<T><<<(unsigned)g, 256, 0, st>>>(part, p.z, m, c, out, ld, part_sums, sums);
+    return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+}
+template <class Go>
+aq_status with_tile(int s, Go&& go) {
+    if (s == 256) return go(std::integral_constant<int, 256>());
+    if (s == 128) return go(std::integral_constant<int, 128>());
+    return go(std::integral_constant<int, 64>());
+}
+// whether a matrix's pieces of eight values begin at whole words and, with `whole`, end with its rows
+template <class T>
+bool any_pieces(const aq_matrix& m, bool whole) {
+    return (sizeof(T) == 2 && ((uintptr_t)m.d & 3 || m.ld & 1)) || (whole && m.cols % 8);
 }
 
 }  // namespace
 
 int64_t weight_grad_workspace(int64_t rows, int64_t n, int64_t k) {
-    const Plan p = plan(n, k, rows, true);
+    const Plan p = plan(n, k, rows);
     return p.z > 1 ? p.z * (n * k + n) * (int64_t)sizeof(float) : 0;
 }
 
 aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq_matrix& dw, float* db, void* ws, hipStream_t st) {
     const int64_t n = dy.cols, k = kept.cols, rows = dy.rows;
-    const Plan p = plan(n, k, rows, true);
-    const bool join = p.z > 1;
-    float* const out = join ? (float*)ws : (float*)dw.d;
-    float* const sums = !db ? nullptr : join ? (float*)ws + p.z * n * k : db;
+    const Plan p = plan(n, k, rows);
+    const bool split_t = p.z > 1;
+    float* const out = split_t ? (float*)ws : (float*)dw.d;
+    float* const sums = !db ? nullptr : split_t ? (float*)ws + p.z * n * k : db;
     const aq_status s = with_dtype(dy.dtype, [&](auto t) {
         using T = decltype(t);
-        constexpr int S = 128;
-        return launch<DyRows<T, S>, KeptRows<S>, float, S>({(const T*)dy.d, dy.ld}, {(const uint8_t*)kept.d_codes, kept.d_scales, blocks32(k)}, out,
-                                                           join ? k : dw.ld, n * k, sums, n, k, rows, p, st);
+        return with_tile(p.s, [&](auto sc) {
+            constexpr int S = decltype(sc)::value;
+            const KeptRows<S> b{(const uint8_t*)kept.d_codes, kept.d_scales, blocks32(k), rows};
+            if constexpr (sizeof(T) == 2) {
+                if (any_pieces<T>(dy, false))
+                    return launch<DyRows<T, S, true>, KeptRows<S>, float, S>({words_of<T>(dy)}, b, out, split_t ? k : dw.ld, n * k, sums, n, k, rows, p, st);
+            }
+            return launch<DyRows<T, S, false>, KeptRows<S>, float, S>({words_of<T>(dy)}, b, out, split_t ? k : dw.ld, n * k, sums, n, k, rows, p, st);
+        });
     });
-    if (s != AQ_OK || !join) return s;
-    k_grad_join<<<(unsigned)((n * k + n + 255) / 256), 256, 0, st>>>((const float*)ws, p.z, n, k, (float*)dw.d, dw.ld, sums, db);
-    return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+    if (s != AQ_OK || !split_t) return s;
+    return join((const float*)ws, p, n, k, (float*)dw.d, dw.ld, sums, db, st);
 }
 
-int64_t input_grad_workspace(int64_t rows, int64_t n, int64_t k) { return 0; }
+int64_t input_grad_workspace(int64_t rows, int64_t n, int64_t k) {
+    const Plan p = plan(rows, k, n);
+    return p.z > 1 ? p.z * rows * k * (int64_t)sizeof(float) : 0;
+}
 
 aq_status launch_input_grad(const aq_matrix& dy, const aq_mx4& w, const aq_matrix& dx, void* ws, hipStream_t st) {
     const int64_t n = w.rows, k = w.cols, rows = dy.rows;
-    const Plan p = plan(rows, k, n, false);
+    const Plan p = plan(rows, k, n);
     return with_dtype(dy.dtype, [&](auto t) {
         using T = decltype(t);
-        auto go = [&](auto sc) {
+        const aq_status s = with_tile(p.s, [&](auto sc) {
             constexpr int S = decltype(sc)::value;
-            return launch<DyCols<T, S>, Mx4Rows<S>, T, S>({(const T*)dy.d, dy.ld}, {(const uint8_t*)w.d_codes, w.d_scales, blocks32(k)}, (T*)dx.d,
-                                                          dx.ld, 0, nullptr, rows, k, n, p, st);
-        };
-        return p.s == 64 ? go(std::integral_constant<int, 64>()) : go(std::integral_constant<int, 128>());
+            auto go = [&](auto edge) {
+                using A = DyCols<T, S, decltype(edge)::value>;
+                const A a{words_of<T>(dy)};
+                const Mx4Rows<S> b{(const uint8_t*)w.d_codes, w.d_scales, blocks32(k), n};
+                if (p.z > 1) return launch<A, Mx4Rows<S>, float, S>(a, b, (float*)ws, k, rows * k, nullptr, rows, k, n, p, st);
+                return launch<A, Mx4Rows<S>, T, S>(a, b, (T*)dx.d, dx.ld, 0, nullptr, rows, k, n, p, st);
+            };
+            return any_pieces<T>(dy, true) ? go(std::true_type()) : go(std::false_type());
+        });
+        if (s != AQ_OK || p.z == 1) return s;
+        return join((const float*)ws, p, rows, k, (T*)dx.d, dx.ld, nullptr, nullptr, st);
     });
 }
 

@@ -5,7 +5,7 @@ using namespace aq;
 
 namespace {
 
-constexpr int64_t kMostRows = 0x7fffffffLL, kMostCols = 1LL << 20;
+constexpr int64_t kMostRows = 0x7fffffffLL, kMostCols = 1LL << 20, kMostLd = 1LL << 21;
 
 hipStream_t as_stream(void* s) { return (hipStream_t)s; }
 
@@ -15,8 +15,7 @@ aq_status matrix_ok(const aq_matrix* m) {
     if (m->dtype != AQ_F32 && m->dtype != AQ_F16 && m->dtype != AQ_BF16) return AQ_EINVAL;
     if (!m->d && m->rows > 0) return AQ_EINVAL;
     if ((uintptr_t)m->d % dtype_bytes(m->dtype)) return AQ_EINVAL;
-    // (the last element's address stays within 63 bits)
-    if (m->rows > kMostRows || m->cols < 1 || m->cols > kMostCols || m->ld > (1LL << 30)) return AQ_ESHAPE;
+    if (m->rows > kMostRows || m->cols < 1 || m->cols > kMostCols || m->ld > kMostLd) return AQ_ESHAPE;
     return AQ_OK;
 }
 template <class Blocks32>

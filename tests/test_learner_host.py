@@ -19,7 +19,7 @@ def blk(rows, cols, codes=0x20000, scales=0x30001):
 BAD_MATRICES = [(None, B.EINVAL), (mat(4, 32, d=None), B.EINVAL), (mat(-1, 32), B.EINVAL), (mat(4, -1), B.EINVAL), (mat(4, 32, ld=31), B.EINVAL),
                 (mat(4, 32, dtype=3), B.EINVAL), (mat(4, 32, dtype=-1), B.EINVAL), (mat(4, 32, d=0x10002), B.EINVAL),
                 (mat(4, 32, dtype=2, d=0x10001), B.EINVAL), (mat(4, 0), B.ESHAPE), (mat(4, (1 << 20) + 1), B.ESHAPE),
-                (mat(1 << 31, 32), B.ESHAPE), (mat(4, 32, ld=(1 << 30) + 1), B.ESHAPE)]
+                (mat(1 << 31, 32), B.ESHAPE), (mat(4, 32, ld=(1 << 21) + 1), B.ESHAPE)]
 BAD_BLOCKS = [(None, B.EINVAL), (blk(4, 32, codes=None), B.EINVAL), (blk(4, 32, scales=None), B.EINVAL), (blk(4, 32, codes=0x20008), B.EINVAL),
               (blk(-1, 32), B.EINVAL), (blk(4, -1), B.EINVAL), (blk(4, 0), B.ESHAPE), (blk(4, (1 << 20) + 1), B.ESHAPE), (blk(1 << 31, 32), B.ESHAPE)]
 V = 0x40000  # a vector
