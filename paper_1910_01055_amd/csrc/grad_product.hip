@@ -114,34 +114,66 @@ __device__ __forceinline__ void load_piece(Piece<T>& q, const Window& w, int at)
 }
 template <class T, bool ANY>
 constexpr bool kOdd = ANY && sizeof(T) == 2;
+// Where a thread's units lie in a window, which move 32 t with every fetch.  After `turns` fetches of all units the window itself moves
+// on, so that no offset passes 31 bits.
+template <int U>
+struct Track {
+    Window w;
+    const uint8_t* base;
+    int64_t at, size;  // the window's beginning, a multiple of 4; what it may show, from base on
+    int step;          // bytes
+    int off[U];
+    __device__ __forceinline__ void begin(const uint8_t* b, int64_t first, int64_t bytes, int per_step) {
+        base = b;
+        at = first;
+        size = bytes;
+        step = per_step;
+        w.set(base, at, size);
+    }
+    __device__ __forceinline__ void move(int turns) {
+        at += (int64_t)turns * step;
+        w.set(base, at, size);
+#pragma unroll
+        for (int i = 0; i < U; ++i) off[i] -= turns * step;
+    }
+};
+// most turns for which offsets stay within 31 bits, some fetches ahead included
+inline int track_turns(int64_t step) { return (int)(0x7fffffff / step - 5); }
+
 // dy with t along the rows (weight gradient): [t][m].  ANY: rows of any alignment.
 template <class T, int S, bool ANY>
 struct DyRows {
-    static constexpr int P = kParts<T>, kUnits = S / 64, kPlane = 32 * 2 * S, kPer = S / 8;
+    static constexpr int P = kParts<T>, kUnits = S / 64, kPlane = 32 * 2 * S, kPer = S / 8, kSets = P == 1 ? 2 : 1;
     static constexpr bool kSums = true;
     Words d;
-    int64_t m0;
-    int off, left;
-    Window w;
-    Piece<T> in[kUnits];
-    __device__ __forceinline__ void begin(int64_t m, int64_t) { m0 = m; }
-    __device__ __forceinline__ void at(int64_t t0) {
+    Track<kUnits> k;
+    int left;
+    Piece<T> in[kSets][kUnits];
+    __device__ __forceinline__ void begin(int64_t m0, int64_t t0, int64_t t_end) {
         const int64_t byte = (t0 * d.ld + m0) * (int64_t)sizeof(T) + d.skew;
-        w.set(d.base, byte & ~(int64_t)3, d.size);
-        off = (int)byte & 3;
-        left = (int)(d.rows - t0 < 32 ? d.rows - t0 : 32);
+        const int64_t most = (t_end * d.ld * (int64_t)sizeof(T) + d.skew + 3) & ~(int64_t)3;  // (no row behind the slice's)
+        k.begin(d.base, byte & ~(int64_t)3, d.size < most ? d.size : most, 32 * (int)d.ld * (int)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const int u = threadIdx.x + 256 * i;
+            k.off[i] = ((int)byte & 3) + ((u / kPer) * (int)d.ld + 8 * (u % kPer)) * (int)sizeof(T);
+        }
+        left = (int)(t_end - t0) - threadIdx.x / kPer;
     }
-    __device__ __forceinline__ void fetch(int i) {
-        const int u = threadIdx.x + 256 * i;
-        int at = off + ((u / kPer) * (int)d.ld + 8 * (u % kPer)) * (int)sizeof(T);
-        // (the last word may hold what would be the first value of a row behind the last)
-        if (kOdd<T, ANY> && u / kPer >= left) at = Window::kOutside;
-        load_piece<T, kOdd<T, ANY>>(in[i], w, at);
+    __device__ __forceinline__ void move(int turns) { k.move(turns); }
+    __device__ __forceinline__ void fetch(int set, int i) {
+        int at = k.off[i];
+        k.off[i] += k.step;
+        if constexpr (kOdd<T, ANY>) {  // (the last word may hold what would be the first value of a row behind the last)
+            if (left <= 256 / kPer * i) at = Window::kOutside;
+            if (i == kUnits - 1) left -= 32;
+        }
+        load_piece<T, kOdd<T, ANY>>(in[set][i], k.w, at);
     }
-    __device__ __forceinline__ void put(int i, uint8_t* to) const {
+    __device__ __forceinline__ void put(int set, int i, uint8_t* to) const {
         const int u = threadIdx.x + 256 * i;
         v4u q[P];
-        split<T, P>(in[i], q);
+        split<T, P>(in[set][i], q);
 #pragma unroll
         for (int p = 0; p < P; ++p) *(v4u*)(to + p * kPlane + t_at<S>(u / kPer, 8 * (u % kPer))) = q[p];
     }
@@ -151,36 +183,40 @@ struct DyRows {
 // values are the next row's.
 template <class T, int S, bool ANY>
 struct DyCols {
-    static constexpr int P = kParts<T>, kUnits = S / 64, kPlane = 32 * 2 * S;
+    static constexpr int P = kParts<T>, kUnits = S / 64, kPlane = 32 * 2 * S, kSets = P == 1 ? 2 : 1;
     static constexpr bool kSums = false;
     Words d;
-    int64_t m0;
-    int tn, off, left, held;  // values that exist of the pieces that this thread fetches and of those that it puts
-    Window w;
-    Piece<T> in[kUnits];
-    __device__ __forceinline__ void begin(int64_t m, int64_t t_end) {
-        m0 = m;
-        tn = (int)t_end;
-    }
-    __device__ __forceinline__ void at(int64_t t0) {
+    Track<kUnits> k;
+    int left[kSets], next;  // values that exist of this thread's pieces
+    Piece<T> in[kSets][kUnits];
+    __device__ __forceinline__ void begin(int64_t m0, int64_t t0, int64_t t_end) {
         const int64_t byte = (m0 * d.ld + t0) * (int64_t)sizeof(T) + d.skew;
-        w.set(d.base, byte & ~(int64_t)3, d.size);
-        off = (int)byte & 3;
-        held = left;
-        left = tn - (int)t0 - 8 * (threadIdx.x & 3);
-    }
-    __device__ __forceinline__ void fetch(int i) {
-        const int u = threadIdx.x + 256 * i;
-        load_piece<T, kOdd<T, ANY>>(in[i], w, left > 0 ? off + ((u >> 2) * (int)d.ld + 8 * (u & 3)) * (int)sizeof(T) : Window::kOutside);
-    }
-    __device__ __forceinline__ void put(int i, uint8_t* to) const {
-        const int u = threadIdx.x + 256 * i;
-        Piece<T> own = in[i];
-        if constexpr (ANY) {
+        k.begin(d.base, byte & ~(int64_t)3, d.size, 32 * (int)sizeof(T));
 #pragma unroll
-            for (int k = 0; k < Piece<T>::kWords; ++k) {
-                if constexpr (sizeof(T) == 4) own.w[k] = k < held ? own.w[k] : 0;
-                else own.w[k] &= 2 * k + 1 < held ? 0xffffffffu : 2 * k < held ? 0xffffu : 0u;
+        for (int i = 0; i < kUnits; ++i) {
+            const int u = threadIdx.x + 256 * i;
+            k.off[i] = ((int)byte & 3) + ((u >> 2) * (int)d.ld + 8 * (u & 3)) * (int)sizeof(T);
+        }
+        next = (int)(t_end - t0) - 8 * (threadIdx.x & 3);
+    }
+    __device__ __forceinline__ void move(int turns) { k.move(turns); }
+    __device__ __forceinline__ void fetch(int set, int i) {
+        load_piece<T, kOdd<T, ANY>>(in[set][i], k.w, next > 0 ? k.off[i] : Window::kOutside);
+        k.off[i] += k.step;
+        if (i == kUnits - 1) {
+            left[set] = next;
+            next -= 32;
+        }
+    }
+    __device__ __forceinline__ void put(int set, int i, uint8_t* to) const {
+        const int u = threadIdx.x + 256 * i;
+        Piece<T> own = in[set][i];
+        if constexpr (ANY) {
+            const int n = left[set];
+#pragma unroll
+            for (int j = 0; j < Piece<T>::kWords; ++j) {
+                if constexpr (sizeof(T) == 4) own.w[j] = j < n ? own.w[j] : 0;
+                else own.w[j] &= 2 * j + 1 < n ? 0xffffffffu : 2 * j < n ? 0xffffu : 0u;
             }
         }
         v4u q[P];
@@ -192,70 +228,58 @@ struct DyCols {
         return *(const v8bf16*)(tile + m_at(m + (lane & 31), t0 / 8 + (lane >> 5)));
     }
 };
-// rows of the checkpoint
-template <int S>
-struct KeptRows {
+// rows of a checkpoint (CODE bytes of codes to eight values: 8) or of 4-bit weights (4)
+template <int S, int SETS, int CODE>
+struct BlockRows {
     static constexpr int kUnits = S / 64, kPlane = 32 * 2 * S, kPer = S / 8;
+    typedef typename std::conditional<CODE == 8, v2u, uint32_t>::type Codes;
     const uint8_t* codes;
     const uint8_t* scales;
     int64_t blocks, rows;
-    int64_t c0;
-    int off;
-    Window wc, ws;
-    v2u c[kUnits];
-    uint32_t s[kUnits];
-    __device__ __forceinline__ void begin(int64_t col) { c0 = col; }
-    __device__ __forceinline__ void at(int64_t t0) {
-        wc.set(codes, t0 * blocks * 32 + c0, rows * blocks * 32);
-        const int64_t byte = t0 * blocks + (c0 >> 5) + ((uintptr_t)scales & 3);
-        ws.set((const uint8_t*)((uintptr_t)scales & ~(uintptr_t)3), byte & ~(int64_t)3, rows * blocks + ((uintptr_t)scales & 3));
-        off = (int)byte & 3;
+    Track<kUnits> kc, ks;
+    Codes c[SETS][kUnits];
+    uint32_t s[SETS][kUnits];
+    __device__ __forceinline__ void begin(int64_t c0, int64_t t0, int64_t t_end) {
+        const int64_t last = rows < t_end ? rows : t_end;
+        const int skew = (int)((uintptr_t)scales & 3);
+        const int64_t byte = t0 * blocks + (c0 >> 5) + skew;
+        kc.begin(codes, (t0 * blocks * 4 + c0 / 8) * CODE, last * blocks * 4 * CODE, 32 * (int)blocks * 4 * CODE);
+        ks.begin(scales - skew, byte & ~(int64_t)3, last * blocks + skew, 32 * (int)blocks);
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const int u = threadIdx.x + 256 * i, t = u / kPer, piece = u % kPer;
+            kc.off[i] = (t * (int)blocks * 4 + piece) * CODE;
+            ks.off[i] = ((int)byte & 3) + t * (int)blocks + (piece >> 2);
+        }
     }
-    __device__ __forceinline__ void fetch(int i) {
-        const int u = threadIdx.x + 256 * i, t = u / kPer, col = 8 * (u % kPer);
-        c[i] = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(wc.r, t * (int)blocks * 32 + col, 0, 0));
-        s[i] = __builtin_amdgcn_raw_buffer_load_b8(ws.r, off + t * (int)blocks + (col >> 5), 0, 0);
+    __device__ __forceinline__ void move(int turns) {
+        kc.move(turns);
+        ks.move(turns);
     }
-    __device__ __forceinline__ void put(int i, uint8_t* to) const {
+    __device__ __forceinline__ void fetch(int set, int i) {
+        if constexpr (CODE == 8) c[set][i] = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(kc.w.r, kc.off[i], 0, 0));
+        else c[set][i] = __builtin_amdgcn_raw_buffer_load_b32(kc.w.r, kc.off[i], 0, 0);
+        s[set][i] = __builtin_amdgcn_raw_buffer_load_b8(ks.w.r, ks.off[i], 0, 0);
+        kc.off[i] += kc.step;
+        ks.off[i] += ks.step;
+    }
+    __device__ __forceinline__ void put(int set, int i, uint8_t* to) const {
         const int u = threadIdx.x + 256 * i;
-        float v[8];
-        ckpt8_values(c[i], ckpt8_step(s[i]), v);
-        Piece<bf16_t> o;
-        o.set(v);
-        *(v4u*)(to + t_at<S>(u / kPer, 8 * (u % kPer))) = v4u{o.w[0], o.w[1], o.w[2], o.w[3]};
-    }
-};
-// rows of 4-bit weights
-template <int S>
-struct Mx4Rows {
-    static constexpr int kUnits = S / 64, kPlane = 32 * 2 * S, kPer = S / 8;
-    const uint8_t* codes;
-    const uint8_t* scales;
-    int64_t blocks, rows;
-    int64_t c0;
-    int off;
-    Window wc, ws;
-    uint32_t c[kUnits], s[kUnits];
-    __device__ __forceinline__ void begin(int64_t col) { c0 = col; }
-    __device__ __forceinline__ void at(int64_t t0) {
-        wc.set(codes, t0 * blocks * 16 + c0 / 2, rows * blocks * 16);
-        const int64_t byte = t0 * blocks + (c0 >> 5) + ((uintptr_t)scales & 3);
-        ws.set((const uint8_t*)((uintptr_t)scales & ~(uintptr_t)3), byte & ~(int64_t)3, rows * blocks + ((uintptr_t)scales & 3));
-        off = (int)byte & 3;
-    }
-    __device__ __forceinline__ void fetch(int i) {
-        const int u = threadIdx.x + 256 * i, t = u / kPer, col = 8 * (u % kPer);
-        c[i] = __builtin_amdgcn_raw_buffer_load_b32(wc.r, t * (int)blocks * 16 + col / 2, 0, 0);
-        s[i] = __builtin_amdgcn_raw_buffer_load_b8(ws.r, off + t * (int)blocks + (col >> 5), 0, 0);
-    }
-    __device__ __forceinline__ void put(int i, uint8_t* to) const {
-        const int u = threadIdx.x + 256 * i;
-        const float step = mx4_step(s[i]);
         v4u o;
-        o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], step, 0));
-        o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], step, 1));
-        o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], step, 2));
-        o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[i], step, 3));
+        if constexpr (CODE == 8) {
+            float v[8];
+            ckpt8_values(c[set][i], ckpt8_step(s[set][i]), v);
+            Piece<bf16_t> q;
+            q.set(v);
+            o = v4u{q.w[0], q.w[1], q.w[2], q.w[3]};
+        } else {
+            const float step = mx4_step(s[set][i]);
+            const uint32_t w = c[set][i];
+            o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, step, 0));
+            o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, step, 1));
+            o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, step, 2));
+            o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, step, 3));
+        }
         *(v4u*)(to + t_at<S>(u / kPer, 8 * (u % kPer))) = o;
     }
 };
@@ -264,13 +288,13 @@ struct Mx4Rows {
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // C tile of S x S, four wavefronts of S/2 x S/2.  blockIdx.z takes t in [z * chunks * 32, + chunks * 32) and writes its own C (and its
-// own sums of A over t, where `sums` is given).  While the products of one 32 t run, the next 32 t go from registers to LDS and the
-// ones behind those into the registers, unit by unit; with three buffers the barrier lies two groups of products before the
-// end, and the next operands are read behind it.
+// own sums of A over t, where `sums` is given).  While the products of one 32 t run, the next 32 t go from registers to LDS, unit
+// by unit, and one or two more are on their way from memory behind them; with three buffers the barrier lies
+// two groups of products before the end, and the next operands are read behind it.
 template <class A, class B, class T, int S>
 __global__ void __launch_bounds__(256, 1)
     k_grad(A a, B b, T* __restrict__ out, int64_t ld, int64_t out_stride, float* __restrict__ sums, int64_t mn, int64_t cn, int64_t tn,
-           int chunks) {
+           int chunks, int turns) {
     constexpr int P = A::P, H = S / 2, N = H / 32, kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(kBuf);
     constexpr int G = 2 * P * N;  // groups of N products: 16 t, part, row tile
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -279,8 +303,8 @@ __global__ void __launch_bounds__(256, 1)
     const int wm = (wave & 1) * H, wc = (wave >> 1) * H;
     const int64_t t_first = (int64_t)blockIdx.z * chunks * 32;
     if (t_first + (int64_t)chunks * 32 < tn) tn = t_first + (int64_t)chunks * 32;
-    a.begin(m0, tn);
-    b.begin(c0);
+    a.begin(m0, t_first, tn);
+    b.begin(c0, t_first, tn);
     v16f32 acc[N][N];
     float acc_sum[N];
 #pragma unroll
@@ -291,15 +315,12 @@ __global__ void __launch_bounds__(256, 1)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     }
-    auto at = [&](int64_t t) __attribute__((always_inline)) {  // where the next units are fetched
-        a.at(t);
-        b.at(t);
-    };
-    auto fetch_all = [&]() __attribute__((always_inline)) {
+    auto fetch_all = [&](int set) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < A::kUnits; ++i) a.fetch(i);
-#pragma unroll
-        for (int i = 0; i < B::kUnits; ++i) b.fetch(i);
+        for (int i = 0; i < A::kUnits; ++i) {
+            a.fetch(set, i);
+            b.fetch(set, i);
+        }
     };
     // group q: 16 t from 16 (q / (P N)), part P - 1 - q / N mod P (the smallest first), row tile q mod N
     auto read_a = [&](const uint8_t* tile, int q) __attribute__((always_inline)) {
@@ -311,27 +332,27 @@ __global__ void __launch_bounds__(256, 1)
     auto run = [&](auto summing) __attribute__((always_inline)) {
         constexpr bool kSumming = decltype(summing)::value;
         const v2bf16 ones = __builtin_bit_cast(v2bf16, 0x3f803f80u);
-        at(t_first);
-        fetch_all();
-        at(t_first + 32);
 #pragma unroll
-        for (int i = 0; i < A::kUnits; ++i) a.put(i, lds);
+        for (int i = 0; i < A::kSets; ++i) fetch_all(i);
 #pragma unroll
-        for (int i = 0; i < B::kUnits; ++i) b.put(i, lds + P * A::kPlane);
-        fetch_all();
+        for (int i = 0; i < A::kUnits; ++i) {
+            a.put(0, i, lds);
+            b.put(0, i, lds + P * A::kPlane);
+        }
+        fetch_all(0);
         lds_barrier();
         v8bf16 ob[2 * N], oa;
 #pragma unroll
         for (int j = 0; j < 2 * N; ++j) ob[j] = read_b(lds, j);
         oa = read_a(lds, 0);
         int now = 0;
-        for (int64_t t = t_first; t < tn; t += 32) {
-            const int then = now + 1 == kBufs ? 0 : now + 1;
-            const uint8_t* const tile = lds + now * kBuf;
-            uint8_t* const next = lds + then * kBuf;
-            at(t + 64);
+        auto step = [&](auto then) __attribute__((always_inline)) {
+            constexpr int kThen = decltype(then)::value;  // the set that holds the next 32 t
+            const uint8_t* const tile = lds + now;
+            now = now + kBuf == kBufs * kBuf ? 0 : now + kBuf;
+            uint8_t* const next = lds + now;
             v8bf16 ob_next[2 * N], oa_next;
-            constexpr int kTasks = A::kUnits + B::kUnits, kSlots = G > 2 ? G - 2 : 1;
+            constexpr int kTasks = 2 * A::kUnits, kSlots = G > 2 ? G - 2 : 1;
 #pragma unroll
             for (int q = 0; q < G; ++q) {
                 if (kBufs == 3 && q >= kSlots) {
@@ -355,15 +376,16 @@ __global__ void __launch_bounds__(256, 1)
 #pragma unroll
                 for (int k = 0; k < kTasks; ++k)
                     if (k * kSlots / kTasks == q) {
-                        if (k & 1 ? k / 2 < B::kUnits : k / 2 >= A::kUnits) {
-                            b.put(k / 2, next + P * A::kPlane);
-                            b.fetch(k / 2);
+                        if (k & 1) {
+                            b.put(kThen, k / 2, next + P * A::kPlane);
+                            b.fetch(kThen, k / 2);
                         } else {
-                            a.put(k / 2, next);
-                            a.fetch(k / 2);
+                            a.put(kThen, k / 2, next);
+                            a.fetch(kThen, k / 2);
                         }
                     }
                 oa = oa_next;
+                __builtin_amdgcn_sched_barrier(0);  // (loads stay in the order in which they are waited for)
             }
             if constexpr (kBufs == 3) {
 #pragma unroll
@@ -374,7 +396,16 @@ __global__ void __launch_bounds__(256, 1)
                 for (int j = 0; j < 2 * N; ++j) ob[j] = read_b(next, j);
                 oa = read_a(next, 0);
             }
-            now = then;
+        };
+        int to_move = turns;
+        for (int left = (int)(tn - t_first); left > 0; left -= 64) {  // (32 t behind the end are zeros)
+            step(std::integral_constant<int, A::kSets - 1>());
+            step(std::integral_constant<int, 0>());
+            if ((to_move -= 2) <= 0) {
+                a.move(turns);
+                b.move(turns);
+                to_move = turns;
+            }
         }
     };
     if constexpr (A::kSums) {
@@ -419,7 +450,7 @@ __global__ void __launch_bounds__(256) k_grad_join(const float* __restrict__ par
     }
 }
 
-// how a product of m x c over t runs: tiles of s x s, z slices of `chunks` times 32 t
+// how a product of m x c over t runs: tiles of s x s, z slices of `chunks` (an even number) times 32 t
 struct Plan {
     int s, z, chunks;
 };
@@ -433,20 +464,20 @@ Plan plan(int64_t m, int64_t c, int64_t t) {
     int64_t z = 256 / tiles(p.s);
     if (z > all / 4) z = all / 4;
     if (z < 1) z = 1;
-    p.chunks = (int)((all + z - 1) / z);
+    p.chunks = (int)((all + z - 1) / z + 1) & ~1;
     p.z = p.chunks ? (int)((all + p.chunks - 1) / p.chunks) : 1;
     return p;
 }
 
 template <class A, class B, class T, int S>
 aq_status launch(const A& a, const B& b, T* out, int64_t ld, int64_t stride, float* sums, int64_t m, int64_t c, int64_t t, const Plan& p,
-                 hipStream_t st) {
+                 int64_t bytes_per_t, hipStream_t st) {
     constexpr int kBuf = A::P * A::kPlane + B::kPlane, kLds = grad_buffers(kBuf) * kBuf;
     const int64_t x = (m + S - 1) / S, y = (c + S - 1) / S;
     if (!grid_ok(x, 256)) return AQ_ESHAPE;
     auto* const k = k_grad<A, B, T, S>;
     if (hip_failed(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds))) return AQ_EHIP;
-    k<<<dim3((unsigned)x, (unsigned)y, (unsigned)p.z), 256, kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks);
+    k<<<dim3((unsigned)x, (unsigned)y, (unsigned)p.z), 256, kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks, track_turns(32 * bytes_per_t) & ~1);
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }
 template <class T>
@@ -484,13 +515,14 @@ aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq
     const aq_status s = with_dtype(dy.dtype, [&](auto t) {
         using T = decltype(t);
         return with_tile(p.s, [&](auto sc) {
-            constexpr int S = decltype(sc)::value;
-            const KeptRows<S> b{(const uint8_t*)kept.d_codes, kept.d_scales, blocks32(k), rows};
+            constexpr int S = decltype(sc)::value, kSets = DyRows<T, S, false>::kSets;
+            const int64_t code_bytes = 32 * blocks32(k), dy_bytes = dy.ld * (int64_t)sizeof(T), bytes_per_t = dy_bytes > code_bytes ? dy_bytes : code_bytes;
+            const BlockRows<S, kSets, 8> b{(const uint8_t*)kept.d_codes, kept.d_scales, blocks32(k), rows};
             if constexpr (sizeof(T) == 2) {
                 if (any_pieces<T>(dy, false))
-                    return launch<DyRows<T, S, true>, KeptRows<S>, float, S>({words_of<T>(dy)}, b, out, split_t ? k : dw.ld, n * k, sums, n, k, rows, p, st);
+                    return launch<DyRows<T, S, true>, BlockRows<S, kSets, 8>, float, S>({words_of<T>(dy)}, b, out, split_t ? k : dw.ld, n * k, sums, n, k, rows, p, bytes_per_t, st);
             }
-            return launch<DyRows<T, S, false>, KeptRows<S>, float, S>({words_of<T>(dy)}, b, out, split_t ? k : dw.ld, n * k, sums, n, k, rows, p, st);
+            return launch<DyRows<T, S, false>, BlockRows<S, kSets, 8>, float, S>({words_of<T>(dy)}, b, out, split_t ? k : dw.ld, n * k, sums, n, k, rows, p, bytes_per_t, st);
         });
     });
     if (s != AQ_OK || !split_t) return s;
@@ -511,10 +543,11 @@ aq_status launch_input_grad(const aq_matrix& dy, const aq_mx4& w, const aq_matri
             constexpr int S = decltype(sc)::value;
             auto go = [&](auto edge) {
                 using A = DyCols<T, S, decltype(edge)::value>;
+                constexpr int kSets = A::kSets;
                 const A a{words_of<T>(dy)};
-                const Mx4Rows<S> b{(const uint8_t*)w.d_codes, w.d_scales, blocks32(k), n};
-                if (p.z > 1) return launch<A, Mx4Rows<S>, float, S>(a, b, (float*)ws, k, rows * k, nullptr, rows, k, n, p, st);
-                return launch<A, Mx4Rows<S>, T, S>(a, b, (T*)dx.d, dx.ld, 0, nullptr, rows, k, n, p, st);
+                const BlockRows<S, kSets, 4> b{(const uint8_t*)w.d_codes, w.d_scales, blocks32(k), n};
+                if (p.z > 1) return launch<A, BlockRows<S, kSets, 4>, float, S>(a, b, (float*)ws, k, rows * k, nullptr, rows, k, n, p, 16 * blocks32(k), st);
+                return launch<A, BlockRows<S, kSets, 4>, T, S>(a, b, (T*)dx.d, dx.ld, 0, nullptr, rows, k, n, p, 16 * blocks32(k), st);
             };
             return any_pieces<T>(dy, true) ? go(std::true_type()) : go(std::false_type());
         });

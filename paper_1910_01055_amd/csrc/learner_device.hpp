@@ -148,8 +148,8 @@ __device__ __forceinline__ v2u ckpt8_codes(const float (&v)[8], uint32_t scale) 
 }
 // what one code step stands for, 2^(scale - 133); a NaN for 255
 __device__ __forceinline__ float ckpt8_step(uint32_t scale) {
-    const float s = __uint_as_float(scale == 255 ? 0x7fc00000u : scale << 23);  // 2^(scale - 127), but scale 0
-    return scale == 0 ? 0x1p-133f : s * 0x1p-6f;
+    const float s = __builtin_amdgcn_ldexpf(1.0f, (int)scale - 133);
+    return scale == 255 ? __uint_as_float(0x7fc00000u) : s;
 }
 __device__ __forceinline__ void ckpt8_values(v2u c, float step, float (&v)[8]) {
 #pragma unroll
