@@ -17,6 +17,8 @@ namespace {
 typedef short v4s16 __attribute__((ext_vector_type(4)));
 typedef float v16f32 __attribute__((ext_vector_type(16)));
 
+// Threads of a workgroup with tiles of S x S: wavefronts two by four, or two by two.
+constexpr int grad_threads(int s) { return s == 256 ? 512 : 256; }
 constexpr int kMostLds = 160 * 1024;
 constexpr int grad_buffers(int bytes) { return 3 * bytes <= kMostLds ? 3 : 2; }
 
@@ -68,7 +70,7 @@ __device__ __forceinline__ v8bf16 t_operand(const uint8_t* tile, int t0, int col
 // [row m][32 t]: 16-byte pieces, piece p of row m in place p ^ (m / 4 mod 4)
 __device__ __forceinline__ int m_at(int m, int piece) { return m * 64 + ((piece ^ ((m >> 2) & 3)) << 4); }
 
-// ---- the operands.  Of 32 t and S columns (or rows) each thread fetches S / 64 units of eight values into registers and later puts them
+// ---- the operands.  Of 32 t and S columns (or rows) each thread fetches kUnits units of eight values into registers and later puts them
 // into LDS as bf16.  Loads go through windows on the matrix that begin at the workgroup's first row: what lies behind the
 // matrix's end comes as zeros, without a branch.  Columns of an operand that do not exist only reach results that are not stored.
 struct Window {
@@ -143,7 +145,7 @@ inline int track_turns(int64_t step) { return (int)(0x7fffffff / step - 5); }
 // dy with t along the rows (weight gradient): [t][m].  ANY: rows of any alignment.
 template <class T, int S, bool ANY>
 struct DyRows {
-    static constexpr int P = kParts<T>, kUnits = S / 64, kPlane = 32 * 2 * S, kPer = S / 8, kSets = P == 1 ? 2 : 1;
+    static constexpr int P = kParts<T>, NT = grad_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kPer = S / 8, kSets = P == 1 ? 2 : 1;
     static constexpr bool kSums = true;
     Words d;
     Track<kUnits> k;
@@ -155,7 +157,7 @@ struct DyRows {
         k.begin(d.base, byte & ~(int64_t)3, d.size < most ? d.size : most, 32 * (int)d.ld * (int)sizeof(T));
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i;
+            const int u = threadIdx.x + NT * i;
             k.off[i] = ((int)byte & 3) + ((u / kPer) * (int)d.ld + 8 * (u % kPer)) * (int)sizeof(T);
         }
         left = (int)(t_end - t0) - threadIdx.x / kPer;
@@ -165,13 +167,13 @@ struct DyRows {
         int at = k.off[i];
         k.off[i] += k.step;
         if constexpr (kOdd<T, ANY>) {  // (the last word may hold what would be the first value of a row behind the last)
-            if (left <= 256 / kPer * i) at = Window::kOutside;
+            if (left <= NT / kPer * i) at = Window::kOutside;
             if (i == kUnits - 1) left -= 32;
         }
         load_piece<T, kOdd<T, ANY>>(in[set][i], k.w, at);
     }
     __device__ __forceinline__ void put(int set, int i, uint8_t* to) const {
-        const int u = threadIdx.x + 256 * i;
+        const int u = threadIdx.x + NT * i;
         v4u q[P];
         split<T, P>(in[set][i], q);
 #pragma unroll
@@ -183,7 +185,7 @@ struct DyRows {
 // values are the next row's.
 template <class T, int S, bool ANY>
 struct DyCols {
-    static constexpr int P = kParts<T>, kUnits = S / 64, kPlane = 32 * 2 * S, kSets = P == 1 ? 2 : 1;
+    static constexpr int P = kParts<T>, NT = grad_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kSets = P == 1 ? 2 : 1;
     static constexpr bool kSums = false;
     Words d;
     Track<kUnits> k;
@@ -194,7 +196,7 @@ struct DyCols {
         k.begin(d.base, byte & ~(int64_t)3, d.size, 32 * (int)sizeof(T));
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i;
+            const int u = threadIdx.x + NT * i;
             k.off[i] = ((int)byte & 3) + ((u >> 2) * (int)d.ld + 8 * (u & 3)) * (int)sizeof(T);
         }
         next = (int)(t_end - t0) - 8 * (threadIdx.x & 3);
@@ -209,7 +211,7 @@ struct DyCols {
         }
     }
     __device__ __forceinline__ void put(int set, int i, uint8_t* to) const {
-        const int u = threadIdx.x + 256 * i;
+        const int u = threadIdx.x + NT * i;
         Piece<T> own = in[set][i];
         if constexpr (ANY) {
             const int n = left[set];
@@ -231,7 +233,7 @@ struct DyCols {
 // rows of a checkpoint (CODE bytes of codes to eight values: 8) or of 4-bit weights (4)
 template <int S, int SETS, int CODE>
 struct BlockRows {
-    static constexpr int kUnits = S / 64, kPlane = 32 * 2 * S, kPer = S / 8;
+    static constexpr int NT = grad_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kPer = S / 8;
     typedef typename std::conditional<CODE == 8, v2u, uint32_t>::type Codes;
     const uint8_t* codes;
     const uint8_t* scales;
@@ -247,7 +249,7 @@ struct BlockRows {
         ks.begin(scales - skew, byte & ~(int64_t)3, last * blocks + skew, 32 * (int)blocks);
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + 256 * i, t = u / kPer, piece = u % kPer;
+            const int u = threadIdx.x + NT * i, t = u / kPer, piece = u % kPer;
             kc.off[i] = (t * (int)blocks * 4 + piece) * CODE;
             ks.off[i] = ((int)byte & 3) + t * (int)blocks + (piece >> 2);
         }
@@ -264,7 +266,7 @@ struct BlockRows {
         ks.off[i] += ks.step;
     }
     __device__ __forceinline__ void put(int set, int i, uint8_t* to) const {
-        const int u = threadIdx.x + 256 * i;
+        const int u = threadIdx.x + NT * i;
         v4u o;
         if constexpr (CODE == 8) {
             float v[8];
@@ -287,31 +289,46 @@ struct BlockRows {
 // every outstanding LDS operation of the wavefront, then the barrier; loads from memory stay in flight
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// C tile of S x S, four wavefronts of S/2 x S/2.  blockIdx.z takes t in [z * chunks * 32, + chunks * 32) and writes its own C (and its
+// Which tile and slice a workgroup takes.  Workgroups go to the 8 XCDs, each with an L2 of its own, in turn: every eighth of them
+// gets one eighth of all places in a row, and places go along four rows of tiles at once, so that an XCD's workgroups
+// read few different rows and columns (65536 x 2048 x 2048, 64 tiles by 4 slices: XX against XX us with places in order).
+struct Place {
+    uint32_t m, c, z;
+};
+__device__ __forceinline__ Place place_of_workgroup(uint32_t gm, uint32_t gc) {
+    const uint32_t all = gridDim.x, xcd = blockIdx.x % 8, each = all / 8, more = all % 8;
+    const uint32_t p = xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8;
+    const uint32_t z = p / (gm * gc), tile = p % (gm * gc), strip = tile / (4 * gc), in = tile % (4 * gc);
+    const uint32_t high = gm - 4 * strip < 4 ? gm - 4 * strip : 4;
+    return {4 * strip + in % high, in / high, z};
+}
+
+// C tile of S x S, a wavefront takes S / 2 rows and NC * 32 columns of it.  Slice z takes t in [z * chunks * 32, + chunks * 32) and writes its own C (and its
 // own sums of A over t, where `sums` is given).  While the products of one 32 t run, the next 32 t go from registers to LDS, unit
 // by unit, and one or two more are on their way from memory behind them; with three buffers the barrier lies
 // two groups of products before the end, and the next operands are read behind it.
 template <class A, class B, class T, int S>
-__global__ void __launch_bounds__(256, 1)
+__global__ void __launch_bounds__(grad_threads(S), 1)
     k_grad(A a, B b, T* __restrict__ out, int64_t ld, int64_t out_stride, float* __restrict__ sums, int64_t mn, int64_t cn, int64_t tn,
            int chunks, int turns) {
-    constexpr int P = A::P, H = S / 2, N = H / 32, kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(kBuf);
-    constexpr int G = 2 * P * N;  // groups of N products: 16 t, part, row tile
+    constexpr int P = A::P, NT = grad_threads(S), N = S / 64, NC = S / (NT / 128) / 32, kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(kBuf);
+    constexpr int G = 2 * P * N;  // groups of NC products: 16 t, part, row tile
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
-    const int64_t m0 = (int64_t)blockIdx.x * S, c0 = (int64_t)blockIdx.y * S;
-    const int wm = (wave & 1) * H, wc = (wave >> 1) * H;
-    const int64_t t_first = (int64_t)blockIdx.z * chunks * 32;
+    const Place at = place_of_workgroup((uint32_t)((mn + S - 1) / S), (uint32_t)((cn + S - 1) / S));
+    const int64_t m0 = (int64_t)at.m * S, c0 = (int64_t)at.c * S;
+    const int wm = (wave & 1) * (S / 2), wc = (wave >> 1) * (32 * NC);
+    const int64_t t_first = (int64_t)at.z * chunks * 32;
     if (t_first + (int64_t)chunks * 32 < tn) tn = t_first + (int64_t)chunks * 32;
     a.begin(m0, t_first, tn);
     b.begin(c0, t_first, tn);
-    v16f32 acc[N][N];
+    v16f32 acc[N][NC];
     float acc_sum[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         acc_sum[i] = 0.0f;
 #pragma unroll
-        for (int j = 0; j < N; ++j)
+        for (int j = 0; j < NC; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     }
@@ -326,11 +343,11 @@ __global__ void __launch_bounds__(256, 1)
     auto read_a = [&](const uint8_t* tile, int q) __attribute__((always_inline)) {
         return A::operand(tile + (P - 1 - q / N % P) * A::kPlane, 16 * (q / (P * N)), wm + 32 * (q % N), lane);
     };
-    auto read_b = [&](const uint8_t* tile, int j) __attribute__((always_inline)) {  // j: 16 t from 16 (j / N), column tile j mod N
-        return t_operand<S>(tile + P * A::kPlane, 16 * (j / N), wc + 32 * (j % N), lane);
+    auto read_b = [&](const uint8_t* tile, int j) __attribute__((always_inline)) {  // j: 16 t from 16 (j / NC), column tile j mod NC
+        return t_operand<S>(tile + P * A::kPlane, 16 * (j / NC), wc + 32 * (j % NC), lane);
     };
-    auto run = [&](auto summing) __attribute__((always_inline)) {
-        constexpr bool kSumming = decltype(summing)::value;
+    const bool summing = A::kSums && sums && at.c == 0 && wave < 2;  // (wavefronts 0 and 1 have all rows between them)
+    {
         const v2bf16 ones = __builtin_bit_cast(v2bf16, 0x3f803f80u);
 #pragma unroll
         for (int i = 0; i < A::kSets; ++i) fetch_all(i);
@@ -341,9 +358,9 @@ __global__ void __launch_bounds__(256, 1)
         }
         fetch_all(0);
         lds_barrier();
-        v8bf16 ob[2 * N], oa;
+        v8bf16 ob[2 * NC], oa;
 #pragma unroll
-        for (int j = 0; j < 2 * N; ++j) ob[j] = read_b(lds, j);
+        for (int j = 0; j < 2 * NC; ++j) ob[j] = read_b(lds, j);
         oa = read_a(lds, 0);
         int now = 0;
         auto step = [&](auto then) __attribute__((always_inline)) {
@@ -351,21 +368,21 @@ __global__ void __launch_bounds__(256, 1)
             const uint8_t* const tile = lds + now;
             now = now + kBuf == kBufs * kBuf ? 0 : now + kBuf;
             uint8_t* const next = lds + now;
-            v8bf16 ob_next[2 * N], oa_next;
+            v8bf16 ob_next[2 * NC], oa_next;
             constexpr int kTasks = 2 * A::kUnits, kSlots = G > 2 ? G - 2 : 1;
 #pragma unroll
             for (int q = 0; q < G; ++q) {
                 if (kBufs == 3 && q >= kSlots) {
                     if (q == kSlots) lds_barrier();
 #pragma unroll
-                    for (int j = (q - kSlots) * 2 * N / (G - kSlots); j < (q - kSlots + 1) * 2 * N / (G - kSlots); ++j) ob_next[j] = read_b(next, j);
+                    for (int j = (q - kSlots) * 2 * NC / (G - kSlots); j < (q - kSlots + 1) * 2 * NC / (G - kSlots); ++j) ob_next[j] = read_b(next, j);
                 }
                 if (q + 1 < G) oa_next = read_a(tile, q + 1);
                 else if (kBufs == 3) oa_next = read_a(next, 0);
 #pragma unroll
-                for (int j = 0; j < N; ++j)
-                    acc[q % N][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ob[q / (P * N) * N + j], oa, acc[q % N][j], 0, 0, 0);
-                if (kSumming) {
+                for (int j = 0; j < NC; ++j)
+                    acc[q % N][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ob[q / (P * N) * NC + j], oa, acc[q % N][j], 0, 0, 0);
+                if (summing) {
                     const v4u w = __builtin_bit_cast(v4u, oa);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -389,11 +406,11 @@ __global__ void __launch_bounds__(256, 1)
             }
             if constexpr (kBufs == 3) {
 #pragma unroll
-                for (int j = 0; j < 2 * N; ++j) ob[j] = ob_next[j];
+                for (int j = 0; j < 2 * NC; ++j) ob[j] = ob_next[j];
             } else {
                 lds_barrier();
 #pragma unroll
-                for (int j = 0; j < 2 * N; ++j) ob[j] = read_b(next, j);
+                for (int j = 0; j < 2 * NC; ++j) ob[j] = read_b(next, j);
                 oa = read_a(next, 0);
             }
         };
@@ -407,19 +424,13 @@ __global__ void __launch_bounds__(256, 1)
                 to_move = turns;
             }
         }
-    };
-    if constexpr (A::kSums) {
-        if (sums && blockIdx.y == 0) run(std::true_type());
-        else run(std::false_type());
-    } else {
-        run(std::false_type());
     }
-    out += blockIdx.z * out_stride;
+    out += at.z * out_stride;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int64_t m = m0 + wm + 32 * i + r;
 #pragma unroll
-        for (int j = 0; j < N; ++j)
+        for (int j = 0; j < NC; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int64_t c = c0 + wc + 32 * j + 8 * e + 4 * g;
@@ -429,7 +440,7 @@ __global__ void __launch_bounds__(256, 1)
             }
         if constexpr (A::kSums) {
             const float s = acc_sum[i] + __shfl_xor(acc_sum[i], 32, 64);
-            if (sums && blockIdx.y == 0 && wc == 0 && g == 0 && m < mn) sums[blockIdx.z * mn + m] = s;
+            if (summing && g == 0 && m < mn) sums[at.z * mn + m] = s;
         }
     }
 }
@@ -474,10 +485,10 @@ aq_status launch(const A& a, const B& b, T* out, int64_t ld, int64_t stride, flo
                  int64_t bytes_per_t, hipStream_t st) {
     constexpr int kBuf = A::P * A::kPlane + B::kPlane, kLds = grad_buffers(kBuf) * kBuf;
     const int64_t x = (m + S - 1) / S, y = (c + S - 1) / S;
-    if (!grid_ok(x, 256)) return AQ_ESHAPE;
+    if (!grid_ok(x * y * p.z, grad_threads(S))) return AQ_ESHAPE;
     auto* const k = k_grad<A, B, T, S>;
     if (hip_failed(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds))) return AQ_EHIP;
-    k<<<dim3((unsigned)x, (unsigned)y, (unsigned)p.z), 256, kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks, track_turns(32 * bytes_per_t) & ~1);
+    k<<<(unsigned)(x * y * p.z), grad_threads(S), kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks, track_turns(32 * bytes_per_t) & ~1);
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }
 template <class T>
