@@ -9,17 +9,13 @@
 // gradient), and is transposed on its way to the registers: ds_read_b64_tr_b16 hands lane i of 16 the four t of column i out of
 // four rows of 16 columns.
 #include "learner.hpp"
-#include "learner_device.hpp"
+#include "product_device.hpp"
 
 namespace aq {
 namespace {
 
 typedef short v4s16 __attribute__((ext_vector_type(4)));
-typedef float v16f32 __attribute__((ext_vector_type(16)));
 
-// Threads of a workgroup with tiles of S x S: wavefronts two by four, or two by two.
-constexpr int grad_threads(int s) { return s == 256 ? 512 : 256; }
-constexpr int kMostLds = 160 * 1024;
 constexpr int grad_buffers(int bytes) { return 3 * bytes <= kMostLds ? 3 : 2; }
 
 template <class T>
@@ -71,17 +67,7 @@ __device__ __forceinline__ v8bf16 t_operand(const uint8_t* tile, int t0, int col
 __device__ __forceinline__ int m_at(int m, int piece) { return m * 64 + ((piece ^ ((m >> 2) & 3)) << 4); }
 
 // ---- the operands.  Of 32 t and S columns (or rows) each thread fetches kUnits units of eight values into registers and later puts them
-// into LDS as bf16.  Loads go through windows on the matrix that begin at the workgroup's first row: what lies behind the
-// matrix's end comes as zeros, without a branch.  Columns of an operand that do not exist only reach results that are not stored.
-struct Window {
-    __amdgpu_buffer_rsrc_t r;
-    // of the bytes from `at` (a multiple of 4) on of `size` bytes at `base`
-    __device__ __forceinline__ void set(const uint8_t* base, int64_t at, int64_t size) {
-        const int64_t left = size - at;
-        r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (left > 0 ? at : 0)), 0, left <= 0 ? 0 : left < kMost ? (int)left : kMost, 0x00020000);
-    }
-    static constexpr int kMost = 0x7ffffff0, kOutside = (int)0x80000000u;
-};
+// into LDS as bf16.  Loads go through windows on the matrix (see Window).  Columns of an operand that do not exist only reach results that are not stored.
 // A matrix in whole words of memory: from the word of its first element to that of its last.
 struct Words {
     const uint8_t* base;
@@ -145,7 +131,7 @@ inline int track_turns(int64_t step) { return (int)(0x7fffffff / step - 5); }
 // dy with t along the rows (weight gradient): [t][m].  ANY: rows of any alignment.
 template <class T, int S, bool ANY>
 struct DyRows {
-    static constexpr int P = kParts<T>, NT = grad_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kPer = S / 8, kSets = P == 1 ? 2 : 1;
+    static constexpr int P = kParts<T>, NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kPer = S / 8, kSets = P == 1 ? 2 : 1;
     static constexpr bool kSums = true;
     Words d;
     Track<kUnits> k;
@@ -185,7 +171,7 @@ struct DyRows {
 // values are the next row's.
 template <class T, int S, bool ANY>
 struct DyCols {
-    static constexpr int P = kParts<T>, NT = grad_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kSets = P == 1 ? 2 : 1;
+    static constexpr int P = kParts<T>, NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kSets = P == 1 ? 2 : 1;
     static constexpr bool kSums = false;
     Words d;
     Track<kUnits> k;
@@ -233,7 +219,7 @@ struct DyCols {
 // rows of a checkpoint (CODE bytes of codes to eight values: 8) or of 4-bit weights (4)
 template <int S, int SETS, int CODE>
 struct BlockRows {
-    static constexpr int NT = grad_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kPer = S / 8;
+    static constexpr int NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kPer = S / 8;
     typedef typename std::conditional<CODE == 8, v2u, uint32_t>::type Codes;
     const uint8_t* codes;
     const uint8_t* scales;
@@ -286,32 +272,15 @@ struct BlockRows {
     }
 };
 
-// every outstanding LDS operation of the wavefront, then the barrier; loads from memory stay in flight
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-// Which tile and slice a workgroup takes.  Workgroups go to the 8 XCDs, each with an L2 of its own, in turn: every eighth of them
-// gets one eighth of all places in a row, and places go along four rows of tiles at once, so that an XCD's workgroups
-// read few different rows and columns (65536 x 2048 x 2048, 64 tiles by 4 slices: XX against XX us with places in order).
-struct Place {
-    uint32_t m, c, z;
-};
-__device__ __forceinline__ Place place_of_workgroup(uint32_t gm, uint32_t gc) {
-    const uint32_t all = gridDim.x, xcd = blockIdx.x % 8, each = all / 8, more = all % 8;
-    const uint32_t p = xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8;
-    const uint32_t z = p / (gm * gc), tile = p % (gm * gc), strip = tile / (4 * gc), in = tile % (4 * gc);
-    const uint32_t high = gm - 4 * strip < 4 ? gm - 4 * strip : 4;
-    return {4 * strip + in % high, in / high, z};
-}
-
 // C tile of S x S, a wavefront takes S / 2 rows and NC * 32 columns of it.  Slice z takes t in [z * chunks * 32, + chunks * 32) and writes its own C (and its
 // own sums of A over t, where `sums` is given).  While the products of one 32 t run, the next 32 t go from registers to LDS, unit
 // by unit, and one or two more are on their way from memory behind them; with three buffers the barrier lies
 // two groups of products before the end, and the next operands are read behind it.
 template <class A, class B, class T, int S>
-__global__ void __launch_bounds__(grad_threads(S), 1)
+__global__ void __launch_bounds__(tile_threads(S), 1)
     k_grad(A a, B b, T* __restrict__ out, int64_t ld, int64_t out_stride, float* __restrict__ sums, int64_t mn, int64_t cn, int64_t tn,
            int chunks, int turns) {
-    constexpr int P = A::P, NT = grad_threads(S), N = S / 64, NC = S / (NT / 128) / 32, kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(kBuf);
+    constexpr int P = A::P, NT = tile_threads(S), N = S / 64, NC = S / (NT / 128) / 32, kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(kBuf);
     constexpr int G = 2 * P * N;  // groups of NC products: 16 t, part, row tile
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
@@ -485,10 +454,10 @@ aq_status launch(const A& a, const B& b, T* out, int64_t ld, int64_t stride, flo
                  int64_t bytes_per_t, hipStream_t st) {
     constexpr int kBuf = A::P * A::kPlane + B::kPlane, kLds = grad_buffers(kBuf) * kBuf;
     const int64_t x = (m + S - 1) / S, y = (c + S - 1) / S;
-    if (!grid_ok(x * y * p.z, grad_threads(S))) return AQ_ESHAPE;
+    if (!grid_ok(x * y * p.z, tile_threads(S))) return AQ_ESHAPE;
     auto* const k = k_grad<A, B, T, S>;
     if (hip_failed(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds))) return AQ_EHIP;
-    k<<<(unsigned)(x * y * p.z), grad_threads(S), kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks, track_turns(32 * bytes_per_t) & ~1);
+    k<<<(unsigned)(x * y * p.z), tile_threads(S), kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks, track_turns(32 * bytes_per_t) & ~1);
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }
 template <class T>

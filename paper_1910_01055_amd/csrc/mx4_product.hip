@@ -5,13 +5,12 @@
 // v_mfma_scale_f32_32x32x64: row l mod 32, block l / 32 of two.  The weights are the first operand, so that a lane ends up with
 // four neighbouring features of one row of y.
 #include "learner.hpp"
-#include "learner_device.hpp"
+#include "product_device.hpp"
 
 namespace aq {
 namespace {
 
 typedef int v8i32 __attribute__((ext_vector_type(8)));
-typedef float v16f32 __attribute__((ext_vector_type(16)));
 constexpr int kFp4 = 4;  // the instructions' number of the 4-bit format
 
 __device__ __forceinline__ v8i32 operand(v4u c) { return v8i32{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}; }
@@ -92,57 +91,63 @@ __global__ void __launch_bounds__(64 * W)
     }
 }
 
-// ---- many rows: BM rows x BN features to a workgroup of four wavefronts (2 x 2), 256 k at a time through LDS.  A chunk of a row
-// is 128 bytes; its 16-byte block s lies in place s ^ (row / 2 mod 8), so that the 16 rows which a read takes at once lie in
-// different banks.
-template <class T, int BM, int BN>
-__global__ void __launch_bounds__(256, 1)
+// ---- many rows: S rows x S features to a workgroup, a wavefront takes 32 TM rows and 32 TN features.  128 k of a row are 64 bytes, a
+// chunk; its 16-byte block s lies in LDS in place s ^ (row / 4 mod 4), so that the 16 rows which a read takes at once lie in different
+// banks.  Chunks go from memory to LDS by themselves (buffer loads to LDS, which fill it with zeros behind a matrix's end), two
+// to three ahead of their products, into four buffers; the barrier that makes the next chunk visible lies between the two halves of
+// the products of the present one, behind which the next operands are read.  Scales go four chunks at a time through registers.
+template <class T, int S>
+__global__ void __launch_bounds__(tile_threads(S), 1)
     k_mx4_tiles(Blocks x, Blocks w, const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int rows, int n, int blocks) {
-    constexpr int R = BM + BN, U = R / 32, SU = (R + 255) / 256, TM = BM / 64, TN = BN / 64;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // two buffers: [R][128] codes, [R][8] scales
-    constexpr int kBuf = R * 136;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5;
-    const int64_t m0 = (int64_t)blockIdx.x * BM, n0 = (int64_t)blockIdx.y * BN;
-    const int wm = (wave & 1) * (BM / 2), wn = (wave >> 1) * (BN / 2);
-    v4u c[U];
-    v2u s[SU];
-    auto fetch = [&](int b0) __attribute__((always_inline)) {
+    constexpr int NT = tile_threads(S), R = 2 * S, J = R * 4 / NT, TM = S / 64, TN = S / (NT / 128) / 32, kBuf = R * 64, kScales = R * 16;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // four buffers of chunks, two of scales
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, g = lane >> 5;
+    const Place at = place_of_workgroup((uint32_t)((rows + S - 1) / S), (uint32_t)((n + S - 1) / S));
+    const int64_t m0 = (int64_t)at.m * S, n0 = (int64_t)at.c * S, pitch = (int64_t)blocks * 16;
+    const int wm = (wave & 1) * (S / 2), wn = S + (wave >> 1) * (32 * TN), chunks = (blocks + 3) / 4;
+    Window win_x, win_w;
+    win_x.set(x.codes, m0 * pitch, rows * pitch);
+    win_w.set(w.codes, n0 * pitch, n * pitch);
+    // unit j of a thread: row (tid + NT j) / 4 of both matrices' rows, place tid mod 4
+    const int block = (tid & 3) ^ ((tid >> 4) & 3);
+    int off[J];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int u = tid + 256 * i, row = u >> 3, b = b0 + (u & 7);
-            const bool is_x = i < BM / 32;  // (rows of x first)
-            const int64_t at = is_x ? m0 + row : n0 + row - BM;
-            c[i] = v4u{0, 0, 0, 0};
-            if (b < blocks && at < (is_x ? rows : n)) c[i] = *(const v4u AQ_GLOBAL*)((is_x ? x.codes : w.codes) + (at * blocks + b) * 16);
-        }
+    for (int j = 0; j < J; ++j) off[j] = (((tid + NT * j) >> 2) % S) * (int)pitch + block * 16;
+    auto fetch = [&](int chunk, int buf) __attribute__((always_inline)) {
+        const int from = 4 * chunk + block < blocks ? 64 * chunk : Window::kOutside;
 #pragma unroll
-        for (int i = 0; i < SU; ++i) {
-            const int row = tid + 256 * i;
-            const bool is_x = row < BM;
-            const int64_t at = is_x ? m0 + row : n0 + row - BM;
-            s[i] = v2u{0, 0};
-            if (row < R && at < (is_x ? rows : n)) {
-                const uint8_t* p = (is_x ? x.scales : w.scales) + at * blocks + b0;
-                if (b0 + 8 <= blocks) {
-                    typedef v2u v2u_byte __attribute__((aligned(1)));
-                    s[i] = *(const v2u_byte AQ_GLOBAL*)p;
-                } else {
+        for (int j = 0; j < J; ++j)
+            load_to_lds(j < J / 2 ? win_x : win_w, off[j] + from, lds + buf * kBuf + (wave * 64 + NT * j) * 16);
+    };
+    // a thread's row of scales (some row that exists where it has none: what comes of it is not stored)
+    auto clamp = [](int64_t row, int most) __attribute__((always_inline)) { return row < most ? row : (int64_t)most - 1; };
+    const uint8_t* const scale_row =
+        tid % R < S ? x.scales + clamp(m0 + tid % R, rows) * blocks : w.scales + clamp(n0 + tid % R - S, n) * blocks;
+    v4u sc;
+    auto fetch_scales = [&](int b0) __attribute__((always_inline)) {
+        if (b0 + 16 <= blocks) {
+            typedef v4u v4u_byte __attribute__((aligned(1)));
+            sc = *(const v4u_byte AQ_GLOBAL*)(scale_row + b0);
+        } else {
+            sc = v4u{0, 0, 0, 0};
+            for (int j = 0; b0 + j < blocks; ++j) {
+                const uint32_t byte = (uint32_t)scale_row[b0 + j] << (8 * (j & 3));
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (b0 + j < blocks) s[i][j / 4] |= (uint32_t)p[j] << (8 * (j & 3));
-                }
+                for (int i = 0; i < 4; ++i) sc[i] |= j >> 2 == i ? byte : 0u;
             }
         }
     };
-    auto put = [&](uint8_t* to) __attribute__((always_inline)) {
+    uint8_t* const lds_scales = lds + 4 * kBuf;
+    auto put_scales = [&](int parity) __attribute__((always_inline)) {
+        if (tid < R) *(v4u*)(lds_scales + parity * kScales + tid * 16) = sc;
+    };
+    // a lane's blocks are 2 k + g of the sixteen: moved to the bytes 0 and 2 of the words
+    v4u sx[TM], sw[TN];
+    auto read_scales = [&](int parity) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int u = tid + 256 * i, row = u >> 3;
-            *(v4u*)(to + row * 128 + (((u & 7) ^ ((row >> 1) & 7)) << 4)) = c[i];
-        }
+        for (int j = 0; j < TM; ++j) sx[j] = *(const v4u*)(lds_scales + parity * kScales + (wm + 32 * j + r) * 16) >> (8 * g);
 #pragma unroll
-        for (int i = 0; i < SU; ++i)
-            if (tid + 256 * i < R) *(v2u*)(to + R * 128 + (tid + 256 * i) * 8) = s[i];
+        for (int i = 0; i < TN; ++i) sw[i] = *(const v4u*)(lds_scales + parity * kScales + (wn + 32 * i + r) * 16) >> (8 * g);
     };
     v16f32 acc[TN][TM];
 #pragma unroll
@@ -151,67 +156,77 @@ __global__ void __launch_bounds__(256, 1)
         for (int j = 0; j < TM; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    fetch(0);
-    put(lds);
-    __syncthreads();
-    int buf = 0;
-    for (int b0 = 0; b0 < blocks; b0 += 8) {
-        const bool more = b0 + 8 < blocks;
-        if (more) fetch(b0 + 8);
-        const uint8_t* from = lds + buf * kBuf;
-        v2u sx[TM], sw[TN];
+    v4u cx[2][TM], cw[2][TN];  // operands of the two halves of a chunk
+    auto read = [&](auto half, const uint8_t* from) __attribute__((always_inline)) {
+        constexpr int H = decltype(half)::value;
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
-            sx[j] = *(const v2u*)(from + R * 128 + (wm + 32 * j + r) * 8);
-            sx[j] = v2u{sx[j][0] >> (8 * g), sx[j][1] >> (8 * g)};
+            const int row = wm + 32 * j + r;
+            cx[H][j] = *(const v4u*)(from + row * 64 + (((2 * H + g) ^ ((row >> 2) & 3)) << 4));
         }
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
-            sw[i] = *(const v2u*)(from + R * 128 + (BM + wn + 32 * i + r) * 8);
-            sw[i] = v2u{sw[i][0] >> (8 * g), sw[i][1] >> (8 * g)};
+            const int row = wn + 32 * i + r;
+            cw[H][i] = *(const v4u*)(from + row * 64 + (((2 * H + g) ^ ((row >> 2) & 3)) << 4));
         }
-        auto turn = [&](auto k) __attribute__((always_inline)) {
-            constexpr int K = decltype(k)::value;  // 64 of the chunk's 256
-            v4u cx[TM], cw[TN];
+    };
+    auto products = [&](auto half, auto word) __attribute__((always_inline)) {
+        constexpr int H = decltype(half)::value, W = decltype(word)::value;
 #pragma unroll
-            for (int j = 0; j < TM; ++j) {
-                const int row = wm + 32 * j + r;
-                cx[j] = *(const v4u*)(from + row * 128 + (((2 * K + g) ^ ((row >> 1) & 7)) << 4));
-            }
+        for (int i = 0; i < TN; ++i)
 #pragma unroll
-            for (int i = 0; i < TN; ++i) {
-                const int row = BM + wn + 32 * i + r;
-                cw[i] = *(const v4u*)(from + row * 128 + (((2 * K + g) ^ ((row >> 1) & 7)) << 4));
-            }
-#pragma unroll
-            for (int i = 0; i < TN; ++i)
-#pragma unroll
-                for (int j = 0; j < TM; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(cw[i]), operand(cx[j]), acc[i][j], kFp4, kFp4, 2 * (K & 1),
-                                                                            (int)sw[i][K / 2], 2 * (K & 1), (int)sx[j][K / 2]);
+            for (int j = 0; j < TM; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(cw[H][i]), operand(cx[H][j]), acc[i][j], kFp4, kFp4, 2 * H,
+                                                                        (int)sw[i][W], 2 * H, (int)sx[j][W]);
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> second{};
+    fetch_scales(0);
+    put_scales(0);
+    fetch(0, 0);
+    fetch(1, 1);
+    fetch(2, 2);
+    wait_loads<2 * J>();
+    lds_barrier();
+    read(first, lds);
+    int parity = 0;
+    for (int c0 = 0; c0 < chunks; c0 += 4) {
+        read_scales(parity);
+        parity ^= 1;
+        fetch_scales(4 * c0 + 16);
+        auto chunk = [&](auto k) __attribute__((always_inline)) {
+            constexpr int K = decltype(k)::value;
+            read(second, lds + K * kBuf);
+            products(first, k);
+            if constexpr (K == 3) put_scales(parity);
+            wait_loads<J>();  // the next chunk is there: only the one behind it may be on its way
+            lds_barrier();
+            fetch(c0 + K + 3, (K + 3) % 4);
+            read(first, lds + (K + 1) % 4 * kBuf);
+            products(second, k);
         };
-        turn(std::integral_constant<int, 0>());
-        turn(std::integral_constant<int, 1>());
-        turn(std::integral_constant<int, 2>());
-        turn(std::integral_constant<int, 3>());
-        buf ^= 1;
-        if (more) put(lds + buf * kBuf);
-        __syncthreads();
+        chunk(std::integral_constant<int, 0>());
+        if (c0 + 1 < chunks) {
+            chunk(std::integral_constant<int, 1>());
+            if (c0 + 2 < chunks) {
+                chunk(std::integral_constant<int, 2>());
+                if (c0 + 3 < chunks) chunk(std::integral_constant<int, 3>());
+            }
+        }
     }
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
         const int64_t row = m0 + wm + 32 * j + r;
-        if (row >= rows) continue;
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int64_t f = n0 + wn + 32 * i + 8 * q + 4 * g;
-                if (f >= n) continue;
+                const int64_t f = n0 + wn - S + 32 * i + 8 * q + 4 * g;
                 float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e] + (bias && f + e < n ? bias[f + e] : 0.0f);
-                store4(y + row * ldy, f, n, v);
+                if (row < rows && f < n) store4(y + row * ldy, f, n, v);
+                __builtin_amdgcn_sched_barrier(0);  // (not all sums in vector registers at once)
             }
     }
 }
@@ -227,13 +242,15 @@ aq_status launch_rows(const X& x, int64_t rows, const aq_mx4& w, const float* bi
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }
 
-template <class T>
+template <class T, int S>
 aq_status launch_tiles(const aq_mx4& x, const aq_mx4& w, const float* bias, const aq_matrix& y, hipStream_t st) {
-    constexpr int BM = 128, BN = 128, kLds = 2 * (BM + BN) * 136;
-    auto* const k = k_mx4_tiles<T, BM, BN>;
+    constexpr int kLds = 4 * 2 * S * 64 + 2 * 2 * S * 16;
+    const int64_t tiles = ((x.rows + S - 1) / S) * ((w.rows + S - 1) / S);
+    if (!grid_ok(tiles, tile_threads(S))) return AQ_ESHAPE;
+    auto* const k = k_mx4_tiles<T, S>;
     if (hip_failed(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds))) return AQ_EHIP;
-    const dim3 grid((unsigned)((x.rows + BM - 1) / BM), (unsigned)((w.rows + BN - 1) / BN));
-    k<<<grid, 256, kLds, st>>>(blocks_of(x), blocks_of(w), bias, (T*)y.d, y.ld, (int)x.rows, (int)w.rows, (int)blocks32(w.cols));
+    k<<<(unsigned)tiles, tile_threads(S), kLds, st>>>(blocks_of(x), blocks_of(w), bias, (T*)y.d, y.ld, (int)x.rows, (int)w.rows,
+                                                      (int)blocks32(w.cols));
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }
 
@@ -249,7 +266,10 @@ aq_status launch_mx4_matmul(const aq_mx4& x, const aq_mx4& w, const float* bias,
     return with_dtype(y.dtype, [&](auto t) {
         using T = decltype(t);
         if (x.rows <= kFewRows) return launch_rows<Blocks, T>(blocks_of(x), x.rows, w, bias, y, st);
-        return launch_tiles<T>(x, w, bias, y, st);
+        auto tiles = [&](int64_t s) { return ((x.rows + s - 1) / s) * ((w.rows + s - 1) / s); };
+        if (tiles(256) >= 256) return launch_tiles<T, 256>(x, w, bias, y, st);
+        if (tiles(128) >= 256) return launch_tiles<T, 128>(x, w, bias, y, st);
+        return launch_tiles<T, 64>(x, w, bias, y, st);
     });
 }
 
