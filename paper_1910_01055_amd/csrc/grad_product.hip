@@ -395,18 +395,13 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
         }
     }
     out += at.z * out_stride;
+    wait_loads<0>();
+    lds_barrier();  // (every wavefront has read its last operands)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int64_t m = m0 + wm + 32 * i + r;
-#pragma unroll
-        for (int j = 0; j < NC; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t c = c0 + wc + 32 * j + 8 * e + 4 * g;
-                const float v[4] = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
-                if (m < mn && c < cn) store4(out + m * ld, c, cn, v);
-                __builtin_amdgcn_sched_barrier(0);  // (not all sums in vector registers at once)
-            }
+        const int64_t row = m0 + wm + 32 * i, m = row + r;
+        store_rows<T, NC>(lds + wave * (32 * kOutRow<T, NC>), lane, out + row * ld + c0 + wc, ld, mn - row, cn - c0 - wc,
+                          [&](int j, int q, int e) { return acc[i][j][4 * q + e]; });
         if constexpr (A::kSums) {
             const float s = acc_sum[i] + __shfl_xor(acc_sum[i], 32, 64);
             if (summing && g == 0 && m < mn) sums[at.z * mn + m] = s;

@@ -90,27 +90,6 @@ struct Piece {
     }
 };
 
-// four neighbouring values of a row: values n .. n + 3, of which those below `most` exist
-template <class T>
-__device__ __forceinline__ void store4(T* __restrict__ y, int64_t n, int64_t most, const float (&v)[4]) {
-    if constexpr (std::is_same<T, float>::value) {
-        if (n + 4 <= most) {
-            *(v4u_any*)((uint32_t AQ_GLOBAL*)(y + n)) = (v4u){__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-            return;
-        }
-    } else {
-        typedef T v2 __attribute__((ext_vector_type(2)));
-        if (n + 4 <= most) {
-            *(v2u_any*)((uint32_t AQ_GLOBAL*)(y + n)) = (v2u){__builtin_bit_cast(uint32_t, __builtin_convertvector((v2f32{v[0], v[1]}), v2)),
-                                                          __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f32{v[2], v[3]}), v2))};
-            return;
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (n + j < most) y[n + j] = (T)v[j];
-}
-
 // ---- blocks of 32 values: lanes 4 i .. 4 i + 3 hold one, eight values each
 // the largest magnitude's bits (as whole numbers, so that NaNs and infinities win)
 __device__ __forceinline__ uint32_t most_of8(const float (&v)[8]) {

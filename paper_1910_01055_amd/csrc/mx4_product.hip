@@ -83,10 +83,9 @@ __global__ void __launch_bounds__(64 * W)
         for (int j = 1; j < W; ++j) s += part[j][i][lane];
         const int64_t row = m0 + 16 * i + r, f = n0 + 4 * g;
         if (row < rows && f < n) {
-            float v[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = s[j] + (bias && f + j < n ? bias[f + j] : 0.0f);
-            store4(y + row * ldy, f, n, v);
+            for (int j = 0; j < 4; ++j)
+                if (f + j < n) y[row * ldy + f + j] = (T)(s[j] + (bias ? bias[f + j] : 0.0f));
         }
     }
 }
@@ -196,14 +195,19 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
         fetch_scales(4 * c0 + 16);
         auto chunk = [&](auto k) __attribute__((always_inline)) {
             constexpr int K = decltype(k)::value;
-            read(second, lds + K * kBuf);
-            products(first, k);
+            // (the order stays: operands are requested half a chunk of products ahead)
             if constexpr (K == 3) put_scales(parity);
+            read(second, lds + K * kBuf);
+            __builtin_amdgcn_sched_barrier(0);
+            products(first, k);
+            __builtin_amdgcn_sched_barrier(0);
             wait_loads<J>();  // the next chunk is there: only the one behind it may be on its way
             lds_barrier();
-            fetch(c0 + K + 3, (K + 3) % 4);
             read(first, lds + (K + 1) % 4 * kBuf);
+            fetch(c0 + K + 3, (K + 3) % 4);
+            __builtin_amdgcn_sched_barrier(0);
             products(second, k);
+            __builtin_amdgcn_sched_barrier(0);
         };
         chunk(std::integral_constant<int, 0>());
         if (c0 + 1 < chunks) {
@@ -214,20 +218,24 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
             }
         }
     }
+    wait_loads<0>();  // (chunks behind the last one, which arrive as zeros)
+    lds_barrier();
+    v4f32 b[TN][4];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t f = n0 + wn - S + 32 * i + 8 * q + 4 * g + e;
+                b[i][q][e] = bias && f < n ? bias[f] : 0.0f;
+            }
+    const int64_t f0 = n0 + wn - S;
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
-        const int64_t row = m0 + wm + 32 * j + r;
-#pragma unroll
-        for (int i = 0; i < TN; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t f = n0 + wn - S + 32 * i + 8 * q + 4 * g;
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e] + (bias && f + e < n ? bias[f + e] : 0.0f);
-                if (row < rows && f < n) store4(y + row * ldy, f, n, v);
-                __builtin_amdgcn_sched_barrier(0);  // (not all sums in vector registers at once)
-            }
+        const int64_t row = m0 + wm + 32 * j;
+        store_rows<T, TN>(lds + wave * (32 * kOutRow<T, TN>), lane, y + row * ldy + f0, ldy, rows - row, n - f0,
+                          [&](int i, int q, int e) { return acc[i][j][4 * q + e] + b[i][q][e]; });
     }
 }
 

@@ -49,4 +49,41 @@ __device__ __forceinline__ Place place_of_workgroup(uint32_t gm, uint32_t gc) {
     return {4 * strip + in % high, in / high, z};
 }
 
+// 32 rows and 32 C columns of sums in the layout of a 32x32 MFMA (lane l: row l mod 32 here, columns 32 i + 8 q + 4 (l / 32) + e),
+// rounded and stored as whole lines through 32 kOutRow<T, C> bytes of LDS of the wavefront's own.  get(i, q, e): the sums.  Of the
+// rows from `out` on `rows` exist, and `cols` of their columns.
+template <class T, int C>
+constexpr int kOutRow = 32 * C * (int)sizeof(T) + 16;
+template <class T, int C, class Get>
+__device__ __forceinline__ void store_rows(uint8_t* place, int lane, T* __restrict__ out, int64_t ld, int64_t rows, int64_t cols, Get&& get) {
+    constexpr int kRow = kOutRow<T, C>, kPieces = 32 * C * (int)sizeof(T) / 16, kEach = 16 / (int)sizeof(T);
+    uint8_t* const row = place + (lane & 31) * kRow + (lane >> 5) * (4 * (int)sizeof(T));
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float v0 = get(i, q, 0), v1 = get(i, q, 1), v2 = get(i, q, 2), v3 = get(i, q, 3);
+            uint8_t* const to = row + (32 * i + 8 * q) * (int)sizeof(T);
+            if constexpr (std::is_same<T, float>::value) {
+                *(v4f32*)to = v4f32{v0, v1, v2, v3};
+            } else {
+                typedef T t2 __attribute__((ext_vector_type(2)));
+                *(v2u*)to = v2u{__builtin_bit_cast(uint32_t, __builtin_convertvector((v2f32{v0, v1}), t2)),
+                                __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f32{v2, v3}), t2))};
+            }
+        }
+#pragma unroll
+    for (int k = 0; k < 32 * kPieces / 64; ++k) {
+        const int m = (lane + 64 * k) / kPieces, c = (lane + 64 * k) % kPieces * kEach;
+        const v4u v = *(const v4u*)(place + m * kRow + c * (int)sizeof(T));
+        if (m >= rows) continue;
+        T* const to = out + m * ld + c;
+        if (c + kEach <= cols) {
+            *(v4u_any AQ_GLOBAL*)to = v;
+        } else {
+            for (int e = 0; e < kEach && c + e < cols; ++e) to[e] = *((const T*)(place + m * kRow) + c + e);
+        }
+    }
+}
+
 }  // namespace aq
