@@ -90,63 +90,68 @@ __global__ void __launch_bounds__(64 * W)
     }
 }
 
-// ---- many rows: S rows x S features to a workgroup, a wavefront takes 32 TM rows and 32 TN features.  128 k of a row are 64 bytes, a
-// chunk; its 16-byte block s lies in LDS in place s ^ (row / 4 mod 4), so that the 16 rows which a read takes at once lie in different
-// banks.  Chunks go from memory to LDS by themselves (buffer loads to LDS, which fill it with zeros behind a matrix's end), two
-// to three ahead of their products, into four buffers; the barrier that makes the next chunk visible lies between the two halves of
-// the products of the present one, behind which the next operands are read.  Scales go four chunks at a time through registers.
-template <class T, int S>
-__global__ void __launch_bounds__(tile_threads(S), 1)
+// ---- many rows: S rows x S features to a workgroup, a wavefront takes 32 TM rows and 32 TN features.  256 k of a row are 128 bytes, a
+// chunk; its 16-byte block s lies in LDS in place s ^ (row / 2 mod 8), so that the 16 rows which a read takes at once lie in different
+// banks.  Chunks go from memory to LDS by themselves (buffer loads to LDS, which fill it with zeros behind a matrix's end) into
+// two buffers.  A chunk's products come in four turns of 64 k, whose operands are read a turn ahead; behind the third all of a
+// chunk is in registers, and the barrier there hands its buffer to the chunk after the next.  Scales come for two chunks at a time
+// through registers.
+template <class T, int S, int NT>
+__global__ void __launch_bounds__(NT, 1)
     k_mx4_tiles(Blocks x, Blocks w, const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int rows, int n, int blocks) {
-    constexpr int NT = tile_threads(S), R = 2 * S, J = R * 4 / NT, TM = S / 64, TN = S / (NT / 128) / 32, kBuf = R * 64, kScales = R * 16;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // four buffers of chunks, two of scales
+    constexpr int R = 2 * S, SU = (R + NT - 1) / NT, J = R * 8 / NT, TM = S / 64, TN = S / (NT / 128) / 32, kBuf = R * 128;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // two buffers of chunks; scales of four chunks
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, g = lane >> 5;
     const Place at = place_of_workgroup((uint32_t)((rows + S - 1) / S), (uint32_t)((n + S - 1) / S));
     const int64_t m0 = (int64_t)at.m * S, n0 = (int64_t)at.c * S, pitch = (int64_t)blocks * 16;
-    const int wm = (wave & 1) * (S / 2), wn = S + (wave >> 1) * (32 * TN), chunks = (blocks + 3) / 4;
+    const int wm = (wave & 1) * (S / 2), wn = S + (wave >> 1) * (32 * TN), chunks = (blocks + 7) / 8;
     Window win_x, win_w;
     win_x.set(x.codes, m0 * pitch, rows * pitch);
     win_w.set(w.codes, n0 * pitch, n * pitch);
-    // unit j of a thread: row (tid + NT j) / 4 of both matrices' rows, place tid mod 4
-    const int block = (tid & 3) ^ ((tid >> 4) & 3);
+    // unit j of a thread: row (tid + NT j) / 8 of both matrices' rows, place tid mod 8
+    const int block = (tid & 7) ^ ((tid >> 4) & 7);
     int off[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) off[j] = (((tid + NT * j) >> 2) % S) * (int)pitch + block * 16;
-    auto fetch = [&](int chunk, int buf) __attribute__((always_inline)) {
-        const int from = 4 * chunk + block < blocks ? 64 * chunk : Window::kOutside;
+    for (int j = 0; j < J; ++j) off[j] = (((tid + NT * j) >> 3) % S) * (int)pitch + block * 16;
+    auto fetch = [&](int chunk) __attribute__((always_inline)) {
+        const int from = 8 * chunk + block < blocks ? 128 * chunk : Window::kOutside;
 #pragma unroll
         for (int j = 0; j < J; ++j)
-            load_to_lds(j < J / 2 ? win_x : win_w, off[j] + from, lds + buf * kBuf + (wave * 64 + NT * j) * 16);
+            load_to_lds(j < J / 2 ? win_x : win_w, off[j] + from, lds + (chunk & 1) * kBuf + (wave * 64 + NT * j) * 16);
     };
-    // a thread's row of scales (some row that exists where it has none: what comes of it is not stored)
+    // a thread's rows of scales (some row that exists where it has none: what comes of it is not stored)
     auto clamp = [](int64_t row, int most) __attribute__((always_inline)) { return row < most ? row : (int64_t)most - 1; };
-    const uint8_t* const scale_row =
-        tid % R < S ? x.scales + clamp(m0 + tid % R, rows) * blocks : w.scales + clamp(n0 + tid % R - S, n) * blocks;
-    v4u sc;
+    const uint8_t* scale_row[SU];
+    v4u sc[SU];
+#pragma unroll
+    for (int i = 0; i < SU; ++i) {
+        const int row = (tid + NT * i) % R;
+        scale_row[i] = row < S ? x.scales + clamp(m0 + row, rows) * blocks : w.scales + clamp(n0 + row - S, n) * blocks;
+    }
     auto fetch_scales = [&](int b0) __attribute__((always_inline)) {
         if (b0 + 16 <= blocks) {
             typedef v4u v4u_byte __attribute__((aligned(1)));
-            sc = *(const v4u_byte AQ_GLOBAL*)(scale_row + b0);
-        } else {
-            sc = v4u{0, 0, 0, 0};
-            for (int j = 0; b0 + j < blocks; ++j) {
-                const uint32_t byte = (uint32_t)scale_row[b0 + j] << (8 * (j & 3));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[i] |= j >> 2 == i ? byte : 0u;
+            for (int i = 0; i < SU; ++i) sc[i] = *(const v4u_byte AQ_GLOBAL*)(scale_row[i] + b0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < SU; ++i) {
+                sc[i] = v4u{0, 0, 0, 0};
+                for (int j = 0; b0 + j < blocks; ++j) {
+                    const uint32_t byte = (uint32_t)scale_row[i][b0 + j] << (8 * (j & 3));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sc[i][k] |= j >> 2 == k ? byte : 0u;
+                }
             }
         }
     };
-    uint8_t* const lds_scales = lds + 4 * kBuf;
-    auto put_scales = [&](int parity) __attribute__((always_inline)) {
-        if (tid < R) *(v4u*)(lds_scales + parity * kScales + tid * 16) = sc;
-    };
-    // a lane's blocks are 2 k + g of the sixteen: moved to the bytes 0 and 2 of the words
-    v4u sx[TM], sw[TN];
-    auto read_scales = [&](int parity) __attribute__((always_inline)) {
+    uint32_t* const lds_scales = (uint32_t*)(lds + 2 * kBuf);  // [8 words][R]: two words to a chunk
+    auto put_scales = [&](int chunk) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < TM; ++j) sx[j] = *(const v4u*)(lds_scales + parity * kScales + (wm + 32 * j + r) * 16) >> (8 * g);
+        for (int i = 0; i < SU; ++i)
 #pragma unroll
-        for (int i = 0; i < TN; ++i) sw[i] = *(const v4u*)(lds_scales + parity * kScales + (wn + 32 * i + r) * 16) >> (8 * g);
+            for (int k = 0; k < 4; ++k)
+                if (NT * SU == R || tid < R) lds_scales[((2 * chunk + k) & 7) * R + tid + NT * i] = sc[i][k];
     };
     v16f32 acc[TN][TM];
 #pragma unroll
@@ -155,68 +160,75 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
         for (int j = 0; j < TM; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    v4u cx[2][TM], cw[2][TN];  // operands of the two halves of a chunk
-    auto read = [&](auto half, const uint8_t* from) __attribute__((always_inline)) {
+    // operands of a turn and of the next; a lane's blocks of a chunk are 2 turn + g
+    v4u cx[2][TM], cw[2][TN];
+    uint32_t sx[2][TM], sw[2][TN];  // scales of a chunk's two halves
+    const int place = ((g ^ ((lane >> 1) & 7)) << 4) + r * 128;
+    auto read = [&](auto turn, const uint8_t* from) __attribute__((always_inline)) {
+        constexpr int Q = decltype(turn)::value;
+        const uint8_t* const at = from + (place ^ (32 * Q));
+#pragma unroll
+        for (int j = 0; j < TM; ++j) cx[Q & 1][j] = *(const v4u*)(at + (wm + 32 * j) * 128);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) cw[Q & 1][i] = *(const v4u*)(at + (wn + 32 * i) * 128);
+    };
+    auto read_scales = [&](auto half, int chunk) __attribute__((always_inline)) {
+        constexpr int H = decltype(half)::value;
+        const uint32_t* const at = lds_scales + ((2 * chunk + H) & 7) * R + r;
+#pragma unroll
+        for (int j = 0; j < TM; ++j) sx[H][j] = at[wm + 32 * j];
+#pragma unroll
+        for (int i = 0; i < TN; ++i) sw[H][i] = at[wn + 32 * i];
+    };
+    auto own_scales = [&](auto half) __attribute__((always_inline)) {  // this lane's blocks to bytes 0 and 2
         constexpr int H = decltype(half)::value;
 #pragma unroll
-        for (int j = 0; j < TM; ++j) {
-            const int row = wm + 32 * j + r;
-            cx[H][j] = *(const v4u*)(from + row * 64 + (((2 * H + g) ^ ((row >> 2) & 3)) << 4));
-        }
+        for (int j = 0; j < TM; ++j) sx[H][j] >>= 8 * g;
 #pragma unroll
-        for (int i = 0; i < TN; ++i) {
-            const int row = wn + 32 * i + r;
-            cw[H][i] = *(const v4u*)(from + row * 64 + (((2 * H + g) ^ ((row >> 2) & 3)) << 4));
-        }
+        for (int i = 0; i < TN; ++i) sw[H][i] >>= 8 * g;
     };
-    auto products = [&](auto half, auto word) __attribute__((always_inline)) {
-        constexpr int H = decltype(half)::value, W = decltype(word)::value;
+    auto products = [&](auto turn) __attribute__((always_inline)) {
+        constexpr int Q = decltype(turn)::value;
+        __builtin_amdgcn_sched_barrier(0);  // (the order stays: operands are requested a turn ahead)
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
             for (int j = 0; j < TM; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(cw[H][i]), operand(cx[H][j]), acc[i][j], kFp4, kFp4, 2 * H,
-                                                                        (int)sw[i][W], 2 * H, (int)sx[j][W]);
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(cw[Q & 1][i]), operand(cx[Q & 1][j]), acc[i][j], kFp4, kFp4,
+                                                                        2 * (Q & 1), (int)sw[Q / 2][i], 2 * (Q & 1), (int)sx[Q / 2][j]);
+        __builtin_amdgcn_sched_barrier(0);
     };
-    constexpr std::integral_constant<int, 0> first{};
-    constexpr std::integral_constant<int, 1> second{};
+    constexpr std::integral_constant<int, 0> q0{};
+    constexpr std::integral_constant<int, 1> q1{};
+    constexpr std::integral_constant<int, 2> q2{};
+    constexpr std::integral_constant<int, 3> q3{};
     fetch_scales(0);
+    fetch(0);
     put_scales(0);
-    fetch(0, 0);
-    fetch(1, 1);
-    fetch(2, 2);
-    wait_loads<2 * J>();
+    wait_loads<0>();
     lds_barrier();
-    read(first, lds);
-    int parity = 0;
-    for (int c0 = 0; c0 < chunks; c0 += 4) {
-        read_scales(parity);
-        parity ^= 1;
-        fetch_scales(4 * c0 + 16);
-        auto chunk = [&](auto k) __attribute__((always_inline)) {
-            constexpr int K = decltype(k)::value;
-            // (the order stays: operands are requested half a chunk of products ahead)
-            if constexpr (K == 3) put_scales(parity);
-            read(second, lds + K * kBuf);
-            __builtin_amdgcn_sched_barrier(0);
-            products(first, k);
-            __builtin_amdgcn_sched_barrier(0);
-            wait_loads<J>();  // the next chunk is there: only the one behind it may be on its way
-            lds_barrier();
-            read(first, lds + (K + 1) % 4 * kBuf);
-            fetch(c0 + K + 3, (K + 3) % 4);
-            __builtin_amdgcn_sched_barrier(0);
-            products(second, k);
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        chunk(std::integral_constant<int, 0>());
-        if (c0 + 1 < chunks) {
-            chunk(std::integral_constant<int, 1>());
-            if (c0 + 2 < chunks) {
-                chunk(std::integral_constant<int, 2>());
-                if (c0 + 3 < chunks) chunk(std::integral_constant<int, 3>());
-            }
-        }
+    fetch(1);
+    read(q0, lds);
+    read_scales(q0, 0);
+    for (int c = 0; c < chunks; ++c) {
+        const uint8_t* const now = lds + (c & 1) * kBuf;
+        own_scales(q0);
+        if ((c & 1) == 0) fetch_scales(8 * c + 16);
+        read_scales(q1, c);
+        read(q1, now);
+        products(q0);
+        read(q2, now);
+        products(q1);
+        own_scales(q1);
+        if ((c & 1) == 1) put_scales(c + 1);
+        read(q3, now);
+        products(q2);
+        wait_loads<0>();  // the next chunk is there,
+        lds_barrier();    // and all of this one in registers
+        fetch(c + 2);
+        read(q0, lds + ((c + 1) & 1) * kBuf);
+        read_scales(q0, c + 1);
+        products(q3);
     }
     wait_loads<0>();  // (chunks behind the last one, which arrive as zeros)
     lds_barrier();
@@ -252,12 +264,13 @@ aq_status launch_rows(const X& x, int64_t rows, const aq_mx4& w, const float* bi
 
 template <class T, int S>
 aq_status launch_tiles(const aq_mx4& x, const aq_mx4& w, const float* bias, const aq_matrix& y, hipStream_t st) {
-    constexpr int kLds = 4 * 2 * S * 64 + 2 * 2 * S * 16;
+    constexpr int kLds = 2 * 2 * S * 128 + 8 * 2 * S * 4;
     const int64_t tiles = ((x.rows + S - 1) / S) * ((w.rows + S - 1) / S);
-    if (!grid_ok(tiles, tile_threads(S))) return AQ_ESHAPE;
-    auto* const k = k_mx4_tiles<T, S>;
+    if (!grid_ok(tiles, 512)) return AQ_ESHAPE;
+    constexpr int NT = tile_threads(S);
+    auto* const k = k_mx4_tiles<T, S, NT>;
     if (hip_failed(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds))) return AQ_EHIP;
-    k<<<(unsigned)tiles, tile_threads(S), kLds, st>>>(blocks_of(x), blocks_of(w), bias, (T*)y.d, y.ld, (int)x.rows, (int)w.rows,
+    k<<<(unsigned)tiles, NT, kLds, st>>>(blocks_of(x), blocks_of(w), bias, (T*)y.d, y.ld, (int)x.rows, (int)w.rows,
                                                       (int)blocks32(w.cols));
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }
