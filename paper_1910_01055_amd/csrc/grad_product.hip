@@ -131,7 +131,7 @@ inline int track_turns(int64_t step) { return (int)(0x7fffffff / step - 5); }
 // dy with t along the rows (weight gradient): [t][m].  ANY: rows of any alignment.
 template <class T, int S, bool ANY>
 struct DyRows {
-    static constexpr int P = kParts<T>, NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kPer = S / 8, kSets = P == 1 ? 2 : 1;
+    static constexpr int P = kParts<T>, NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kPer = S / 8, kSets = P == 1 || S < 256 ? 2 : 1;
     static constexpr bool kSums = true;
     Words d;
     Track<kUnits> k;
@@ -171,7 +171,7 @@ struct DyRows {
 // values are the next row's.
 template <class T, int S, bool ANY>
 struct DyCols {
-    static constexpr int P = kParts<T>, NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kSets = P == 1 ? 2 : 1;
+    static constexpr int P = kParts<T>, NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kSets = P == 1 || S < 256 ? 2 : 1;
     static constexpr bool kSums = false;
     Words d;
     Track<kUnits> k;
@@ -414,15 +414,21 @@ template <class T>
 __global__ void __launch_bounds__(256) k_grad_join(const float* __restrict__ part, int slices, int64_t m, int64_t c, T* __restrict__ out,
                                                    int64_t ld, const float* __restrict__ part_sums, float* __restrict__ sums) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < m * c) {
+    auto total = [slices](const float* p, int64_t step) __attribute__((always_inline)) {
         float s = 0.0f;
-        for (int k = 0; k < slices; ++k) s += part[k * m * c + i];
-        out[i / c * ld + i % c] = (T)s;
-    } else if (sums && i < m * c + m) {
-        float s = 0.0f;
-        for (int k = 0; k < slices; ++k) s += part_sums[k * m + (i - m * c)];
-        sums[i - m * c] = s;
-    }
+        int k = 0;
+        for (; k + 8 <= slices; k += 8) {  // eight on their way at a time
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = p[(k + j) * step];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += v[j];
+        }
+        for (; k < slices; ++k) s += p[k * step];
+        return s;
+    };
+    if (i < m * c) out[i / c * ld + i % c] = (T)total(part + i, m * c);
+    else if (sums && i < m * c + m) sums[i - m * c] = total(part_sums + (i - m * c), m);
 }
 
 // how a product of m x c over t runs: tiles of s x s, z slices of `chunks` (an even number) times 32 t
@@ -436,8 +442,8 @@ Plan plan(int64_t m, int64_t c, int64_t t) {
     p.s = 256;
     if (tiles(256) * all < 256 * 16) p.s = 128;
     if (p.s == 128 && tiles(128) * all < 256 * 8) p.s = 64;
-    int64_t z = 256 / tiles(p.s);
-    if (z > all / 4) z = all / 4;
+    int64_t z = (p.s == 64 ? 1024 : 256) / tiles(p.s);
+    if (z > all / (p.s == 64 ? 2 : 4)) z = all / (p.s == 64 ? 2 : 4);
     if (z < 1) z = 1;
     p.chunks = (int)((all + z - 1) / z + 1) & ~1;
     p.z = p.chunks ? (int)((all + p.chunks - 1) / p.chunks) : 1;
@@ -451,7 +457,7 @@ aq_status launch(const A& a, const B& b, T* out, int64_t ld, int64_t stride, flo
     const int64_t x = (m + S - 1) / S, y = (c + S - 1) / S;
     if (!grid_ok(x * y * p.z, tile_threads(S))) return AQ_ESHAPE;
     auto* const k = k_grad<A, B, T, S>;
-    if (hip_failed(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds))) return AQ_EHIP;
+    if (!allow_lds<A, B, T, std::integral_constant<int, S>>((const void*)k, kLds)) return AQ_EHIP;
     k<<<(unsigned)(x * y * p.z), tile_threads(S), kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks, track_turns(32 * bytes_per_t) & ~1);
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }

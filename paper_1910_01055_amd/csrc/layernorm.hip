@@ -243,7 +243,13 @@ __global__ void __launch_bounds__(1024) k_layernorm_join(const float* __restrict
     const int64_t width = 2 * (int64_t)cols;
     float s = 0.0f;
     if (c < width)
-        for (int i = slice; i < parts; i += 32) s += part[i * width + c];
+        for (int i = slice; i < parts; i += 32 * 8) {  // eight on their way at a time
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = i + 32 * j < parts ? part[(i + 32 * j) * width + c] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += v[j];
+        }
     red[slice][threadIdx.x & 31] = s;
     __syncthreads();
     if (slice == 0 && c < width) {
@@ -289,7 +295,7 @@ int64_t at_a_time(const Form& f) { return f.g < 256 ? 256 / f.g : 1; }
 // workgroups of the backward pass: every one leaves 8 bytes a column behind
 int64_t backward_workgroups(int64_t rows, int64_t cols) {
     const int64_t turns = (rows + at_a_time(row_form(cols)) - 1) / at_a_time(row_form(cols));
-    const int64_t g = (turns + 3) / 4;
+    const int64_t g = (turns + 1) / 2;
     return g < 1 ? 1 : g > 512 ? 512 : g;
 }
 

@@ -14,6 +14,17 @@ inline aq_status with_dtype(int32_t dtype, Go&& go) {
 inline size_t dtype_bytes(int32_t dtype) { return dtype == AQ_F32 ? 4 : 2; }
 inline int64_t blocks32(int64_t cols) { return (cols + 31) / 32; }
 
+// Lets a kernel have `bytes` of dynamic LDS, once (Key...: what tells it from the others).
+template <class... Key>
+inline bool allow_lds(const void* kernel, int bytes) {
+    static std::atomic<bool> set{false};
+    if (bytes > 64 * 1024 && !set) {
+        if (hip_failed(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes))) return false;
+        set = true;
+    }
+    return true;
+}
+
 // ---- layernorm.hip
 aq_status launch_layernorm_forward(const aq_matrix& x, const float* gamma, const float* beta, float eps, const aq_matrix& y,
                                    float* mean, float* rstd, const aq_ckpt8* kept, hipStream_t st);

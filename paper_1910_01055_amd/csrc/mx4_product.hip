@@ -20,9 +20,21 @@ struct Blocks {  // rows that are quantized already
     const uint8_t* codes;
     const uint8_t* scales;
     int64_t blocks;
-    __device__ __forceinline__ void get(int64_t row, int64_t b, v4u& c, uint32_t& scale) const {
-        c = *(const v4u AQ_GLOBAL*)(codes + (row * blocks + b) * 16);
-        scale = ((const uint8_t AQ_GLOBAL*)scales)[row * blocks + b];
+    struct Raw {
+        v4u c;
+        uint32_t scale;
+    };
+    __device__ __forceinline__ void request(int64_t row, int64_t b, bool there, Raw& q) const {
+        q.c = v4u{0, 0, 0, 0};
+        q.scale = 0;
+        if (there) {
+            q.c = *(const v4u AQ_GLOBAL*)(codes + (row * blocks + b) * 16);
+            q.scale = ((const uint8_t AQ_GLOBAL*)scales)[row * blocks + b];
+        }
+    }
+    __device__ __forceinline__ void get(const Raw& q, v4u& c, uint32_t& scale) const {
+        c = q.c;
+        scale = q.scale;
     }
 };
 template <class T>
@@ -30,17 +42,26 @@ struct Values {  // rows of values, quantized in the lane that needs them
     const T* x;
     int64_t ld;
     int cols;
-    __device__ __forceinline__ void get(int64_t row, int64_t b, v4u& c, uint32_t& scale) const {
-        const T* p = x + row * ld + b * 32;
-        const int n = cols - (int)b * 32;
+    struct Raw {
         Piece<T> q[4];
+    };
+    __device__ __forceinline__ void request(int64_t row, int64_t b, bool there, Raw& raw) const {
+        const T* p = x + row * ld + b * 32;
+        const int n = there ? cols - (int)b * 32 : 0;
+        if (n >= 32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i].load(p + 8 * i, n - 8 * i);
+            for (int i = 0; i < 4; ++i) raw.q[i].load_all(p + 8 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw.q[i].load(p + 8 * i, n - 8 * i);
+        }
+    }
+    __device__ __forceinline__ void get(const Raw& raw, v4u& c, uint32_t& scale) const {
         float v[4][8];
         uint32_t most = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            q[i].get(v[i]);
+            raw.q[i].get(v[i]);
             const uint32_t m = most_of8(v[i]);
             most = m > most ? m : most;
         }
@@ -59,20 +80,31 @@ __global__ void __launch_bounds__(64 * W)
     v4f32 acc[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[i] = v4f32{0, 0, 0, 0};
-    for (int b0 = 4 * wave; b0 < blocks; b0 += 4 * W) {
-        const int b = b0 + g;
-        v4u cw{0, 0, 0, 0}, cx[RT];
-        uint32_t sw = 0, sx[RT];
-        if (b < blocks && n0 + r < n) w.get(n0 + r, b, cw, sw);
+    constexpr int U = 2;  // turns whose operands are requested together
+    for (int b0 = 4 * wave; b0 < blocks; b0 += 4 * W * U) {
+        v4u cw[U], cx[U][RT];
+        uint32_t sw[U], sx[U][RT];
+        typename X::Raw raw[U][RT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            cx[i] = v4u{0, 0, 0, 0};
-            sx[i] = 0;
-            if (b < blocks && m0 + 16 * i + r < rows) x.get(m0 + 16 * i + r, b, cx[i], sx[i]);
+        for (int u = 0; u < U; ++u) {
+            const int b = b0 + 4 * W * u + g;
+            cw[u] = v4u{0, 0, 0, 0};
+            sw[u] = 0;
+            if (b < blocks && n0 + r < n) {
+                cw[u] = *(const v4u AQ_GLOBAL*)(w.codes + ((n0 + r) * blocks + b) * 16);
+                sw[u] = ((const uint8_t AQ_GLOBAL*)w.scales)[(n0 + r) * blocks + b];
+            }
+#pragma unroll
+            for (int i = 0; i < RT; ++i) x.request(m0 + 16 * i + r, b, b < blocks && m0 + 16 * i + r < rows, raw[u][i]);
         }
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-            acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(cw), operand(cx[i]), acc[i], kFp4, kFp4, 0, (int)sw, 0, (int)sx[i]);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                x.get(raw[u][i], cx[u][i], sx[u][i]);
+                acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(cw[u]), operand(cx[u][i]), acc[i], kFp4, kFp4, 0, (int)sw[u], 0,
+                                                                        (int)sx[u][i]);
+            }
     }
 #pragma unroll
     for (int i = 0; i < RT; ++i) part[wave][i][lane] = acc[i];
@@ -269,7 +301,7 @@ aq_status launch_tiles(const aq_mx4& x, const aq_mx4& w, const float* bias, cons
     if (!grid_ok(tiles, 512)) return AQ_ESHAPE;
     constexpr int NT = tile_threads(S);
     auto* const k = k_mx4_tiles<T, S, NT>;
-    if (hip_failed(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds))) return AQ_EHIP;
+    if (!allow_lds<Blocks, T, std::integral_constant<int, S>>((const void*)k, kLds)) return AQ_EHIP;
     k<<<(unsigned)tiles, NT, kLds, st>>>(blocks_of(x), blocks_of(w), bias, (T*)y.d, y.ld, (int)x.rows, (int)w.rows,
                                                       (int)blocks32(w.cols));
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;

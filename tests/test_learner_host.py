@@ -9,11 +9,11 @@ M, K = B.AqMatrix, B.AqBlocks
 
 
 def mat(rows, cols, dtype=0, ld=None, d=0x10000):
-    return M(d, rows, cols, cols if ld is None else ld, dtype)
+    return C.byref(M(d, rows, cols, cols if ld is None else ld, dtype))
 
 
 def blk(rows, cols, codes=0x20000, scales=0x30001):
-    return K(codes, scales, rows, cols)
+    return C.byref(K(codes, scales, rows, cols))
 
 
 BAD_MATRICES = [(None, B.EINVAL), (mat(4, 32, d=None), B.EINVAL), (mat(-1, 32), B.EINVAL), (mat(4, -1), B.EINVAL), (mat(4, 32, ld=31), B.EINVAL),
@@ -141,7 +141,7 @@ def test_the_binding_checks_tensors():
         B._matrix(x.double())
     with pytest.raises(ValueError):
         B._matrix(x[0])
-    m = B._matrix(x[:, 3:40])
+    m = M.from_buffer_copy(B._matrix(x[:, 3:40]))
     assert (m.rows, m.cols, m.ld, m.dtype) == (4, 37, 64, 0) and m.d == x.data_ptr() + 12
     with pytest.raises(ValueError):
         B._vector(torch.zeros(5), 4, "v")
@@ -151,6 +151,8 @@ def test_the_binding_checks_tensors():
         B._vector(torch.zeros(4, dtype=torch.float16), 4, "v")
     for make in (B.ckpt8_empty, B.mx4_empty):
         q = make(3, 70, device="cpu")
+        c = K.from_buffer_copy(q._c)
+        assert (c.rows, c.cols) == (3, 70) and c.d_codes == q.codes.data_ptr() and c.d_scales == q.scales.data_ptr()
         assert tuple(q.scales.shape) == (3, 3) and q.codes.shape[1] == 3 * q.CODE_BYTES
         with pytest.raises(ValueError):
             type(q)(q.codes, q.scales, 97)
