@@ -8,6 +8,8 @@
 // A workgroup's 32 t of both operands go through LDS.  B lies there as it does in memory, t by t (and so does A for the weight
 // gradient), and is transposed on its way to the registers: ds_read_b64_tr_b16 hands lane i of 16 the four t of column i out of
 // four rows of 16 columns.
+#include <utility>
+
 #include "learner.hpp"
 #include "product_device.hpp"
 
@@ -272,6 +274,16 @@ struct BlockRows {
     }
 };
 
+// calls f(integral_constant i) for i = 0 .. N - 1
+template <int N, class F, int... I>
+__device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+    static_for<N>(f, std::make_integer_sequence<int, N>());
+}
+
 // C tile of S x S, a wavefront takes S / 2 rows and NC * 32 columns of it.  Slice z takes t in [z * chunks * 32, + chunks * 32) and writes its own C (and its
 // own sums of A over t, where `sums` is given).  While the products of one 32 t run, the next 32 t go from registers to LDS, unit
 // by unit, and one or two more are on their way from memory behind them; with three buffers the barrier lies
@@ -292,10 +304,9 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
     a.begin(m0, t_first, tn);
     b.begin(c0, t_first, tn);
     v16f32 acc[N][NC];
-    float acc_sum[N];
+    float acc_sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        acc_sum[i] = 0.0f;
 #pragma unroll
         for (int j = 0; j < NC; ++j)
 #pragma unroll
@@ -308,14 +319,16 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
             b.fetch(set, i);
         }
     };
+    // A wavefront begins with the row tile of its own number among those that share the rows, whose sums it takes: all rows' sums at a
+    // fraction of the cost that one wavefront's would have, and no jumps.
+    auto tile_of = [&](int i) __attribute__((always_inline)) { return A::kSums ? (i + (wave >> 1)) % N : i; };
     // group q: 16 t from 16 (q / (P N)), part P - 1 - q / N mod P (the smallest first), row tile q mod N
     auto read_a = [&](const uint8_t* tile, int q) __attribute__((always_inline)) {
-        return A::operand(tile + (P - 1 - q / N % P) * A::kPlane, 16 * (q / (P * N)), wm + 32 * (q % N), lane);
+        return A::operand(tile + (P - 1 - q / N % P) * A::kPlane, 16 * (q / (P * N)), wm + 32 * tile_of(q % N), lane);
     };
     auto read_b = [&](const uint8_t* tile, int j) __attribute__((always_inline)) {  // j: 16 t from 16 (j / NC), column tile j mod NC
         return t_operand<S>(tile + P * A::kPlane, 16 * (j / NC), wc + 32 * (j % NC), lane);
     };
-    const bool summing = A::kSums && sums && at.c == 0 && wave < 2;  // (wavefronts 0 and 1 have all rows between them)
     {
         const v2bf16 ones = __builtin_bit_cast(v2bf16, 0x3f803f80u);
 #pragma unroll
@@ -339,8 +352,8 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
             uint8_t* const next = lds + now;
             v8bf16 ob_next[2 * NC], oa_next;
             constexpr int kTasks = 2 * A::kUnits, kSlots = G > 2 ? G - 2 : 1;
-#pragma unroll
-            for (int q = 0; q < G; ++q) {
+            static_for<G>([&](auto group) __attribute__((always_inline)) {
+                constexpr int q = decltype(group)::value;
                 if (kBufs == 3 && q >= kSlots) {
                     if (q == kSlots) lds_barrier();
 #pragma unroll
@@ -351,12 +364,12 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
 #pragma unroll
                 for (int j = 0; j < NC; ++j)
                     acc[q % N][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ob[q / (P * N) * NC + j], oa, acc[q % N][j], 0, 0, 0);
-                if (summing) {
+                if constexpr (A::kSums && q % N == 0) {
                     const v4u w = __builtin_bit_cast(v4u, oa);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const uint32_t pair = w[j];  // (a vector's element itself is not cast right: the first one is taken for all)
-                        acc_sum[q % N] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf16, pair), ones, acc_sum[q % N], false);
+                        acc_sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf16, pair), ones, acc_sum, false);
                     }
                 }
 #pragma unroll
@@ -372,7 +385,7 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
                     }
                 oa = oa_next;
                 __builtin_amdgcn_sched_barrier(0);  // (loads stay in the order in which they are waited for)
-            }
+            });
             if constexpr (kBufs == 3) {
 #pragma unroll
                 for (int j = 0; j < 2 * NC; ++j) ob[j] = ob_next[j];
@@ -399,12 +412,14 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
     lds_barrier();  // (every wavefront has read its last operands)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int64_t row = m0 + wm + 32 * i, m = row + r;
+        const int64_t row = m0 + wm + 32 * tile_of(i), m = row + r;
         store_rows<T, NC>(lds + wave * (32 * kOutRow<T, NC>), lane, out + row * ld + c0 + wc, ld, mn - row, cn - c0 - wc,
                           [&](int j, int q, int e) { return acc[i][j][4 * q + e]; });
         if constexpr (A::kSums) {
-            const float s = acc_sum[i] + __shfl_xor(acc_sum[i], 32, 64);
-            if (summing && g == 0 && m < mn) sums[at.z * mn + m] = s;
+            if (i == 0) {
+                const float s = acc_sum + __shfl_xor(acc_sum, 32, 64);
+                if (sums && at.c == 0 && wave >> 1 < N && g == 0 && m < mn) sums[at.z * mn + m] = s;
+            }
         }
     }
 }
