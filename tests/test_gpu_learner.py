@@ -379,7 +379,8 @@ def test_weight_grad_of_wide_ranges():
 # ---- 4-bit layers
 
 LINEAR_SHAPES = [(1, 1, 1), (1, 256, 67), (1, 17, 2048), (2, 40, 33), (15, 100, 130), (16, 64, 128), (17, 21, 256), (64, 130, 1000), (65, 33, 257),
-                 (128, 128, 256), (129, 257, 300), (300, 403, 1111), (700, 64, 64), (1030, 8, 4096)]
+                 (128, 128, 256), (129, 257, 300), (300, 403, 1111), (700, 64, 64), (1030, 8, 4096),
+                 (2051, 2100, 300), (4101, 4099, 200)]  # the larger tiles
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
@@ -431,7 +432,8 @@ def test_mx4_linear_of_what_is_not_finite(rows):
     assert torch.equal(torch.isnan(y.cpu()), bad) and bool(torch.isfinite(y.cpu()[~bad]).all())
 
 
-IG_SHAPES = [(1, 1, 1), (1, 17, 256), (2, 40, 33), (63, 65, 67), (64, 64, 128), (129, 128, 129), (300, 403, 1111), (700, 21, 64), (4100, 33, 40)]
+IG_SHAPES = [(1, 1, 1), (1, 17, 256), (2, 40, 33), (63, 65, 67), (64, 64, 128), (129, 128, 129), (300, 403, 1111), (700, 21, 64), (4100, 33, 40),
+             (520, 2885, 523), (1030, 5443, 1029), (1030, 5440, 1024)]  # the larger tiles; rows that end inside a piece and not
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
@@ -454,6 +456,74 @@ def test_mx4_input_grad(rows, n, k, kind):
         near(X.get(), want, off + OUT[kind] * (want.abs() + off) + TINY[kind])
         results.append(X.get())
     assert all(torch.equal(r, results[0]) for r in results)
+
+
+# ---- far apart, and many
+
+FAR = 1 << 21  # the largest distance between rows
+
+
+def far(rows, cols, values):
+    """Rows that lie as far apart as they may."""
+    m = torch.empty(rows * FAR, dtype=values.dtype, device=DEV).view(rows, FAR)[:, 3:3 + cols]
+    m.copy_(values)
+    return m
+
+
+def test_rows_far_apart():
+    """Offsets that pass 32 bits; the gradients' windows, which hold two or three dozen of such rows, move on."""
+    rows, k, n = 600, 40, 33
+    g = rng("far")
+    x, dy, w = normal(g, rows, k), normal(g, rows, n), normal(g, n, k)
+    X, D = far(rows, k, x), far(rows, n, dy)
+    kept, near_kept, q = B.ckpt8_empty(rows, k), B.ckpt8_empty(rows, k), B.mx4_empty(n, k)
+    B.ckpt8_pack(X, kept)
+    B.ckpt8_pack(x.to(DEV), near_kept)
+    assert torch.equal(kept.codes, near_kept.codes) and torch.equal(kept.scales, near_kept.scales)
+    B.mx4_quantize(w.to(DEV), q)
+    ws = torch.empty(max(16, B.ckpt8_weight_grad_workspace(rows, n, k), B.mx4_linear_workspace(rows, n, k), B.mx4_input_grad_workspace(rows, n, k),
+                         B.layernorm_backward_workspace(rows, k)), dtype=torch.uint8, device=DEV)
+    both = []
+    for a, d in ((X, D), (x.to(DEV), dy.to(DEV))):
+        out = [torch.empty(s, device=DEV) for s in ((n, k), (n,), (rows, n), (rows, k), (rows, k), (rows,), (rows,), (rows, k), (k,), (k,))]
+        dw, db, y, dx, h, mean, rstd, dh, dg, dbe = out
+        B.ckpt8_weight_grad(d, kept, dw, db, ws)
+        B.mx4_linear(a, q, None, y, ws)
+        B.mx4_input_grad(d, q, dx, ws)
+        B.layernorm_forward(a, None, None, 1e-5, h, mean, rstd)
+        B.layernorm_backward(a, a, None, mean, rstd, dh, dg, dbe, ws)
+        both.append(out)
+    assert all(torch.equal(p, q) for p, q in zip(*both))
+    near(both[0][0].cpu().double(), dy.double().t() @ ckpt8_values(kept), (3 * rows + 8) * U * (dy.double().abs().t() @ ckpt8_values(kept).abs()))
+    del X, D
+    # the same of a tensor that one call writes
+    out = torch.full((rows, FAR), SENTINEL, device=DEV)
+    B.ckpt8_unpack(kept, out[:, 5:5 + k])
+    assert torch.equal(out[:, 5:5 + k].cpu().double(), ckpt8_values(kept)) and bool((out[:, :5] == SENTINEL).all()) and bool((out[:, 5 + k:] == SENTINEL).all())
+
+
+def test_many_rows():
+    """More rows than a launch has rows of workgroups, for the formats, and than all workgroups hold at once."""
+    rows, cols = 4_300_003, 20
+    x = torch.randn(rows, cols, device=DEV, dtype=torch.bfloat16)
+    some = torch.cat([torch.arange(0, 300), torch.arange(rows - 300, rows), torch.randint(0, rows, (500,), generator=rng("many"))])
+    kept, q = B.ckpt8_empty(rows, cols), B.mx4_empty(rows, cols)
+    back = torch.empty_like(x)
+    xs = x[some.to(DEV)].cpu().double()
+    for pack, unpack, b, ref in ((B.ckpt8_pack, B.ckpt8_unpack, kept, ckpt8_ref), (B.mx4_quantize, B.mx4_dequantize, q, mx4_ref)):
+        pack(x, b)
+        unpack(b, back.fill_(SENTINEL))
+        assert torch.equal(back[some.to(DEV)].cpu().double(), ref(xs)[3])
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    B.layernorm_forward(x, None, None, 1e-5, y, mean, rstd)
+    m = xs.mean(1, keepdim=True)
+    want = (xs - m) / torch.sqrt(((xs - m) ** 2).mean(1, keepdim=True) + 1e-5)
+    near(y[some.to(DEV)].cpu().double(), want, 2.0 ** -8 * want.abs() + 64 * U * (1 + want.abs()) * 8)
+    dx, dg, db = torch.empty_like(x), torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+    ws = torch.empty(max(16, B.layernorm_backward_workspace(rows, cols)), dtype=torch.uint8, device=DEV)
+    B.layernorm_backward(x, kept, None, mean, rstd, dx, dg, db, ws)
+    total, size = x.double().sum(0), x.double().abs().sum(0)
+    near(db.cpu().double(), total.cpu(), ((rows // 8192 + 64) * U * size).cpu())  # 512 workgroups of 16 rows at a time
 
 
 # ---- how they are called
