@@ -8,6 +8,8 @@
 // A workgroup's 32 t of both operands go through LDS.  B lies there as it does in memory, t by t (and so does A for the weight
 // gradient), and is transposed on its way to the registers: ds_read_b64_tr_b16 hands lane i of 16 the four t of column i out of
 // four rows of 16 columns.
+#include <math.h>
+
 #include <utility>
 
 #include "learner.hpp"
@@ -450,19 +452,47 @@ __global__ void __launch_bounds__(256) k_grad_join(const float* __restrict__ par
 struct Plan {
     int s, z, chunks;
 };
-Plan plan(int64_t m, int64_t c, int64_t t) {
-    auto tiles = [&](int64_t s) { return ((m < 1 ? 1 : m) + s - 1) / s * ((c + s - 1) / s); };
+// The tile and the slices by an estimate in us: what a launch takes besides its chunks; the chunks of a workgroup one after the
+// other, each as long as `alone` while few workgroups are about and `full` while as many as fit are (`at_once`); the join's launch
+// and bytes.  Fitted to weight gradients of 2048 rows with every tile in one slice, us on tiles of 64 / 128 / 256:
+//   bfloat16 2048 x 2048 50.9 / 38.9 / 55.4, 1024 x 1024 20.4 / 32.9 / 50.5, 128 x 128 18.3 / 31.3 / 49.1 (256 rows 5.0 / 7.7 / 12.1)
+//   binary16            106.3 / 107.6 / 143.5,            56.0 / 102.6 / 141.1,          54.6 / 100.7 / 139.4 (9.7 / 17.3 / 24.4)
+//   fp32                163.8 / 146.2 / 199.4,            76.1 / 144.3 / 196.1,          75.1 / 141.8 / 194.2 (12.6 / 23.0 / 31.9)
+Plan plan(int64_t m, int64_t c, int64_t t, int parts) {
+    constexpr struct {
+        int s, at_once;
+        float launch, alone, full;
+    } kinds[3][3] = {{{64, 1024, 3.1f, 0.24f, 0.75f}, {128, 512, 4.3f, 0.42f, 0.86f}, {256, 256, 6.8f, 0.66f, 1.07f}},
+                     {{64, 1024, 3.3f, 0.80f, 1.61f}, {128, 512, 5.4f, 1.49f, 2.16f}, {256, 256, 8.0f, 2.05f, 2.30f}},
+                     {{64, 1024, 3.7f, 1.12f, 2.50f}, {128, 256, 6.0f, 2.12f, 2.20f}, {256, 256, 8.7f, 2.90f, 3.10f}}};
     const int64_t all = (t + 31) / 32;
-    Plan p;
-    p.s = 256;
-    if (tiles(256) * all < 256 * 16) p.s = 128;
-    if (p.s == 128 && tiles(128) * all < 256 * 8) p.s = 64;
-    int64_t z = (p.s == 64 ? 1024 : 256) / tiles(p.s);
-    if (z > all / (p.s == 64 ? 2 : 4)) z = all / (p.s == 64 ? 2 : 4);
-    if (z < 1) z = 1;
-    p.chunks = (int)((all + z - 1) / z + 1) & ~1;
-    p.z = p.chunks ? (int)((all + p.chunks - 1) / p.chunks) : 1;
-    return p;
+    Plan best{64, 1, (int)((all + 1) & ~1)};
+    float least = 3.0e38f;
+    for (const auto& k : kinds[parts - 1]) {
+        const int64_t tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + k.s - 1) / k.s);
+        for (int64_t want = 1; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
+            const int64_t chunks = ((all + want - 1) / want + 1) & ~1, z = chunks ? (all + chunks - 1) / chunks : 1;
+            const float full = (float)(tiles * z) / (float)k.at_once;
+            float us = k.launch + (float)chunks * (full < 1.0f ? k.alone + (k.full - k.alone) * full * full : k.full * ceilf(full));
+            if (z > 1) us += 2.5f + (float)(z * m * c * 4) * (1.0f / 3.5e6f);
+            if (us < least) {
+                least = us;
+                best = {k.s, (int)z, (int)chunks};
+            }
+        }
+    }
+    return best;
+}
+int parts_of(int32_t dtype) { return dtype == AQ_BF16 ? 1 : dtype == AQ_F16 ? 2 : 3; }
+int64_t slices_bytes(int64_t z, int64_t values) { return z > 1 ? z * values * (int64_t)sizeof(float) : 0; }
+// the most slices that a product of any type takes
+int64_t most_slices(int64_t m, int64_t c, int64_t t) {
+    int64_t z = 1;
+    for (int parts = 1; parts <= 3; ++parts) {
+        const int64_t own = plan(m, c, t, parts).z;
+        z = own > z ? own : z;
+    }
+    return z;
 }
 
 template <class A, class B, class T, int S>
@@ -497,15 +527,14 @@ bool any_pieces(const aq_matrix& m, bool whole) {
 
 }  // namespace
 
-int64_t weight_grad_workspace(int64_t rows, int64_t n, int64_t k) {
-    const Plan p = plan(n, k, rows);
-    return p.z > 1 ? p.z * (n * k + n) * (int64_t)sizeof(float) : 0;
-}
+int64_t weight_grad_workspace(int64_t rows, int64_t n, int64_t k) { return slices_bytes(most_slices(n, k, rows), n * k + n); }
 
-aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq_matrix& dw, float* db, void* ws, hipStream_t st) {
+aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq_matrix& dw, float* db, void* ws, uint64_t ws_bytes,
+                             hipStream_t st) {
     const int64_t n = dy.cols, k = kept.cols, rows = dy.rows;
-    const Plan p = plan(n, k, rows);
+    const Plan p = plan(n, k, rows, parts_of(dy.dtype));
     const bool split_t = p.z > 1;
+    if (!workspace_ok(ws, ws_bytes, slices_bytes(p.z, n * k + n))) return AQ_EINVAL;
     float* const out = split_t ? (float*)ws : (float*)dw.d;
     float* const sums = !db ? nullptr : split_t ? (float*)ws + p.z * n * k : db;
     const aq_status s = with_dtype(dy.dtype, [&](auto t) {
@@ -525,14 +554,12 @@ aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq
     return join((const float*)ws, p, n, k, (float*)dw.d, dw.ld, sums, db, st);
 }
 
-int64_t input_grad_workspace(int64_t rows, int64_t n, int64_t k) {
-    const Plan p = plan(rows, k, n);
-    return p.z > 1 ? p.z * rows * k * (int64_t)sizeof(float) : 0;
-}
+int64_t input_grad_workspace(int64_t rows, int64_t n, int64_t k) { return slices_bytes(most_slices(rows, k, n), rows * k); }
 
-aq_status launch_input_grad(const aq_matrix& dy, const aq_mx4& w, const aq_matrix& dx, void* ws, hipStream_t st) {
+aq_status launch_input_grad(const aq_matrix& dy, const aq_mx4& w, const aq_matrix& dx, void* ws, uint64_t ws_bytes, hipStream_t st) {
     const int64_t n = w.rows, k = w.cols, rows = dy.rows;
-    const Plan p = plan(rows, k, n);
+    const Plan p = plan(rows, k, n, parts_of(dy.dtype));
+    if (!workspace_ok(ws, ws_bytes, slices_bytes(p.z, rows * k))) return AQ_EINVAL;
     return with_dtype(dy.dtype, [&](auto t) {
         using T = decltype(t);
         const aq_status s = with_tile(p.s, [&](auto sc) {

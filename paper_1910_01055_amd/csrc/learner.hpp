@@ -25,6 +25,11 @@ inline bool allow_lds(const void* kernel, int bytes) {
     return true;
 }
 
+// scratch of the caller's: enough, and where 16-byte accesses may begin
+inline bool workspace_ok(const void* ws, uint64_t have, int64_t need) {
+    return (uint64_t)need <= have && (need == 0 || ws) && ((uintptr_t)ws & 15) == 0;
+}
+
 // ---- layernorm.hip
 aq_status launch_layernorm_forward(const aq_matrix& x, const float* gamma, const float* beta, float eps, const aq_matrix& y,
                                    float* mean, float* rstd, const aq_ckpt8* kept, hipStream_t st);
@@ -42,8 +47,9 @@ aq_status launch_mx4_linear(const aq_matrix& x, const aq_mx4& w, const float* bi
 aq_status launch_mx4_matmul(const aq_mx4& x, const aq_mx4& w, const float* bias, const aq_matrix& y, hipStream_t st);
 // ---- grad_product.hip
 int64_t weight_grad_workspace(int64_t rows, int64_t n, int64_t k);
-aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq_matrix& dw, float* db, void* ws, hipStream_t st);
+aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq_matrix& dw, float* db, void* ws, uint64_t ws_bytes,
+                             hipStream_t st);
 int64_t input_grad_workspace(int64_t rows, int64_t n, int64_t k);
-aq_status launch_input_grad(const aq_matrix& dy, const aq_mx4& w, const aq_matrix& dx, void* ws, hipStream_t st);
+aq_status launch_input_grad(const aq_matrix& dy, const aq_mx4& w, const aq_matrix& dx, void* ws, uint64_t ws_bytes, hipStream_t st);
 
 }  // namespace aq

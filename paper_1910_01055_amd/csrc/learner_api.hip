@@ -27,11 +27,6 @@ aq_status blocks_ok(const Blocks32* b) {
     return AQ_OK;
 }
 bool floats_ok(const void* p) { return ((uintptr_t)p & 3) == 0; }
-// optional vectors of floats and scratch
-aq_status workspace_ok(const void* ws, uint64_t have, int64_t need) {
-    if ((uint64_t)need > have || (need > 0 && !ws) || ((uintptr_t)ws & 15)) return AQ_EINVAL;
-    return AQ_OK;
-}
 aq_status sizes_ok(int64_t rows, int64_t n, int64_t k, const uint64_t* bytes) {
     if (!bytes || rows < 0 || n < 0 || k < 0) return AQ_EINVAL;
     return rows > kMostRows || n < 1 || n > kMostCols || k < 1 || k > kMostCols ? AQ_ESHAPE : AQ_OK;
@@ -77,7 +72,7 @@ extern "C" aq_status aq_layernorm_backward(const aq_matrix* dy, const aq_matrix*
     if (dy->cols > AQ_LAYERNORM_MAX_COLS || dx->rows != dy->rows || dx->cols != dy->cols || dx->dtype != dy->dtype) return AQ_ESHAPE;
     if (x && (x->rows != dy->rows || x->cols != dy->cols || x->dtype != dy->dtype)) return AQ_ESHAPE;
     if (kept && (kept->rows != dy->rows || kept->cols != dy->cols)) return AQ_ESHAPE;
-    AQ_TRY(workspace_ok(d_workspace, workspace_bytes, layernorm_backward_workspace(dy->rows, dy->cols)));
+    if (!workspace_ok(d_workspace, workspace_bytes, layernorm_backward_workspace(dy->rows, dy->cols))) return AQ_EINVAL;
     return launch_layernorm_backward(*dy, x, kept, d_gamma, d_mean, d_rstd, *dx, d_dgamma, d_dbeta, (float*)d_workspace, as_stream(stream));
 }
 
@@ -108,8 +103,7 @@ extern "C" aq_status aq_ckpt8_weight_grad(const aq_matrix* dy, const aq_ckpt8* k
     AQ_TRY(matrix_ok(dw));
     if (!floats_ok(d_db)) return AQ_EINVAL;
     if (kept->rows != dy->rows || dw->rows != dy->cols || dw->cols != kept->cols || dw->dtype != AQ_F32) return AQ_ESHAPE;
-    AQ_TRY(workspace_ok(d_workspace, workspace_bytes, weight_grad_workspace(dy->rows, dy->cols, kept->cols)));
-    return launch_weight_grad(*dy, *kept, *dw, d_db, d_workspace, as_stream(stream));
+    return launch_weight_grad(*dy, *kept, *dw, d_db, d_workspace, workspace_bytes, as_stream(stream));
 }
 
 extern "C" aq_status aq_mx4_quantize(const aq_matrix* x, const aq_mx4* q, void* stream) {
@@ -139,7 +133,7 @@ extern "C" aq_status aq_mx4_linear(const aq_matrix* x, const aq_mx4* w, const fl
     AQ_TRY(matrix_ok(y));
     if (!floats_ok(d_bias)) return AQ_EINVAL;
     if (w->cols != x->cols || y->rows != x->rows || y->cols != w->rows || y->dtype != x->dtype) return AQ_ESHAPE;
-    AQ_TRY(workspace_ok(d_workspace, workspace_bytes, mx4_linear_workspace(x->rows, w->rows, w->cols)));
+    if (!workspace_ok(d_workspace, workspace_bytes, mx4_linear_workspace(x->rows, w->rows, w->cols))) return AQ_EINVAL;
     return x->rows == 0 ? AQ_OK : launch_mx4_linear(*x, *w, d_bias, *y, d_workspace, as_stream(stream));
 }
 
@@ -164,6 +158,5 @@ extern "C" aq_status aq_mx4_input_grad(const aq_matrix* dy, const aq_mx4* w, con
     AQ_TRY(blocks_ok(w));
     AQ_TRY(matrix_ok(dx));
     if (w->rows != dy->cols || dx->rows != dy->rows || dx->cols != w->cols || dx->dtype != dy->dtype) return AQ_ESHAPE;
-    AQ_TRY(workspace_ok(d_workspace, workspace_bytes, input_grad_workspace(dy->rows, w->rows, w->cols)));
-    return dy->rows == 0 ? AQ_OK : launch_input_grad(*dy, *w, *dx, d_workspace, as_stream(stream));
+    return dy->rows == 0 ? AQ_OK : launch_input_grad(*dy, *w, *dx, d_workspace, workspace_bytes, as_stream(stream));
 }

@@ -15,7 +15,9 @@ constexpr int kFp4 = 4;  // the instructions' number of the 4-bit format
 
 __device__ __forceinline__ v8i32 operand(v4u c) { return v8i32{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}; }
 
-// ---- few rows: 16 features to a workgroup, whose W wavefronts take turns along k and join their sums in LDS; RT tiles of 16 rows.
+// ---- few rows: 16 features by 16 rows to a workgroup, whose eight wavefronts take turns along k and join their sums in LDS.  Bound by
+// latency: a launch, one trip to memory, a barrier (2048 x 2048 weights, one bfloat16 row: 4.1 us, of which an empty kernel is 2.3;
+// four wavefronts 4.4, two tiles of rows to a workgroup 5.2).
 struct Blocks {  // rows that are quantized already
     const uint8_t* codes;
     const uint8_t* scales;
@@ -71,20 +73,18 @@ struct Values {  // rows of values, quantized in the lane that needs them
     }
 };
 
-template <class X, class T, int RT, int W>
-__global__ void __launch_bounds__(64 * W)
+template <class X, class T>
+__global__ void __launch_bounds__(512)
     k_mx4_rows(X x, Blocks w, const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int rows, int n, int blocks) {
-    __shared__ v4f32 part[W][RT][64];
+    constexpr int W = 8, U = 2;  // wavefronts; turns whose operands are requested together
+    __shared__ v4f32 part[W][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * RT);
-    v4f32 acc[RT];
-#pragma unroll
-    for (int i = 0; i < RT; ++i) acc[i] = v4f32{0, 0, 0, 0};
-    constexpr int U = 2;  // turns whose operands are requested together
+    const int64_t n0 = (int64_t)blockIdx.x * 16, row = (int64_t)blockIdx.y * 16 + r;
+    v4f32 acc{0, 0, 0, 0};
     for (int b0 = 4 * wave; b0 < blocks; b0 += 4 * W * U) {
-        v4u cw[U], cx[U][RT];
-        uint32_t sw[U], sx[U][RT];
-        typename X::Raw raw[U][RT];
+        v4u cw[U], cx[U];
+        uint32_t sw[U], sx[U];
+        typename X::Raw raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int b = b0 + 4 * W * u + g;
@@ -94,31 +94,24 @@ __global__ void __launch_bounds__(64 * W)
                 cw[u] = *(const v4u AQ_GLOBAL*)(w.codes + ((n0 + r) * blocks + b) * 16);
                 sw[u] = ((const uint8_t AQ_GLOBAL*)w.scales)[(n0 + r) * blocks + b];
             }
-#pragma unroll
-            for (int i = 0; i < RT; ++i) x.request(m0 + 16 * i + r, b, b < blocks && m0 + 16 * i + r < rows, raw[u][i]);
+            x.request(row, b, b < blocks && row < rows, raw[u]);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                x.get(raw[u][i], cx[u][i], sx[u][i]);
-                acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(cw[u]), operand(cx[u][i]), acc[i], kFp4, kFp4, 0, (int)sw[u], 0,
-                                                                        (int)sx[u][i]);
-            }
+        for (int u = 0; u < U; ++u) {
+            x.get(raw[u], cx[u], sx[u]);
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(cw[u]), operand(cx[u]), acc, kFp4, kFp4, 0, (int)sw[u], 0, (int)sx[u]);
+        }
     }
-#pragma unroll
-    for (int i = 0; i < RT; ++i) part[wave][i][lane] = acc[i];
+    part[wave][lane] = acc;
     __syncthreads();
-    for (int i = wave; i < RT; i += W) {
-        v4f32 s = part[0][i][lane];
+    if (wave == 0) {
+        v4f32 s = part[0][lane];
 #pragma unroll
-        for (int j = 1; j < W; ++j) s += part[j][i][lane];
-        const int64_t row = m0 + 16 * i + r, f = n0 + 4 * g;
-        if (row < rows && f < n) {
+        for (int j = 1; j < W; ++j) s += part[j][lane];
+        const int64_t f = n0 + 4 * g;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (f + j < n) y[row * ldy + f + j] = (T)(s[j] + (bias ? bias[f + j] : 0.0f));
-        }
+        for (int j = 0; j < 4; ++j)
+            if (row < rows && f + j < n) y[row * ldy + f + j] = (T)(s[j] + (bias ? bias[f + j] : 0.0f));
     }
 }
 
@@ -285,12 +278,20 @@ __global__ void __launch_bounds__(NT, 1)
 
 Blocks blocks_of(const aq_mx4& q) { return {(const uint8_t*)q.d_codes, q.d_scales, blocks32(q.cols)}; }
 
-constexpr int64_t kFewRows = 64;
+// Whether the few-row kernel takes a product, by its 16 x 16 tiles and the bytes of a row of x: up to a workgroup to a CU always, up
+// to two where a row is not long, as every workgroup quantizes its rows again.  us on it / on the tiles, the quantization included:
+// 2048 x 2048, bfloat16, 32 rows (256 tiles) 5.5 / 9.1, 64 (512) 8.2 / 9.3, 96 (768) 11.3 / 9.2; fp32, 64 rows 11.4 / 9.3.
+// 4096 x 4096, bfloat16, 16 rows (256) 8.0 / 12.6, 32 (512) 13.2 / 12.8.  403 x 1111, fp32, 256 rows (416) 6.6 / 9.1, 384 (624) 9.2 / 8.9.
+// 512 x 3136, bfloat16, 256 rows (512) 9.5 / 12.6; fp32 14.4 / 12.9.  256 x 256, bfloat16, 512 rows (512) 3.7 / 6.5.
+bool few_rows(int64_t rows, int64_t n, int64_t row_bytes) {
+    const int64_t tiles = ((rows + 15) / 16) * ((n + 15) / 16);
+    return tiles <= 256 || (tiles <= 512 && row_bytes <= 7168);
+}
 
 template <class X, class T>
 aq_status launch_rows(const X& x, int64_t rows, const aq_mx4& w, const float* bias, const aq_matrix& y, hipStream_t st) {
     const dim3 grid((unsigned)((w.rows + 15) / 16), (unsigned)((rows + 15) / 16));
-    k_mx4_rows<X, T, 1, 8><<<grid, 512, 0, st>>>(x, blocks_of(w), bias, (T*)y.d, y.ld, (int)rows, (int)w.rows, (int)blocks32(w.cols));
+    k_mx4_rows<X, T><<<grid, 512, 0, st>>>(x, blocks_of(w), bias, (T*)y.d, y.ld, (int)rows, (int)w.rows, (int)blocks32(w.cols));
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }
 
@@ -310,7 +311,7 @@ aq_status launch_tiles(const aq_mx4& x, const aq_mx4& w, const float* bias, cons
 }  // namespace
 
 int64_t mx4_linear_workspace(int64_t rows, int64_t n, int64_t k) {
-    if (rows <= kFewRows) return 0;
+    if (few_rows(rows, n, 4 * k)) return 0;  // (whatever the type)
     const int64_t b = rows * blocks32(k);
     return 16 * b + (b + 15) / 16 * 16;
 }
@@ -318,7 +319,7 @@ int64_t mx4_linear_workspace(int64_t rows, int64_t n, int64_t k) {
 aq_status launch_mx4_matmul(const aq_mx4& x, const aq_mx4& w, const float* bias, const aq_matrix& y, hipStream_t st) {
     return with_dtype(y.dtype, [&](auto t) {
         using T = decltype(t);
-        if (x.rows <= kFewRows) return launch_rows<Blocks, T>(blocks_of(x), x.rows, w, bias, y, st);
+        if (few_rows(x.rows, w.rows, (x.cols + 1) / 2)) return launch_rows<Blocks, T>(blocks_of(x), x.rows, w, bias, y, st);
         auto tiles = [&](int64_t s) { return ((x.rows + s - 1) / s) * ((w.rows + s - 1) / s); };
         if (tiles(256) >= 256) return launch_tiles<T, 256>(x, w, bias, y, st);
         if (tiles(128) >= 256) return launch_tiles<T, 128>(x, w, bias, y, st);
@@ -327,7 +328,7 @@ aq_status launch_mx4_matmul(const aq_mx4& x, const aq_mx4& w, const float* bias,
 }
 
 aq_status launch_mx4_linear(const aq_matrix& x, const aq_mx4& w, const float* bias, const aq_matrix& y, void* ws, hipStream_t st) {
-    if (x.rows <= kFewRows)
+    if (few_rows(x.rows, w.rows, x.cols * (int64_t)dtype_bytes(x.dtype)))
         return with_dtype(x.dtype, [&](auto t) {
             using T = decltype(t);
             return launch_rows<Values<T>, T>(Values<T>{(const T*)x.d, x.ld, (int)x.cols}, x.rows, w, bias, y, st);
