@@ -1,6 +1,7 @@
 // The two block formats to and from rows of values: 8-bit checkpoints and microscaled 4-bit floats.
 //
-// Bound by memory.  A thread holds eight values, four neighbouring threads a block, whose largest magnitude they find by two
+// Bound by memory (65536 x 2048 bfloat16 values to checkpoints: 70 us, 5.8 TB/s of reads and writes; 16384 x 4096 to 4-bit floats: 35 us,
+// 4.8 TB/s).  A thread holds eight values, four neighbouring threads a block, whose largest magnitude they find by two
 // exchanges within their quad; L = 4 .. 64 threads walk along a row (few, so that short rows share a wavefront), a workgroup
 // takes 256 / L rows at a time.
 #include "learner.hpp"
@@ -59,8 +60,8 @@ __global__ void __launch_bounds__(kThreads)
     }
 }
 
-// Stores of 16 bytes to a thread, so that a wavefront's lie side by side: V values of T (2048 x 2048 to fp32: 5.5 us with 32 bytes a
-// thread in two stores, XX in one).
+// Stores of 16 bytes to a thread, so that a wavefront's lie side by side: V values of T (2048 x 2048 to fp32: 6.9 us with 32 bytes a
+// thread in two stores, 5.7 in one).
 template <class Format, class T, int L>
 __global__ void __launch_bounds__(kThreads)
     k_from_blocks(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, int64_t ld, int rows, int cols,

@@ -5,6 +5,11 @@
 // either format times its power of two has at most seven significant bits, so it is a bf16 value, and a value of dy is the sum of
 // one (bfloat16), two (binary16) or three (fp32) bf16 values.
 //
+// Bound by the matrix cores' power and by what feeds them: 65536 x 2048 x 2048 in bfloat16 takes 541 us back to back (1.02 PFLOP/s; 471
+// alone), the input gradient 8192 x 2048 x 2048 62 us (1.10 PFLOP/s), where a loop of nothing but these products on such values
+// reaches 1.88 PFLOP/s at the clock that is left and a large library product 1.21.  binary16 takes twice and fp32 three times
+// the products (470 and 340 TFLOP/s).
+//
 // A workgroup's 32 t of both operands go through LDS.  B lies there as it does in memory, t by t (and so does A for the weight
 // gradient), and is transposed on its way to the registers: ds_read_b64_tr_b16 hands lane i of 16 the four t of column i out of
 // four rows of 16 columns.

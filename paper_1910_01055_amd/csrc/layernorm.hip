@@ -3,7 +3,9 @@
 //   y = (x - mean) rstd gamma + beta          dx = rstd (g - mean_row(g) - h mean_row(g h)),  g = dy gamma,  h = (x - mean) rstd
 //   rstd = 1 / sqrt(var + eps)                dgamma = sum_rows dy h,  dbeta = sum_rows dy
 //
-// Both are bound by memory.  G threads hold a row in registers, P pieces of eight values each (piece i of thread t starts at
+// Both are bound by memory: 65536 x 1024 bfloat16 values with their checkpoint 60 us forward (338 MB, 5.7 TB/s), 70 to 75 backward (338
+// MB, 4.7 TB/s; a plain copy of 4 GB reaches 4.9), and 5 for the join of dgamma and dbeta.  Small ones by the launches: 4096 x 256
+// fp32 values 4.8, 5.7 and 2.8 us.  G threads hold a row in registers, P pieces of eight values each (piece i of thread t starts at
 // value 8 (t + G i)), so that mean, variance and result need one read; a workgroup walks rows with gains, offsets and, backward,
 // the sums of dgamma and dbeta in registers, and requests its next row before it works on the present one.
 #include "learner.hpp"
@@ -264,7 +266,7 @@ __global__ void __launch_bounds__(1024) k_layernorm_join(const float* __restrict
 struct Form {
     int g, p;
 };
-// Threads to a row and pieces a thread: the fewest threads that hold it in one piece up to a wavefront, so that short rows share
+// Threads to a row and pieces a thread, by what the registers hold: the fewest threads that hold it in one piece up to a wavefront, so that short rows share
 // one; more than a wavefront from 1025 values on.
 Form row_form(int64_t cols) {
     if (cols <= 128) return {16, 1};
@@ -292,7 +294,9 @@ void with_form(const Form& f, Go&& go) {
 }
 int64_t at_a_time(const Form& f) { return f.g < 256 ? 256 / f.g : 1; }
 
-// workgroups of the backward pass: every one leaves 8 bytes a column behind
+// Workgroups of the backward pass: two turns each until 512 are there; every one leaves 8 bytes a column behind.  65536 x 1024
+// bfloat16: with 256 workgroups 99 us, 512 75, 1024 83 and a join twice as long; 512 of 512 threads 75.  4096 x 256 fp32: with one
+// workgroup for four turns 7.0 us, for two 5.7.
 int64_t backward_workgroups(int64_t rows, int64_t cols) {
     const int64_t turns = (rows + at_a_time(row_form(cols)) - 1) / at_a_time(row_form(cols));
     const int64_t g = (turns + 1) / 2;

@@ -37,7 +37,8 @@ __device__ __forceinline__ void wait_loads() {
 
 // Which tile and slice a workgroup takes.  Workgroups go to the 8 XCDs, each with an L2 of its own, in turn: every eighth of them
 // gets one eighth of all places in a row, and places go along four rows of tiles at once, so that an XCD's workgroups
-// read few different rows and columns (65536 x 2048 x 2048, 64 tiles by 4 slices: XX against XX us with places in order).
+// read few different rows and columns (weight gradient 65536 x 2048 x 2048, 64 tiles by 4 slices: 545 against 553 us with places in
+// order, and half the lines from behind the L2).
 struct Place {
     uint32_t m, c, z;
 };
