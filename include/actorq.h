@@ -456,7 +456,8 @@ aq_status aq_ckpt8_pack(const aq_matrix* x, const aq_ckpt8* kept, void* stream);
 aq_status aq_ckpt8_unpack(const aq_ckpt8* kept, const aq_matrix* x, void* stream);
 /* The gradients of a fully connected layer y = x W^T + b from its checkpointed input: dw[n][k] = sum over rows of
  * dy[row][n] * x[row][k] (fp32, n = dy's columns, k = kept's), d_db[n] = sum over rows of dy[row][n] (may be NULL).
- * The products are exact and their sums are fp32, whatever dy's type.  */
+ * The products are exact (bits of a value of dy below 2^-133 do not count) and their sums are fp32, whatever dy's
+ * type. */
 aq_status aq_ckpt8_weight_grad_workspace(int64_t rows, int64_t n, int64_t k, uint64_t* bytes);
 aq_status aq_ckpt8_weight_grad(const aq_matrix* dy, const aq_ckpt8* kept, const aq_matrix* dw, float* d_db,
                                void* d_workspace, uint64_t workspace_bytes, void* stream);

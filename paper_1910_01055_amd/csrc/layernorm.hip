@@ -67,6 +67,8 @@ __global__ void __launch_bounds__(threads_for(G))
         const int col = 8 * (t + G * i);
         n[i] = cols - col;
         cur[i].load(x + row * ldx + col, n[i]);
+        ga[i].zero();
+        be[i].zero();
         if (gamma) ga[i].load(gamma + col, n[i]);
         if (beta) be[i].load(beta + col, n[i]);
     }
@@ -159,6 +161,7 @@ __global__ void __launch_bounds__(threads_for(G))
         const int col = 8 * (t + G * i);
         n[i] = cols - col;
         Piece<float> q;
+        q.zero();
         if (gamma) q.load(gamma + col, n[i]);
         q.get(ga[i]);
 #pragma unroll

@@ -376,6 +376,24 @@ def test_weight_grad_of_wide_ranges():
     assert bool(torch.isnan(d[9])) and float(d[10]) == math.inf and bool(torch.isfinite(d[keep]).all())
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_weight_grad_of_the_smallest_values(kind):
+    """Products of denormals are products too: checkpoints down to 2^-133, gradients down to there."""
+    rows, n, k = 64, 3, 64
+    x, dy = torch.zeros(rows, k), torch.full((rows, n), 2.0 ** 100)
+    x[:, 0], x[:, 1], x[:, 2], x[:, 32], x[:, 33] = 2.0 ** -126, 2.0 ** -130, -2.0 ** -132, 2.0 ** -128, 2.0 ** -133
+    big = torch.full((rows, k), 2.0 ** 100)
+    dy[:, 1], dy[:, 2] = 2.0 ** -130, 1.5 * 2.0 ** -127
+    for v, columns in ((x, slice(0, 1)), (big, slice(1, 3))):  # (the others pass fp32's ends)
+        kept, dw, db = B.ckpt8_empty(rows, k), torch.empty(n, k, device=DEV), torch.empty(n, device=DEV)
+        ws = torch.empty(max(16, B.ckpt8_weight_grad_workspace(rows, n, k)), dtype=torch.uint8, device=DEV)
+        B.ckpt8_pack(v.to(DEV, TYPES[kind]), kept)
+        assert torch.equal(ckpt8_values(kept), v.double())
+        B.ckpt8_weight_grad(dy.to(DEV, TYPES[kind]), kept, dw, db, ws)
+        assert torch.equal(dw.cpu().double()[columns], (dy.double().t() @ v.double())[columns])  # sums of 64 equal powers of two: exact
+        assert torch.equal(db.cpu().double(), dy.double().sum(0))
+
+
 # ---- 4-bit layers
 
 LINEAR_SHAPES = [(1, 1, 1), (1, 256, 67), (1, 17, 2048), (2, 40, 33), (15, 100, 130), (16, 64, 128), (17, 21, 256), (64, 130, 1000), (65, 33, 257),
@@ -433,7 +451,8 @@ def test_mx4_linear_of_what_is_not_finite(rows):
 
 
 IG_SHAPES = [(1, 1, 1), (1, 17, 256), (2, 40, 33), (63, 65, 67), (64, 64, 128), (129, 128, 129), (300, 403, 1111), (700, 21, 64), (4100, 33, 40),
-             (520, 2885, 523), (1030, 5443, 1029), (1030, 5440, 1024)]  # the larger tiles; rows that end inside a piece and not
+             (520, 2885, 523), (1030, 5443, 1029), (1030, 5440, 1024),  # the larger tiles; rows that end inside a piece and not
+             (1500, 500, 1490), (4100, 903, 2050)]  # and in one slice
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
