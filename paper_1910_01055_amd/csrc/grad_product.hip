@@ -31,7 +31,8 @@ template <class T>
 constexpr int kParts = std::is_same<T, float>::value ? 3 : std::is_same<T, f16_t>::value ? 2 : 1;
 
 // Eight values as P bf16 parts, each the rest of the one before cut to bf16 (cut, not rounded: no part overflows, and three times
-// eight bits are fp32's 24).  What is not finite is whole in the first.
+// eight bits are fp32's 24).  An infinity's or a NaN's first part is one itself (a NaN is made quiet, so that the cut leaves it one);
+// what remains of it, a NaN, becomes some number, which changes neither.
 template <class T, int P>
 __device__ __forceinline__ void split(const Piece<T>& in, v4u (&out)[P]) {
     if constexpr (P == 1) {
@@ -40,17 +41,18 @@ __device__ __forceinline__ void split(const Piece<T>& in, v4u (&out)[P]) {
         float v[8];
         in.get(v);
 #pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __builtin_canonicalizef(v[j]);
+#pragma unroll
         for (int q = 0; q < P; ++q) {
-            uint32_t b[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                b[j] = __float_as_uint(v[j]) & 0xffff0000u;
-                const bool finite = (__float_as_uint(v[j]) & 0x7fffffffu) < kInfBits;
-                if (!finite && v[j] != v[j]) b[j] |= 0x00400000u;  // (a NaN stays one)
-                v[j] = finite ? v[j] - __uint_as_float(b[j]) : 0.0f;
+            for (int j = 0; j < 4; ++j) out[q][j] = __builtin_amdgcn_perm(__float_as_uint(v[2 * j + 1]), __float_as_uint(v[2 * j]), 0x07060302u);
+            if (q + 1 < P) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] -= __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
+                    if (q == 0) v[j] = __builtin_amdgcn_fmed3f(v[j], -3.0e38f, 3.0e38f);
+                }
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) out[q][j] = (b[2 * j] >> 16) | b[2 * j + 1];
         }
     }
 }
