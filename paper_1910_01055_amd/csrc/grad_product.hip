@@ -8,7 +8,7 @@
 // Bound by the matrix cores' power and by what feeds them: 65536 x 2048 x 2048 in bfloat16 takes 541 us back to back (1.02 PFLOP/s; 471
 // alone), the input gradient 8192 x 2048 x 2048 62 us (1.10 PFLOP/s), where a loop of nothing but these products on such values
 // reaches 1.88 PFLOP/s at the clock that is left and a large library product 1.21.  binary16 takes twice and fp32 three times
-// the products (470 and 340 TFLOP/s).
+// the products (610 and 410 TFLOP/s).
 //
 // A workgroup's 32 t of both operands go through LDS.  B lies there as it does in memory, t by t (and so does A for the weight
 // gradient), and is transposed on its way to the registers: ds_read_b64_tr_b16 hands lane i of 16 the four t of column i out of
@@ -462,16 +462,16 @@ struct Plan {
 // The tile and the slices by an estimate in us: what a launch takes besides its chunks; the chunks of a workgroup one after the
 // other, each as long as `alone` while few workgroups are about and `full` while as many as fit are (`at_once`); the join's launch
 // and bytes.  Fitted to weight gradients of 2048 rows with every tile in one slice, us on tiles of 64 / 128 / 256:
-//   bfloat16 2048 x 2048 50.9 / 38.9 / 55.4, 1024 x 1024 20.4 / 32.9 / 50.5, 128 x 128 18.3 / 31.3 / 49.1 (256 rows 5.0 / 7.7 / 12.1)
-//   binary16            106.3 / 107.6 / 143.5,            56.0 / 102.6 / 141.1,          54.6 / 100.7 / 139.4 (9.7 / 17.3 / 24.4)
-//   fp32                163.8 / 146.2 / 199.4,            76.1 / 144.3 / 196.1,          75.1 / 141.8 / 194.2 (12.6 / 23.0 / 31.9)
+//   bfloat16 2048 x 2048  51.1 / 38.4 / 54.8,   1024 x 1024 20.5 / 32.9 / 50.4,   128 x 128 18.5 / 31.3 / 49.1 (256 rows 4.9 / 7.7 / 12.1)
+//   binary16              73.2 / 55.8 / 97.1,               30.9 / 47.2 / 93.8,             27.8 / 46.2 / 91.9 (6.2 / 9.8 / 17.6)
+//   fp32                 103.4 / 76.1 / 137.5,              37.9 / 63.9 / 135.8,            33.7 / 61.7 / 132.5 (6.9 / 11.9 / 23.1)
 Plan plan(int64_t m, int64_t c, int64_t t, int parts) {
     constexpr struct {
         int s, at_once;
         float launch, alone, full;
     } kinds[3][3] = {{{64, 1024, 3.1f, 0.24f, 0.75f}, {128, 512, 4.3f, 0.42f, 0.86f}, {256, 256, 6.8f, 0.66f, 1.07f}},
-                     {{64, 1024, 3.3f, 0.80f, 1.61f}, {128, 512, 5.4f, 1.49f, 2.16f}, {256, 256, 8.0f, 2.05f, 2.30f}},
-                     {{64, 1024, 3.7f, 1.12f, 2.50f}, {128, 256, 6.0f, 2.12f, 2.20f}, {256, 256, 8.7f, 2.90f, 3.10f}}};
+                     {{64, 1024, 3.1f, 0.39f, 1.10f}, {128, 512, 4.6f, 0.65f, 1.52f}, {256, 256, 7.0f, 1.33f, 1.75f}},
+                     {{64, 1024, 3.1f, 0.48f, 1.57f}, {128, 256, 4.8f, 0.89f, 1.20f}, {256, 256, 7.4f, 1.95f, 2.60f}}};
     const int64_t all = (t + 31) / 32;
     Plan best{64, 1, (int)((all + 1) & ~1)};
     float least = 3.0e38f;
