@@ -155,11 +155,24 @@ __device__ __forceinline__ uint32_t mx4_codes(const float (&v)[8], uint32_t scal
     return scale == 255 ? 0 : c;
 }
 
-// ---- sums over groups of G = 4 .. 64 neighbouring lanes, the same value in every lane
+// ---- sums over groups of G = 16, 32 or 64 neighbouring lanes, the same value in every lane, without a trip through LDS
 template <int G>
 __device__ __forceinline__ float lanes_sum(float s) {
-#pragma unroll
-    for (int o = G / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    auto step = [&](auto ctrl) __attribute__((always_inline)) {
+        s += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(s), decltype(ctrl)::value, 15, 15, true));
+    };
+    step(std::integral_constant<int, 0xB1>());   // lane ^ 1
+    step(std::integral_constant<int, 0x4E>());   // lane ^ 2
+    step(std::integral_constant<int, 0x141>());  // the other four of eight
+    step(std::integral_constant<int, 0x140>());  // the other eight of 16
+    if constexpr (G >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(s), __float_as_uint(s), false, false);
+        s = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    if constexpr (G >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(s), __float_as_uint(s), false, false);
+        s = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
     return s;
 }
 
