@@ -14,8 +14,11 @@ constexpr int kThreads = 256;
 
 struct Ckpt8 {
     static constexpr int kBits = 8;  // of a code
-    static __device__ __forceinline__ void pack(const float (&v)[8], uint8_t* codes, uint32_t& scale) {
-        scale = ckpt8_scale(most_of4lanes(most_of8(v)));
+    template <class T>
+    static __device__ __forceinline__ void pack(const Piece<T>& p, uint8_t* codes, uint32_t& scale) {
+        scale = ckpt8_scale(most_of4lanes(most_of(p)));
+        float v[8];
+        p.get(v);
         *(v2u*)codes = ckpt8_codes(v, scale);
     }
     // four values
@@ -28,9 +31,10 @@ struct Ckpt8 {
 };
 struct Mx4 {
     static constexpr int kBits = 4;
-    static __device__ __forceinline__ void pack(const float (&v)[8], uint8_t* codes, uint32_t& scale) {
-        scale = mx4_scale(most_of4lanes(most_of8(v)));
-        *(uint32_t*)codes = mx4_codes(v, scale);
+    template <class T>
+    static __device__ __forceinline__ void pack(const Piece<T>& p, uint8_t* codes, uint32_t& scale) {
+        scale = mx4_scale(most_of4lanes(most_of(p)));
+        *(uint32_t*)codes = mx4_codes(p, scale);
     }
     typedef uint16_t Codes4;
     static __device__ __forceinline__ void unpack4(uint32_t c, uint32_t scale, float* v) {
@@ -52,10 +56,8 @@ __global__ void __launch_bounds__(kThreads)
     for (int64_t row = (int64_t)blockIdx.y * (kThreads / L) + threadIdx.x / L; row < rows; row += step) {
         Piece<T> in;
         in.load(x + row * ld + 8 * (int64_t)piece, cols - 8 * piece);
-        float v[8];
-        in.get(v);
         uint32_t scale;
-        Format::pack(v, codes + (row * blocks * 4 + piece) * Format::kBits, scale);
+        Format::pack(in, codes + (row * blocks * 4 + piece) * Format::kBits, scale);
         if ((threadIdx.x & 3) == 0) scales[row * blocks + (piece >> 2)] = (uint8_t)scale;
     }
 }

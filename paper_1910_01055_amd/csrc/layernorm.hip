@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(threads_for(G))
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             if constexpr (KEEP) {
-                const uint32_t scale = ckpt8_scale(most_of4lanes(most_of8(v[i])));
+                const uint32_t scale = ckpt8_scale(most_of4lanes(most_of(cur[i])));
                 const int col = 8 * (t + G * i);
                 if ((col & ~31) < cols) *(v2u*)(codes + row * blocks * 32 + col) = ckpt8_codes(v[i], scale);
                 if ((t & 3) == 0 && col < cols) scales[row * blocks + (col >> 5)] = (uint8_t)scale;

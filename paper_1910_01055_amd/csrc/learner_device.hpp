@@ -91,15 +91,26 @@ struct Piece {
 };
 
 // ---- blocks of 32 values: lanes 4 i .. 4 i + 3 hold one, eight values each
-// the largest magnitude's bits (as whole numbers, so that NaNs and infinities win)
-__device__ __forceinline__ uint32_t most_of8(const float (&v)[8]) {
-    uint32_t m = 0;
+// The largest magnitude's bits as fp32's, found among whole numbers so that NaNs and infinities win; 16-bit values two at a time.
+typedef uint16_t v2u16 __attribute__((ext_vector_type(2)));
+template <class T>
+__device__ __forceinline__ uint32_t most_of(const Piece<T>& p) {
+    if constexpr (sizeof(T) == 4) {
+        uint32_t m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
-        m = b > m ? b : m;
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t b = p.w[j] & 0x7fffffffu;
+            m = b > m ? b : m;
+        }
+        return m;
+    } else {
+        v2u16 m{0, 0};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(v2u16, p.w[j] & 0x7fff7fffu));
+        const uint16_t most = m[0] > m[1] ? m[0] : m[1];
+        if constexpr (std::is_same<T, bf16_t>::value) return (uint32_t)most << 16;
+        else return __float_as_uint((float)__builtin_bit_cast(f16_t, most));
     }
-    return m;
 }
 __device__ __forceinline__ uint32_t most_of4lanes(uint32_t m) {
     uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 15, 15, true);  // lane ^ 1
@@ -143,15 +154,33 @@ __device__ __forceinline__ uint32_t mx4_scale(uint32_t most) {
 }
 // 2^(scale - 127); a NaN for 255
 __device__ __forceinline__ float mx4_step(uint32_t scale) { return __uint_as_float(scale == 255 ? 0x7fc00000u : scale ? scale << 23 : 0x00400000u); }
-// Eight codes, the first value in the lowest half byte.  The hardware's conversion divides by the scale, rounds to nearest even and
-// saturates at 6, denormals included (compared with the definition over ties, edges and all three types).
-__device__ __forceinline__ uint32_t mx4_codes(const float (&v)[8], uint32_t scale) {
+// Eight codes, the first value in the lowest half byte.  The hardware's conversions divide by the scale, round to nearest even and
+// saturate at 6, denormals included (compared with the definition over ties, edges and all three types).
+template <class T>
+__device__ __forceinline__ uint32_t mx4_codes(const Piece<T>& p, uint32_t scale) {
     const float s = __uint_as_float(scale ? scale << 23 : 0x00400000u);
     uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], s, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], s, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], s, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], s, 3);
+    auto two = [&](int j) __attribute__((always_inline)) {
+        if constexpr (std::is_same<T, float>::value) return v2f32{__uint_as_float(p.w[2 * j]), __uint_as_float(p.w[2 * j + 1])};
+        else if constexpr (std::is_same<T, bf16_t>::value) return __builtin_bit_cast(v2bf16, p.w[j]);
+        else return __builtin_bit_cast(v2f16, p.w[j]);
+    };
+    if constexpr (std::is_same<T, float>::value) {
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, two(0)[0], two(0)[1], s, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, two(1)[0], two(1)[1], s, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, two(2)[0], two(2)[1], s, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, two(3)[0], two(3)[1], s, 3);
+    } else if constexpr (std::is_same<T, bf16_t>::value) {
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, two(0), s, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, two(1), s, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, two(2), s, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, two(3), s, 3);
+    } else {
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, two(0), s, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, two(1), s, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, two(2), s, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, two(3), s, 3);
+    }
     return scale == 255 ? 0 : c;
 }
 

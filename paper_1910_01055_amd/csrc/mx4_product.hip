@@ -59,17 +59,15 @@ struct Values {  // rows of values, quantized in the lane that needs them
         }
     }
     __device__ __forceinline__ void get(const Raw& raw, v4u& c, uint32_t& scale) const {
-        float v[4][8];
         uint32_t most = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            raw.q[i].get(v[i]);
-            const uint32_t m = most_of8(v[i]);
+            const uint32_t m = most_of(raw.q[i]);
             most = m > most ? m : most;
         }
         scale = mx4_scale(most);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = mx4_codes(v[i], scale);
+        for (int i = 0; i < 4; ++i) c[i] = mx4_codes(raw.q[i], scale);
     }
 };
 
