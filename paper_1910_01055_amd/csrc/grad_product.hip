@@ -5,8 +5,8 @@
 // either format times its power of two has at most seven significant bits, so it is a bf16 value, and a value of dy is the sum of
 // one (bfloat16), two (binary16) or three (fp32) bf16 values.
 //
-// Bound by the matrix cores' power and by what feeds them: 65536 x 2048 x 2048 in bfloat16 takes 541 us back to back (1.02 PFLOP/s; 471
-// alone), the input gradient 8192 x 2048 x 2048 62 us (1.10 PFLOP/s), where a loop of nothing but these products on such values
+// Bound by the matrix cores' power and by what feeds them: 65536 x 2048 x 2048 in bfloat16 takes 521 to 545 us back to back (1.03 PFLOP/s; 471
+// alone), the input gradient 8192 x 2048 x 2048 61 us (1.13 PFLOP/s), where a loop of nothing but these products on such values
 // reaches 1.88 PFLOP/s at the clock that is left and a large library product 1.21.  binary16 takes twice and fp32 three times
 // the products (610 and 410 TFLOP/s).
 //
@@ -303,6 +303,7 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
            int chunks, int turns) {
     constexpr int P = A::P, NT = tile_threads(S), N = S / 64, NC = S / (NT / 128) / 32, kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(kBuf);
     constexpr int G = 2 * P * N;  // groups of NC products: 16 t, part, row tile
+    static_assert(NT / 64 * 32 * kOutRow<T, NC> <= kBufs * kBuf, "results leave through the buffers");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
     const Place at = place_of_workgroup((uint32_t)((mn + S - 1) / S), (uint32_t)((cn + S - 1) / S));

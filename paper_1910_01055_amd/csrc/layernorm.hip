@@ -5,7 +5,7 @@
 //
 // Both are bound by memory: 65536 x 1024 bfloat16 values with their checkpoint 60 us forward (338 MB, 5.7 TB/s), 70 to 75 backward (338
 // MB, 4.7 TB/s; a plain copy of 4 GB reaches 4.9), and 5 for the join of dgamma and dbeta.  Small ones by the launches: 4096 x 256
-// fp32 values 4.8, 5.7 and 2.8 us.  G threads hold a row in registers, P pieces of eight values each (piece i of thread t starts at
+// fp32 values 4.4, 5.3 and 2.9 us.  G threads hold a row in registers, P pieces of eight values each (piece i of thread t starts at
 // value 8 (t + G i)), so that mean, variance and result need one read; a workgroup walks rows with gains, offsets and, backward,
 // the sums of dgamma and dbeta in registers, and requests its next row before it works on the present one.
 #include "learner.hpp"

@@ -127,6 +127,7 @@ template <class T, int S, int NT>
 __global__ void __launch_bounds__(NT, 1)
     k_mx4_tiles(Blocks x, Blocks w, const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int rows, int n, int blocks) {
     constexpr int R = 2 * S, SU = (R + NT - 1) / NT, J = R * 8 / NT, TM = S / 64, TN = S / (NT / 128) / 32, kBuf = R * 128;
+    static_assert(NT / 64 * 32 * kOutRow<T, TN> <= 2 * kBuf, "results leave through the buffers");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // two buffers of chunks; scales of four chunks
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, g = lane >> 5;
     const Place at = place_of_workgroup((uint32_t)((rows + S - 1) / S), (uint32_t)((n + S - 1) / S));
