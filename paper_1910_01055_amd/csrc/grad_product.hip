@@ -32,7 +32,7 @@ constexpr int kParts = std::is_same<T, float>::value ? 3 : std::is_same<T, f16_t
 
 // Eight values as P bf16 parts, each the rest of the one before cut to bf16 (cut, not rounded: no part overflows, and three times
 // eight bits are fp32's 24).  An infinity's or a NaN's first part is one itself (a NaN is made quiet, so that the cut leaves it one);
-// what remains of it, a NaN, becomes some number, which changes neither.
+// the others are those of the largest number, of an infinity's sign: no product of theirs overflows to the other infinity.
 template <class T, int P>
 __device__ __forceinline__ void split(const Piece<T>& in, v4u (&out)[P]) {
     if constexpr (P == 1) {
@@ -49,8 +49,8 @@ __device__ __forceinline__ void split(const Piece<T>& in, v4u (&out)[P]) {
             if (q + 1 < P) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
+                    if (q == 0) v[j] = __builtin_amdgcn_fmed3f(v[j], -3.40282347e38f, 3.40282347e38f);
                     v[j] -= __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
-                    if (q == 0) v[j] = __builtin_amdgcn_fmed3f(v[j], -3.0e38f, 3.0e38f);
                 }
             }
         }

@@ -477,6 +477,29 @@ def test_mx4_input_grad(rows, n, k, kind):
     assert all(torch.equal(r, results[0]) for r in results)
 
 
+@pytest.mark.parametrize("rows,n,k", [(40, 96, 70), (300, 40, 33)])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_gradients_of_infinities(rows, n, k, kind):
+    """An infinite gradient stays infinite, with the right sign, whatever the values that it meets; the others stay as near as ever."""
+    g = rng("infinite", rows, n, k, kind)
+    sign = lambda *s: 1.0 - 2.0 * torch.randint(0, 2, s, generator=g)
+    dy = normal(g, rows, n).to(TYPES[kind])
+    dy[5, 3], dy[rows - 1, n - 1] = math.inf, -math.inf
+    kept, q = B.ckpt8_empty(rows, k), B.mx4_empty(n, k)
+    B.ckpt8_pack((sign(rows, k) * (2.0 + 30.0 * torch.rand(rows, k, generator=g))).to(DEV), kept)
+    B.mx4_quantize((sign(n, k) * (2.0 + 4.0 * torch.rand(n, k, generator=g))).to(DEV), q)
+    xv, wv, dyd = ckpt8_values(kept), mx4_values(q), dy.double()
+    ws = torch.empty(max(16, B.ckpt8_weight_grad_workspace(rows, n, k), B.mx4_input_grad_workspace(rows, n, k)), dtype=torch.uint8, device=DEV)
+    finite = torch.where(torch.isfinite(dyd), dyd, torch.zeros_like(dyd)).abs()
+    dw, db, dx = torch.empty(n, k, device=DEV), torch.empty(n, device=DEV), torch.empty(rows, k, dtype=TYPES[kind], device=DEV)
+    B.ckpt8_weight_grad(dy.to(DEV), kept, dw, db, ws)
+    near(dw.cpu().double(), dyd.t() @ xv, (3 * rows + 8) * U * (finite.t() @ xv.abs()))
+    near(db.cpu().double(), dyd.sum(0), (rows + 8) * U * finite.sum(0))
+    B.mx4_input_grad(dy.to(DEV), q, dx, ws)
+    want, off = dyd @ wv, (3 * n + 8) * U * (finite @ wv.abs())
+    near(dx.cpu().double(), want, off + OUT[kind] * (want.abs() + off) + TINY[kind])
+
+
 # ---- far apart, and many
 
 FAR = 1 << 21  # the largest distance between rows
