@@ -16,9 +16,12 @@ constexpr int kFp4 = 4;  // the instructions' number of the 4-bit format
 __device__ __forceinline__ v8i32 operand(v4u c) { return v8i32{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0}; }
 
 // ---- few rows: 16 features by 16 rows to a workgroup, whose eight wavefronts take turns along k and join their sums in LDS.  Bound by
-// latency: a launch, one trip to memory, a barrier (2048 x 2048 weights, one bfloat16 row: 4.1 us, of which an empty kernel is 2.3;
-// four wavefronts 4.4, two tiles of rows to a workgroup 5.2).
+// latency: a launch, a trip to memory for every 1024 k, a barrier (2048 x 2048 weights, one bfloat16 row: 3.9 us, of which an empty
+// kernel is 2.3, 16 rows 4.1; with four wavefronts 4.3 and 4.5, with the next turn requested before the present one's work 4.2 and 4.4, as
+// fewer wavefronts fit).
+// What 64 lanes need of 16 rows and four blocks of them: lane l the block l / 16 of row l mod 16.
 struct Blocks {  // rows that are quantized already
+    static constexpr int kLds = 0;
     const uint8_t* codes;
     const uint8_t* scales;
     int64_t blocks;
@@ -26,79 +29,74 @@ struct Blocks {  // rows that are quantized already
         v4u c;
         uint32_t scale;
     };
-    __device__ __forceinline__ void request(int64_t row, int64_t b, bool there, Raw& q) const {
-        q.c = v4u{0, 0, 0, 0};
-        q.scale = 0;
-        if (there) {
-            q.c = *(const v4u AQ_GLOBAL*)(codes + (row * blocks + b) * 16);
-            q.scale = ((const uint8_t AQ_GLOBAL*)scales)[row * blocks + b];
-        }
+    // Rows from row0 on, of which `rows` exist, and blocks from b0 on; where there is none the last one, whose results are not stored or,
+    // with zeros for x, add nothing (a NaN's block only to a row that is NaN).
+    __device__ __forceinline__ void request(int row0, int rows, int b0, int lane, Raw& q) const {
+        const int row = row0 + (lane & 15), b = b0 + (lane >> 4);
+        const int64_t at = (row < rows ? row : rows - 1) * blocks + (b < blocks ? b : (int)blocks - 1);
+        q.c = *(const v4u AQ_GLOBAL*)(codes + at * 16);
+        q.scale = ((const uint8_t AQ_GLOBAL*)scales)[at];
     }
-    __device__ __forceinline__ void get(const Raw& q, v4u& c, uint32_t& scale) const {
-        c = q.c;
+    __device__ __forceinline__ void get(const Raw& q, uint8_t*, int lane, int left, v4u& c, uint32_t& scale) const {
+        c = lane >> 4 < left ? q.c : v4u{0, 0, 0, 0};
         scale = q.scale;
     }
 };
+// Rows of values, quantized here.  Four lanes load a block, so that they read whole lines (each lane a block of its own: 16 fp32 rows
+// of 4096 into 4096 features 11.4 us for 6.1), lane l eight values of row l / 4; the codes change lanes in LDS.
 template <class T>
-struct Values {  // rows of values, quantized in the lane that needs them
+struct Values {
+    static constexpr int kLds = 1024;  // bytes of a wavefront's own
     const T* x;
     int64_t ld;
     int cols;
     struct Raw {
         Piece<T> q[4];
     };
-    __device__ __forceinline__ void request(int64_t row, int64_t b, bool there, Raw& raw) const {
-        const T* p = x + row * ld + b * 32;
-        const int n = there ? cols - (int)b * 32 : 0;
-        if (n >= 32) {
+    __device__ __forceinline__ void request(int row0, int rows, int b0, int lane, Raw& raw) const {
+        const int row = row0 + (lane >> 2), col = 32 * b0 + 8 * (lane & 3);
+        const T* const p = x + (row < rows ? row : rows - 1) * ld + col;
+        if (32 * b0 + 128 <= cols) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) raw.q[i].load_all(p + 8 * i);
+            for (int i = 0; i < 4; ++i) raw.q[i].load_all(p + 32 * i);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) raw.q[i].load(p + 8 * i, n - 8 * i);
+            for (int i = 0; i < 4; ++i) raw.q[i].load(p + 32 * i, cols - col - 32 * i);
         }
     }
-    __device__ __forceinline__ void get(const Raw& raw, v4u& c, uint32_t& scale) const {
-        uint32_t most = 0;
+    __device__ __forceinline__ void get(const Raw& raw, uint8_t* lds, int lane, int, v4u& c, uint32_t& scale) const {
+        uint32_t scales = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t m = most_of(raw.q[i]);
-            most = m > most ? m : most;
+            const uint32_t s = mx4_scale(most_of4lanes(most_of(raw.q[i])));
+            scales |= s << (8 * i);
+            *(uint32_t*)(lds + 256 * i + 4 * lane) = mx4_codes(raw.q[i], s);
         }
-        scale = mx4_scale(most);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = mx4_codes(raw.q[i], scale);
+        __builtin_amdgcn_wave_barrier();  // (a wavefront's accesses to LDS are done in their order)
+        c = *(const v4u*)(lds + 16 * lane);
+        scale = (uint32_t)__builtin_amdgcn_ds_bpermute(16 * (lane & 15), (int)scales) >> (8 * (lane >> 4));
+        __builtin_amdgcn_wave_barrier();
     }
 };
 
 template <class X, class T>
 __global__ void __launch_bounds__(512)
     k_mx4_rows(X x, Blocks w, const float* __restrict__ bias, T* __restrict__ y, int64_t ldy, int rows, int n, int blocks) {
-    constexpr int W = 8, U = 2;  // wavefronts; turns whose operands are requested together
+    constexpr int W = 8;  // wavefronts
     __shared__ v4f32 part[W][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16, row = (int64_t)blockIdx.y * 16 + r;
+    static_assert(X::kLds <= sizeof(part[0]), "");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16, row0 = blockIdx.y * 16, row = row0 + r;
     v4f32 acc{0, 0, 0, 0};
-    for (int b0 = 4 * wave; b0 < blocks; b0 += 4 * W * U) {
-        v4u cw[U], cx[U];
-        uint32_t sw[U], sx[U];
-        typename X::Raw raw[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int b = b0 + 4 * W * u + g;
-            cw[u] = v4u{0, 0, 0, 0};
-            sw[u] = 0;
-            if (b < blocks && n0 + r < n) {
-                cw[u] = *(const v4u AQ_GLOBAL*)(w.codes + ((n0 + r) * blocks + b) * 16);
-                sw[u] = ((const uint8_t AQ_GLOBAL*)w.scales)[(n0 + r) * blocks + b];
-            }
-            x.request(row, b, b < blocks && row < rows, raw[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            x.get(raw[u], cx[u], sx[u]);
-            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(cw[u]), operand(cx[u]), acc, kFp4, kFp4, 0, (int)sw[u], 0, (int)sx[u]);
-        }
+    for (int b = 4 * wave; b < blocks; b += 4 * W) {
+        typename Blocks::Raw own;
+        typename X::Raw raw;
+        w.request(n0, n, b, lane, own);
+        x.request(row0, rows, b, lane, raw);
+        v4u cx;
+        uint32_t sx;
+        x.get(raw, (uint8_t*)part[wave], lane, blocks - b, cx, sx);
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(own.c), operand(cx), acc, kFp4, kFp4, 0, (int)own.scale, 0, (int)sx);
     }
     part[wave][lane] = acc;
     __syncthreads();
@@ -106,7 +104,7 @@ __global__ void __launch_bounds__(512)
         v4f32 s = part[0][lane];
 #pragma unroll
         for (int j = 1; j < W; ++j) s += part[j][lane];
-        const int64_t f = n0 + 4 * g;
+        const int f = n0 + 4 * g;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (row < rows && f + j < n) y[row * ldy + f + j] = (T)(s[j] + (bias ? bias[f + j] : 0.0f));
@@ -281,14 +279,20 @@ __global__ void __launch_bounds__(NT, 1)
 
 Blocks blocks_of(const aq_mx4& q) { return {(const uint8_t*)q.d_codes, q.d_scales, blocks32(q.cols)}; }
 
-// Whether the few-row kernel takes a product, by its 16 x 16 tiles and the bytes of a row of x: up to a workgroup to a CU always, up
-// to two where a row is not long, as every workgroup quantizes its rows again.  us on it / on the tiles, the quantization included:
-// 2048 x 2048, bfloat16, 32 rows (256 tiles) 5.5 / 9.1, 64 (512) 8.2 / 9.3, 96 (768) 11.3 / 9.2; fp32, 64 rows 11.4 / 9.3.
-// 4096 x 4096, bfloat16, 16 rows (256) 8.0 / 12.6, 32 (512) 13.2 / 12.8.  403 x 1111, fp32, 256 rows (416) 6.6 / 9.1, 384 (624) 9.2 / 8.9.
-// 512 x 3136, bfloat16, 256 rows (512) 9.5 / 12.6; fp32 14.4 / 12.9.  256 x 256, bfloat16, 512 rows (512) 3.7 / 6.5.
-bool few_rows(int64_t rows, int64_t n, int64_t row_bytes) {
+// Whether the few-row kernel takes a product, by its 16 x 16 tiles, as many workgroups, and the bytes of a row of x, which each of them
+// reads and, where they are values, quantizes again; up to a workgroup to a CU always.  us on it / on the tiles, for values with the
+// quantization that goes before them.
+// Values: 256 tiles  2048 x 2048 bfloat16 4.2 / 9.1, 4096 x 4096 fp32 6.1 / 13.2
+//         512        2048 x 2048 bfloat16 5.7 / 9.1, 4096 x 4096 fp32 10.1 / 13.2, 1024 x 8192 18.4 / 21.8
+//         1024       512 x 3136 bfloat16 9.7 / 13.1, fp32 15.0 / 13.2;  2048 x 2048 bfloat16 8.5 / 9.2, fp32 10.2 / 9.5
+//         1536       1024 x 1024 bfloat16 7.0 / 7.4, fp32 8.4 / 7.6
+//         2048       256 x 256 fp32 5.5 / 6.9;  1024 x 512 fp32 6.5 / 6.6, 3072 tiles of bfloat16 7.6 / 6.5
+// Blocks: 512 tiles  2048 x 2048 5.7 / 5.8, 512 x 3136 5.8 / 7.8, 1024 x 8192 16.4 / 13.7;  1024  1024 x 512 3.8 / 4.0, 2048 x 2048 9.4 / 5.8
+//         2048       256 x 256 4.1 / 4.2, 1024 x 512 5.4 / 4.0
+bool few_rows(int64_t rows, int64_t n, int64_t row_bytes, bool values) {
     const int64_t tiles = ((rows + 15) / 16) * ((n + 15) / 16);
-    return tiles <= 256 || (tiles <= 512 && row_bytes <= 7168);
+    if (values) return tiles <= 512 || row_bytes + 3000 <= 9500000 / tiles;
+    return tiles <= 256 || row_bytes + 400 <= 1050000 / tiles;
 }
 
 template <class X, class T>
@@ -314,7 +318,7 @@ aq_status launch_tiles(const aq_mx4& x, const aq_mx4& w, const float* bias, cons
 }  // namespace
 
 int64_t mx4_linear_workspace(int64_t rows, int64_t n, int64_t k) {
-    if (few_rows(rows, n, 4 * k)) return 0;  // (whatever the type)
+    if (few_rows(rows, n, 4 * k, true)) return 0;  // (whatever the type)
     const int64_t b = rows * blocks32(k);
     return 16 * b + (b + 15) / 16 * 16;
 }
@@ -322,7 +326,7 @@ int64_t mx4_linear_workspace(int64_t rows, int64_t n, int64_t k) {
 aq_status launch_mx4_matmul(const aq_mx4& x, const aq_mx4& w, const float* bias, const aq_matrix& y, hipStream_t st) {
     return with_dtype(y.dtype, [&](auto t) {
         using T = decltype(t);
-        if (few_rows(x.rows, w.rows, (x.cols + 1) / 2)) return launch_rows<Blocks, T>(blocks_of(x), x.rows, w, bias, y, st);
+        if (few_rows(x.rows, w.rows, 16 * blocks32(x.cols), false)) return launch_rows<Blocks, T>(blocks_of(x), x.rows, w, bias, y, st);
         // The largest tiles that give every CU one.  us on tiles of 64 / 128 / 256: 2048 x 2048, 2048 rows 13.3 / 11.7 / 19.0, 8192 rows
         // 42.9 / 31.4 / 25.5; 4096 x 4096, 1024 rows 22.1 / 17.3 / 30.7; 1024 x 1024, 2048 rows 6.2 / 8.0 / 12.3.
         auto tiles = [&](int64_t s) { return ((x.rows + s - 1) / s) * ((w.rows + s - 1) / s); };
@@ -333,7 +337,7 @@ aq_status launch_mx4_matmul(const aq_mx4& x, const aq_mx4& w, const float* bias,
 }
 
 aq_status launch_mx4_linear(const aq_matrix& x, const aq_mx4& w, const float* bias, const aq_matrix& y, void* ws, hipStream_t st) {
-    if (few_rows(x.rows, w.rows, x.cols * (int64_t)dtype_bytes(x.dtype)))
+    if (few_rows(x.rows, w.rows, x.cols * (int64_t)dtype_bytes(x.dtype), true))
         return with_dtype(x.dtype, [&](auto t) {
             using T = decltype(t);
             return launch_rows<Values<T>, T>(Values<T>{(const T*)x.d, x.ld, (int)x.cols}, x.rows, w, bias, y, st);

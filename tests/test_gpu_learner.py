@@ -398,7 +398,7 @@ def test_weight_grad_of_the_smallest_values(kind):
 
 LINEAR_SHAPES = [(1, 1, 1), (1, 256, 67), (1, 17, 2048), (2, 40, 33), (15, 100, 130), (16, 64, 128), (17, 21, 256), (64, 130, 1000), (65, 33, 257),
                  (128, 128, 256), (129, 257, 300), (300, 403, 1111), (700, 64, 64), (1030, 8, 4096),
-                 (2051, 2100, 300), (4101, 4099, 200)]  # the larger tiles
+                 (700, 730, 1500), (2051, 2100, 300), (4101, 4099, 200)]  # the larger tiles
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
