@@ -139,6 +139,12 @@ struct Track {
 // most turns for which offsets stay within 31 bits, some fetches ahead included
 inline int track_turns(int64_t step) { return (int)(0x7fffffff / step - 5); }
 
+// a thread's place among those that share a tile of S x S (only the smallest tiles are shared by several groups)
+template <int S>
+__device__ __forceinline__ uint32_t thread_of() {
+    return S == 64 ? threadIdx.x % tile_threads(S) : threadIdx.x;
+}
+
 // dy with t along the rows (weight gradient): [t][m].  ANY: rows of any alignment.
 template <class T, int S, bool ANY>
 struct DyRows {
@@ -154,10 +160,10 @@ struct DyRows {
         k.begin(d.base, byte & ~(int64_t)3, d.size < most ? d.size : most, 32 * (int)d.ld * (int)sizeof(T));
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + NT * i;
+            const int u = thread_of<S>() + NT * i;
             k.off[i] = ((int)byte & 3) + ((u / kPer) * (int)d.ld + 8 * (u % kPer)) * (int)sizeof(T);
         }
-        left = (int)(t_end - t0) - threadIdx.x / kPer;
+        left = (int)(t_end - t0) - thread_of<S>() / kPer;
     }
     __device__ __forceinline__ void move(int turns) { k.move(turns); }
     __device__ __forceinline__ void fetch(int set, int i) {
@@ -170,7 +176,7 @@ struct DyRows {
         load_piece<T, kOdd<T, ANY>>(in[set][i], k.w, at);
     }
     __device__ __forceinline__ void put(int set, int i, uint8_t* to) const {
-        const int u = threadIdx.x + NT * i;
+        const int u = thread_of<S>() + NT * i;
         v4u q[P];
         split<T, P>(in[set][i], q);
 #pragma unroll
@@ -193,10 +199,10 @@ struct DyCols {
         k.begin(d.base, byte & ~(int64_t)3, d.size, 32 * (int)sizeof(T));
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + NT * i;
+            const int u = thread_of<S>() + NT * i;
             k.off[i] = ((int)byte & 3) + ((u >> 2) * (int)d.ld + 8 * (u & 3)) * (int)sizeof(T);
         }
-        next = (int)(t_end - t0) - 8 * (threadIdx.x & 3);
+        next = (int)(t_end - t0) - 8 * (thread_of<S>() & 3);
     }
     __device__ __forceinline__ void move(int turns) { k.move(turns); }
     __device__ __forceinline__ void fetch(int set, int i) {
@@ -208,7 +214,7 @@ struct DyCols {
         }
     }
     __device__ __forceinline__ void put(int set, int i, uint8_t* to) const {
-        const int u = threadIdx.x + NT * i;
+        const int u = thread_of<S>() + NT * i;
         Piece<T> own = in[set][i];
         if constexpr (ANY) {
             const int n = left[set];
@@ -246,7 +252,7 @@ struct BlockRows {
         ks.begin(scales - skew, byte & ~(int64_t)3, last * blocks + skew, 32 * (int)blocks);
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
-            const int u = threadIdx.x + NT * i, t = u / kPer, piece = u % kPer;
+            const int u = thread_of<S>() + NT * i, t = u / kPer, piece = u % kPer;
             kc.off[i] = (t * (int)blocks * 4 + piece) * CODE;
             ks.off[i] = ((int)byte & 3) + t * (int)blocks + (piece >> 2);
         }
@@ -263,7 +269,7 @@ struct BlockRows {
         ks.off[i] += ks.step;
     }
     __device__ __forceinline__ void put(int set, int i, uint8_t* to) const {
-        const int u = threadIdx.x + NT * i;
+        const int u = thread_of<S>() + NT * i;
         v4u o;
         if constexpr (CODE == 8) {
             float v[8];
@@ -297,19 +303,27 @@ __device__ __forceinline__ void static_for(F&& f) {
 // own sums of A over t, where `sums` is given).  While the products of one 32 t run, the next 32 t go from registers to LDS, unit
 // by unit, and one or two more are on their way from memory behind them; with three buffers the barrier lies
 // two groups of products before the end, and the next operands are read behind it.
-template <class A, class B, class T, int S>
-__global__ void __launch_bounds__(tile_threads(S), 1)
+//
+// H: as many groups of wavefronts share a tile, each with buffers of its own and a slice of its own; their sums join in LDS, in their
+// order.  Two halve the chain of chunks that bounds small products, without slices' way through memory: input gradient 300 x 403 x
+// 1111 binary16 9.7 us with one, 8.5 with two, 8.8 with four.
+template <class A, class B, class T, int S, int H>
+__global__ void __launch_bounds__(H * tile_threads(S), 1)
     k_grad(A a, B b, T* __restrict__ out, int64_t ld, int64_t out_stride, float* __restrict__ sums, int64_t mn, int64_t cn, int64_t tn,
            int chunks, int turns) {
-    constexpr int P = A::P, NT = tile_threads(S), N = S / 64, NC = S / (NT / 128) / 32, kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(kBuf);
+    constexpr int P = A::P, NT = tile_threads(S), N = S / 64, NC = S / (NT / 128) / 32, kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(H * kBuf);
     constexpr int G = 2 * P * N;  // groups of NC products: 16 t, part, row tile
     static_assert(NT / 64 * 32 * kOutRow<T, NC> <= kBufs * kBuf, "results leave through the buffers");
+    static_assert(H == 1 || NT * (N * NC * 64 + 4) <= kBufs * kBuf, "and so do a group's sums");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5;
+    const int group = H > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
+    const int own = group * (kBufs * kBuf);  // where this group's buffers begin
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(thread_of<S>() >> 6), r = lane & 31, g = lane >> 5;
     const Place at = place_of_workgroup((uint32_t)((mn + S - 1) / S), (uint32_t)((cn + S - 1) / S));
     const int64_t m0 = (int64_t)at.m * S, c0 = (int64_t)at.c * S;
     const int wm = (wave & 1) * (S / 2), wc = (wave >> 1) * (32 * NC);
-    const int64_t t_first = (int64_t)at.z * chunks * 32;
+    const int64_t t_all = (int64_t)at.z * H * chunks * 32, t_first = t_all + (int64_t)group * chunks * 32;
+    const int64_t t_behind = tn;
     if (t_first + (int64_t)chunks * 32 < tn) tn = t_first + (int64_t)chunks * 32;
     a.begin(m0, t_first, tn);
     b.begin(c0, t_first, tn);
@@ -345,20 +359,20 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
         for (int i = 0; i < A::kSets; ++i) fetch_all(i);
 #pragma unroll
         for (int i = 0; i < A::kUnits; ++i) {
-            a.put(0, i, lds);
-            b.put(0, i, lds + P * A::kPlane);
+            a.put(0, i, lds + own);
+            b.put(0, i, lds + own + P * A::kPlane);
         }
         fetch_all(0);
         lds_barrier();
         v8bf16 ob[2 * NC], oa;
 #pragma unroll
-        for (int j = 0; j < 2 * NC; ++j) ob[j] = read_b(lds, j);
-        oa = read_a(lds, 0);
-        int now = 0;
+        for (int j = 0; j < 2 * NC; ++j) ob[j] = read_b(lds + own, j);
+        oa = read_a(lds + own, 0);
+        int now = own;
         auto step = [&](auto then) __attribute__((always_inline)) {
             constexpr int kThen = decltype(then)::value;  // the set that holds the next 32 t
             const uint8_t* const tile = lds + now;
-            now = now + kBuf == kBufs * kBuf ? 0 : now + kBuf;
+            now = now + kBuf == own + kBufs * kBuf ? own : now + kBuf;
             uint8_t* const next = lds + now;
             v8bf16 ob_next[2 * NC], oa_next;
             constexpr int kTasks = 2 * A::kUnits, kSlots = G > 2 ? G - 2 : 1;
@@ -407,7 +421,9 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
             }
         };
         int to_move = turns;
-        for (int left = (int)(tn - t_first); left > 0; left -= 64) {  // (32 t behind the end are zeros)
+        int left = (int)(tn - t_first);
+        if (H > 1) left = (int)(t_behind - t_all < (int64_t)chunks * 32 ? t_behind - t_all : (int64_t)chunks * 32);  // the first group's, which has the most
+        for (; left > 0; left -= 64) {  // (32 t behind the end are zeros)
             step(std::integral_constant<int, A::kSets - 1>());
             step(std::integral_constant<int, 0>());
             if ((to_move -= 2) <= 0) {
@@ -420,6 +436,30 @@ __global__ void __launch_bounds__(tile_threads(S), 1)
     out += at.z * out_stride;
     wait_loads<0>();
     lds_barrier();  // (every wavefront has read its last operands)
+    if constexpr (H > 1) {
+        constexpr int kEach = N * NC * 4;  // v4f32 of a thread
+        const int thread = thread_of<S>();
+        if (group) {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                const v16f32& v = acc[k / (NC * 4)][k / 4 % NC];
+                ((v4f32*)(lds + own))[k * NT + thread] = v4f32{v[k % 4 * 4], v[k % 4 * 4 + 1], v[k % 4 * 4 + 2], v[k % 4 * 4 + 3]};
+            }
+            ((float*)(lds + own))[kEach * 4 * NT + thread] = acc_sum;
+        }
+        lds_barrier();
+        if (group) return;
+        for (int h = 1; h < H; ++h) {
+            const uint8_t* const from = lds + h * (kBufs * kBuf);
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                const v4f32 v = ((const v4f32*)from)[k * NT + thread];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[k / (NC * 4)][k / 4 % NC][k % 4 * 4 + e] += v[e];
+            }
+            acc_sum += ((const float*)from)[kEach * 4 * NT + thread];
+        }
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int64_t row = m0 + wm + 32 * tile_of(i), m = row + r;
@@ -456,9 +496,9 @@ __global__ void __launch_bounds__(256) k_grad_join(const float* __restrict__ par
     else if (sums && i < m * c + m) sums[i - m * c] = total(part_sums + (i - m * c), m);
 }
 
-// how a product of m x c over t runs: tiles of s x s, z slices of `chunks` (an even number) times 32 t
+// how a product of m x c over t runs: tiles of s x s, z times h slices of `chunks` (an even number) times 32 t, h of them in one workgroup
 struct Plan {
-    int s, z, chunks;
+    int s, z, h, chunks;
 };
 // The tile and the slices by an estimate in us: what a launch takes besides its chunks; the chunks of a workgroup one after the
 // other, each as long as `alone` while few workgroups are about and `full` while as many as fit are (`at_once`); the join's launch
@@ -466,26 +506,31 @@ struct Plan {
 //   bfloat16 2048 x 2048  51.1 / 38.4 / 54.8,   1024 x 1024 20.5 / 32.9 / 50.4,   128 x 128 18.5 / 31.3 / 49.1 (256 rows 4.9 / 7.7 / 12.1)
 //   binary16              73.2 / 55.8 / 97.1,               30.9 / 47.2 / 93.8,             27.8 / 46.2 / 91.9 (6.2 / 9.8 / 17.6)
 //   fp32                 103.4 / 76.1 / 137.5,              37.9 / 63.9 / 135.8,            33.7 / 61.7 / 132.5 (6.9 / 11.9 / 23.1)
+// and with two groups to a tile of 64
+//   bfloat16              50.3, 16.4, 13.7 (4.9),   binary16 75.3, 24.3, 21.0 (5.8),   fp32 115.8, 29.9, 25.4 (6.4)
+// (the fitted figures of two groups are a little below these, as other shapes gave them on the same machine as the others).
+constexpr int kGroups = 2;  // of wavefronts, where a workgroup has several
 Plan plan(int64_t m, int64_t c, int64_t t, int parts) {
     constexpr struct {
-        int s, at_once;
+        int s, h, at_once;
         float launch, alone, full;
-    } kinds[3][3] = {{{64, 1024, 3.1f, 0.24f, 0.75f}, {128, 512, 4.3f, 0.42f, 0.86f}, {256, 256, 6.8f, 0.66f, 1.07f}},
-                     {{64, 1024, 3.1f, 0.39f, 1.10f}, {128, 512, 4.6f, 0.65f, 1.52f}, {256, 256, 7.0f, 1.33f, 1.75f}},
-                     {{64, 1024, 3.1f, 0.48f, 1.57f}, {128, 256, 4.8f, 0.89f, 1.20f}, {256, 256, 7.4f, 1.95f, 2.60f}}};
+    } kinds[3][4] = {{{64, 1, 1024, 3.1f, 0.23f, 0.75f}, {64, kGroups, 512, 3.6f, 0.29f, 0.66f}, {128, 1, 512, 4.3f, 0.42f, 0.86f}, {256, 1, 256, 6.8f, 0.66f, 1.07f}},
+                     {{64, 1, 1024, 3.1f, 0.40f, 1.10f}, {64, kGroups, 512, 3.6f, 0.50f, 1.00f}, {128, 1, 512, 4.6f, 0.65f, 1.52f}, {256, 1, 256, 7.0f, 1.33f, 1.75f}},
+                     {{64, 1, 1024, 3.1f, 0.48f, 1.57f}, {64, kGroups, 256, 3.7f, 0.62f, 0.76f}, {128, 1, 256, 4.8f, 0.89f, 1.20f}, {256, 1, 256, 7.4f, 1.95f, 2.60f}}};
     const int64_t all = (t + 31) / 32;
-    Plan best{64, 1, (int)((all + 1) & ~1)};
+    Plan best{64, 1, 1, (int)((all + 1) & ~1)};
     float least = 3.0e38f;
     for (const auto& k : kinds[parts - 1]) {
         const int64_t tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + k.s - 1) / k.s);
-        for (int64_t want = 1; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
-            const int64_t chunks = ((all + want - 1) / want + 1) & ~1, z = chunks ? (all + chunks - 1) / chunks : 1;
-            const float full = (float)(tiles * z) / (float)k.at_once;
+        for (int64_t want = k.h; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
+            const int64_t chunks = ((all + want - 1) / want + 1) & ~1, z = chunks ? (all + chunks * k.h - 1) / (chunks * k.h) : 1;
+            const int64_t wgs = tiles * z, busy = wgs <= 256 ? wgs : (wgs + 255) / 256 * 256;  // (256 CUs; the last turn is as long as a whole one)
+            const float full = (float)busy / (float)k.at_once;
             float us = k.launch + (float)chunks * (full < 1.0f ? k.alone + (k.full - k.alone) * full * full : k.full * ceilf(full));
-            if (z > 1) us += 2.5f + (float)(z * m * c * 4) * (1.0f / 3.5e6f);
+            if (z > 1) us += 2.3f + 0.02f * (float)z + (float)(z * m * c * 4) * (1.0f / 3.5e6f);
             if (us < least) {
                 least = us;
-                best = {k.s, (int)z, (int)chunks};
+                best = {k.s, (int)z, k.h, (int)chunks};
             }
         }
     }
@@ -503,16 +548,25 @@ int64_t most_slices(int64_t m, int64_t c, int64_t t) {
     return z;
 }
 
+template <class A, class B, class T, int S, int H>
+aq_status launch_groups(const A& a, const B& b, T* out, int64_t ld, int64_t stride, float* sums, int64_t m, int64_t c, int64_t t,
+                        const Plan& p, int64_t bytes_per_t, hipStream_t st) {
+    constexpr int kBuf = A::P * A::kPlane + B::kPlane, kLds = H * grad_buffers(H * kBuf) * kBuf;
+    static_assert(kLds <= kMostLds, "");
+    const int64_t x = (m + S - 1) / S, y = (c + S - 1) / S;
+    if (!grid_ok(x * y * p.z, H * tile_threads(S))) return AQ_ESHAPE;
+    auto* const k = k_grad<A, B, T, S, H>;
+    if (!allow_lds<A, B, T, std::integral_constant<int, S>, std::integral_constant<int, H>>((const void*)k, kLds)) return AQ_EHIP;
+    k<<<(unsigned)(x * y * p.z), H * tile_threads(S), kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks, track_turns(32 * bytes_per_t) & ~1);
+    return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+}
 template <class A, class B, class T, int S>
 aq_status launch(const A& a, const B& b, T* out, int64_t ld, int64_t stride, float* sums, int64_t m, int64_t c, int64_t t, const Plan& p,
                  int64_t bytes_per_t, hipStream_t st) {
-    constexpr int kBuf = A::P * A::kPlane + B::kPlane, kLds = grad_buffers(kBuf) * kBuf;
-    const int64_t x = (m + S - 1) / S, y = (c + S - 1) / S;
-    if (!grid_ok(x * y * p.z, tile_threads(S))) return AQ_ESHAPE;
-    auto* const k = k_grad<A, B, T, S>;
-    if (!allow_lds<A, B, T, std::integral_constant<int, S>>((const void*)k, kLds)) return AQ_EHIP;
-    k<<<(unsigned)(x * y * p.z), tile_threads(S), kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks, track_turns(32 * bytes_per_t) & ~1);
-    return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+    if constexpr (S == 64) {
+        if (p.h > 1) return launch_groups<A, B, T, S, kGroups>(a, b, out, ld, stride, sums, m, c, t, p, bytes_per_t, st);
+    }
+    return launch_groups<A, B, T, S, 1>(a, b, out, ld, stride, sums, m, c, t, p, bytes_per_t, st);
 }
 template <class T>
 aq_status join(const float* part, const Plan& p, int64_t m, int64_t c, T* out, int64_t ld, const float* part_sums, float* sums, hipStream_t st) {
