@@ -13,8 +13,6 @@
 // A workgroup's 32 t of both operands go through LDS.  B lies there as it does in memory, t by t (and so does A for the weight
 // gradient), and is transposed on its way to the registers: ds_read_b64_tr_b16 hands lane i of 16 the four t of column i out of
 // four rows of 16 columns.
-#include <math.h>
-
 #include <utility>
 
 #include "learner.hpp"
@@ -510,43 +508,50 @@ struct Plan {
 //   bfloat16              50.3, 16.4, 13.7 (4.9),   binary16 75.3, 24.3, 21.0 (5.8),   fp32 115.8, 29.9, 25.4 (6.4)
 // (the fitted figures of two groups are a little below these, as other shapes gave them on the same machine as the others).
 constexpr int kGroups = 2;  // of wavefronts, where a workgroup has several
-Plan plan(int64_t m, int64_t c, int64_t t, int parts) {
-    constexpr struct {
-        int s, h, at_once;
+struct Kind {
+    int s, h;
+    struct {
+        int bits;  // 2^bits workgroups at once
         float launch, alone, full;
-    } kinds[3][4] = {{{64, 1, 1024, 3.1f, 0.23f, 0.75f}, {64, kGroups, 512, 3.6f, 0.29f, 0.66f}, {128, 1, 512, 4.3f, 0.42f, 0.86f}, {256, 1, 256, 6.8f, 0.66f, 1.07f}},
-                     {{64, 1, 1024, 3.1f, 0.40f, 1.10f}, {64, kGroups, 512, 3.6f, 0.50f, 1.00f}, {128, 1, 512, 4.6f, 0.65f, 1.52f}, {256, 1, 256, 7.0f, 1.33f, 1.75f}},
-                     {{64, 1, 1024, 3.1f, 0.48f, 1.57f}, {64, kGroups, 256, 3.7f, 0.62f, 0.76f}, {128, 1, 256, 4.8f, 0.89f, 1.20f}, {256, 1, 256, 7.4f, 1.95f, 2.60f}}};
-    const int64_t all = (t + 31) / 32;
-    Plan best{64, 1, 1, (int)((all + 1) & ~1)};
-    float least = 3.0e38f;
-    for (const auto& k : kinds[parts - 1]) {
+    } cost[3];  // of bfloat16, binary16, fp32
+};
+struct Plans {
+    Plan of[3];
+    int most_slices;  // the scratch's, which is the same for every type
+};
+Plans plans(int64_t m, int64_t c, int64_t t) {
+    constexpr Kind kinds[] = {{64, 1, {{10, 3.1f, 0.23f, 0.75f}, {10, 3.1f, 0.40f, 1.10f}, {10, 3.1f, 0.48f, 1.57f}}},
+                              {64, kGroups, {{9, 3.6f, 0.29f, 0.66f}, {9, 3.6f, 0.50f, 1.00f}, {8, 3.7f, 0.62f, 0.76f}}},
+                              {128, 1, {{9, 4.3f, 0.42f, 0.86f}, {9, 4.6f, 0.65f, 1.52f}, {8, 4.8f, 0.89f, 1.20f}}},
+                              {256, 1, {{8, 6.8f, 0.66f, 1.07f}, {8, 7.0f, 1.33f, 1.75f}, {8, 7.4f, 1.95f, 2.60f}}}};
+    const int32_t all = (int32_t)((t + 31) / 32);
+    const Plan none{64, 1, 1, (all + 1) & ~1};
+    Plans best{{none, none, none}, 1};
+    float least[3] = {3.0e38f, 3.0e38f, 3.0e38f};
+    for (const Kind& k : kinds) {
         const int64_t tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + k.s - 1) / k.s);
-        for (int64_t want = k.h; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
-            const int64_t chunks = ((all + want - 1) / want + 1) & ~1, z = chunks ? (all + chunks * k.h - 1) / (chunks * k.h) : 1;
+        for (int32_t want = k.h; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
+            const int32_t chunks = ((all + want - 1) / want + 1) & ~1, z = chunks ? (all + chunks * k.h - 1) / (chunks * k.h) : 1;
             const int64_t wgs = tiles * z, busy = wgs <= 256 ? wgs : (wgs + 255) / 256 * 256;  // (256 CUs; the last turn is as long as a whole one)
-            const float full = (float)busy / (float)k.at_once;
-            float us = k.launch + (float)chunks * (full < 1.0f ? k.alone + (k.full - k.alone) * full * full : k.full * ceilf(full));
-            if (z > 1) us += 2.3f + 0.02f * (float)z + (float)(z * m * c * 4) * (1.0f / 3.5e6f);
-            if (us < least) {
-                least = us;
-                best = {k.s, (int)z, k.h, (int)chunks};
+            const float join = z > 1 ? 2.3f + 0.02f * (float)z + (float)(z * m * c * 4) * (1.0f / 3.5e6f) : 0.0f;
+            for (int i = 0; i < 3; ++i) {
+                const auto& cost = k.cost[i];
+                const int64_t turns = (busy + (1 << cost.bits) - 1) >> cost.bits;
+                const float full = (float)busy * (1.0f / (float)(1 << cost.bits));
+                const float us = cost.launch + join +
+                                 (float)chunks * (turns > 1 ? cost.full * (float)turns : cost.alone + (cost.full - cost.alone) * full * full);
+                if (us < least[i]) {
+                    least[i] = us;
+                    best.of[i] = {k.s, z, k.h, chunks};
+                }
             }
         }
     }
+    for (const Plan& p : best.of) best.most_slices = p.z > best.most_slices ? p.z : best.most_slices;
     return best;
 }
-int parts_of(int32_t dtype) { return dtype == AQ_BF16 ? 1 : dtype == AQ_F16 ? 2 : 3; }
+int type_of(int32_t dtype) { return dtype == AQ_BF16 ? 0 : dtype == AQ_F16 ? 1 : 2; }
 int64_t slices_bytes(int64_t z, int64_t values) { return z > 1 ? z * values * (int64_t)sizeof(float) : 0; }
-// the most slices that a product of any type takes
-int64_t most_slices(int64_t m, int64_t c, int64_t t) {
-    int64_t z = 1;
-    for (int parts = 1; parts <= 3; ++parts) {
-        const int64_t own = plan(m, c, t, parts).z;
-        z = own > z ? own : z;
-    }
-    return z;
-}
 
 template <class A, class B, class T, int S, int H>
 aq_status launch_groups(const A& a, const B& b, T* out, int64_t ld, int64_t stride, float* sums, int64_t m, int64_t c, int64_t t,
@@ -589,14 +594,15 @@ bool any_pieces(const aq_matrix& m, bool whole) {
 
 }  // namespace
 
-int64_t weight_grad_workspace(int64_t rows, int64_t n, int64_t k) { return slices_bytes(most_slices(n, k, rows), n * k + n); }
+int64_t weight_grad_workspace(int64_t rows, int64_t n, int64_t k) { return slices_bytes(plans(n, k, rows).most_slices, n * k + n); }
 
 aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq_matrix& dw, float* db, void* ws, uint64_t ws_bytes,
                              hipStream_t st) {
     const int64_t n = dy.cols, k = kept.cols, rows = dy.rows;
-    const Plan p = plan(n, k, rows, parts_of(dy.dtype));
+    const Plans all = plans(n, k, rows);
+    const Plan p = all.of[type_of(dy.dtype)];
     const bool split_t = p.z > 1;
-    if (!workspace_ok(ws, ws_bytes, slices_bytes(p.z, n * k + n))) return AQ_EINVAL;
+    if (!workspace_ok(ws, ws_bytes, slices_bytes(all.most_slices, n * k + n))) return AQ_EINVAL;
     float* const out = split_t ? (float*)ws : (float*)dw.d;
     float* const sums = !db ? nullptr : split_t ? (float*)ws + p.z * n * k : db;
     const aq_status s = with_dtype(dy.dtype, [&](auto t) {
@@ -616,12 +622,13 @@ aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq
     return join((const float*)ws, p, n, k, (float*)dw.d, dw.ld, sums, db, st);
 }
 
-int64_t input_grad_workspace(int64_t rows, int64_t n, int64_t k) { return slices_bytes(most_slices(rows, k, n), rows * k); }
+int64_t input_grad_workspace(int64_t rows, int64_t n, int64_t k) { return slices_bytes(plans(rows, k, n).most_slices, rows * k); }
 
 aq_status launch_input_grad(const aq_matrix& dy, const aq_mx4& w, const aq_matrix& dx, void* ws, uint64_t ws_bytes, hipStream_t st) {
     const int64_t n = w.rows, k = w.cols, rows = dy.rows;
-    const Plan p = plan(rows, k, n, parts_of(dy.dtype));
-    if (!workspace_ok(ws, ws_bytes, slices_bytes(p.z, rows * k))) return AQ_EINVAL;
+    const Plans all = plans(rows, k, n);
+    const Plan p = all.of[type_of(dy.dtype)];
+    if (!workspace_ok(ws, ws_bytes, slices_bytes(all.most_slices, rows * k))) return AQ_EINVAL;
     return with_dtype(dy.dtype, [&](auto t) {
         using T = decltype(t);
         const aq_status s = with_tile(p.s, [&](auto sc) {
