@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(512)
 // chunk is in registers, and the barrier there hands its buffer to the chunk after the next.  Scales come for two chunks at a time
 // through registers.
 //
-// 16384 x 4096 x 4096 to bfloat16: 160 us alone, 186 to 202 back to back (2.7 to 3.4 PFLOP/s), where a loop of nothing but these
+// 16384 x 4096 x 4096 to bfloat16: 160 us alone, 177 to 202 back to back (2.7 to 3.4 PFLOP/s), where a loop of nothing but these
 // products on such values reaches 6.5 at the clock that is left.  Without the loads it would take 129, without the products 112: the two
 // do not overlap wholly.  128 k at a time, half a line of memory to a row: 170; tiles of 128 x 128 to a wavefront, one to a SIMD: 186.
 template <class T, int S, int NT>
