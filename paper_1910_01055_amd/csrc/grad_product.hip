@@ -5,10 +5,10 @@
 // either format times its power of two has at most seven significant bits, so it is a bf16 value, and a value of dy is the sum of
 // one (bfloat16), two (binary16) or three (fp32) bf16 values.
 //
-// Bound by the matrix cores' power and by what feeds them: 65536 x 2048 x 2048 in bfloat16 takes 521 to 545 us back to back (1.03 PFLOP/s; 471
-// alone), the input gradient 8192 x 2048 x 2048 61 us (1.13 PFLOP/s), where a loop of nothing but these products on such values
-// reaches 1.88 PFLOP/s at the clock that is left and a large library product 1.21.  binary16 takes twice and fp32 three times
-// the products (610 and 410 TFLOP/s).
+// Bound by the matrix cores' power and by what feeds them: 65536 x 2048 x 2048 in bfloat16 takes 521 to 555 us back to back
+// (1.02 PFLOP/s; 471 alone), the input gradient 8192 x 2048 x 2048 61 us (1.13 PFLOP/s), where a loop of nothing but these
+// products on such values reaches 1.88 PFLOP/s at the clock that is left and a large library product 1.21.  binary16 takes twice
+// and fp32 three times the products (610 and 410 TFLOP/s).
 //
 // A workgroup's 32 t of both operands go through LDS.  B lies there as it does in memory, t by t (and so does A for the weight
 // gradient), and is transposed on its way to the registers: ds_read_b64_tr_b16 hands lane i of 16 the four t of column i out of
@@ -43,7 +43,8 @@ __device__ __forceinline__ void split(const Piece<T>& in, v4u (&out)[P]) {
 #pragma unroll
         for (int q = 0; q < P; ++q) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) out[q][j] = __builtin_amdgcn_perm(__float_as_uint(v[2 * j + 1]), __float_as_uint(v[2 * j]), 0x07060302u);
+            for (int j = 0; j < 4; ++j)
+                out[q][j] = __builtin_amdgcn_perm(__float_as_uint(v[2 * j + 1]), __float_as_uint(v[2 * j]), 0x07060302u);
             if (q + 1 < P) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -76,7 +77,8 @@ __device__ __forceinline__ v8bf16 t_operand(const uint8_t* tile, int t0, int col
 __device__ __forceinline__ int m_at(int m, int piece) { return m * 64 + ((piece ^ ((m >> 2) & 3)) << 4); }
 
 // ---- the operands.  Of 32 t and S columns (or rows) each thread fetches kUnits units of eight values into registers and later puts them
-// into LDS as bf16.  Loads go through windows on the matrix (see Window).  Columns of an operand that do not exist only reach results that are not stored.
+// into LDS as bf16.  Loads go through windows on the matrix (see Window).  Columns of an operand that do not exist only reach results
+// that are not stored.
 // A matrix in whole words of memory: from the word of its first element to that of its last.
 struct Words {
     const uint8_t* base;
@@ -146,7 +148,8 @@ __device__ __forceinline__ uint32_t thread_of() {
 // dy with t along the rows (weight gradient): [t][m].  ANY: rows of any alignment.
 template <class T, int S, bool ANY>
 struct DyRows {
-    static constexpr int P = kParts<T>, NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kPer = S / 8, kSets = P == 1 || S < 256 ? 2 : 1;
+    static constexpr int P = kParts<T>, NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kPer = S / 8;
+    static constexpr int kSets = P == 1 || S < 256 ? 2 : 1;
     static constexpr bool kSums = true;
     Words d;
     Track<kUnits> k;
@@ -186,7 +189,8 @@ struct DyRows {
 // values are the next row's.
 template <class T, int S, bool ANY>
 struct DyCols {
-    static constexpr int P = kParts<T>, NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S, kSets = P == 1 || S < 256 ? 2 : 1;
+    static constexpr int P = kParts<T>, NT = tile_threads(S), kUnits = 4 * S / NT, kPlane = 32 * 2 * S;
+    static constexpr int kSets = P == 1 || S < 256 ? 2 : 1;
     static constexpr bool kSums = false;
     Words d;
     Track<kUnits> k;
@@ -297,10 +301,10 @@ __device__ __forceinline__ void static_for(F&& f) {
     static_for<N>(f, std::make_integer_sequence<int, N>());
 }
 
-// C tile of S x S, a wavefront takes S / 2 rows and NC * 32 columns of it.  Slice z takes t in [z * chunks * 32, + chunks * 32) and writes its own C (and its
-// own sums of A over t, where `sums` is given).  While the products of one 32 t run, the next 32 t go from registers to LDS, unit
-// by unit, and one or two more are on their way from memory behind them; with three buffers the barrier lies
-// two groups of products before the end, and the next operands are read behind it.
+// C tile of S x S, a wavefront takes S / 2 rows and NC * 32 columns of it.  Slice z takes t in [z * chunks * 32, + chunks * 32) and
+// writes its own C (and its own sums of A over t, where `sums` is given).  While the products of one 32 t run, the next 32 t go from
+// registers to LDS, unit by unit, and one or two more are on their way from memory behind them (three or four gain nothing); with
+// three buffers the barrier lies two groups of products before the end, and the next operands are read behind it.
 //
 // H: as many groups of wavefronts share a tile, each with buffers of its own and a slice of its own; their sums join in LDS, in their
 // order.  Two halve the chain of chunks that bounds small products, without slices' way through memory: input gradient 300 x 403 x
@@ -309,7 +313,8 @@ template <class A, class B, class T, int S, int H>
 __global__ void __launch_bounds__(H * tile_threads(S), 1)
     k_grad(A a, B b, T* __restrict__ out, int64_t ld, int64_t out_stride, float* __restrict__ sums, int64_t mn, int64_t cn, int64_t tn,
            int chunks, int turns) {
-    constexpr int P = A::P, NT = tile_threads(S), N = S / 64, NC = S / (NT / 128) / 32, kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(H * kBuf);
+    constexpr int P = A::P, NT = tile_threads(S), N = S / 64, NC = S / (NT / 128) / 32;
+    constexpr int kBuf = P * A::kPlane + B::kPlane, kBufs = grad_buffers(H * kBuf);
     constexpr int G = 2 * P * N;  // groups of NC products: 16 t, part, row tile
     static_assert(NT / 64 * 32 * kOutRow<T, NC> <= kBufs * kBuf, "results leave through the buffers");
     static_assert(H == 1 || NT * (N * NC * 64 + 4) <= kBufs * kBuf, "and so do a group's sums");
@@ -379,7 +384,8 @@ __global__ void __launch_bounds__(H * tile_threads(S), 1)
                 if (kBufs == 3 && q >= kSlots) {
                     if (q == kSlots) lds_barrier();
 #pragma unroll
-                    for (int j = (q - kSlots) * 2 * NC / (G - kSlots); j < (q - kSlots + 1) * 2 * NC / (G - kSlots); ++j) ob_next[j] = read_b(next, j);
+                    for (int j = (q - kSlots) * 2 * NC / (G - kSlots); j < (q - kSlots + 1) * 2 * NC / (G - kSlots); ++j)
+                        ob_next[j] = read_b(next, j);
                 }
                 if (q + 1 < G) oa_next = read_a(tile, q + 1);
                 else if (kBufs == 3) oa_next = read_a(next, 0);
@@ -420,7 +426,8 @@ __global__ void __launch_bounds__(H * tile_threads(S), 1)
         };
         int to_move = turns;
         int left = (int)(tn - t_first);
-        if (H > 1) left = (int)(t_behind - t_all < (int64_t)chunks * 32 ? t_behind - t_all : (int64_t)chunks * 32);  // the first group's, which has the most
+        if (H > 1)  // the first group's, which has the most
+            left = (int)(t_behind - t_all < (int64_t)chunks * 32 ? t_behind - t_all : (int64_t)chunks * 32);
         for (; left > 0; left -= 64) {  // (32 t behind the end are zeros)
             step(std::integral_constant<int, A::kSets - 1>());
             step(std::integral_constant<int, 0>());
@@ -532,14 +539,15 @@ Plans plans(int64_t m, int64_t c, int64_t t) {
         const int64_t tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + k.s - 1) / k.s);
         for (int32_t want = k.h; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
             const int32_t chunks = ((all + want - 1) / want + 1) & ~1, z = chunks ? (all + chunks * k.h - 1) / (chunks * k.h) : 1;
-            const int64_t wgs = tiles * z, busy = wgs <= 256 ? wgs : (wgs + 255) / 256 * 256;  // (256 CUs; the last turn is as long as a whole one)
+            // (256 CUs; the last turn is as long as a whole one)
+            const int64_t wgs = tiles * z, busy = wgs <= 256 ? wgs : (wgs + 255) / 256 * 256;
             const float join = z > 1 ? 2.3f + 0.02f * (float)z + (float)(z * m * c * 4) * (1.0f / 3.5e6f) : 0.0f;
             for (int i = 0; i < 3; ++i) {
                 const auto& cost = k.cost[i];
                 const int64_t turns = (busy + (1 << cost.bits) - 1) >> cost.bits;
                 const float full = (float)busy * (1.0f / (float)(1 << cost.bits));
-                const float us = cost.launch + join +
-                                 (float)chunks * (turns > 1 ? cost.full * (float)turns : cost.alone + (cost.full - cost.alone) * full * full);
+                const float chunk = turns > 1 ? cost.full * (float)turns : cost.alone + (cost.full - cost.alone) * full * full;
+                const float us = cost.launch + join + (float)chunks * chunk;
                 if (us < least[i]) {
                     least[i] = us;
                     best.of[i] = {k.s, z, k.h, chunks};
@@ -562,7 +570,8 @@ aq_status launch_groups(const A& a, const B& b, T* out, int64_t ld, int64_t stri
     if (!grid_ok(x * y * p.z, H * tile_threads(S))) return AQ_ESHAPE;
     auto* const k = k_grad<A, B, T, S, H>;
     if (!allow_lds<A, B, T, std::integral_constant<int, S>, std::integral_constant<int, H>>((const void*)k, kLds)) return AQ_EHIP;
-    k<<<(unsigned)(x * y * p.z), H * tile_threads(S), kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks, track_turns(32 * bytes_per_t) & ~1);
+    k<<<(unsigned)(x * y * p.z), H * tile_threads(S), kLds, st>>>(a, b, out, ld, stride, sums, m, c, t, p.chunks,
+                                                               track_turns(32 * bytes_per_t) & ~1);
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }
 template <class A, class B, class T, int S>
@@ -574,7 +583,8 @@ aq_status launch(const A& a, const B& b, T* out, int64_t ld, int64_t stride, flo
     return launch_groups<A, B, T, S, 1>(a, b, out, ld, stride, sums, m, c, t, p, bytes_per_t, st);
 }
 template <class T>
-aq_status join(const float* part, const Plan& p, int64_t m, int64_t c, T* out, int64_t ld, const float* part_sums, float* sums, hipStream_t st) {
+aq_status join(const float* part, const Plan& p, int64_t m, int64_t c, T* out, int64_t ld, const float* part_sums, float* sums,
+               hipStream_t st) {
     const int64_t g = (m * c + m + 255) / 256;
     if (!grid_ok(g, 256)) return AQ_ESHAPE;
     k_grad_join<T><<<(unsigned)g, 256, 0, st>>>(part, p.z, m, c, out, ld, part_sums, sums);
@@ -609,13 +619,16 @@ aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq
         using T = decltype(t);
         return with_tile(p.s, [&](auto sc) {
             constexpr int S = decltype(sc)::value, kSets = DyRows<T, S, false>::kSets;
-            const int64_t code_bytes = 32 * blocks32(k), dy_bytes = dy.ld * (int64_t)sizeof(T), bytes_per_t = dy_bytes > code_bytes ? dy_bytes : code_bytes;
+            const int64_t code_bytes = 32 * blocks32(k), dy_bytes = dy.ld * (int64_t)sizeof(T);
+            const int64_t bytes_per_t = dy_bytes > code_bytes ? dy_bytes : code_bytes, ld = split_t ? k : dw.ld;
             const BlockRows<S, kSets, 8> b{(const uint8_t*)kept.d_codes, kept.d_scales, blocks32(k), rows};
             if constexpr (sizeof(T) == 2) {
                 if (any_pieces<T>(dy, false))
-                    return launch<DyRows<T, S, true>, BlockRows<S, kSets, 8>, float, S>({words_of<T>(dy)}, b, out, split_t ? k : dw.ld, n * k, sums, n, k, rows, p, bytes_per_t, st);
+                    return launch<DyRows<T, S, true>, BlockRows<S, kSets, 8>, float, S>({words_of<T>(dy)}, b, out, ld, n * k, sums, n, k, rows, p,
+                                                                                       bytes_per_t, st);
             }
-            return launch<DyRows<T, S, false>, BlockRows<S, kSets, 8>, float, S>({words_of<T>(dy)}, b, out, split_t ? k : dw.ld, n * k, sums, n, k, rows, p, bytes_per_t, st);
+            return launch<DyRows<T, S, false>, BlockRows<S, kSets, 8>, float, S>({words_of<T>(dy)}, b, out, ld, n * k, sums, n, k, rows, p,
+                                                                               bytes_per_t, st);
         });
     });
     if (s != AQ_OK || !split_t) return s;
@@ -637,9 +650,11 @@ aq_status launch_input_grad(const aq_matrix& dy, const aq_mx4& w, const aq_matri
                 using A = DyCols<T, S, decltype(edge)::value>;
                 constexpr int kSets = A::kSets;
                 const A a{words_of<T>(dy)};
-                const BlockRows<S, kSets, 4> b{(const uint8_t*)w.d_codes, w.d_scales, blocks32(k), n};
-                if (p.z > 1) return launch<A, BlockRows<S, kSets, 4>, float, S>(a, b, (float*)ws, k, rows * k, nullptr, rows, k, n, p, 16 * blocks32(k), st);
-                return launch<A, BlockRows<S, kSets, 4>, T, S>(a, b, (T*)dx.d, dx.ld, 0, nullptr, rows, k, n, p, 16 * blocks32(k), st);
+                using Weights = BlockRows<S, kSets, 4>;
+                const Weights b{(const uint8_t*)w.d_codes, w.d_scales, blocks32(k), n};
+                const int64_t bytes_per_t = 16 * blocks32(k);
+                if (p.z > 1) return launch<A, Weights, float, S>(a, b, (float*)ws, k, rows * k, nullptr, rows, k, n, p, bytes_per_t, st);
+                return launch<A, Weights, T, S>(a, b, (T*)dx.d, dx.ld, 0, nullptr, rows, k, n, p, bytes_per_t, st);
             };
             return any_pieces<T>(dy, true) ? go(std::true_type()) : go(std::false_type());
         });

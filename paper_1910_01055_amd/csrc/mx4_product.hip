@@ -185,7 +185,8 @@ __global__ void __launch_bounds__(NT, 1)
                 const int o8 = blocks & 8, o4 = blocks & 12, o2 = blocks & 14;
                 const v2u a = o8 ? *(const v2u_byte AQ_GLOBAL*)row : v2u{0, 0};
                 const uint32_t b = blocks & 4 ? *(const u32_byte AQ_GLOBAL*)(row + o8) : 0;
-                const uint32_t c2 = blocks & 2 ? *(const u16_byte AQ_GLOBAL*)(row + o4) : 0, c1 = blocks & 1 ? *(const uint8_t AQ_GLOBAL*)(row + o2) : 0;
+                const uint32_t c2 = blocks & 2 ? *(const u16_byte AQ_GLOBAL*)(row + o4) : 0;
+                const uint32_t c1 = blocks & 1 ? *(const uint8_t AQ_GLOBAL*)(row + o2) : 0;
                 const uint32_t c = blocks & 2 ? c2 | c1 << 16 : c1;
                 sc[i] = v4u{o8 ? a[0] : blocks & 4 ? b : c, o8 ? a[1] : blocks & 4 ? c : 0, o8 ? blocks & 4 ? b : c : 0, o4 == 12 ? c : 0};
             }

@@ -16,7 +16,8 @@ struct Window {
     // of the bytes from `at` (a multiple of 4) on of `size` bytes at `base`
     __device__ __forceinline__ void set(const uint8_t* base, int64_t at, int64_t size) {
         const int64_t left = size - at;
-        r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (left > 0 ? at : 0)), 0, left <= 0 ? 0 : left < kMost ? (int)left : kMost, 0x00020000);
+        r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (left > 0 ? at : 0)), 0, left <= 0 ? 0 : left < kMost ? (int)left : kMost,
+                                              0x00020000);
     }
     static constexpr int kMost = 0x7ffffff0, kOutside = (int)0x80000000u;
 };
