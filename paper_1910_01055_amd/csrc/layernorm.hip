@@ -14,11 +14,12 @@
 namespace aq {
 namespace {
 
-constexpr int threads_for(int g) { return g < 256 ? 256 : g; }  // of a workgroup
+constexpr int threads_for(int g) { return g <= 64 ? 256 : g; }  // of a workgroup: four wavefronts, or a row
 template <int G, int P>
 struct RowForm {
     static constexpr int kThreads = threads_for(G);
     static constexpr int kRows = kThreads / G;  // rows at a time in a workgroup
+    static_assert(G <= 64 || kRows == 1, "wavefronts of one row share `red`");
     // sum over the threads of a row (G > 64: over LDS; `red` must not be in use by a sum whose barrier some thread has not passed)
     static __device__ __forceinline__ float sum(float s, float* red) {
         s = lanes_sum<G < 64 ? G : 64>(s);
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(threads_for(G))
     for (int i = 0; i < P; ++i) {
         const int col = 8 * (t + G * i);
         n[i] = cols - col;
-        cur[i].load(x + row * ldx + col, n[i]);
+        cur[i].request(x + row * ldx + col, n[i], col);
         ga[i].zero();
         be[i].zero();
         if (gamma) ga[i].load(gamma + col, n[i]);
@@ -76,11 +77,12 @@ __global__ void __launch_bounds__(threads_for(G))
     for (; row < rows; row += step) {
         if (row + step < rows) {
 #pragma unroll
-            for (int i = 0; i < P; ++i) next[i].load(x + (row + step) * ldx + 8 * (t + G * i), n[i]);
+            for (int i = 0; i < P; ++i) next[i].request(x + (row + step) * ldx + 8 * (t + G * i), n[i], 8 * (t + G * i));
         }
         float v[P][8], s = 0.0f;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
+            if (cols & 7) cur[i].settle(n[i], 8 * (t + G * i));
             cur[i].get(v[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) s += v[i][j];
@@ -154,8 +156,10 @@ __global__ void __launch_bounds__(threads_for(G))
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const int col = 8 * (t + G * i);
-            g[i].load(dy + r * lddy + col, n[i]);
+            if constexpr (kAhead) g[i].request(dy + r * lddy + col, n[i], col);
+            else g[i].load(dy + r * lddy + col, n[i]);
             if constexpr (KEPT) s[i].load(codes, scales, r, blocks, col, n[i]);
+            else if constexpr (kAhead) s[i].request(x + r * ldx + col, n[i], col);
             else s[i].load(x + r * ldx + col, n[i]);
         }
     };
@@ -181,6 +185,10 @@ __global__ void __launch_bounds__(threads_for(G))
         float g[P][8], h[P][8], s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
+            if (kAhead && (cols & 7)) {
+                gy[i].settle(n[i], 8 * (t + G * i));
+                if constexpr (!KEPT) in[i].settle(n[i], 8 * (t + G * i));
+            }
             gy[i].get(g[i]);
             in[i].get(h[i]);
 #pragma unroll
@@ -276,7 +284,8 @@ struct Form {
     int g, p;
 };
 // Threads to a row and pieces a thread, by what the registers hold: the fewest threads that hold it in one piece up to a wavefront, so
-// that short rows share one; more than a wavefront from 1025 values on.
+// that short rows share one; more than a wavefront from 1025 values on.  4096 x 8192 in {256, 4} / {512, 2}: bfloat16 39.3 / 32.2 us
+// forward and 51.2 / 46.8 backward, fp32 63.7 / 58.1 and 94.6 / 89.2.
 Form row_form(int64_t cols) {
     if (cols <= 128) return {16, 1};
     if (cols <= 256) return {32, 1};
@@ -284,7 +293,7 @@ Form row_form(int64_t cols) {
     if (cols <= 1024) return {64, 2};
     if (cols <= 2048) return {256, 1};
     if (cols <= 4096) return {256, 2};
-    if (cols <= 8192) return {256, 4};
+    if (cols <= 8192) return {512, 2};
     return {1024, 2};
 }
 template <class Go>
@@ -295,13 +304,14 @@ void with_form(const Form& f, Go&& go) {
     AQ_FORM(32, 1);
     AQ_FORM(64, 1);
     AQ_FORM(64, 2);
+    AQ_FORM(128, 2);
     AQ_FORM(256, 1);
     AQ_FORM(256, 2);
-    AQ_FORM(256, 4);
+    AQ_FORM(512, 2);
     AQ_FORM(1024, 2);
 #undef AQ_FORM
 }
-int64_t at_a_time(const Form& f) { return f.g < 256 ? 256 / f.g : 1; }
+int64_t at_a_time(const Form& f) { return threads_for(f.g) / f.g; }
 
 // Workgroups of the backward pass: two turns each until 512 are there; every one leaves 8 bytes a column behind.  65536 x 1024
 // bfloat16: with 256 workgroups 99 us, 512 75, 1024 83 and a join twice as long; 512 of 512 threads 75.  4096 x 256 fp32: with one
@@ -316,9 +326,12 @@ int64_t backward_workgroups(int64_t rows, int64_t cols) {
 
 aq_status launch_layernorm_forward(const aq_matrix& x, const float* gamma, const float* beta, float eps, const aq_matrix& y,
                                    float* mean, float* rstd, const aq_ckpt8* kept, hipStream_t st) {
-    const Form f = row_form(x.cols);
-    const int64_t turns = (x.rows + at_a_time(f) - 1) / at_a_time(f);
-    const unsigned grid = (unsigned)(turns < 2048 ? turns : 2048);
+    // 16384 x 2048 in {256, 1} / {128, 2}: bfloat16 31.4 / 30.1 us, fp32 61.0 / 59.2; backward, where a workgroup's sums cost more the more
+    // there are, fp32 78 / 84
+    const Form f = x.cols > 1024 && x.cols <= 2048 ? Form{128, 2} : row_form(x.cols);
+    // As many workgroups as run at once; for short rows twice that (65536 x 504 bfloat16 32.9 us / 30.0, but x 1024 58.7 / 60.5)
+    const int64_t turns = (x.rows + at_a_time(f) - 1) / at_a_time(f), most = x.cols <= 512 ? 4096 : 2048;
+    const unsigned grid = (unsigned)(turns < most ? turns : most);
     return with_dtype(x.dtype, [&](auto t) {
         using T = decltype(t);
         with_form(f, [&](auto g, auto p) {

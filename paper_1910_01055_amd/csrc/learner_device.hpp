@@ -48,6 +48,36 @@ struct Piece {
         zero();
         if (n > 0) load_some(p, n);
     }
+    // The same of a row that has `before` values in front of these, to be settled before use: 16-bit values that a row ends among
+    // come as its last eight, in one load that nothing waits for (value by value LayerNorm's gradients of 65536 x 501 took 71 us
+    // for 59).
+    __device__ __forceinline__ void request(const T* __restrict__ p, int n, int before) {
+        if (n >= 8) {
+            load_all(p);
+        } else if (sizeof(T) == 2 && n > 0 && before + n >= 8) {
+            load_all(p - (8 - n));
+        } else {
+            zero();
+            if (n > 0) load_some(p, n);
+        }
+    }
+    __device__ __forceinline__ void settle(int n, int before) {
+        if constexpr (sizeof(T) == 2) {
+            if (n > 0 && n < 8 && before + n >= 8) {
+                const int skip = 8 - n;
+                if (skip & 4) {
+                    w[0] = w[2], w[1] = w[3], w[2] = 0, w[3] = 0;
+                }
+                if (skip & 2) {
+                    w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = 0;
+                }
+                if (skip & 1) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_alignbit(i < 3 ? w[i < 3 ? i + 1 : 0] : 0, w[i], 16);
+                }
+            }
+        }
+    }
     __device__ __forceinline__ void load_some(const T* __restrict__ p, int n) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
