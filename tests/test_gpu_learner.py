@@ -182,7 +182,8 @@ def test_block_formats(rows, cols, kind):
 # ---- LayerNorm
 
 LN_SHAPES = [(1, 1), (5, 1), (3, 2), (17, 31), (40, 128), (9, 129), (300, 256), (11, 257), (130, 512), (6, 513), (70, 777), (33, 1024), (5, 1025),
-             (9, 2048), (3, 2049), (4, 4097), (2, 8192), (3, 8193), (2, 16384), (1, 256), (3000, 64)]
+             (9, 2048), (3, 2049), (4, 4097), (2, 8192), (3, 8193), (2, 16384), (1, 256), (3000, 64),
+             (2100, 1501), (1100, 5003), (16500, 301), (600, 8205)]  # more rows than run at once, that end inside a piece
 
 
 def ln_inputs(rows, cols, kind, *key):
