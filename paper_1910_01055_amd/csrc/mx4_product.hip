@@ -307,7 +307,7 @@ Blocks blocks_of(const aq_mx4& q) { return {(const uint8_t*)q.d_codes, q.d_scale
 //         512        2048 x 2048 bfloat16 5.7 / 9.1, 4096 x 4096 fp32 10.1 / 13.2, 1024 x 8192 18.4 / 21.8
 //         1024       512 x 3136 bfloat16 9.7 / 13.1, fp32 15.0 / 13.2;  2048 x 2048 bfloat16 8.5 / 9.2, fp32 10.2 / 9.5
 //         1536       1024 x 1024 bfloat16 7.0 / 7.4, fp32 8.4 / 7.6
-//         2048       256 x 256 fp32 5.5 / 6.9;  1024 x 512 fp32 6.5 / 6.6, 3072 tiles of bfloat16 7.6 / 6.5
+//         2048       256 x 256 fp32 5.5 / 6.9;  1024 x 512 fp32 6.5 / 6.6 (bfloat16, half as many again, 7.6 / 6.5)
 // Blocks: 512 tiles  2048 x 2048 5.7 / 5.8, 512 x 3136 5.8 / 7.8, 1024 x 8192 16.4 / 13.7;  1024  1024 x 512 3.8 / 4.0, 2048 x 2048 9.4 / 5.8
 //         2048       256 x 256 4.1 / 4.2, 1024 x 512 5.4 / 4.0
 bool few_rows(int64_t rows, int64_t n, int64_t row_bytes, bool values) {
