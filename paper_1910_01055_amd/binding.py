@@ -485,6 +485,20 @@ class Mx4(_Blocks):
     CODE_BYTES = 16
 
 
+def _kept(q):
+    """A Ckpt8 as an aq_ckpt8; whatever else would be taken for one of its sizes."""
+    if not isinstance(q, Ckpt8):
+        raise ValueError("an 8-bit checkpoint is a Ckpt8")
+    return q._c
+
+
+def _mx4(q):
+    """An Mx4 as an aq_mx4."""
+    if not isinstance(q, Mx4):
+        raise ValueError("a 4-bit tensor is an Mx4")
+    return q._c
+
+
 def _blocks_empty(kind, code_type, rows, cols, device):
     import torch
     b = (int(cols) + 31) // 32
@@ -528,52 +542,52 @@ def layernorm_forward(x, gamma, beta, eps, y, mean=None, rstd=None, kept=None):
     """y = LayerNorm(x); kept: a Ckpt8 that receives x."""
     rows, cols = x.shape
     _check(load().aq_layernorm_forward(_matrix(x), _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), float(eps), _matrix(y),
-                                       _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), kept and kept._c, _stream()),
+                                       _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), None if kept is None else _kept(kept), _stream()),
            "aq_layernorm_forward")
 
 
 def layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace=None):
     """x: the forward pass's input, or its Ckpt8."""
     rows, cols = dy.shape
-    kept = x if isinstance(x, Ckpt8) else None
-    _check(load().aq_layernorm_backward(_matrix(dy), None if kept else _matrix(x), kept and kept._c, _vector(gamma, cols, "gamma"),
+    blocks = isinstance(x, _Blocks)
+    _check(load().aq_layernorm_backward(_matrix(dy), None if blocks else _matrix(x), _kept(x) if blocks else None, _vector(gamma, cols, "gamma"),
                                         _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), _matrix(dx),
                                         _vector(dgamma, cols, "dgamma"), _vector(dbeta, cols, "dbeta"), _ptr(workspace),
                                         _bytes(workspace), _stream()), "aq_layernorm_backward")
 
 
 def ckpt8_pack(x, kept):
-    _check(load().aq_ckpt8_pack(_matrix(x), kept._c, _stream()), "aq_ckpt8_pack")
+    _check(load().aq_ckpt8_pack(_matrix(x), _kept(kept), _stream()), "aq_ckpt8_pack")
 
 
 def ckpt8_unpack(kept, x):
-    _check(load().aq_ckpt8_unpack(kept._c, _matrix(x), _stream()), "aq_ckpt8_unpack")
+    _check(load().aq_ckpt8_unpack(_kept(kept), _matrix(x), _stream()), "aq_ckpt8_unpack")
 
 
 def ckpt8_weight_grad(dy, kept, dw, db=None, workspace=None):
-    _check(load().aq_ckpt8_weight_grad(_matrix(dy), kept._c, _matrix(dw), _vector(db, dy.shape[1], "db"), _ptr(workspace),
+    _check(load().aq_ckpt8_weight_grad(_matrix(dy), _kept(kept), _matrix(dw), _vector(db, dy.shape[1], "db"), _ptr(workspace),
                                        _bytes(workspace), _stream()), "aq_ckpt8_weight_grad")
 
 
 def mx4_quantize(x, q):
-    _check(load().aq_mx4_quantize(_matrix(x), q._c, _stream()), "aq_mx4_quantize")
+    _check(load().aq_mx4_quantize(_matrix(x), _mx4(q), _stream()), "aq_mx4_quantize")
 
 
 def mx4_dequantize(q, x):
-    _check(load().aq_mx4_dequantize(q._c, _matrix(x), _stream()), "aq_mx4_dequantize")
+    _check(load().aq_mx4_dequantize(_mx4(q), _matrix(x), _stream()), "aq_mx4_dequantize")
 
 
 def mx4_linear(x, w, bias, y, workspace=None):
     """y = Q(x) w^T + bias; w: Mx4 [n][k]."""
-    _check(load().aq_mx4_linear(_matrix(x), w._c, _vector(bias, w.rows, "bias"), _matrix(y), _ptr(workspace), _bytes(workspace), _stream()),
+    _check(load().aq_mx4_linear(_matrix(x), _mx4(w), _vector(bias, w.rows, "bias"), _matrix(y), _ptr(workspace), _bytes(workspace), _stream()),
            "aq_mx4_linear")
 
 
 def mx4_matmul(x, w, bias, y):
     """The same from an Mx4 x."""
-    _check(load().aq_mx4_matmul(x._c, w._c, _vector(bias, w.rows, "bias"), _matrix(y), _stream()), "aq_mx4_matmul")
+    _check(load().aq_mx4_matmul(_mx4(x), _mx4(w), _vector(bias, w.rows, "bias"), _matrix(y), _stream()), "aq_mx4_matmul")
 
 
 def mx4_input_grad(dy, w, dx, workspace=None):
     """dx = dy w; w: Mx4 [n][k]."""
-    _check(load().aq_mx4_input_grad(_matrix(dy), w._c, _matrix(dx), _ptr(workspace), _bytes(workspace), _stream()), "aq_mx4_input_grad")
+    _check(load().aq_mx4_input_grad(_matrix(dy), _mx4(w), _matrix(dx), _ptr(workspace), _bytes(workspace), _stream()), "aq_mx4_input_grad")
