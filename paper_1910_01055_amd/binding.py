@@ -71,8 +71,8 @@ class AqBlocks(C.Structure):
 
 
 # The same as bytes, a third of the time of a Structure's construction and conversion (0.7 against 1.05 us a matrix; a small
-# LayerNorm's two passes take five).
-_pack_matrix = struct.Struct("PqqqiI").pack
+# LayerNorm's two passes take five).  (The type as 64 bits: it and the padding behind it.)
+_pack_matrix = struct.Struct("Pqqqq").pack
 _pack_blocks = struct.Struct("PPqq").pack
 
 
@@ -418,6 +418,8 @@ def quantize_tensor(w, rows, cols, wscheme, qdenom, codes, scale, zp, workspace)
 
 # ---- the learner's operators.  Matrices are two-dimensional device tensors whose rows are contiguous (any distance between rows);
 # vectors are contiguous fp32 tensors; `workspace` is a uint8 tensor of the size that the matching *_workspace call gives (None for 0).
+# Tensors in ordinary host memory, whose addresses fault the GPU, are refused: 0.05 us a tensor, which the calls save where they ask less of
+# Python otherwise (`_lib or load()`).
 
 _DTYPES = {}
 _F32 = None
@@ -430,34 +432,50 @@ def _learn_dtypes():
     _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
 
 
+def _reachable(*tensors):
+    """Refuses tensors that the GPU does not reach (callers ask is_cuda first; this is for pinned memory and the refusal)."""
+    for t in tensors:
+        if not t.is_cuda and t.numel() and not t.is_pinned():
+            raise ValueError("a tensor lies in host memory that the GPU does not reach")
+
+
 def _matrix(t):
     """A tensor as an aq_matrix."""
-    if _F32 is None:
-        _learn_dtypes()
     try:
         rows, cols = t.shape
         dtype = _DTYPES[t.dtype]
     except (ValueError, KeyError):
+        if _F32 is None:
+            _learn_dtypes()
+            return _matrix(t)
         raise ValueError("a matrix is a two-dimensional tensor of float32, float16 or bfloat16") from None
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("the values of a row are contiguous")
-    return _pack_matrix(t.data_ptr(), rows, cols, ld if rows > 1 else cols, dtype, 0)
+    return _pack_matrix(t.data_ptr(), rows, cols, ld if rows > 1 else cols, dtype)
 
 
 def _vector(t, n, what):
     """A contiguous fp32 vector of n values as a pointer; None stays None."""
     if t is None:
         return None
-    if _F32 is None:
-        _learn_dtypes()
     if t.dtype is not _F32 or t.numel() != n or not t.is_contiguous():
+        if _F32 is None:
+            _learn_dtypes()
+            return _vector(t, n, what)
         raise ValueError(f"{what} is a contiguous float32 tensor of {n} values")
+    if not t.is_cuda:
+        _reachable(t)
     return t.data_ptr()
 
 
 def _bytes(workspace):
-    return 0 if workspace is None else workspace.nbytes
+    """The size of a workspace."""
+    if workspace is None:
+        return 0
+    if not workspace.is_cuda:
+        _reachable(workspace)
+    return workspace.nbytes
 
 
 class _Blocks:
@@ -473,6 +491,7 @@ class _Blocks:
             raise ValueError("codes and scales are contiguous tensors of bytes")
         self.codes, self.scales, self.rows, self.cols = codes, scales, rows, int(cols)
         self._c = _pack_blocks(codes.data_ptr(), scales.data_ptr(), rows, int(cols))
+        self._near = codes.is_cuda and scales.is_cuda
 
 
 class Ckpt8(_Blocks):
@@ -489,6 +508,8 @@ def _kept(q):
     """A Ckpt8 as an aq_ckpt8; whatever else would be taken for one of its sizes."""
     if not isinstance(q, Ckpt8):
         raise ValueError("an 8-bit checkpoint is a Ckpt8")
+    if not q._near:
+        _reachable(q.codes, q.scales)
     return q._c
 
 
@@ -496,6 +517,8 @@ def _mx4(q):
     """An Mx4 as an aq_mx4."""
     if not isinstance(q, Mx4):
         raise ValueError("a 4-bit tensor is an Mx4")
+    if not q._near:
+        _reachable(q.codes, q.scales)
     return q._c
 
 
@@ -541,7 +564,9 @@ def mx4_input_grad_workspace(rows, n, k):
 def layernorm_forward(x, gamma, beta, eps, y, mean=None, rstd=None, kept=None):
     """y = LayerNorm(x); kept: a Ckpt8 that receives x."""
     rows, cols = x.shape
-    _check(load().aq_layernorm_forward(_matrix(x), _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), float(eps), _matrix(y),
+    if not (x.is_cuda and y.is_cuda):
+        _reachable(x, y)
+    _check((_lib or load()).aq_layernorm_forward(_matrix(x), _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, _matrix(y),
                                        _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), None if kept is None else _kept(kept), _stream()),
            "aq_layernorm_forward")
 
@@ -550,44 +575,62 @@ def layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace=No
     """x: the forward pass's input, or its Ckpt8."""
     rows, cols = dy.shape
     blocks = isinstance(x, _Blocks)
-    _check(load().aq_layernorm_backward(_matrix(dy), None if blocks else _matrix(x), _kept(x) if blocks else None, _vector(gamma, cols, "gamma"),
+    if not (dy.is_cuda and dx.is_cuda and (blocks or x.is_cuda)):
+        _reachable(dy, dx, dy if blocks else x)
+    _check((_lib or load()).aq_layernorm_backward(_matrix(dy), None if blocks else _matrix(x), _kept(x) if blocks else None, _vector(gamma, cols, "gamma"),
                                         _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), _matrix(dx),
-                                        _vector(dgamma, cols, "dgamma"), _vector(dbeta, cols, "dbeta"), _ptr(workspace),
-                                        _bytes(workspace), _stream()), "aq_layernorm_backward")
+                                        _vector(dgamma, cols, "dgamma"), _vector(dbeta, cols, "dbeta"), _ptr(workspace), _bytes(workspace), _stream()),
+           "aq_layernorm_backward")
 
 
 def ckpt8_pack(x, kept):
-    _check(load().aq_ckpt8_pack(_matrix(x), _kept(kept), _stream()), "aq_ckpt8_pack")
+    if not x.is_cuda:
+        _reachable(x)
+    _check((_lib or load()).aq_ckpt8_pack(_matrix(x), _kept(kept), _stream()), "aq_ckpt8_pack")
 
 
 def ckpt8_unpack(kept, x):
-    _check(load().aq_ckpt8_unpack(_kept(kept), _matrix(x), _stream()), "aq_ckpt8_unpack")
+    if not x.is_cuda:
+        _reachable(x)
+    _check((_lib or load()).aq_ckpt8_unpack(_kept(kept), _matrix(x), _stream()), "aq_ckpt8_unpack")
 
 
 def ckpt8_weight_grad(dy, kept, dw, db=None, workspace=None):
-    _check(load().aq_ckpt8_weight_grad(_matrix(dy), _kept(kept), _matrix(dw), _vector(db, dy.shape[1], "db"), _ptr(workspace),
-                                       _bytes(workspace), _stream()), "aq_ckpt8_weight_grad")
+    if not (dy.is_cuda and dw.is_cuda):
+        _reachable(dy, dw)
+    _check((_lib or load()).aq_ckpt8_weight_grad(_matrix(dy), _kept(kept), _matrix(dw), _vector(db, dy.shape[1], "db"), _ptr(workspace), _bytes(workspace), _stream()),
+           "aq_ckpt8_weight_grad")
 
 
 def mx4_quantize(x, q):
-    _check(load().aq_mx4_quantize(_matrix(x), _mx4(q), _stream()), "aq_mx4_quantize")
+    if not x.is_cuda:
+        _reachable(x)
+    _check((_lib or load()).aq_mx4_quantize(_matrix(x), _mx4(q), _stream()), "aq_mx4_quantize")
 
 
 def mx4_dequantize(q, x):
-    _check(load().aq_mx4_dequantize(_mx4(q), _matrix(x), _stream()), "aq_mx4_dequantize")
+    if not x.is_cuda:
+        _reachable(x)
+    _check((_lib or load()).aq_mx4_dequantize(_mx4(q), _matrix(x), _stream()), "aq_mx4_dequantize")
 
 
 def mx4_linear(x, w, bias, y, workspace=None):
     """y = Q(x) w^T + bias; w: Mx4 [n][k]."""
-    _check(load().aq_mx4_linear(_matrix(x), _mx4(w), _vector(bias, w.rows, "bias"), _matrix(y), _ptr(workspace), _bytes(workspace), _stream()),
+    if not (x.is_cuda and y.is_cuda):
+        _reachable(x, y)
+    _check((_lib or load()).aq_mx4_linear(_matrix(x), _mx4(w), _vector(bias, w.rows, "bias"), _matrix(y), _ptr(workspace), _bytes(workspace), _stream()),
            "aq_mx4_linear")
 
 
 def mx4_matmul(x, w, bias, y):
     """The same from an Mx4 x."""
-    _check(load().aq_mx4_matmul(_mx4(x), _mx4(w), _vector(bias, w.rows, "bias"), _matrix(y), _stream()), "aq_mx4_matmul")
+    if not y.is_cuda:
+        _reachable(y)
+    _check((_lib or load()).aq_mx4_matmul(_mx4(x), _mx4(w), _vector(bias, w.rows, "bias"), _matrix(y), _stream()), "aq_mx4_matmul")
 
 
 def mx4_input_grad(dy, w, dx, workspace=None):
     """dx = dy w; w: Mx4 [n][k]."""
-    _check(load().aq_mx4_input_grad(_matrix(dy), _mx4(w), _matrix(dx), _ptr(workspace), _bytes(workspace), _stream()), "aq_mx4_input_grad")
+    if not (dy.is_cuda and dx.is_cuda):
+        _reachable(dy, dx)
+    _check((_lib or load()).aq_mx4_input_grad(_matrix(dy), _mx4(w), _matrix(dx), _ptr(workspace), _bytes(workspace), _stream()), "aq_mx4_input_grad")

@@ -16,11 +16,22 @@ class Library:
         return lambda *args: self.calls.append(name) or B.OK
 
 
+class Near(torch.Tensor):
+    """Host memory that passes for the GPU's."""
+    is_cuda = True
+
+
+class Pinned(torch.Tensor):
+    def is_pinned(self):
+        return True
+
+
 @pytest.fixture
 def lib(monkeypatch):
     library = Library()
-    monkeypatch.setattr(B, "load", lambda: library)
+    monkeypatch.setattr(B, "_lib", library)
     monkeypatch.setattr(B, "_stream", lambda: 0)
+    monkeypatch.setattr(B, "_reachable", lambda *tensors: None, raising=False)
     return library
 
 
@@ -71,3 +82,52 @@ def test_each_call_takes_its_own_kind_of_blocks(lib):
                 with pytest.raises(ValueError, match="8-bit checkpoint|4-bit tensor"):
                     call()
                 assert not lib.calls, name
+
+
+def test_tensors_in_host_memory_are_refused(monkeypatch):
+    """A kernel that is handed the address of ordinary host memory faults the GPU.  Pinned memory, which the GPU reaches, is taken."""
+    library = Library()
+    monkeypatch.setattr(B, "_lib", library)
+    monkeypatch.setattr(B, "_stream", lambda: 0)
+    near, far = Near, torch.Tensor
+
+    def tensors(kind, host=None):
+        """Operands of `kind`, the one called `host` in ordinary memory."""
+        def make(name, *shape, dtype=torch.float32):
+            t = torch.zeros(shape, dtype=dtype)
+            return t.as_subclass(far if name == host else kind)
+
+        def blocked(name, of, rows, cols, code_type):
+            b = (cols + 31) // 32
+            return of(make(name + " codes", rows, of.CODE_BYTES * b, dtype=code_type), make(name + " scales", rows, b, dtype=torch.uint8), cols)
+
+        t = {n: make(n, ROWS, K) for n in ("x", "dx", "out")}
+        t.update({n: make(n, ROWS, N) for n in ("y", "dy")})
+        t.update({n: make(n, K) for n in ("gamma", "beta", "dgamma", "dbeta")})
+        t.update({n: make(n, ROWS) for n in ("mean", "rstd")})
+        t.update(dw=make("dw", N, K), db=make("db", N), bias=make("bias", N), ws=make("ws", 64, dtype=torch.uint8),
+                 kept=blocked("kept", B.Ckpt8, ROWS, K, torch.int8), q=blocked("q", B.Mx4, ROWS, K, torch.uint8), w=blocked("w", B.Mx4, N, K, torch.uint8))
+        return t
+
+    taken = {"ln forward": (lambda t: B.layernorm_forward(t["x"], t["gamma"], t["beta"], 1e-5, t["out"], t["mean"], t["rstd"], t["kept"]),
+                            "x gamma beta out mean rstd kept"),
+             "ln backward": (lambda t: B.layernorm_backward(t["dx"], t["x"], t["gamma"], t["mean"], t["rstd"], t["out"], t["dgamma"], t["dbeta"], t["ws"]),
+                             "dx x gamma mean rstd out dgamma dbeta ws"),
+             "ln backward of a checkpoint": (lambda t: B.layernorm_backward(t["dx"], t["kept"], None, t["mean"], t["rstd"], t["out"], None, None), "kept"),
+             "pack": (lambda t: B.ckpt8_pack(t["x"], t["kept"]), "x kept"),
+             "unpack": (lambda t: B.ckpt8_unpack(t["kept"], t["x"]), "x kept"),
+             "weight grad": (lambda t: B.ckpt8_weight_grad(t["dy"], t["kept"], t["dw"], t["db"], t["ws"]), "dy kept dw db ws"),
+             "quantize": (lambda t: B.mx4_quantize(t["x"], t["q"]), "x q"),
+             "dequantize": (lambda t: B.mx4_dequantize(t["q"], t["x"]), "x q"),
+             "linear": (lambda t: B.mx4_linear(t["x"], t["w"], t["bias"], t["y"], t["ws"]), "x w bias y ws"),
+             "matmul": (lambda t: B.mx4_matmul(t["q"], t["w"], t["bias"], t["y"]), "q w bias y"),
+             "input grad": (lambda t: B.mx4_input_grad(t["dy"], t["w"], t["out"], t["ws"]), "dy w out ws")}
+    for name, (call, reads) in taken.items():
+        for kind in (Near, Pinned):
+            call(tensors(kind))
+            assert len(library.calls) == 1 and library.calls.pop(), name
+        for host in reads.split():
+            for part in ((host + " codes", host + " scales") if host in ("kept", "q", "w") else (host,)):
+                with pytest.raises(ValueError, match="GPU"):
+                    call(tensors(near, part))
+                assert not library.calls, (name, part)
