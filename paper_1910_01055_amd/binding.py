@@ -473,6 +473,8 @@ def _bytes(workspace):
     """The size of a workspace."""
     if workspace is None:
         return 0
+    if not workspace.is_contiguous():  # (a tensor that repeats values has fewer bytes than it counts)
+        raise ValueError("a workspace is contiguous")
     if not workspace.is_cuda:
         _reachable(workspace)
     return workspace.nbytes

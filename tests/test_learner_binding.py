@@ -131,3 +131,13 @@ def test_tensors_in_host_memory_are_refused(monkeypatch):
                 with pytest.raises(ValueError, match="GPU"):
                     call(tensors(near, part))
                 assert not library.calls, (name, part)
+
+
+def test_scratch_is_as_large_as_it_says(lib):
+    """A workspace that repeats one value has fewer bytes than its size tells."""
+    x, y, kept, q, w, w8 = operands()
+    with pytest.raises(ValueError):
+        B.mx4_linear(x, w, None, y, torch.zeros(1, dtype=torch.uint8).expand(4096))
+    assert not lib.calls
+    B.mx4_linear(x, w, None, y, torch.zeros(4096, dtype=torch.uint8))
+    assert lib.calls == ["aq_mx4_linear"]
