@@ -491,9 +491,11 @@ class _Blocks:
             raise ValueError(f"codes are [rows][{self.CODE_BYTES} B] and scales [rows][B], B = ceil(cols / 32)")
         if scales.dtype != torch.uint8 or codes.element_size() != 1 or not codes.is_contiguous() or not scales.is_contiguous():
             raise ValueError("codes and scales are contiguous tensors of bytes")
-        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, int(cols)
-        self._c = _pack_blocks(codes.data_ptr(), scales.data_ptr(), rows, int(cols))
-        self._near = codes.is_cuda and scales.is_cuda
+        self.__dict__.update(codes=codes, scales=scales, rows=rows, cols=int(cols), _near=codes.is_cuda and scales.is_cuda,
+                             _c=_pack_blocks(codes.data_ptr(), scales.data_ptr(), rows, int(cols)))
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name}: blocks of other tensors are made anew, as calls are handed these tensors' addresses")
 
 
 class Ckpt8(_Blocks):

@@ -141,3 +141,14 @@ def test_scratch_is_as_large_as_it_says(lib):
     assert not lib.calls
     B.mx4_linear(x, w, None, y, torch.zeros(4096, dtype=torch.uint8))
     assert lib.calls == ["aq_mx4_linear"]
+
+
+def test_blocks_keep_their_tensors():
+    """Calls go to the tensors that blocks were made of: others cannot be put in their place behind the address that is handed on."""
+    for make in (B.ckpt8_empty, B.mx4_empty):
+        q = blocks(make, ROWS, K)
+        for name, value in (("codes", torch.zeros_like(q.codes)), ("scales", torch.zeros_like(q.scales)), ("rows", ROWS + 1), ("cols", K + 1)):
+            before = getattr(q, name)
+            with pytest.raises(AttributeError):
+                setattr(q, name, value)
+            assert getattr(q, name) is before
