@@ -6,6 +6,7 @@ on the library's learner's operators:
 
   forward   y = Q4(x) W4^T + b on microscaled 4-bit floats; LayerNorm; what the backward pass needs is kept in 8 bits
   backward  the weights' gradients from the 8-bit checkpoints, the inputs' through the 4-bit weights, LayerNorm's from its checkpoint
+            (a ReLU's mask is that of its input, in full)
 
 The weights themselves, their updates (Adam) and what is element by element (tanh, ReLU, the loss) are torch's, in fp32.  In the
 end the student acts for one observation at a time on its 4-bit layers, and is handed to the 8-bit actor as any policy is.
@@ -62,15 +63,14 @@ class Layer:
 
     def backward(self, dy, kept_out, first):
         """dy: the gradient of what forward returned, which the next layer keeps as `kept_out`."""
-        if self.act != "none":
+        if self.act == "relu":  # (of z itself: small positive values are zeros in a checkpoint)
+            dy = dy * (self.z > 0)
+        elif self.act == "ln_tanh":
             h = torch.empty_like(self.z)
             aq.ckpt8_unpack(kept_out, h)
-            if self.act == "relu":
-                dy = dy * (h > 0)
-            else:
-                dn = dy * (1 - h * h)
-                aq.layernorm_backward(dn, self.kept_z, self.gamma, self.mean, self.rstd, self.dz, self.dgamma, self.dbeta, self.ws)
-                dy = self.dz
+            dn = dy * (1 - h * h)
+            aq.layernorm_backward(dn, self.kept_z, self.gamma, self.mean, self.rstd, self.dz, self.dgamma, self.dbeta, self.ws)
+            dy = self.dz
         aq.ckpt8_weight_grad(dy, self.kept_in, self.dw, self.db, self.ws)
         if first:
             return None
