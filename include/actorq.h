@@ -405,7 +405,7 @@ aq_status aq_policy_forward_fp16(aq_policy* p, const void* d_obs, int64_t batch,
  * AQ_EINVAL: a NULL argument that is not said to be optional, a negative size, ld < cols, an unknown type, an
  * address that is no multiple of its element's size, a workspace that is too small.  AQ_ESHAPE: operands
  * whose sizes or types do not go together, no columns, or beyond the limits: rows < 2^31, columns <= 2^20, ld <= 2^21
- * (256 rows lie within 2 GiB), and what a call states. */
+ * (256 rows lie within 2 GiB), results of products of fewer than 2^23 tiles of 256 x 256, and what a call states. */
 typedef enum { AQ_F32 = 0, AQ_F16 = 1, AQ_BF16 = 2 } aq_dtype;
 typedef struct {
     void* d;

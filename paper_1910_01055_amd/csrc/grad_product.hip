@@ -479,11 +479,14 @@ __global__ void __launch_bounds__(H * tile_threads(S), 1)
     }
 }
 
+constexpr int kJoinThreads = 256;
+constexpr int64_t kMostThreads = 0xffffffffLL;  // of a launch
+
 // the slices' results join, in their order, and are rounded; dy's sums behind them
 template <class T>
-__global__ void __launch_bounds__(256) k_grad_join(const float* __restrict__ part, int slices, int64_t m, int64_t c, T* __restrict__ out,
+__global__ void __launch_bounds__(kJoinThreads) k_grad_join(const float* __restrict__ part, int slices, int64_t m, int64_t c, T* __restrict__ out,
                                                    int64_t ld, const float* __restrict__ part_sums, float* __restrict__ sums) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t i = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
     auto total = [slices](const float* p, int64_t step) __attribute__((always_inline)) {
         float s = 0.0f;
         int k = 0;
@@ -536,11 +539,12 @@ Plans plans(int64_t m, int64_t c, int64_t t) {
     Plans best{{none, none, none}, 1};
     float least[3] = {3.0e38f, 3.0e38f, 3.0e38f};
     for (const Kind& k : kinds) {
-        const int64_t tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + k.s - 1) / k.s);
+        const int64_t tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + k.s - 1) / k.s), threads = k.h * tile_threads(k.s);
         for (int32_t want = k.h; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
             const int32_t chunks = ((all + want - 1) / want + 1) & ~1, z = chunks ? (all + chunks * k.h - 1) / (chunks * k.h) : 1;
             // (256 CUs; the last turn is as long as a whole one)
             const int64_t wgs = tiles * z, busy = wgs <= 256 ? wgs : (wgs + 255) / 256 * 256;
+            if (wgs * threads > kMostThreads || (z > 1 && m * c + m > kMostThreads - kJoinThreads)) continue;  // (no launch holds them)
             const float join = z > 1 ? 2.3f + 0.02f * (float)z + (float)(z * m * c * 4) * (1.0f / 3.5e6f) : 0.0f;
             for (int i = 0; i < 3; ++i) {
                 const auto& cost = k.cost[i];
@@ -585,9 +589,7 @@ aq_status launch(const A& a, const B& b, T* out, int64_t ld, int64_t stride, flo
 template <class T>
 aq_status join(const float* part, const Plan& p, int64_t m, int64_t c, T* out, int64_t ld, const float* part_sums, float* sums,
                hipStream_t st) {
-    const int64_t g = (m * c + m + 255) / 256;
-    if (!grid_ok(g, 256)) return AQ_ESHAPE;
-    k_grad_join<T><<<(unsigned)g, 256, 0, st>>>(part, p.z, m, c, out, ld, part_sums, sums);
+    k_grad_join<T><<<(unsigned)((m * c + m + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, st>>>(part, p.z, m, c, out, ld, part_sums, sums);
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }
 template <class Go>

@@ -316,6 +316,14 @@ bool few_rows(int64_t rows, int64_t n, int64_t row_bytes, bool values) {
     return tiles <= 256 || row_bytes + 400 <= 1050000 / tiles;
 }
 
+int64_t tiles_of(int64_t rows, int64_t n, int64_t side) { return ((rows + side - 1) / side) * ((n + side - 1) / side); }
+// The largest tiles that give every CU one; 0 where no launch holds them.  us on tiles of 64 / 128 / 256: 2048 x 2048, 2048 rows
+// 13.3 / 11.7 / 19.0, 8192 rows 42.9 / 31.4 / 25.5; 4096 x 4096, 1024 rows 22.1 / 17.3 / 30.7; 1024 x 1024, 2048 rows 6.2 / 8.0 / 12.3.
+int tile_side(int64_t rows, int64_t n) {
+    if (tiles_of(rows, n, 256) >= 256) return grid_ok(tiles_of(rows, n, 256), tile_threads(256)) ? 256 : 0;
+    return tiles_of(rows, n, 128) >= 256 ? 128 : 64;
+}
+
 template <class X, class T>
 aq_status launch_rows(const X& x, int64_t rows, const aq_mx4& w, const float* bias, const aq_matrix& y, hipStream_t st) {
     const dim3 grid((unsigned)((w.rows + 15) / 16), (unsigned)((rows + 15) / 16));
@@ -326,13 +334,11 @@ aq_status launch_rows(const X& x, int64_t rows, const aq_mx4& w, const float* bi
 template <class T, int S>
 aq_status launch_tiles(const aq_mx4& x, const aq_mx4& w, const float* bias, const aq_matrix& y, hipStream_t st) {
     constexpr int kLds = 2 * 2 * S * 128 + 8 * 2 * S * 4;
-    const int64_t tiles = ((x.rows + S - 1) / S) * ((w.rows + S - 1) / S);
-    if (!grid_ok(tiles, 512)) return AQ_ESHAPE;
     constexpr int NT = tile_threads(S);
     auto* const k = k_mx4_tiles<T, S, NT>;
     if (!allow_lds<Blocks, T, std::integral_constant<int, S>>((const void*)k, kLds)) return AQ_EHIP;
-    k<<<(unsigned)tiles, NT, kLds, st>>>(blocks_of(x), blocks_of(w), bias, (T*)y.d, y.ld, (int)x.rows, (int)w.rows,
-                                                      (int)blocks32(w.cols));
+    k<<<(unsigned)tiles_of(x.rows, w.rows, S), NT, kLds, st>>>(blocks_of(x), blocks_of(w), bias, (T*)y.d, y.ld, (int)x.rows, (int)w.rows,
+                                                               (int)blocks32(w.cols));
     return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
 }
 
@@ -348,12 +354,12 @@ aq_status launch_mx4_matmul(const aq_mx4& x, const aq_mx4& w, const float* bias,
     return with_dtype(y.dtype, [&](auto t) {
         using T = decltype(t);
         if (few_rows(x.rows, w.rows, 16 * blocks32(x.cols), false)) return launch_rows<Blocks, T>(blocks_of(x), x.rows, w, bias, y, st);
-        // The largest tiles that give every CU one.  us on tiles of 64 / 128 / 256: 2048 x 2048, 2048 rows 13.3 / 11.7 / 19.0, 8192 rows
-        // 42.9 / 31.4 / 25.5; 4096 x 4096, 1024 rows 22.1 / 17.3 / 30.7; 1024 x 1024, 2048 rows 6.2 / 8.0 / 12.3.
-        auto tiles = [&](int64_t s) { return ((x.rows + s - 1) / s) * ((w.rows + s - 1) / s); };
-        if (tiles(256) >= 256) return launch_tiles<T, 256>(x, w, bias, y, st);
-        if (tiles(128) >= 256) return launch_tiles<T, 128>(x, w, bias, y, st);
-        return launch_tiles<T, 64>(x, w, bias, y, st);
+        switch (tile_side(x.rows, w.rows)) {
+            case 256: return launch_tiles<T, 256>(x, w, bias, y, st);
+            case 128: return launch_tiles<T, 128>(x, w, bias, y, st);
+            case 64: return launch_tiles<T, 64>(x, w, bias, y, st);
+        }
+        return AQ_ESHAPE;
     });
 }
 
@@ -363,6 +369,7 @@ aq_status launch_mx4_linear(const aq_matrix& x, const aq_mx4& w, const float* bi
             using T = decltype(t);
             return launch_rows<Values<T>, T>(Values<T>{(const T*)x.d, x.ld, (int)x.cols}, x.rows, w, bias, y, st);
         });
+    if (!tile_side(x.rows, w.rows)) return AQ_ESHAPE;  // (before the quantization)
     const int64_t b = x.rows * blocks32(x.cols);
     const aq_mx4 q = {ws, (uint8_t*)ws + 16 * b, x.rows, x.cols};
     const aq_status s = launch_mx4_quantize(x, q, st);
