@@ -10,6 +10,7 @@ import pytest
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, HERE)
+import learner_shapes as shapes  # noqa: E402
 from test_host_routes import LAUNCH, Host, fake  # noqa: E402,F401
 
 TYPES = {"f32": 0, "f16": 1, "bf16": 2}
@@ -63,7 +64,34 @@ def products_of_many_rows_and_few_columns(h):
             assert status == h.aq.ESHAPE and not launches, (call.__name__, rows, n, k, status)
 
 
-SCENARIOS = [products_of_many_rows_and_few_columns]
+def gradients_on_every_tile(h):
+    """The sizes of the tests reach every tile, several groups of wavefronts and several slices, for every type."""
+    for fn, listed in ((h.weight_grad, shapes.WEIGHT_GRAD), (h.input_grad, shapes.INPUT_GRAD)):
+        reached = set()
+        for sizes, *plans in listed:
+            rows, n, k = sizes
+            m, c = (n, k) if fn == h.weight_grad else (rows, k)
+            for kind, want in zip(TYPES, plans):
+                status, launches = fn(rows, n, k, kind)
+                side, groups = map(int, re.search(rb"Li(\d+)ELi(\d+)EE+v", launches[0].name).groups())
+                slices, rest = divmod(launches[0].grid[0], -(-m // side) * -(-c // side))
+                assert status == h.aq.OK and b"6k_gradI" in launches[0].name and rest == 0
+                assert len(launches) == (2 if slices > 1 else 1) and all(b"k_grad_join" in e.name for e in launches[1:])
+                assert (side, groups, slices > 1) == want and (slices == 1 or slices > 2), (fn.__name__, sizes, kind, side, groups, slices)
+                reached.add((kind, *want))
+        assert reached == {(kind, *tile, split) for kind in TYPES for tile in ((64, 1), (64, 2), (128, 1), (256, 1)) for split in (False, True)}
+
+
+def products_on_every_tile(h):
+    for sizes, side in shapes.MX4:
+        for kind in TYPES:
+            status, launches = h.matmul(*sizes, kind)
+            assert status == h.aq.OK and len(launches) == 1
+            found = re.search(rb"k_mx4_tilesI.*?Li(\d+)E", launches[0].name)
+            assert (int(found[1]) if found else 0) == side and (found or b"k_mx4_rows" in launches[0].name), (sizes, kind, launches[0].name)
+
+
+SCENARIOS = [gradients_on_every_tile, products_on_every_tile, products_of_many_rows_and_few_columns]
 
 
 @pytest.mark.parametrize("name", [s.__name__ for s in SCENARIOS])
