@@ -471,13 +471,13 @@ def _vector(t, n, what):
 
 def _bytes(workspace):
     """The size of a workspace."""
-    if workspace is None:
-        return 0
-    if not workspace.is_contiguous():  # (a tensor that repeats values has fewer bytes than it counts)
-        raise ValueError("a workspace is contiguous")
-    if not workspace.is_cuda:
-        _reachable(workspace)
-    return workspace.nbytes
+    size = 0 if workspace is None else workspace.nbytes
+    if size:
+        if not workspace.is_contiguous():  # (a tensor that repeats values has fewer bytes than it counts)
+            raise ValueError("a workspace is contiguous")
+        if not workspace.is_cuda:
+            _reachable(workspace)
+    return size
 
 
 class _Blocks:
@@ -510,20 +510,20 @@ class Mx4(_Blocks):
 
 def _kept(q):
     """A Ckpt8 as an aq_ckpt8; whatever else would be taken for one of its sizes."""
-    if not isinstance(q, Ckpt8):
-        raise ValueError("an 8-bit checkpoint is a Ckpt8")
-    if not q._near:
-        _reachable(q.codes, q.scales)
-    return q._c
+    if isinstance(q, Ckpt8):
+        if not q._near:
+            _reachable(q.codes, q.scales)
+        return q._c
+    raise ValueError("an 8-bit checkpoint is a Ckpt8")
 
 
 def _mx4(q):
     """An Mx4 as an aq_mx4."""
-    if not isinstance(q, Mx4):
-        raise ValueError("a 4-bit tensor is an Mx4")
-    if not q._near:
-        _reachable(q.codes, q.scales)
-    return q._c
+    if isinstance(q, Mx4):
+        if not q._near:
+            _reachable(q.codes, q.scales)
+        return q._c
+    raise ValueError("a 4-bit tensor is an Mx4")
 
 
 def _blocks_empty(kind, code_type, rows, cols, device):
@@ -570,9 +570,11 @@ def layernorm_forward(x, gamma, beta, eps, y, mean=None, rstd=None, kept=None):
     rows, cols = x.shape
     if not (x.is_cuda and y.is_cuda):
         _reachable(x, y)
-    _check((_lib or load()).aq_layernorm_forward(_matrix(x), _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, _matrix(y),
-                                       _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), None if kept is None else _kept(kept), _stream()),
-           "aq_layernorm_forward")
+    status = (_lib or load()).aq_layernorm_forward(_matrix(x), _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, _matrix(y),
+                                                   _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"),
+                                                   None if kept is None else _kept(kept), _stream())
+    if status:
+        raise AqError(status, "aq_layernorm_forward")
 
 
 def layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace=None):
@@ -581,60 +583,78 @@ def layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace=No
     blocks = isinstance(x, _Blocks)
     if not (dy.is_cuda and dx.is_cuda and (blocks or x.is_cuda)):
         _reachable(dy, dx, dy if blocks else x)
-    _check((_lib or load()).aq_layernorm_backward(_matrix(dy), None if blocks else _matrix(x), _kept(x) if blocks else None, _vector(gamma, cols, "gamma"),
-                                        _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), _matrix(dx),
-                                        _vector(dgamma, cols, "dgamma"), _vector(dbeta, cols, "dbeta"), _ptr(workspace), _bytes(workspace), _stream()),
-           "aq_layernorm_backward")
+    status = (_lib or load()).aq_layernorm_backward(_matrix(dy), None if blocks else _matrix(x), _kept(x) if blocks else None,
+                                                    _vector(gamma, cols, "gamma"), _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"),
+                                                    _matrix(dx), _vector(dgamma, cols, "dgamma"), _vector(dbeta, cols, "dbeta"),
+                                                    _ptr(workspace), _bytes(workspace), _stream())
+    if status:
+        raise AqError(status, "aq_layernorm_backward")
 
 
 def ckpt8_pack(x, kept):
     if not x.is_cuda:
         _reachable(x)
-    _check((_lib or load()).aq_ckpt8_pack(_matrix(x), _kept(kept), _stream()), "aq_ckpt8_pack")
+    status = (_lib or load()).aq_ckpt8_pack(_matrix(x), _kept(kept), _stream())
+    if status:
+        raise AqError(status, "aq_ckpt8_pack")
 
 
 def ckpt8_unpack(kept, x):
     if not x.is_cuda:
         _reachable(x)
-    _check((_lib or load()).aq_ckpt8_unpack(_kept(kept), _matrix(x), _stream()), "aq_ckpt8_unpack")
+    status = (_lib or load()).aq_ckpt8_unpack(_kept(kept), _matrix(x), _stream())
+    if status:
+        raise AqError(status, "aq_ckpt8_unpack")
 
 
 def ckpt8_weight_grad(dy, kept, dw, db=None, workspace=None):
     if not (dy.is_cuda and dw.is_cuda):
         _reachable(dy, dw)
-    _check((_lib or load()).aq_ckpt8_weight_grad(_matrix(dy), _kept(kept), _matrix(dw), _vector(db, dy.shape[1], "db"), _ptr(workspace), _bytes(workspace), _stream()),
-           "aq_ckpt8_weight_grad")
+    status = (_lib or load()).aq_ckpt8_weight_grad(_matrix(dy), _kept(kept), _matrix(dw), _vector(db, dy.shape[1], "db"), _ptr(workspace),
+                                                   _bytes(workspace), _stream())
+    if status:
+        raise AqError(status, "aq_ckpt8_weight_grad")
 
 
 def mx4_quantize(x, q):
     if not x.is_cuda:
         _reachable(x)
-    _check((_lib or load()).aq_mx4_quantize(_matrix(x), _mx4(q), _stream()), "aq_mx4_quantize")
+    status = (_lib or load()).aq_mx4_quantize(_matrix(x), _mx4(q), _stream())
+    if status:
+        raise AqError(status, "aq_mx4_quantize")
 
 
 def mx4_dequantize(q, x):
     if not x.is_cuda:
         _reachable(x)
-    _check((_lib or load()).aq_mx4_dequantize(_mx4(q), _matrix(x), _stream()), "aq_mx4_dequantize")
+    status = (_lib or load()).aq_mx4_dequantize(_mx4(q), _matrix(x), _stream())
+    if status:
+        raise AqError(status, "aq_mx4_dequantize")
 
 
 def mx4_linear(x, w, bias, y, workspace=None):
     """y = Q(x) w^T + bias; w: Mx4 [n][k]."""
     if not (x.is_cuda and y.is_cuda):
         _reachable(x, y)
-    _check((_lib or load()).aq_mx4_linear(_matrix(x), _mx4(w), _vector(bias, w.rows, "bias"), _matrix(y), _ptr(workspace), _bytes(workspace), _stream()),
-           "aq_mx4_linear")
+    status = (_lib or load()).aq_mx4_linear(_matrix(x), _mx4(w), _vector(bias, w.rows, "bias"), _matrix(y), _ptr(workspace),
+                                            _bytes(workspace), _stream())
+    if status:
+        raise AqError(status, "aq_mx4_linear")
 
 
 def mx4_matmul(x, w, bias, y):
     """The same from an Mx4 x."""
     if not y.is_cuda:
         _reachable(y)
-    _check((_lib or load()).aq_mx4_matmul(_mx4(x), _mx4(w), _vector(bias, w.rows, "bias"), _matrix(y), _stream()), "aq_mx4_matmul")
+    status = (_lib or load()).aq_mx4_matmul(_mx4(x), _mx4(w), _vector(bias, w.rows, "bias"), _matrix(y), _stream())
+    if status:
+        raise AqError(status, "aq_mx4_matmul")
 
 
 def mx4_input_grad(dy, w, dx, workspace=None):
     """dx = dy w; w: Mx4 [n][k]."""
     if not (dy.is_cuda and dx.is_cuda):
         _reachable(dy, dx)
-    _check((_lib or load()).aq_mx4_input_grad(_matrix(dy), _mx4(w), _matrix(dx), _ptr(workspace), _bytes(workspace), _stream()), "aq_mx4_input_grad")
+    status = (_lib or load()).aq_mx4_input_grad(_matrix(dy), _mx4(w), _matrix(dx), _ptr(workspace), _bytes(workspace), _stream())
+    if status:
+        raise AqError(status, "aq_mx4_input_grad")
