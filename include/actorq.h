@@ -422,7 +422,9 @@ typedef struct {
  *     bits and one mantissa bit (0, .5, 1, 1.5, 2, 3, 4, 6), value = element * 2^(scale - 127).  scale = max(0, the
  *     biased exponent of the block's largest magnitude - 2); elements round to nearest even and saturate at 6.  (The
  *     OCP microscaling formats' E2M1 with E8M0 scales, and their conversion.)
- * A block that holds a NaN or an infinity has scale 255 and stands for NaNs: nothing of it is lost silently. */
+ * A block that holds a NaN or an infinity has scale 255 and stands for NaNs: nothing of it is lost silently.  Scales 253 and
+ * 254, which the conversion to aq_mx4 never makes, let elements reach 2^128 and more: those are infinities to aq_mx4_dequantize
+ * and aq_mx4_input_grad, and what they stand for to the products of 4-bit tensors. */
 typedef struct {
     void* d_codes;
     uint8_t* d_scales;

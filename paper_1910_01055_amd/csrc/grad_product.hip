@@ -2,8 +2,8 @@
 //   weight gradient  dw[n][k] = sum_row dy[row][n] x8[row][k]      x8: the 8-bit checkpoint of its input
 //   input gradient   dx[row][k] = sum_n dy[row][n] w4[n][k]        w4: its microscaled 4-bit weights
 // Both are C[m][c] = sum_t A[m][t] B[t][c] on the bf16 matrix cores, without a rounding in front of the sums: a code of
-// either format times its power of two has at most seven significant bits, so it is a bf16 value, and a value of dy is the sum of
-// one (bfloat16), two (binary16) or three (fp32) bf16 values.
+// either format times its power of two has at most seven significant bits, so it is a bf16 value (4-bit values of 2^128 and more are
+// infinities), and a value of dy is the sum of one (bfloat16), two (binary16) or three (fp32) bf16 values.
 //
 // Bound by the matrix cores' power and by what feeds them: 65536 x 2048 x 2048 in bfloat16 takes 521 to 555 us back to back
 // (1.02 PFLOP/s; 471 alone), the input gradient 8192 x 2048 x 2048 61 us (1.13 PFLOP/s), where a loop of nothing but these
