@@ -1,7 +1,7 @@
 // The two block formats to and from rows of values: 8-bit checkpoints and microscaled 4-bit floats.
 //
-// Bound by memory (65536 x 2048 bfloat16 values to checkpoints: 70 us, 5.8 TB/s of reads and writes; 16384 x 4096 to 4-bit floats: 35 us,
-// 4.8 TB/s).  A thread holds eight values, four neighbouring threads a block, whose largest magnitude they find by two
+// Bound by memory (65536 x 2048 bfloat16 values to checkpoints: 70 us, 5.8 TB/s of reads and writes, and back 68, 6.0 TB/s; 16384 x 4096
+// to 4-bit floats: 35 us, 4.8 TB/s).  A thread holds eight values, four neighbouring threads a block, whose largest magnitude they find by two
 // exchanges within their quad; L = 4 .. 64 threads walk along a row (few, so that short rows share a wavefront), a workgroup
 // takes 256 / L rows at a time.
 #include "learner.hpp"

@@ -82,3 +82,15 @@ def test_every_scale():
             y = torch.empty(32 * times, 256 * times, device=DEV)
             B.mx4_matmul(x, many, None, y)
             same(y, (w.t() * 2.0 ** (scale - 127)).repeat(times, times), ("matmul", scale, times))
+
+
+def test_pinned_memory():
+    """Tensors that the host allocated for the GPU are tensors like others."""
+    x = torch.randn(33, 70, generator=torch.Generator().manual_seed(3))
+    pinned = torch.empty(33, 70, pin_memory=True).copy_(x)
+    there, here = B.mx4_empty(33, 70), B.mx4_empty(33, 70)
+    B.mx4_quantize(pinned, there)
+    B.mx4_quantize(x.to(DEV), here)
+    assert torch.equal(there.codes, here.codes) and torch.equal(there.scales, here.scales)
+    with pytest.raises(ValueError):
+        B.mx4_quantize(x, here)
