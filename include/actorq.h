@@ -479,6 +479,73 @@ aq_status aq_mx4_input_grad_workspace(int64_t rows, int64_t n, int64_t k, uint64
 aq_status aq_mx4_input_grad(const aq_matrix* dy, const aq_mx4* w, const aq_matrix* dx, void* d_workspace,
                             uint64_t workspace_bytes, void* stream);
 
+/* ---- A policy with a memory, while it learns: a gated recurrence over sequences, and the optimizer's step.  What is
+ * said above of the learner's operators holds for these. */
+
+/* A gated linear recurrence, unit by unit:  h_t = f_t h_{t-1} + (1 - f_t) v_t,  f = sigmoid(z).
+ * z, v and y (which receives h) have one type, one row to a step.  `count` sequences lie behind each other: sequence s has the rows from
+ * d_offsets[s] up to d_offsets[s + 1] (int32 [count + 1], device; they do not fall; each is taken as lying within 0 .. rows), or,
+ * where d_offsets is NULL, one `count`-th of all rows each.  Sequences may be empty, and rows that belong to none are left as they are.
+ * States are fp32 [count][cols]: d_first (NULL: zeros) before the first step, d_last (may be NULL) after the last one.
+ * d_starts (may be NULL): uint8 [rows], not 0 where an episode begins: h_{t-1} counts as zero there, whatever it is.
+ * The backward pass, from dy and d_dlast (NULL: zeros), the gradient of the last states:
+ *   g_t = dy_t + f_{t+1} g_{t+1} (without the second term where t + 1 starts an episode),
+ *   dv_t = (1 - f_t) g_t,  dz_t = g_t (h_{t-1} - v_t) f_t (1 - f_t),  d_dfirst (may be NULL) = f_0 g_0 (0 where it starts one).
+ * It reads h_{t-1} as y holds it.
+ * The single step of `rows` memories: state = f state + (1 - f) v in place (fp32 [rows][cols]), y (may be NULL) the same rounded. */
+#define AQ_RECURRENCE_MAX_STATES (1LL << 28) /* count * cols */
+aq_status aq_recurrence_workspace(int64_t rows, int64_t count, int64_t cols, uint64_t* bytes);
+aq_status aq_recurrence_forward(const aq_matrix* z, const aq_matrix* v, const int32_t* d_offsets, int64_t count, const uint8_t* d_starts,
+                                const float* d_first, const aq_matrix* y, float* d_last, void* d_workspace, uint64_t workspace_bytes,
+                                void* stream);
+aq_status aq_recurrence_backward(const aq_matrix* dy, const float* d_dlast, const aq_matrix* z, const aq_matrix* v, const aq_matrix* y,
+                                 const int32_t* d_offsets, int64_t count, const uint8_t* d_starts, const float* d_first,
+                                 const aq_matrix* dz, const aq_matrix* dv, float* d_dfirst, void* d_workspace, uint64_t workspace_bytes,
+                                 void* stream);
+aq_status aq_recurrence_step(const aq_matrix* z, const aq_matrix* v, const uint8_t* d_starts, float* d_state, const aq_matrix* y,
+                             void* stream);
+
+/* AdamW over all tensors of a policy:
+ *   g = gradient * min(1, max_norm / norm);  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
+ *   w = (1 - lr weight_decay) w - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)   (weight_decay where `decay` is not 0)
+ * and, in the same pass, a copy of w in 16 bits.  A tensor is n <= 2^34 consecutive values; none of a call's outputs overlap.
+ * moment_bits 32: d_m and d_v are fp32 [n], the scales NULL.  moment_bits 8: with B = ceil(n / 32), d_m and d_v are uint8 [32 B], 16-byte
+ * aligned, padded with zeros, and each block of 32 codes has a scale byte in uint8 [B], the biased fp32 exponent of its largest
+ * magnitude (255: the block stands for NaNs).  A code's bits are the upper ones of an fp32 number x, the lowest codes denormal, that
+ * stands for x * 2^(scale - 15):
+ *   d_m  a sign, four exponent bits, three mantissa bits, of m;   d_v  four exponent bits, four mantissa bits, of sqrt(v), at least 1
+ *   where v is not 0.
+ * All zeros stand for zeros.  A step adds to the bits that are cut, as a fraction of the last one that is kept, the upper bits of
+ * (index * 0xC13FA9A9 + step * 0x9E3779B9) mod 2^32 (of its sum with 2^31 for d_v), so that codes are right on the mean of
+ * the steps and results do not change from run to run.
+ * The host's lr and step (>= 1) are replaced by d_lr and d_step (device, each may be NULL) where a captured graph needs them to change;
+ * d_norm (device, may be NULL): the norm that max_norm is compared with; one that is not finite leaves every tensor as it is. */
+typedef struct {
+    float* d_w;
+    const void* d_g; /* of type g_dtype */
+    void* d_m;
+    void* d_v;
+    uint8_t* d_m_scales;
+    uint8_t* d_v_scales;
+    void* d_copy; /* may be NULL; of type copy_dtype, AQ_F16 or AQ_BF16 */
+    int64_t n;
+    int32_t g_dtype, copy_dtype, moment_bits, decay;
+} aq_learned;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay, max_norm;
+    int64_t step;
+    const float* d_lr;
+    const int64_t* d_step;
+    const float* d_norm;
+} aq_adamw;
+aq_status aq_adamw_step(const aq_learned* tensors, int64_t count, const aq_adamw* how, void* stream);
+/* The norm (2-norm, summed in 64 bits) over the gradients of all tensors, a float at d_norm. */
+aq_status aq_grad_norm_workspace(const aq_learned* tensors, int64_t count, uint64_t* bytes);
+aq_status aq_grad_norm(const aq_learned* tensors, int64_t count, float* d_norm, void* d_workspace, uint64_t workspace_bytes, void* stream);
+/* The moments of `from` in the form that `to` has (for a checkpoint of the learner, or to change their width); to 8 bits they go to the
+ * nearest code.  Nothing else of either is read or written. */
+aq_status aq_moments_convert(const aq_learned* from, const aq_learned* to, int64_t count, void* stream);
+
 const char* aq_status_string(aq_status s);
 
 #ifdef __cplusplus

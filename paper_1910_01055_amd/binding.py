@@ -33,7 +33,9 @@ EXPORTS = ["aq_policy_create", "aq_policy_destroy", "aq_policy_reserve", "aq_pol
            "aq_mfma_loop_reference", "aq_policy_subbyte_layers", "aq_policy_fp32_plan", "aq_policy_fp16_plan",
            "aq_layernorm_forward", "aq_layernorm_backward", "aq_layernorm_backward_workspace", "aq_ckpt8_pack", "aq_ckpt8_unpack",
            "aq_ckpt8_weight_grad", "aq_ckpt8_weight_grad_workspace", "aq_mx4_quantize", "aq_mx4_dequantize", "aq_mx4_linear",
-           "aq_mx4_linear_workspace", "aq_mx4_matmul", "aq_mx4_input_grad", "aq_mx4_input_grad_workspace"]
+           "aq_mx4_linear_workspace", "aq_mx4_matmul", "aq_mx4_input_grad", "aq_mx4_input_grad_workspace",
+           "aq_recurrence_forward", "aq_recurrence_backward", "aq_recurrence_step", "aq_recurrence_workspace",
+           "aq_adamw_step", "aq_grad_norm", "aq_grad_norm_workspace", "aq_moments_convert"]
 
 
 class AqLayer(C.Structure):
@@ -74,6 +76,20 @@ class AqBlocks(C.Structure):
 # LayerNorm's two passes take five).  (The type as 64 bits: it and the padding behind it.)
 _pack_matrix = struct.Struct("Pqqqq").pack
 _pack_blocks = struct.Struct("PPqq").pack
+
+
+class AqLearned(C.Structure):
+    _fields_ = [("d_w", C.c_void_p), ("d_g", C.c_void_p), ("d_m", C.c_void_p), ("d_v", C.c_void_p), ("d_m_scales", C.c_void_p),
+                ("d_v_scales", C.c_void_p), ("d_copy", C.c_void_p), ("n", C.c_int64), ("g_dtype", C.c_int32), ("copy_dtype", C.c_int32),
+                ("moment_bits", C.c_int32), ("decay", C.c_int32)]
+
+
+class AqAdamw(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("max_norm", C.c_double), ("step", C.c_int64), ("d_lr", C.c_void_p), ("d_step", C.c_void_p), ("d_norm", C.c_void_p)]
+
+
+_pack_adamw = struct.Struct("ddddddqPPP").pack
 
 
 class AqError(RuntimeError):
@@ -144,6 +160,14 @@ def load():
     lib.aq_mx4_input_grad.argtypes = [mat, blk, mat, vp, u64, vp]
     for name in ("aq_ckpt8_weight_grad_workspace", "aq_mx4_linear_workspace", "aq_mx4_input_grad_workspace"):
         getattr(lib, name).argtypes = [i64, i64, i64, C.POINTER(u64)]
+    lib.aq_recurrence_workspace.argtypes = [i64, i64, i64, C.POINTER(u64)]
+    lib.aq_recurrence_forward.argtypes = [mat, mat, vp, i64, vp, vp, mat, vp, vp, u64, vp]
+    lib.aq_recurrence_backward.argtypes = [mat, vp, mat, mat, mat, vp, i64, vp, vp, mat, mat, vp, vp, u64, vp]
+    lib.aq_recurrence_step.argtypes = [mat, mat, vp, vp, mat, vp]
+    lib.aq_adamw_step.argtypes = [vp, i64, vp, vp]
+    lib.aq_grad_norm_workspace.argtypes = [vp, i64, C.POINTER(u64)]
+    lib.aq_grad_norm.argtypes = [vp, i64, vp, vp, u64, vp]
+    lib.aq_moments_convert.argtypes = [vp, vp, i64, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         # (addresses travel as plain integers, which ctypes cuts to 32 bits where no argument types are declared)
@@ -658,3 +682,210 @@ def mx4_input_grad(dy, w, dx, workspace=None):
     status = (_lib or load()).aq_mx4_input_grad(_matrix(dy), _mx4(w), _matrix(dx), _ptr(workspace), _bytes(workspace), _stream())
     if status:
         raise AqError(status, "aq_mx4_input_grad")
+
+
+# ---- a policy with a memory, while it learns.  Tensors of these calls lie on the current device or in pinned memory.
+
+def _first_device():
+    global _device
+    import torch
+    torch.cuda.current_device()  # (initializes CUDA)
+    _device = torch._C._cuda_getDevice
+    return _device()
+
+
+_device = _first_device
+
+
+def _here(*tensors):
+    """Refuses tensors of another device than the current one, whose stream the call takes, and of ordinary host memory."""
+    device = _device()
+    for t in tensors:
+        if t is not None and t.get_device() != device and t.numel():
+            if t.is_cuda:
+                raise ValueError(f"a tensor lies on device {t.get_device()}, and {device} is the current one")
+            _reachable(t)
+
+
+def _plain(t, dtype, n, what):
+    """A contiguous tensor of n values of a type as a pointer; None stays None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} is a contiguous {dtype} tensor of {n} values")
+    return t.data_ptr()
+
+
+def recurrence_workspace(rows, count, cols):
+    return _size("aq_recurrence_workspace", rows, count, cols)
+
+
+def _sequences(z, offsets, starts, state, what):
+    """Pointers to offsets, starts and the states of the sequences, and how many these are (as many as `state` has rows, if there are no
+    offsets; one without either)."""
+    import torch
+    rows, cols = z.shape
+    count = offsets.numel() - 1 if offsets is not None else 1 if state is None else state.shape[0]
+    if count < 0:
+        raise ValueError("offsets holds one value more than there are sequences")
+    return (_plain(offsets, torch.int32, count + 1, "offsets"), count, _plain(starts, torch.uint8, rows, "starts"))
+
+
+def recurrence_forward(z, v, first, y, last=None, offsets=None, starts=None, workspace=None):
+    """y = h, h_t = f_t h_{t-1} + (1 - f_t) v_t, f = sigmoid(z).  Sequence s has the rows offsets[s] .. offsets[s + 1] (int32), or, without
+    offsets, an equal part of all rows: as many sequences as `first` or `last` has rows.  starts: uint8, not 0 where an episode begins."""
+    _here(z, v, first, y, last, offsets, starts, workspace)
+    where, count, begin = _sequences(z, offsets, starts, last if first is None else first, "states")
+    n = count * z.shape[1]
+    status = (_lib or load()).aq_recurrence_forward(_matrix(z), _matrix(v), where, count, begin, _vector(first, n, "first"), _matrix(y),
+                                                    _vector(last, n, "last"), _ptr(workspace), _bytes(workspace), _stream())
+    if status:
+        raise AqError(status, "aq_recurrence_forward")
+
+
+def recurrence_backward(dy, dlast, z, v, y, first, dz, dv, dfirst=None, offsets=None, starts=None, workspace=None):
+    """The gradients of recurrence_forward, from those of y and (None: zeros) of last."""
+    _here(dy, dlast, z, v, y, first, dz, dv, dfirst, offsets, starts, workspace)
+    where, count, begin = _sequences(z, offsets, starts, next((t for t in (first, dlast, dfirst) if t is not None), None), "states")
+    n = count * z.shape[1]
+    status = (_lib or load()).aq_recurrence_backward(_matrix(dy), _vector(dlast, n, "dlast"), _matrix(z), _matrix(v), _matrix(y), where, count,
+                                                     begin, _vector(first, n, "first"), _matrix(dz), _matrix(dv), _vector(dfirst, n, "dfirst"),
+                                                     _ptr(workspace), _bytes(workspace), _stream())
+    if status:
+        raise AqError(status, "aq_recurrence_backward")
+
+
+def recurrence_step(z, v, state, y=None, starts=None):
+    """One step of the memories of all rows: `state` (fp32) in place, y the same rounded."""
+    import torch
+    _here(z, v, state, y, starts)
+    rows, cols = z.shape
+    status = (_lib or load()).aq_recurrence_step(_matrix(z), _matrix(v), _plain(starts, torch.uint8, rows, "starts"),
+                                                 _vector(state, rows * cols, "state"), None if y is None else _matrix(y), _stream())
+    if status:
+        raise AqError(status, "aq_recurrence_step")
+
+
+class Moment8:
+    """A tensor's moment in 8 bits (see aq_learned): codes uint8 [32 B], scales uint8 [B], B = ceil(n / 32)."""
+
+    def __init__(self, codes, scales, n):
+        import torch
+        blocks = (int(n) + 31) // 32
+        for t, size, what in ((codes, 32 * blocks, "codes"), (scales, blocks, "scales")):
+            _plain(t, torch.uint8, size, what)
+        if codes.data_ptr() % 16:
+            raise ValueError("codes begin at a multiple of 16 bytes")
+        self.codes, self.scales, self.n = codes, scales, int(n)
+
+
+def moment8_zeros(n, device="cuda:0"):
+    import torch
+    blocks = (int(n) + 31) // 32
+    return Moment8(torch.zeros(32 * blocks, dtype=torch.uint8, device=device), torch.zeros(blocks, dtype=torch.uint8, device=device), n)
+
+
+class Learned:
+    """One tensor that learns: weights (fp32), their gradient, both moments (fp32 tensors or Moment8s), a copy of the weights in 16 bits."""
+
+    def __init__(self, w, g, m, v, copy=None, decay=True):
+        import torch
+        if not _DTYPES:
+            _learn_dtypes()
+        n = w.numel()
+        _plain(w, torch.float32, n, "w")
+        if g.dtype not in _DTYPES:
+            raise ValueError("g is a tensor of float32, float16 or bfloat16")
+        _plain(g, g.dtype, n, "g")
+        if copy is not None:
+            if copy.dtype not in (torch.float16, torch.bfloat16):
+                raise ValueError("copy is a tensor of float16 or bfloat16")
+            _plain(copy, copy.dtype, n, "copy")
+        bits = 8 if isinstance(m, Moment8) else 32
+        if isinstance(v, Moment8) != (bits == 8):
+            raise ValueError("both moments have the same number of bits")
+        if bits == 8:
+            if m.n != n or v.n != n:
+                raise ValueError(f"moments are of {n} values")
+            self.tensors = [w, g, m.codes, v.codes, m.scales, v.scales, copy]
+        else:
+            _plain(m, torch.float32, n, "m")
+            _plain(v, torch.float32, n, "v")
+            self.tensors = [w, g, m, v, None, None, copy]
+        self.c = AqLearned(*[None if t is None or not t.numel() else t.data_ptr() for t in self.tensors], n, _DTYPES[g.dtype],
+                           0 if copy is None else _DTYPES[copy.dtype], bits, int(bool(decay)))
+
+
+class LearnedSet:
+    """The tensors of a policy, for calls that take all of them: their addresses are written down once, so the tensors stay the same ones.
+    What a step writes belongs to one tensor alone."""
+
+    def __init__(self, learned):
+        self.learned = tuple(learned)
+        written = []
+        for one in self.learned:
+            for i, t in enumerate(one.tensors):
+                if t is not None and t.numel():
+                    written.append((t.data_ptr(), t.data_ptr() + t.nbytes, i != 1))
+        end, last = 0, False  # furthest end of what lies in front, and of what is written of it
+        written_end = 0
+        for begin, behind, writes in sorted(written):
+            if begin < (end if writes else written_end):
+                raise ValueError("tensors that a step writes overlap others")
+            end = max(end, behind)
+            if writes:
+                written_end = max(written_end, behind)
+        self.c = (AqLearned * len(self.learned))(*[one.c for one in self.learned])
+        self.address, self.count = C.addressof(self.c), len(self.learned)
+        self._all = [t for one in self.learned for t in one.tensors if t is not None and t.numel()]
+        self._device = None
+
+    def _near(self):
+        """The address of the tensors' list, for a call on the current device."""
+        if self._device is None or self._device != _device():
+            _here(*self._all)
+            self._device = _device()
+        return self.address
+
+
+def grad_norm_workspace(tensors):
+    n = C.c_uint64(0)
+    _check(load().aq_grad_norm_workspace(tensors.address, tensors.count, C.byref(n)), "aq_grad_norm_workspace")
+    return int(n.value)
+
+
+def grad_norm(tensors, norm, workspace=None):
+    """The 2-norm over the gradients of all tensors of a LearnedSet, into one fp32 value."""
+    _here(norm, workspace)
+    status = (_lib or load()).aq_grad_norm(tensors._near(), tensors.count, _vector(norm, 1, "norm"), _ptr(workspace), _bytes(workspace), _stream())
+    if status:
+        raise AqError(status, "aq_grad_norm")
+
+
+def adamw_step(tensors, lr, beta1, beta2, eps, weight_decay, step, norm=None, max_norm=float("inf")):
+    """One step of AdamW of all tensors of a LearnedSet.  lr: a number, or an fp32 value on the device; step: the step's number from 1 on, or
+    an int64 value on the device; norm: that of grad_norm, to which max_norm is the limit."""
+    d_lr = d_step = None
+    if hasattr(lr, "data_ptr"):
+        _here(lr)
+        d_lr, lr = _vector(lr, 1, "lr"), 0.0
+    if hasattr(step, "data_ptr"):
+        import torch
+        _here(step)
+        d_step, step = _plain(step, torch.int64, 1, "step"), 0
+    if norm is not None:
+        _here(norm)
+    status = (_lib or load()).aq_adamw_step(tensors._near(), tensors.count,
+                                            _pack_adamw(lr, beta1, beta2, eps, weight_decay, max_norm, step, d_lr or 0, d_step or 0,
+                                                        0 if norm is None else _vector(norm, 1, "norm")), _stream())
+    if status:
+        raise AqError(status, "aq_adamw_step")
+
+
+def moments_convert(source, target):
+    """The moments of a LearnedSet in the form that another one of the same sizes keeps them in."""
+    if source.count != target.count:
+        raise ValueError("both sets have the same tensors")
+    status = (_lib or load()).aq_moments_convert(source._near(), target._near(), source.count, _stream())
+    if status:
+        raise AqError(status, "aq_moments_convert")

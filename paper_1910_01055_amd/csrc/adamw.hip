@@ -1,0 +1,372 @@
+// AdamW over all tensors of a policy in one launch, and the norm over all their gradients.
+//
+//   g = scale * gradient, scale = min(1, max_norm / norm)
+//   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  w = (1 - lr wd) w - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+//
+// Bound by memory: 8 + e bytes a weight (e: of a gradient), 16 for moments in 32 bits or 4 1/8 for those in 8, 2 for a 16-bit copy.
+// The tensors' addresses travel as kernel arguments, kTensors of them to a launch, so nothing lies in device memory between calls.  A
+// workgroup takes kValues consecutive values of one tensor, a thread eight at a time; four lanes hold a block of 8-bit moments.
+//
+// Moments in 8 bits (block: 32 values of a tensor that share a power of two, that of their largest magnitude's exponent):
+//   first moment   sign, four exponent bits, three mantissa bits of m
+//   second moment  four exponent bits, four mantissa bits of sqrt(v): the root halves the range of exponents, 20 binades are left
+// Both are the upper bits of an fp32 number whose exponent is moved so that the block's largest lies in the uppermost of 16 binades;
+// the lower ones are denormal.  A code that is rounded to nearest would not move any more: v changes by a thousandth in a step, a
+// code's neighbours lie 3 to 6 % off.  So what is cut goes up or down by a fraction that walks over [0, 1) evenly from step to
+// step and from value to value (multiples of an irrational number): the codes' mean over the steps is the value.  The smallest code
+// of sqrt(v) stands for all that is below it but 0, so that no weight is moved by m / 0.
+#include "learner.hpp"
+#include "learner_device.hpp"
+
+namespace aq {
+namespace {
+
+constexpr int kTensors = 40;  // to a launch, which takes 4 KB of arguments
+constexpr int kThreads = 256;
+constexpr int kValues = 8 * kThreads;
+constexpr uint32_t kPlace = 0xC13FA9A9u, kTurn = 0x9E3779B9u;
+
+constexpr int64_t kMostChunks = 1 << 23;  // to a launch, whose threads 32 bits count
+
+template <int N>
+struct Tensors {
+    aq_learned t[N];
+    uint32_t first[N];  // the first chunk of each; of those behind the last one, 2^32 - 1
+};
+static_assert(sizeof(Tensors<kTensors>) <= 3600, "kernel arguments");
+
+struct Step {
+    float b1, c1, b2, c2, lr, rate, decay, root, eps, max_norm;  // rate = lr / (1 - b1^t), decay = 1 - lr wd, root = 1 / sqrt(1 - b2^t)
+    double beta1, beta2, weight_decay, host_lr;
+    int64_t step;
+    const float *d_lr, *d_norm;
+    const int64_t* d_step;
+};
+
+// x * 2^e for -252 <= e <= 254
+struct Power {
+    float a, b;
+    __device__ __forceinline__ explicit Power(int e) {
+        const int half = e >> 1;
+        a = __uint_as_float((uint32_t)(half + 127) << 23);
+        b = __uint_as_float((uint32_t)(e - half + 127) << 23);
+    }
+    __device__ __forceinline__ float operator()(float x) const { return x * a * b; }
+};
+// eight magnitudes' codes; `place` and `turn` as above (nearest: what is cut is compared with a half)
+template <int BITS>
+__device__ __forceinline__ void moment_codes(const float (&x)[8], uint32_t scale, uint32_t dither, bool nearest, uint32_t (&code)[8]) {
+    const Power to(15 - (int)scale);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t d = nearest ? 1u << (22 - BITS) : (dither + j * kPlace) >> (9 + BITS);
+        const uint32_t c = (__float_as_uint(to(x[j])) + d) >> (23 - BITS);
+        code[j] = c < (16u << BITS) ? c : (16u << BITS) - 1;
+    }
+}
+template <int BITS>
+__device__ __forceinline__ float moment_value(uint32_t code, const Power& from) {
+    return from(__uint_as_float(code << (23 - BITS)));
+}
+__device__ __forceinline__ Power from_scale(uint32_t scale) {
+    Power p((int)scale - 15);
+    if (scale == 255) p.a = __uint_as_float(0x7fc00000u);
+    return p;
+}
+__device__ __forceinline__ v2u bytes_of(const uint32_t (&c)[8]) {
+    return v2u{c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24};
+}
+__device__ __forceinline__ uint32_t most_magnitude(const float (&x)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t b = __float_as_uint(x[j]) & 0x7fffffffu;
+        m = b > m ? b : m;
+    }
+    return most_of4lanes(m);
+}
+__device__ __forceinline__ uint32_t scale_of(uint32_t most) { return most >= kInfBits ? 255u : most >> 23; }
+
+// the moments of eight values from `at` on, of which `left` exist
+struct Moments {
+    v2u m, v;
+    uint32_t ms, vs;
+    Piece<float> m32, v32;
+    __device__ __forceinline__ void load(const aq_learned& t, int64_t at, int left) {
+        if (t.moment_bits == 8) {
+            m = v = v2u{0, 0};
+            ms = vs = 0;
+            if (left > 0) {
+                m = *(const v2u AQ_GLOBAL*)((const uint8_t*)t.d_m + at);
+                v = *(const v2u AQ_GLOBAL*)((const uint8_t*)t.d_v + at);
+                ms = t.d_m_scales[at >> 5];
+                vs = t.d_v_scales[at >> 5];
+            }
+        } else {
+            m32.load((const float*)t.d_m + at, left);
+            v32.load((const float*)t.d_v + at, left);
+        }
+    }
+    __device__ __forceinline__ void get(const aq_learned& t, float (&a)[8], float (&b)[8]) const {
+        if (t.moment_bits == 8) {
+            const Power pm = from_scale(ms), pv = from_scale(vs);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t c = m[j / 4] >> (8 * (j & 3)) & 255, r = v[j / 4] >> (8 * (j & 3)) & 255;
+                const float x = moment_value<3>(c & 127, pm), y = moment_value<4>(r, pv);
+                a[j] = c & 128 ? -x : x;
+                b[j] = y * y;
+            }
+        } else {
+            m32.get(a);
+            v32.get(b);
+        }
+    }
+};
+// a: first moments, b: second moments, r: their roots; every lane of a block calls this
+__device__ __forceinline__ void store_moments(const aq_learned& t, int64_t at, int left, float (&a)[8], const float (&b)[8], const float (&r)[8],
+                                              uint32_t turn, bool nearest) {
+    if (t.moment_bits == 8) {
+        if (left < 8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j >= left) a[j] = 0.0f;
+        }
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = fabsf(a[j]);
+        const uint32_t ms = scale_of(most_magnitude(x)), dither = (uint32_t)at * kPlace + turn;
+        uint32_t c[8];
+        moment_codes<3>(x, ms, dither, nearest, c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c[j] |= __float_as_uint(a[j]) >> 24 & 128u;
+        const v2u m = bytes_of(c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = j < left ? r[j] : 0.0f;
+        const uint32_t vs = scale_of(most_magnitude(x));
+        moment_codes<4>(x, vs, dither + 0x80000000u, nearest, c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c[j] = c[j] == 0 && x[j] > 0.0f ? 1u : c[j];
+        const v2u v = bytes_of(c);
+        if ((at & ~(int64_t)31) < t.n) {
+            *(v2u AQ_GLOBAL*)((uint8_t*)t.d_m + at) = ms == 255 ? v2u{0, 0} : m;
+            *(v2u AQ_GLOBAL*)((uint8_t*)t.d_v + at) = vs == 255 ? v2u{0, 0} : v;
+            if ((at & 31) == 0) {
+                t.d_m_scales[at >> 5] = (uint8_t)ms;
+                t.d_v_scales[at >> 5] = (uint8_t)vs;
+            }
+        }
+    } else {
+        Piece<float> p;
+        p.set(a);
+        p.store((float*)t.d_m + at, left);
+        p.set(b);
+        p.store((float*)t.d_v + at, left);
+    }
+}
+
+// which tensor a chunk belongs to
+template <int N>
+__device__ __forceinline__ int tensor_of(const Tensors<N>& all, uint32_t chunk) {
+    int i = -1;
+#pragma unroll
+    for (int j = 0; j < N; ++j) i += chunk >= all.first[j];
+    return i;
+}
+
+template <class G>
+__device__ __forceinline__ void load_gradient(const void* g, int64_t at, int left, float (&x)[8]) {
+    Piece<G> p;
+    p.load((const G*)g + at, left);
+    p.get(x);
+}
+__device__ __forceinline__ void load_gradient(const aq_learned& t, int64_t at, int left, float (&x)[8]) {
+    if (t.g_dtype == AQ_F32) load_gradient<float>(t.d_g, at, left, x);
+    else if (t.g_dtype == AQ_F16) load_gradient<f16_t>(t.d_g, at, left, x);
+    else load_gradient<bf16_t>(t.d_g, at, left, x);
+}
+
+// b^t, t >= 0
+__device__ __forceinline__ double power(double b, int64_t t) {
+    double p = 1.0;
+    for (; t > 0; t >>= 1, b *= b)
+        if (t & 1) p *= b;
+    return p;
+}
+
+__global__ void __launch_bounds__(kThreads) k_adamw(Tensors<kTensors> all, Step s) {
+    float scale = 1.0f;
+    if (s.d_norm) {
+        const float norm = fabsf(*s.d_norm);
+        if (!(norm <= 3.402823466e38f)) return;  // infinite or NaN: this step is left out
+        const float q = s.max_norm / norm;
+        scale = q < 1.0f ? q : 1.0f;
+    }
+    const int i = tensor_of(all, blockIdx.x);
+    const aq_learned& t = all.t[i];
+    const int64_t at = (int64_t)(blockIdx.x - all.first[i]) * kValues + 8 * (int)threadIdx.x;
+    const int left = t.n - at < 8 ? (int)(t.n - at) : 8;
+    float g[8];
+    Moments k;
+    Piece<float> w;
+    load_gradient(t, at, left, g);
+    k.load(t, at, left);
+    w.load(t.d_w + at, left);
+    if (s.d_lr || s.d_step) {
+        const double lr = s.d_lr ? (double)*s.d_lr : s.host_lr;
+        if (s.d_step) s.step = *s.d_step > 1 ? *s.d_step : 1;
+        s.decay = (float)(1.0 - lr * s.weight_decay);
+        s.rate = (float)(lr / (1.0 - power(s.beta1, s.step)));
+        s.root = (float)(1.0 / sqrt(1.0 - power(s.beta2, s.step)));
+    }
+    const float decay = t.decay ? s.decay : 1.0f;
+    float m[8], v[8], r[8], x[8];
+    k.get(t, m, v);
+    w.get(x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float a = g[j] * scale;
+        m[j] = m[j] * s.b1 + a * s.c1;
+        v[j] = v[j] * s.b2 + a * a * s.c2;
+        r[j] = sqrtf(v[j]);
+        x[j] = x[j] * decay - s.rate * (m[j] / (r[j] * s.root + s.eps));
+    }
+    w.set(x);
+    w.store(t.d_w + at, left);
+    if (t.d_copy) {
+        if (t.copy_dtype == AQ_F16) {
+            Piece<f16_t> c;
+            c.set(x);
+            c.store((f16_t*)t.d_copy + at, left);
+        } else {
+            Piece<bf16_t> c;
+            c.set(x);
+            c.store((bf16_t*)t.d_copy + at, left);
+        }
+    }
+    store_moments(t, at, left, m, v, r, (uint32_t)s.step * kTurn, false);
+}
+
+// moments from one form into another
+__global__ void __launch_bounds__(kThreads) k_moments(Tensors<kTensors / 2> from, Tensors<kTensors / 2> to) {
+    const int i = tensor_of(from, blockIdx.x);
+    const int64_t at = (int64_t)(blockIdx.x - from.first[i]) * kValues + 8 * (int)threadIdx.x;
+    const int left = from.t[i].n - at < 8 ? (int)(from.t[i].n - at) : 8;
+    Moments k;
+    k.load(from.t[i], at, left);
+    float m[8], v[8], r[8];
+    k.get(from.t[i], m, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = sqrtf(v[j]);
+    store_moments(to.t[i], at, left, m, v, r, 0, true);
+}
+
+// ---- the norm: each workgroup's sum of squares, in 64 bits, then one workgroup that adds them in their order
+__device__ __forceinline__ double sum_of_workgroup(double s, double* shared) {
+#pragma unroll
+    for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = 0.0;
+    for (int i = 0; i < (int)blockDim.x / 64; ++i) s += shared[i];
+    return s;
+}
+__global__ void __launch_bounds__(kThreads) k_grad_squares(Tensors<kTensors> all, uint32_t chunks, double* __restrict__ out) {
+    __shared__ double shared[kThreads / 64];
+    double s = 0.0;
+    for (uint32_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+        const int i = tensor_of(all, chunk);
+        const aq_learned& t = all.t[i];
+        const int64_t at = (int64_t)(chunk - all.first[i]) * kValues + 8 * (int)threadIdx.x;
+        float g[8];
+        load_gradient(t, at, t.n - at < 8 ? (int)(t.n - at) : 8, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += (double)g[j] * (double)g[j];
+    }
+    s = sum_of_workgroup(s, shared);
+    if (threadIdx.x == 0) out[blockIdx.x] = s;
+}
+__global__ void __launch_bounds__(1024) k_grad_norm(const double* __restrict__ in, int n, float* __restrict__ norm) {
+    __shared__ double shared[16];
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n; i += 1024) s += in[i];
+    s = sum_of_workgroup(s, shared);
+    if (threadIdx.x == 0) *norm = (float)sqrt(s);
+}
+
+int64_t chunks_of(int64_t n) { return (n + kValues - 1) / kValues; }
+constexpr int64_t kMostSums = 2048;  // workgroups of a launch for the norm
+
+// calls go(tensors, chunks, the indices of the tensors) for every N that hold values
+template <int N, class Go>
+aq_status in_groups(const aq_learned* t, int64_t count, Go&& go) {
+    for (int64_t i = 0; i < count;) {
+        Tensors<N> all;
+        int64_t chunks = 0, which[N];
+        int used = 0;
+        for (; i < count && used < N; ++i) {
+            const int64_t more = chunks_of(t[i].n);
+            if (more == 0) continue;
+            if (chunks + more > kMostChunks) break;  // (one alone has no more: the entry points see to that)
+            all.t[used] = t[i];
+            all.first[used] = (uint32_t)chunks;
+            which[used++] = i;
+            chunks += more;
+        }
+        if (used == 0) continue;
+        for (int j = used; j < N; ++j) all.t[j] = all.t[0], all.first[j] = 0xffffffffu, which[j] = which[0];
+        const aq_status done = go(all, (uint32_t)chunks, which);
+        if (done != AQ_OK) return done;
+    }
+    return AQ_OK;
+}
+
+}  // namespace
+
+int64_t grad_norm_workspace(const aq_learned* t, int64_t count) {
+    int64_t sums = 0;
+    in_groups<kTensors>(t, count, [&](const Tensors<kTensors>&, uint32_t chunks, const int64_t*) {
+        sums += chunks < kMostSums ? chunks : kMostSums;
+        return AQ_OK;
+    });
+    return sums * (int64_t)sizeof(double);
+}
+
+aq_status launch_grad_norm(const aq_learned* t, int64_t count, float* norm, void* ws, hipStream_t st) {
+    int64_t sums = 0;
+    const aq_status done = in_groups<kTensors>(t, count, [&](const Tensors<kTensors>& all, uint32_t chunks, const int64_t*) {
+        const uint32_t grid = chunks < kMostSums ? chunks : (uint32_t)kMostSums;
+        k_grad_squares<<<grid, kThreads, 0, st>>>(all, chunks, (double*)ws + sums);
+        sums += grid;
+        return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+    });
+    if (done != AQ_OK) return done;
+    k_grad_norm<<<1, 1024, 0, st>>>((const double*)ws, (int)sums, norm);
+    return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+}
+
+aq_status launch_adamw(const aq_learned* t, int64_t count, const aq_adamw& h, hipStream_t st) {
+    Step s{};
+    s.b1 = (float)h.beta1, s.c1 = (float)(1.0 - h.beta1), s.b2 = (float)h.beta2, s.c2 = (float)(1.0 - h.beta2);
+    s.eps = (float)h.eps, s.max_norm = (float)h.max_norm;
+    s.beta1 = h.beta1, s.beta2 = h.beta2, s.weight_decay = h.weight_decay, s.host_lr = h.lr;
+    s.step = h.step, s.d_lr = h.d_lr, s.d_norm = h.d_norm, s.d_step = h.d_step;
+    s.decay = (float)(1.0 - h.lr * h.weight_decay);
+    s.rate = (float)(h.lr / (1.0 - pow(h.beta1, (double)h.step)));
+    s.root = (float)(1.0 / sqrt(1.0 - pow(h.beta2, (double)h.step)));
+    return in_groups<kTensors>(t, count, [&](const Tensors<kTensors>& all, uint32_t chunks, const int64_t*) {
+        k_adamw<<<chunks, kThreads, 0, st>>>(all, s);
+        return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+    });
+}
+
+aq_status launch_moments_convert(const aq_learned* from, const aq_learned* to, int64_t count, hipStream_t st) {
+    return in_groups<kTensors / 2>(from, count, [&](const Tensors<kTensors / 2>& all, uint32_t chunks, const int64_t* which) {
+        Tensors<kTensors / 2> other = all;
+        for (int j = 0; j < kTensors / 2; ++j) other.t[j] = to[which[j]];
+        k_moments<<<chunks, kThreads, 0, st>>>(all, other);
+        return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+    });
+}
+
+}  // namespace aq

@@ -51,5 +51,19 @@ aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq
                              hipStream_t st);
 int64_t input_grad_workspace(int64_t rows, int64_t n, int64_t k);
 aq_status launch_input_grad(const aq_matrix& dy, const aq_mx4& w, const aq_matrix& dx, void* ws, uint64_t ws_bytes, hipStream_t st);
+// ---- recurrence.hip
+int64_t recurrence_workspace(int64_t rows, int64_t count, int64_t cols);
+aq_status launch_recurrence_forward(const aq_matrix& z, const aq_matrix& v, const int32_t* offsets, int64_t count, const uint8_t* starts,
+                                    const float* first, const aq_matrix& y, float* last, float* ws, hipStream_t st);
+aq_status launch_recurrence_backward(const aq_matrix& dy, const float* dlast, const aq_matrix& z, const aq_matrix& v, const aq_matrix& y,
+                                     const int32_t* offsets, int64_t count, const uint8_t* starts, const float* first, const aq_matrix& dz,
+                                     const aq_matrix& dv, float* dfirst, float* ws, hipStream_t st);
+aq_status launch_recurrence_step(const aq_matrix& z, const aq_matrix& v, const uint8_t* starts, float* state, const aq_matrix* y, hipStream_t st);
+// ---- adamw.hip
+constexpr int64_t kMostValues = 1LL << 34;  // of a tensor
+int64_t grad_norm_workspace(const aq_learned* t, int64_t count);
+aq_status launch_grad_norm(const aq_learned* t, int64_t count, float* norm, void* ws, hipStream_t st);
+aq_status launch_adamw(const aq_learned* t, int64_t count, const aq_adamw& h, hipStream_t st);
+aq_status launch_moments_convert(const aq_learned* from, const aq_learned* to, int64_t count, hipStream_t st);
 
 }  // namespace aq

@@ -160,3 +160,136 @@ extern "C" aq_status aq_mx4_input_grad(const aq_matrix* dy, const aq_mx4* w, con
     if (w->rows != dy->cols || dx->rows != dy->rows || dx->cols != w->cols || dx->dtype != dy->dtype) return AQ_ESHAPE;
     return dy->rows == 0 ? AQ_OK : launch_input_grad(*dy, *w, *dx, d_workspace, workspace_bytes, as_stream(stream));
 }
+
+// ---- the recurrence
+
+namespace {
+
+// the matrices of a pass: z's sizes and type
+aq_status like(const aq_matrix* m, const aq_matrix* z) {
+    AQ_TRY(matrix_ok(m));
+    return m->rows != z->rows || m->cols != z->cols || m->dtype != z->dtype ? AQ_ESHAPE : AQ_OK;
+}
+// offsets of sequences, or equal parts of all rows
+aq_status sequences_ok(const aq_matrix* z, const int32_t* offsets, int64_t count) {
+    if (count < 0 || ((uintptr_t)offsets & 3)) return AQ_EINVAL;
+    // (32 bits count a launch's threads, up to eight to a unit)
+    if (count > kMostRows || count * z->cols > AQ_RECURRENCE_MAX_STATES) return AQ_ESHAPE;
+    return !offsets && count > 0 && z->rows % count ? AQ_ESHAPE : AQ_OK;
+}
+
+}  // namespace
+
+extern "C" aq_status aq_recurrence_workspace(int64_t rows, int64_t count, int64_t cols, uint64_t* bytes) {
+    AQ_TRY(sizes_ok(rows, 1, cols, bytes));
+    if (count < 0) return AQ_EINVAL;
+    if (count > kMostRows || count * cols > AQ_RECURRENCE_MAX_STATES) return AQ_ESHAPE;
+    *bytes = (uint64_t)recurrence_workspace(rows, count, cols);
+    return AQ_OK;
+}
+
+extern "C" aq_status aq_recurrence_forward(const aq_matrix* z, const aq_matrix* v, const int32_t* d_offsets, int64_t count,
+                                           const uint8_t* d_starts, const float* d_first, const aq_matrix* y, float* d_last, void* d_workspace,
+                                           uint64_t workspace_bytes, void* stream) {
+    AQ_TRY(matrix_ok(z));
+    AQ_TRY(like(v, z));
+    AQ_TRY(like(y, z));
+    AQ_TRY(sequences_ok(z, d_offsets, count));
+    if (!floats_ok(d_first) || !floats_ok(d_last) || (d_first && d_first == d_last)) return AQ_EINVAL;
+    if (!workspace_ok(d_workspace, workspace_bytes, recurrence_workspace(z->rows, count, z->cols))) return AQ_EINVAL;
+    if (count == 0) return AQ_OK;
+    return launch_recurrence_forward(*z, *v, d_offsets, count, d_starts, d_first, *y, d_last, (float*)d_workspace, as_stream(stream));
+}
+
+extern "C" aq_status aq_recurrence_backward(const aq_matrix* dy, const float* d_dlast, const aq_matrix* z, const aq_matrix* v,
+                                            const aq_matrix* y, const int32_t* d_offsets, int64_t count, const uint8_t* d_starts,
+                                            const float* d_first, const aq_matrix* dz, const aq_matrix* dv, float* d_dfirst, void* d_workspace,
+                                            uint64_t workspace_bytes, void* stream) {
+    AQ_TRY(matrix_ok(z));
+    AQ_TRY(like(dy, z));
+    AQ_TRY(like(v, z));
+    AQ_TRY(like(y, z));
+    AQ_TRY(like(dz, z));
+    AQ_TRY(like(dv, z));
+    AQ_TRY(sequences_ok(z, d_offsets, count));
+    if (!floats_ok(d_first) || !floats_ok(d_dlast) || !floats_ok(d_dfirst) || (d_dfirst && (d_dfirst == d_dlast || d_dfirst == d_first)))
+        return AQ_EINVAL;
+    if (!workspace_ok(d_workspace, workspace_bytes, recurrence_workspace(z->rows, count, z->cols))) return AQ_EINVAL;
+    if (count == 0) return AQ_OK;
+    return launch_recurrence_backward(*dy, d_dlast, *z, *v, *y, d_offsets, count, d_starts, d_first, *dz, *dv, d_dfirst, (float*)d_workspace,
+                                      as_stream(stream));
+}
+
+extern "C" aq_status aq_recurrence_step(const aq_matrix* z, const aq_matrix* v, const uint8_t* d_starts, float* d_state, const aq_matrix* y,
+                                        void* stream) {
+    AQ_TRY(matrix_ok(z));
+    AQ_TRY(like(v, z));
+    if (y) AQ_TRY(like(y, z));
+    if (!floats_ok(d_state) || (!d_state && z->rows > 0)) return AQ_EINVAL;
+    return z->rows == 0 ? AQ_OK : launch_recurrence_step(*z, *v, d_starts, d_state, y, as_stream(stream));
+}
+
+// ---- the optimizer
+
+namespace {
+
+constexpr int64_t kMostTensors = 1 << 20;
+
+bool moments_ok(const aq_learned& t) {
+    if (t.moment_bits != 8 && t.moment_bits != 32) return false;
+    if (t.n == 0) return true;
+    if (!t.d_m || !t.d_v) return false;
+    if (t.moment_bits == 8) return t.d_m_scales && t.d_v_scales && !((uintptr_t)t.d_m & 15) && !((uintptr_t)t.d_v & 15);
+    return floats_ok(t.d_m) && floats_ok(t.d_v);
+}
+template <class Each>
+aq_status tensors_ok(const aq_learned* t, int64_t count, Each&& each) {
+    if (count < 0 || (!t && count > 0)) return AQ_EINVAL;
+    if (count > kMostTensors) return AQ_ESHAPE;
+    for (int64_t i = 0; i < count; ++i)
+        if (t[i].n < 0 || !each(t[i])) return AQ_EINVAL;
+    for (int64_t i = 0; i < count; ++i)
+        if (t[i].n > kMostValues) return AQ_ESHAPE;
+    return AQ_OK;
+}
+bool gradient_ok(const aq_learned& t) {
+    if (t.g_dtype != AQ_F32 && t.g_dtype != AQ_F16 && t.g_dtype != AQ_BF16) return false;
+    return (t.n == 0 || t.d_g) && (uintptr_t)t.d_g % dtype_bytes(t.g_dtype) == 0;
+}
+
+}  // namespace
+
+extern "C" aq_status aq_adamw_step(const aq_learned* tensors, int64_t count, const aq_adamw* how, void* stream) {
+    AQ_TRY(tensors_ok(tensors, count, [](const aq_learned& t) {
+        if (!gradient_ok(t) || !moments_ok(t) || (t.n > 0 && !t.d_w) || !floats_ok(t.d_w)) return false;
+        return !t.d_copy || ((t.copy_dtype == AQ_F16 || t.copy_dtype == AQ_BF16) && ((uintptr_t)t.d_copy & 1) == 0);
+    }));
+    if (!how || !(how->beta1 >= 0.0 && how->beta1 < 1.0) || !(how->beta2 >= 0.0 && how->beta2 < 1.0) || !(how->eps >= 0.0) ||
+        !(how->weight_decay >= 0.0) || !(how->max_norm > 0.0))
+        return AQ_EINVAL;
+    if (!how->d_lr && !(how->lr >= 0.0)) return AQ_EINVAL;
+    if (!how->d_step && how->step < 1) return AQ_EINVAL;
+    if (!floats_ok(how->d_lr) || !floats_ok(how->d_norm) || ((uintptr_t)how->d_step & 7)) return AQ_EINVAL;
+    return launch_adamw(tensors, count, *how, as_stream(stream));
+}
+
+extern "C" aq_status aq_grad_norm_workspace(const aq_learned* tensors, int64_t count, uint64_t* bytes) {
+    AQ_TRY(tensors_ok(tensors, count, [](const aq_learned&) { return true; }));
+    if (!bytes) return AQ_EINVAL;
+    *bytes = (uint64_t)grad_norm_workspace(tensors, count);
+    return AQ_OK;
+}
+
+extern "C" aq_status aq_grad_norm(const aq_learned* tensors, int64_t count, float* d_norm, void* d_workspace, uint64_t workspace_bytes, void* stream) {
+    AQ_TRY(tensors_ok(tensors, count, gradient_ok));
+    if (!d_norm || !floats_ok(d_norm) || !workspace_ok(d_workspace, workspace_bytes, grad_norm_workspace(tensors, count))) return AQ_EINVAL;
+    return launch_grad_norm(tensors, count, d_norm, d_workspace, as_stream(stream));
+}
+
+extern "C" aq_status aq_moments_convert(const aq_learned* from, const aq_learned* to, int64_t count, void* stream) {
+    AQ_TRY(tensors_ok(from, count, moments_ok));
+    AQ_TRY(tensors_ok(to, count, moments_ok));
+    for (int64_t i = 0; i < count; ++i)
+        if (from[i].n != to[i].n) return AQ_ESHAPE;
+    return launch_moments_convert(from, to, count, as_stream(stream));
+}
