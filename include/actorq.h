@@ -479,8 +479,24 @@ aq_status aq_mx4_input_grad_workspace(int64_t rows, int64_t n, int64_t k, uint64
 aq_status aq_mx4_input_grad(const aq_matrix* dy, const aq_mx4* w, const aq_matrix* dx, void* d_workspace,
                             uint64_t workspace_bytes, void* stream);
 
-/* ---- A policy with a memory, while it learns: a gated recurrence over sequences, and the optimizer's step.  What is
+/* ---- A policy with a memory, while it learns: gated layers, a gated recurrence over sequences, and the optimizer's step.  What is
  * said above of the learner's operators holds for these. */
+
+/* A gated layer: y = act(gate) * up, gate = x wg^T, up = x wu^T (wg, wu: n rows of k values), and its gradients
+ *   dgate = dy * up * act'(gate), dup = dy * act(gate);  dx = dgate wg + dup wu,  dwg = dgate^T x,  dwu = dup^T x.
+ * All matrices of a call have one type.  The products' sums are fp32; those of fp32 matrices are formed of three bfloat16 parts of
+ * each value (all but 2^-24 of a product), and what depends on a value of theirs that is not finite is not finite, NaN or infinity.
+ * `gate` and `up` may be NULL, both or neither: they receive what the backward pass reads.  dgate and dup are rounded to the
+ * matrices' type in front of its products.  dx may be NULL; dwg and dwu may be NULL, both or neither. */
+typedef enum { AQ_GATE_SIGMOID = 0, AQ_GATE_SILU = 1, AQ_GATE_GELU = 2, AQ_GATE_RELU = 3 } aq_gate; /* silu: a sigmoid(a); gelu: a times the normal distribution's function of a */
+#define AQ_GATED_MAX_VALUES (1LL << 33) /* rows * n, rows * k and n * k */
+aq_status aq_gated_forward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype, uint64_t* bytes);
+aq_status aq_gated_forward(const aq_matrix* x, const aq_matrix* wg, const aq_matrix* wu, int32_t act, const aq_matrix* y,
+                           const aq_matrix* gate, const aq_matrix* up, void* d_workspace, uint64_t workspace_bytes, void* stream);
+aq_status aq_gated_backward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype, uint64_t* bytes);
+aq_status aq_gated_backward(const aq_matrix* dy, const aq_matrix* x, const aq_matrix* wg, const aq_matrix* wu, const aq_matrix* gate,
+                            const aq_matrix* up, int32_t act, const aq_matrix* dx, const aq_matrix* dwg, const aq_matrix* dwu,
+                            void* d_workspace, uint64_t workspace_bytes, void* stream);
 
 /* A gated linear recurrence, unit by unit:  h_t = f_t h_{t-1} + (1 - f_t) v_t,  f = sigmoid(z).
  * z, v and y (which receives h) have one type, one row to a step.  `count` sequences lie behind each other: sequence s has the rows from

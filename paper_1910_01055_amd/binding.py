@@ -34,6 +34,7 @@ EXPORTS = ["aq_policy_create", "aq_policy_destroy", "aq_policy_reserve", "aq_pol
            "aq_layernorm_forward", "aq_layernorm_backward", "aq_layernorm_backward_workspace", "aq_ckpt8_pack", "aq_ckpt8_unpack",
            "aq_ckpt8_weight_grad", "aq_ckpt8_weight_grad_workspace", "aq_mx4_quantize", "aq_mx4_dequantize", "aq_mx4_linear",
            "aq_mx4_linear_workspace", "aq_mx4_matmul", "aq_mx4_input_grad", "aq_mx4_input_grad_workspace",
+           "aq_gated_forward", "aq_gated_backward", "aq_gated_forward_workspace", "aq_gated_backward_workspace",
            "aq_recurrence_forward", "aq_recurrence_backward", "aq_recurrence_step", "aq_recurrence_workspace",
            "aq_adamw_step", "aq_grad_norm", "aq_grad_norm_workspace", "aq_moments_convert"]
 
@@ -160,6 +161,9 @@ def load():
     lib.aq_mx4_input_grad.argtypes = [mat, blk, mat, vp, u64, vp]
     for name in ("aq_ckpt8_weight_grad_workspace", "aq_mx4_linear_workspace", "aq_mx4_input_grad_workspace"):
         getattr(lib, name).argtypes = [i64, i64, i64, C.POINTER(u64)]
+    lib.aq_gated_forward.argtypes = [mat, mat, mat, i32, mat, mat, mat, vp, u64, vp]
+    lib.aq_gated_backward.argtypes = [mat, mat, mat, mat, mat, mat, i32, mat, mat, mat, vp, u64, vp]
+    lib.aq_gated_forward_workspace.argtypes = lib.aq_gated_backward_workspace.argtypes = [i64, i64, i64, i32, C.POINTER(u64)]
     lib.aq_recurrence_workspace.argtypes = [i64, i64, i64, C.POINTER(u64)]
     lib.aq_recurrence_forward.argtypes = [mat, mat, vp, i64, vp, vp, mat, vp, vp, u64, vp]
     lib.aq_recurrence_backward.argtypes = [mat, vp, mat, mat, mat, vp, i64, vp, vp, mat, mat, vp, vp, u64, vp]
@@ -714,6 +718,42 @@ def _plain(t, dtype, n, what):
     if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} is a contiguous {dtype} tensor of {n} values")
     return t.data_ptr()
+
+
+GATE = {"sigmoid": 0, "silu": 1, "gelu": 2, "relu": 3}
+
+
+def _dtype(dtype):
+    if not _DTYPES:
+        _learn_dtypes()
+    return _DTYPES[dtype]
+
+
+def gated_forward_workspace(rows, n, k, dtype):
+    return _size("aq_gated_forward_workspace", rows, n, k, _dtype(dtype))
+
+
+def gated_backward_workspace(rows, n, k, dtype):
+    return _size("aq_gated_backward_workspace", rows, n, k, _dtype(dtype))
+
+
+def gated_forward(x, wg, wu, act, y, gate=None, up=None, workspace=None):
+    """y = act(x wg^T) * (x wu^T); gate and up: what the backward pass reads."""
+    _here(x, wg, wu, y, gate, up, workspace)
+    status = (_lib or load()).aq_gated_forward(_matrix(x), _matrix(wg), _matrix(wu), GATE[act], _matrix(y), None if gate is None else _matrix(gate),
+                                               None if up is None else _matrix(up), _ptr(workspace), _bytes(workspace), _stream())
+    if status:
+        raise AqError(status, "aq_gated_forward")
+
+
+def gated_backward(dy, x, wg, wu, gate, up, act, dx, dwg, dwu, workspace=None):
+    """The gradients of gated_forward; dx may be None, and so may dwg and dwu."""
+    _here(dy, x, wg, wu, gate, up, dx, dwg, dwu, workspace)
+    status = (_lib or load()).aq_gated_backward(_matrix(dy), _matrix(x), _matrix(wg), _matrix(wu), _matrix(gate), _matrix(up), GATE[act],
+                                                None if dx is None else _matrix(dx), None if dwg is None else _matrix(dwg),
+                                                None if dwu is None else _matrix(dwu), _ptr(workspace), _bytes(workspace), _stream())
+    if status:
+        raise AqError(status, "aq_gated_backward")
 
 
 def recurrence_workspace(rows, count, cols):

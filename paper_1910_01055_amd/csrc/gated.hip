@@ -1,0 +1,398 @@
+// Gated layers y = act(x wg^T) * (x wu^T) and their gradients, around the products of gated.hpp: how a product is cut into tiles and
+// slices, what is laid out for it, the gradients of gate and up, the slices' sums, and layers of few rows.
+//
+//   dgate = dy up act'(gate), dup = dy act(gate);  dx = dgate wg + dup wu;  dwg = dgate^T x, dwu = dup^T x
+//
+// The forward pass is one launch: a tile has rows of wg and of wu for the same features, and its gate and up meet in the registers of
+// one lane, where the activation and the product are formed.  The backward pass writes dgate and dup once (a pass over memory), and
+// runs two products on them: both halves of dx are one sum, both weights' gradients one launch.  Operands whose rows are not
+// whole 16-byte pieces are laid out first, and so are fp32 matrices, as three bf16 planes.
+#include "gated.hpp"
+
+namespace aq {
+namespace {
+
+constexpr int kThreads = 256;
+
+// ---- layers of few rows: bound by the weights' way from memory
+// A workgroup takes FEATURES features, each of its four wavefronts a quarter of k: 512 k at a time, eight to a lane.
+constexpr int kFeatures = 2;
+template <class T, int M>
+__global__ void __launch_bounds__(kThreads) k_gated_rows(const T* __restrict__ x, int64_t ldx, const T* __restrict__ wg, int64_t ldg,
+                                                         const T* __restrict__ wu, int64_t ldu, int act, T* __restrict__ y, int64_t ldy,
+                                                         T* __restrict__ gate, int64_t ldgate, T* __restrict__ up, int64_t ldup, int rows, int n, int k) {
+    __shared__ float part[4][2 * kFeatures * M];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, f0 = blockIdx.x * kFeatures;
+    float s[2][kFeatures][M];
+#pragma unroll
+    for (int i = 0; i < 2 * kFeatures * M; ++i) (&s[0][0][0])[i] = 0.0f;
+    for (int at = wave * 512 + lane * 8; at < k; at += 4 * 512) {
+        const int left = k - at;
+        Piece<T> pw[2][kFeatures], px[M];
+#pragma unroll
+        for (int f = 0; f < kFeatures; ++f) {
+            const int64_t row = f0 + f < n ? f0 + f : n - 1;
+            pw[0][f].load(wg + row * ldg + at, left);
+            pw[1][f].load(wu + row * ldu + at, left);
+        }
+#pragma unroll
+        for (int m = 0; m < M; ++m) px[m].load(x + (m < rows ? m : rows - 1) * ldx + at, left);
+        float vx[M][8];
+#pragma unroll
+        for (int m = 0; m < M; ++m) px[m].get(vx[m]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int f = 0; f < kFeatures; ++f) {
+                float w[8];
+                pw[h][f].get(w);
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s[h][f][m] = fmaf(w[j], vx[m][j], s[h][f][m]);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * kFeatures * M; ++i) {
+        const float v = lanes_sum<64>((&s[0][0][0])[i]);
+        if (lane == 0) part[wave][i] = v;
+    }
+    __syncthreads();
+    const int f = threadIdx.x / M, m = threadIdx.x % M;
+    if (f >= kFeatures || f0 + f >= n || m >= rows) return;
+    float g = 0.0f, u = 0.0f, slope;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) g += part[w][f * M + m], u += part[w][kFeatures * M + f * M + m];
+    y[m * ldy + f0 + f] = (T)(gate_act(g, act, slope) * u);
+    if (gate) {
+        gate[m * ldgate + f0 + f] = (T)g;
+        up[m * ldup + f0 + f] = (T)u;
+    }
+}
+
+// ---- what is laid out
+// three bf16 values whose sum a value is (one that rounds up to infinity is cut)
+__device__ __forceinline__ void split3(float v, float& a, float& b, float& c) {
+    const auto round = [](float x) __attribute__((always_inline)) { return (float)(bf16_t)x; };
+    a = round(v);
+    if (fabsf(a) > 3.4e38f && fabsf(v) <= 3.402823466e38f) a = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+    const bool finite = fabsf(a) <= 3.402823466e38f;
+    const float rest = finite ? v - a : 0.0f;
+    b = round(rest);
+    c = rest - b;
+}
+// eight values into a row of H: one plane, or three of an fp32 matrix's
+template <class T, class H>
+__device__ __forceinline__ void put_planes(const float (&v)[8], H* __restrict__ to, int64_t plane) {
+    Piece<H> p;
+    if constexpr (std::is_same<T, float>::value) {
+        float a[8], b[8], c[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) split3(v[j], a[j], b[j], c[j]);
+        p.set(a);
+        p.store(to, 8);
+        p.set(b);
+        p.store(to + plane, 8);
+        p.set(c);
+        p.store(to + 2 * plane, 8);
+    } else {
+        p.set(v);
+        p.store(to, 8);
+    }
+}
+template <class T>
+using Half = typename std::conditional<std::is_same<T, float>::value, bf16_t, T>::type;
+
+struct Lay {
+    const void* from;
+    void* to;
+    int64_t rows, cols, ld, pitch, pieces;  // pitch: of a laid-out row, a multiple of eight; pieces: of eight values, of all rows
+};
+struct Lays {
+    Lay job[3];
+};
+// rows of whole pieces, zeros behind their ends
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_lay_out(Lays all) {
+    int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    int which = 0;
+    while (which < 2 && i >= all.job[which].pieces) i -= all.job[which++].pieces;
+    const Lay& job = all.job[which];
+    if (i >= job.pieces) return;
+    const int64_t across = job.pitch / 8, row = i / across;
+    const int at = (int)(i - row * across) * 8;
+    Piece<T> p;
+    p.load((const T*)job.from + row * job.ld + at, (int)(job.cols - at));
+    float v[8];
+    p.get(v);
+    put_planes<T>(v, (Half<T>*)job.to + row * job.pitch + at, job.rows * job.pitch);
+}
+
+// dgate and dup, [rows][pitch], zeros behind their ends
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_gated_slopes(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ gate, int64_t ldgate,
+                                                           const T* __restrict__ up, int64_t ldup, int act, Half<T>* __restrict__ dgate,
+                                                           Half<T>* __restrict__ dup, int64_t rows, int cols, int pitch) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, across = pitch / 8, row = i / across;
+    if (row >= rows) return;
+    const int at = (int)(i - row * across) * 8, left = cols - at;
+    Piece<T> pd, pg, pu;
+    pd.load(dy + row * lddy + at, left);
+    pg.load(gate + row * ldgate + at, left);
+    pu.load(up + row * ldup + at, left);
+    float d[8], g[8], u[8];
+    pd.get(d);
+    pg.get(g);
+    pu.get(u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float slope;
+        const float h = gate_act(g[j], act, slope);
+        g[j] = d[j] * u[j] * slope;
+        u[j] = d[j] * h;
+    }
+    const int64_t plane = rows * pitch;
+    put_planes<T>(g, dgate + row * pitch + at, plane);
+    put_planes<T>(u, dup + row * pitch + at, plane);
+}
+
+// ---- the slices' sums, in their order
+template <class T, bool GATED>
+__global__ void __launch_bounds__(kThreads) k_gated_join(const float* __restrict__ part, int slices, int64_t stride, int64_t m, int64_t c, Outputs out,
+                                                         int outputs, int act) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    auto total = [slices, stride](const float* p) __attribute__((always_inline)) {
+        float s = 0.0f;
+        int k = 0;
+        for (; k + 4 <= slices; k += 4) {
+            const float a = p[k * stride], b = p[(k + 1) * stride], d = p[(k + 2) * stride], e = p[(k + 3) * stride];
+            s = s + a + b + d + e;
+        }
+        for (; k < slices; ++k) s += p[k * stride];
+        return s;
+    };
+    const int64_t which = i / (m * c), row = (i - which * m * c) / c, col = i - which * m * c - row * c;
+    if (which >= (GATED ? 1 : outputs)) return;
+    if constexpr (GATED) {
+        const float g = total(part + row * out.ld_part + col), u = total(part + out.part_second + row * out.ld_part + col);
+        float slope;
+        ((T*)out.first)[row * out.ld_first + col] = (T)(gate_act(g, act, slope) * u);
+        if (out.second) {
+            ((T*)out.second)[row * out.ld_second + col] = (T)g;
+            ((T*)out.third)[row * out.ld_third + col] = (T)u;
+        }
+    } else {
+        const float s = total(part + which * out.part_second + row * out.ld_part + col);
+        if (which) ((T*)out.second)[row * out.ld_second + col] = (T)s;
+        else ((T*)out.first)[row * out.ld_first + col] = (T)s;
+    }
+}
+
+// ---- plans
+struct Plan {
+    int s, slices, chunks;  // tile, slices of so many chunks
+};
+// The tile and the slices by an estimate in us: a launch, the chunks of a workgroup one after the other, each as long as `alone` while few
+// workgroups are about and `full` while as many as fit are, and the join's launch and bytes.
+Plan plan_of(Form form, int64_t m, int64_t c, int64_t t, int segments) {
+    struct Kind {
+        int s, at_once;
+        float launch, alone, full;
+    };
+    constexpr Kind kinds[] = {{64, 768, 3.0f, 0.35f, 0.90f}, {128, 256, 3.5f, 0.60f, 0.75f}, {256, 256, 5.0f, 1.10f, 1.80f}};
+    const int64_t outputs = form == kWeightGrad ? 2 : 1, each = t > 0 ? (t + kChunk - 1) / kChunk : 1, all = each * segments;
+    Plan best{64, 1, (int)all};
+    float least = 3.0e38f;
+    for (const Kind& k : kinds) {
+        const int64_t tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + (form == kForward ? k.s / 2 : k.s) - 1) / (form == kForward ? k.s / 2 : k.s)) * outputs;
+        for (int64_t want = 1; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
+            const int64_t chunks = (all + want - 1) / want, z = (all + chunks - 1) / chunks, wgs = tiles * z;
+            const int64_t values = z * m * c * (form == kInputGrad ? 1 : 2);
+            if (!grid_ok(wgs, 2 * k.s) || (z > 1 && (!grid_ok((m * c * outputs + kThreads - 1) / kThreads, kThreads) || values * 4 > (1LL << 30)))) continue;
+            const int64_t busy = wgs <= 256 ? wgs : (wgs + 255) / 256 * 256;
+            const int64_t turns = (busy + k.at_once - 1) / k.at_once;
+            const float share = (float)busy / (float)k.at_once;
+            const float chunk = turns > 1 ? k.full * (float)turns : k.alone + (k.full - k.alone) * share * share;
+            const float join = z > 1 ? 3.0f + (float)values * 4.0f * (1.0f / 3.5e6f) : 0.0f;
+            const float us = k.launch + join + (float)chunks * chunk;
+            if (us < least) {
+                least = us;
+                best = {k.s, (int)z, (int)chunks};
+            }
+        }
+    }
+    return best;
+}
+int planes_of(int32_t dtype) { return dtype == AQ_F32 ? 3 : 1; }
+int segments_count(Form form, int32_t dtype) { return (dtype == AQ_F32 ? 6 : 1) * (form == kInputGrad ? 2 : 1); }
+int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
+int64_t up256(int64_t n) { return (n + 255) & ~(int64_t)255; }
+int64_t laid_bytes(int64_t rows, int64_t cols, int32_t dtype) { return up256(rows * up8(cols) * 2 * planes_of(dtype)); }
+int64_t part_bytes(Form form, int64_t m, int64_t c, int64_t t, int32_t dtype) {
+    const Plan p = plan_of(form, m, c, t, segments_count(form, dtype));
+    return p.slices > 1 ? up256((int64_t)p.slices * m * c * (form == kInputGrad ? 1 : 2) * 4) : 0;
+}
+constexpr int64_t kFewRows = 4;
+
+bool in_place(const aq_matrix& m) { return m.dtype != AQ_F32 && ((uintptr_t)m.d & 15) == 0 && m.ld % 8 == 0 && m.cols % 8 == 0; }
+
+// a matrix as an operand: where it lies, or laid out in the workspace
+struct Layer {
+    uint8_t* ws;
+    Lays lays{};
+    int jobs = 0;
+    int32_t dtype;
+    Operand operand(const aq_matrix& m) {
+        Operand o{};
+        if (in_place(m)) {
+            o.base = (const uint8_t*)m.d;
+            o.ld = (int32_t)(m.ld * 2);
+        } else {
+            const int64_t pitch = up8(m.cols);
+            lays.job[jobs++] = {m.d, ws, m.rows, m.cols, m.ld, pitch, m.rows * (pitch / 8)};
+            o.base = ws;
+            o.ld = (int32_t)(pitch * 2);
+            o.plane = m.rows * pitch * 2;
+            ws += laid_bytes(m.rows, m.cols, m.dtype);
+        }
+        o.bytes = m.rows > 0 ? (m.rows - 1) * o.ld + up8(m.cols) * 2 : 0;
+        return o;
+    }
+    aq_status run(hipStream_t st) {
+        int64_t pieces = 0;
+        for (int i = 0; i < jobs; ++i) pieces += lays.job[i].pieces;
+        if (pieces == 0) return AQ_OK;
+        if (!grid_ok((pieces + kThreads - 1) / kThreads, kThreads)) return AQ_ESHAPE;
+        return with_dtype(dtype, [&](auto t) {
+            k_lay_out<decltype(t)><<<(unsigned)((pieces + kThreads - 1) / kThreads), kThreads, 0, st>>>(lays);
+            return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+        });
+    }
+};
+// a product's sums: planned, run, joined
+aq_status run_product(Form form, int32_t dtype, Operand a, Operand b, int64_t m, int64_t c, int64_t t, Outputs out, int act, uint8_t* ws, hipStream_t st) {
+    int count;
+    Product p{};
+    p.segments = segments_of(dtype == AQ_F32, form == kInputGrad ? 2 : 1, count);
+    const Plan plan = plan_of(form, m, c, t, count);
+    p.a = a;
+    p.b = b;
+    p.m = m, p.c = c, p.t = t;
+    p.each = t > 0 ? (int32_t)((t + kChunk - 1) / kChunk) : 1;
+    p.all = p.each * count;
+    p.chunks = plan.chunks;
+    p.tiles_m = (int32_t)((m + plan.s - 1) / plan.s);
+    const int features = form == kForward ? plan.s / 2 : plan.s;
+    p.tiles_c = (int32_t)((c + features - 1) / features);
+    const bool part = plan.slices > 1;
+    const int64_t outputs = form == kInputGrad ? 1 : 2;
+    if (part) {
+        out.part = (float*)ws;
+        out.ld_part = form == kForward ? 2 * c : c;
+        out.part_second = form == kForward ? c : m * c;
+        out.part_stride = outputs * m * c;
+    }
+    const aq_status s = form == kForward      ? launch_gated_forward_product(dtype, plan.s, part, p, out, act, plan.slices, st)
+                        : form == kInputGrad ? launch_gated_input_product(dtype, plan.s, part, p, out, plan.slices, st)
+                                             : launch_gated_weight_product(dtype, plan.s, part, p, out, plan.slices, st);
+    if (s != AQ_OK || !part) return s;
+    const int64_t values = m * c * (form == kWeightGrad ? 2 : 1);
+    return with_dtype(dtype, [&](auto type) {
+        using T = decltype(type);
+        const unsigned grid = (unsigned)((values + kThreads - 1) / kThreads);
+        if (form == kForward) k_gated_join<T, true><<<grid, kThreads, 0, st>>>(out.part, plan.slices, out.part_stride, m, c, out, 1, act);
+        else k_gated_join<T, false><<<grid, kThreads, 0, st>>>(out.part, plan.slices, out.part_stride, m, c, out, (int)(values / (m * c)), act);
+        return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+    });
+}
+
+}  // namespace
+
+int64_t gated_forward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype) {
+    if (rows <= kFewRows) return 0;
+    return laid_bytes(rows, k, dtype) + 2 * laid_bytes(n, k, dtype) + part_bytes(kForward, rows, n, k, dtype);
+}
+int64_t gated_backward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype) {
+    const int64_t dx = part_bytes(kInputGrad, rows, k, n, dtype), dw = part_bytes(kWeightGrad, n, k, rows, dtype);
+    return laid_bytes(rows, k, dtype) + 2 * laid_bytes(n, k, dtype) + 2 * laid_bytes(rows, n, dtype) + (dx > dw ? dx : dw);
+}
+
+aq_status launch_gated_forward(const aq_matrix& x, const aq_matrix& wg, const aq_matrix& wu, int act, const aq_matrix& y, const aq_matrix* gate,
+                               const aq_matrix* up, void* ws, hipStream_t st) {
+    const int64_t n = wg.rows, k = x.cols;
+    if (x.rows <= kFewRows) {
+        return with_dtype(x.dtype, [&](auto t) {
+            using T = decltype(t);
+            auto go = [&](auto rows) {
+                k_gated_rows<T, decltype(rows)::value><<<(unsigned)((n + kFeatures - 1) / kFeatures), kThreads, 0, st>>>(
+                    (const T*)x.d, x.ld, (const T*)wg.d, wg.ld, (const T*)wu.d, wu.ld, act, (T*)y.d, y.ld, gate ? (T*)gate->d : nullptr,
+                    gate ? gate->ld : 0, up ? (T*)up->d : nullptr, up ? up->ld : 0, (int)x.rows, (int)n, (int)k);
+                return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+            };
+            if (x.rows == 1) return go(std::integral_constant<int, 1>());
+            if (x.rows == 2) return go(std::integral_constant<int, 2>());
+            return go(std::integral_constant<int, 4>());
+        });
+    }
+    Layer lay{(uint8_t*)ws};
+    lay.dtype = x.dtype;
+    const Operand a = lay.operand(x);
+    Operand b = lay.operand(wg);
+    const Operand b2 = lay.operand(wu);
+    if (b.ld != b2.ld || b.plane != b2.plane) return AQ_ESHAPE;
+    b.other = b2.base - b.base;
+    const aq_status s = lay.run(st);
+    if (s != AQ_OK) return s;
+    Outputs out{};
+    out.first = y.d, out.ld_first = y.ld;
+    if (gate) out.second = gate->d, out.ld_second = gate->ld, out.third = up->d, out.ld_third = up->ld;
+    return run_product(kForward, x.dtype, a, b, x.rows, n, k, out, act, lay.ws, st);
+}
+
+aq_status launch_gated_backward(const aq_matrix& dy, const aq_matrix& x, const aq_matrix& wg, const aq_matrix& wu, const aq_matrix& gate,
+                                const aq_matrix& up, int act, const aq_matrix* dx, const aq_matrix* dwg, const aq_matrix* dwu, void* ws,
+                                hipStream_t st) {
+    const int64_t m = dy.rows, n = dy.cols, k = x.cols, pitch = up8(n);
+    Layer lay{(uint8_t*)ws};
+    lay.dtype = x.dtype;
+    Operand ox{}, ow{}, d{};
+    if (dwg) ox = lay.operand(x);
+    if (dx && m > 0) {
+        ow = lay.operand(wg);
+        const Operand second = lay.operand(wu);
+        if (ow.ld != second.ld || ow.plane != second.plane) return AQ_ESHAPE;
+        ow.other = second.base - ow.base;
+    }
+    aq_status s = lay.run(st);
+    if (s != AQ_OK) return s;
+    d.base = lay.ws;
+    d.ld = (int32_t)(pitch * 2);
+    d.plane = m * pitch * 2;
+    d.other = laid_bytes(m, n, x.dtype);
+    d.bytes = m * pitch * 2;
+    lay.ws += 2 * d.other;
+    if (m > 0) {
+        const int64_t pieces = m * (pitch / 8);
+        if (!grid_ok((pieces + kThreads - 1) / kThreads, kThreads)) return AQ_ESHAPE;
+        s = with_dtype(x.dtype, [&](auto t) {
+            using T = decltype(t);
+            k_gated_slopes<T><<<(unsigned)((pieces + kThreads - 1) / kThreads), kThreads, 0, st>>>(
+                (const T*)dy.d, dy.ld, (const T*)gate.d, gate.ld, (const T*)up.d, up.ld, act, (Half<T>*)d.base, (Half<T>*)(d.base + d.other), m, (int)n,
+                (int)pitch);
+            return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+        });
+        if (s != AQ_OK) return s;
+    }
+    if (dx && m > 0) {
+        Outputs out{};
+        out.first = dx->d, out.ld_first = dx->ld;
+        s = run_product(kInputGrad, x.dtype, d, ow, m, k, n, out, act, lay.ws, st);
+        if (s != AQ_OK) return s;
+    }
+    if (!dwg) return AQ_OK;
+    Outputs out{};
+    out.first = dwg->d, out.ld_first = dwg->ld, out.second = dwu->d, out.ld_second = dwu->ld;
+    return run_product(kWeightGrad, x.dtype, d, ox, n, k, m, out, act, lay.ws, st);
+}
+
+}  // namespace aq

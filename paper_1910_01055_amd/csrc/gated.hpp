@@ -1,0 +1,291 @@
+// The gated layer's products (internal to the library): C[m][c] = sum_t A(m, t) B(t, c) on the bf16 or fp16 matrix cores, for operands
+// that have t along their rows or along their columns.
+//
+// Values are 16 bits wide.  fp32 matrices come as three bf16 planes, whose sum they are, and their products as the six pairs of planes
+// that reach 2^-24 of them: pairs, like the two halves of dx = dgate wg + dup wu, are segments of one long sum over t.
+#pragma once
+#include "learner.hpp"
+#include "product_device.hpp"
+
+namespace aq {
+
+typedef f16_t v8f16 __attribute__((ext_vector_type(8)));
+typedef short v4s16 __attribute__((ext_vector_type(4)));
+
+constexpr int kChunk = 64;  // t at a time
+
+struct Operand {
+    const uint8_t* base;
+    int64_t plane, other;  // bytes from a plane to the next one, and from the first of two matrices to the second
+    int64_t bytes;         // of a plane, from its first value to its last
+    int32_t ld;            // bytes of a row
+};
+struct Product {
+    Operand a, b;
+    int64_t m, c, t;      // of one output; t: of a segment
+    uint64_t segments;    // five bits each: plane of a, plane of b, which matrices
+    int32_t each, chunks;  // chunks of a segment, of a slice
+    int32_t all;          // of all segments
+    int32_t tiles_m, tiles_c;  // of one output, in tiles (gated: of S / 2 features)
+};
+struct Outputs {
+    void *first, *second, *third;  // gated: y, gate, up (the last two may be NULL); two weight gradients; dx
+    int64_t ld_first, ld_second, ld_third;
+    float* part;          // slices' sums: [slice][m][ld_part], the second output `part_second` columns (or rows) behind the first
+    int64_t ld_part, part_stride, part_second;
+};
+enum Form { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
+
+// what three planes or one hold: pairs in the order of their size, the smallest first
+constexpr int kPlanes3[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+inline uint64_t segments_of(bool planes, int halves, int& count) {
+    uint64_t s = 0;
+    count = 0;
+    for (int p = 0; p < (planes ? 6 : 1); ++p)
+        for (int h = 0; h < halves; ++h) {
+            const uint64_t code = planes ? kPlanes3[p][0] | kPlanes3[p][1] << 2 | h << 4 : h << 4;
+            s |= code << (5 * count++);
+        }
+    return s;
+}
+
+__device__ __forceinline__ float gate_act(float a, int act, float& slope) {
+    if (act == AQ_GATE_RELU) {
+        slope = a > 0.0f ? 1.0f : 0.0f;
+        return a > 0.0f ? a : a != a ? a : 0.0f;
+    }
+    if (act == AQ_GATE_GELU) {
+        // a Phi(a), Phi(a) = erfc(-a / sqrt 2) / 2: without a difference from 1 for negative a
+        const float p = 0.5f * erfcf(-0.70710678f * a);
+        slope = p + a * __builtin_amdgcn_exp2f(-0.72134752f * a * a) * 0.39894228f;
+        if (fabsf(a) > 3.0e18f) slope = p;  // (a^2 infinite)
+        return p == 0.0f ? 0.0f : a * p;
+    }
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(a)), large = 1.0f / (1.0f + e), small = e * large;
+    const float s = a >= 0.0f ? large : small, rest = a >= 0.0f ? small : large;
+    if (act == AQ_GATE_SIGMOID) {
+        slope = s * rest;
+        return s;
+    }
+    slope = s == 0.0f ? 0.0f : s * (1.0f + (rest == 0.0f ? 0.0f : a * rest));
+    return s == 0.0f ? 0.0f : a * s;
+}
+
+template <class H>
+__device__ __forceinline__ v16f32 mfma16(v4u a, v4u b, v16f32 c) {
+    if constexpr (std::is_same<H, bf16_t>::value)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf16, a), __builtin_bit_cast(v8bf16, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8f16, a), __builtin_bit_cast(v8f16, b), c, 0, 0, 0);
+}
+
+// A chunk of an operand in LDS.  t along the rows of memory's matrix (kAcross): S rows of 64 t, 128 bytes each, 16-byte piece s of row r in
+// place s ^ (r / 2 mod 8).  t along its columns: 64 rows of S values, 32-byte piece p of row t in place p ^ 2 (t mod 4); the read
+// transposes four rows of 16 columns at once.  Either way the rows (pieces) that a read takes at once lie in different banks, and either way
+// pieces lie so that a wavefront's loads to LDS fill 1 KB in a row: what is permuted is which piece of memory a lane asks for.
+template <int S, bool kAcross>
+struct Tile {
+    static constexpr int NT = 2 * S, J = 4;
+    // byte offset in memory of this thread's unit j, from the tile's first value of the chunk
+    static __device__ __forceinline__ int offset(int tid, int j, int ld) {
+        const int u = tid + NT * j;
+        if constexpr (kAcross) return (u >> 3) * ld + piece(tid) * 16;
+        const int t = u / (S / 8), s = u % (S / 8);
+        return t * ld + ((((s >> 1) ^ ((t & 3) << 1 & (S / 16 - 1))) << 4) + ((s & 1) << 3)) * 2;
+    }
+    static __device__ __forceinline__ int piece(int tid) { return (tid & 7) ^ ((tid >> 4) & 7); }
+    // 32 rows (columns) from `at` on, 16 t from 16 Q on, as an MFMA operand: lane l has row l mod 32, t = 8 (l / 32) .. + 7
+    static __device__ __forceinline__ v4u read(const uint8_t* tile, int at, int q, int lane) {
+        if constexpr (kAcross) {
+            const int r = lane & 31;
+            return *(const v4u*)(tile + (at + r) * 128 + (((2 * q + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4));
+        } else {
+            typedef __attribute__((address_space(3))) v4s16* lds_ptr;
+            const int i = lane & 15, t = 16 * q + 8 * (lane >> 5) + (i >> 2), col = at + (lane & 16);
+            const uint8_t* p = tile + t * 2 * S + (((col >> 4) ^ ((t & 3) << 1 & (S / 16 - 1))) << 5) + (i & 3) * 8;
+            const v4s16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+            const v4s16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * 2 * S));
+            return __builtin_bit_cast(v4u, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+constexpr int gated_buffers(int s) { return s == 256 ? 2 : 3; }
+constexpr int gated_lds(int s) { return gated_buffers(s) * 2 * s * 128; }
+
+// C tile of S x S (gated: S rows of S / 2 features, gate and up in blocks of 32 columns in turn), a wavefront 32 TM rows of 64 columns.
+// A chunk's products come in four turns of 16 t, whose operands are read a turn ahead; behind the third all of a chunk is in registers, and
+// the barrier there hands its buffer to the chunk kBufs ahead.
+template <class H, class T, int S, Form F, bool PART>
+__global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs out, int act) {
+    constexpr bool kAcrossA = F != kWeightGrad, kAcrossB = F == kForward;
+    using TA = Tile<S, kAcrossA>;
+    using TB = Tile<S, kAcrossB>;
+    constexpr int TM = S / 64, NT = 2 * S, kBufs = gated_buffers(S), kSide = S * 128, kBuf = 2 * kSide, J = 4;
+    static_assert(NT / 64 * 32 * kOutRow<float, 2> <= kBufs * kBuf, "results leave through the buffers");
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31;
+    Place at = place_of_workgroup((uint32_t)(F == kWeightGrad ? 2 * p.tiles_m : p.tiles_m), (uint32_t)p.tiles_c);
+    const int second = F == kWeightGrad && at.m >= (uint32_t)p.tiles_m;  // which of two outputs
+    if (second) at.m -= p.tiles_m;
+    const int64_t m0 = (int64_t)at.m * S, c0 = (int64_t)at.c * (F == kForward ? S / 2 : S);
+    const int wm = (wave & 1) * (S / 2), wc = (wave >> 1) * 64;
+    // ---- loads
+    int off_a[J], off_b[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        off_a[j] = TA::offset(tid, j, p.a.ld);
+        if constexpr (F == kForward) {  // rows 64 i .. of the tile: 32 of wg and 32 of wu from feature 32 i on
+            const int row = (tid + NT * j) >> 3;
+            off_b[j] = ((row >> 6 << 5) + (row & 31)) * p.b.ld + TB::piece(tid) * 16;
+        } else {
+            off_b[j] = TB::offset(tid, j, p.b.ld);
+        }
+    }
+    const int first = (int)at.z * p.chunks, end = first + p.chunks < p.all ? first + p.chunks : p.all;
+    int segment = first / p.each, ahead = first;  // what is loaded next
+    int64_t t0 = (int64_t)(first - segment * p.each) * kChunk;
+    auto fetch = [&](int buf) __attribute__((always_inline)) {
+        const int code = (int)(p.segments >> (5 * (segment < 12 ? segment : 0))) & 31;
+        const int64_t which = F == kWeightGrad ? second : code >> 4;
+        const bool more = ahead < end;
+        const int64_t ta = kAcrossA ? m0 * p.a.ld + t0 * 2 : t0 * p.a.ld + m0 * 2;
+        const int64_t tb = kAcrossB ? c0 * p.b.ld + t0 * 2 : t0 * p.b.ld + c0 * 2;
+        const uint8_t* const pa = p.a.base + (code & 3) * p.a.plane + which * p.a.other;
+        const uint8_t* const pb = p.b.base + (code >> 2 & 3) * p.b.plane + (F == kInputGrad ? which * p.b.other : 0);
+        Window wa, wb, wb2;
+        wa.set(pa, ta, more ? p.a.bytes : 0);
+        wb.set(pb, tb, more ? p.b.bytes : 0);
+        if constexpr (F == kForward) wb2.set(pb + p.b.other, tb, more ? p.b.bytes : 0);
+        const int left = p.t - t0 < kChunk ? (int)(p.t - t0) : kChunk;
+        const bool there_a = !kAcrossA || 8 * TA::piece(tid) < left, there_b = !kAcrossB || 8 * TB::piece(tid) < left;
+        uint8_t* const to = lds + buf * kBuf + wave * 1024;
+#pragma unroll
+        for (int j = 0; j < J; ++j) load_to_lds(wa, there_a ? off_a[j] : Window::kOutside, to + NT * j * 16);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const bool up = F == kForward && ((wave * 64 + NT * j) >> 3 & 32);
+            load_to_lds(up ? wb2 : wb, there_b ? off_b[j] : Window::kOutside, to + kSide + NT * j * 16);
+        }
+        ++ahead;
+        t0 += kChunk;
+        if (t0 >= p.t) t0 = 0, ++segment;
+    };
+    // ---- products
+    v16f32 acc[2][TM];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    v4u oa[2][TM], ob[2][2];
+    auto read = [&](auto turn, const uint8_t* from) __attribute__((always_inline)) {
+        constexpr int Q = decltype(turn)::value;
+#pragma unroll
+        for (int j = 0; j < TM; ++j) oa[Q & 1][j] = TA::read(from, wm + 32 * j, Q, lane);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) ob[Q & 1][i] = TB::read(from + kSide, wc + 32 * i, Q, lane);
+    };
+    auto products = [&](auto turn) __attribute__((always_inline)) {
+        constexpr int Q = decltype(turn)::value;
+        __builtin_amdgcn_sched_barrier(0);  // (the order stays: operands are requested a turn ahead)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < TM; ++j) acc[i][j] = mfma16<H>(ob[Q & 1][i], oa[Q & 1][j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr std::integral_constant<int, 0> q0{};
+    constexpr std::integral_constant<int, 1> q1{};
+    constexpr std::integral_constant<int, 2> q2{};
+    constexpr std::integral_constant<int, 3> q3{};
+#pragma unroll
+    for (int b = 0; b < kBufs; ++b) fetch(b);
+    wait_loads<(kBufs - 1) * 2 * J>();
+    lds_barrier();
+    int buf = 0;
+    read(q0, lds);
+    for (int c = first; c < end; ++c) {
+        const uint8_t* const now = lds + buf * kBuf;
+        const int next = buf + 1 == kBufs ? 0 : buf + 1;
+        read(q1, now);
+        products(q0);
+        read(q2, now);
+        products(q1);
+        read(q3, now);
+        products(q2);
+        wait_loads<(kBufs - 2) * 2 * J>();  // the next chunk is there,
+        lds_barrier();                      // and all of this one in registers
+        fetch(buf);
+        read(q0, lds + next * kBuf);
+        products(q3);
+        buf = next;
+    }
+    wait_loads<0>();  // (chunks behind the last one, which arrive as zeros)
+    lds_barrier();
+    // ---- results
+    uint8_t* const place = lds + wave * (32 * kOutRow<float, 2>);
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+        const int64_t row = m0 + wm + 32 * j, rows = p.m - row;
+        if constexpr (F == kForward) {
+            const int64_t f = c0 + (wave >> 1) * 32, cols = p.c - f;
+            if constexpr (PART) {
+                float* const to = out.part + at.z * out.part_stride + row * out.ld_part + f;
+                store_rows<float, 1>(place, lane, to, out.ld_part, rows, cols, [&](int, int q, int e) { return acc[0][j][4 * q + e]; });
+                store_rows<float, 1>(place, lane, to + out.part_second, out.ld_part, rows, cols, [&](int, int q, int e) { return acc[1][j][4 * q + e]; });
+            } else {
+                store_rows<T, 1>(place, lane, (T*)out.first + row * out.ld_first + f, out.ld_first, rows, cols, [&](int, int q, int e) {
+                    float slope;
+                    return gate_act(acc[0][j][4 * q + e], act, slope) * acc[1][j][4 * q + e];
+                });
+                if (out.second) {
+                    store_rows<T, 1>(place, lane, (T*)out.second + row * out.ld_second + f, out.ld_second, rows, cols,
+                                     [&](int, int q, int e) { return acc[0][j][4 * q + e]; });
+                    store_rows<T, 1>(place, lane, (T*)out.third + row * out.ld_third + f, out.ld_third, rows, cols,
+                                     [&](int, int q, int e) { return acc[1][j][4 * q + e]; });
+                }
+            }
+        } else {
+            const int64_t col = c0 + wc, cols = p.c - col;
+            if constexpr (PART) {
+                store_rows<float, 2>(place, lane, out.part + at.z * out.part_stride + second * out.part_second + row * out.ld_part + col, out.ld_part, rows, cols,
+                                     [&](int i, int q, int e) { return acc[i][j][4 * q + e]; });
+            } else {
+                T* const to = second ? (T*)out.second : (T*)out.first;
+                const int64_t ld = second ? out.ld_second : out.ld_first;
+                store_rows<T, 2>(place, lane, to + row * ld + col, ld, rows, cols, [&](int i, int q, int e) { return acc[i][j][4 * q + e]; });
+            }
+        }
+    }
+}
+
+// one product as planned; `type`: of its matrices (AQ_F32: three planes of bf16)
+aq_status launch_gated_forward_product(int type, int s, bool part, const Product& p, const Outputs& out, int act, int slices, hipStream_t st);
+aq_status launch_gated_input_product(int type, int s, bool part, const Product& p, const Outputs& out, int slices, hipStream_t st);
+aq_status launch_gated_weight_product(int type, int s, bool part, const Product& p, const Outputs& out, int slices, hipStream_t st);
+
+template <Form F>
+aq_status launch_gated_product(int type, int s, bool part, const Product& p, const Outputs& out, int act, int slices, hipStream_t st) {
+    auto go = [&](auto h, auto t, auto size, auto parts) {
+        using H = decltype(h);
+        using T = decltype(t);
+        constexpr int S = decltype(size)::value;
+        auto* const k = k_gated_product<H, T, S, F, decltype(parts)::value>;
+        const int64_t grid = (int64_t)p.tiles_m * (F == kWeightGrad ? 2 : 1) * p.tiles_c * slices;
+        if (!grid_ok(grid, 2 * S)) return AQ_ESHAPE;
+        if (!allow_lds<H, T, decltype(size), decltype(parts), std::integral_constant<int, F>>((const void*)k, gated_lds(S))) return AQ_EHIP;
+        k<<<(unsigned)grid, 2 * S, gated_lds(S), st>>>(p, out, act);
+        return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+    };
+    auto sized = [&](auto h, auto t, auto parts) {
+        if (s == 256) return go(h, t, std::integral_constant<int, 256>(), parts);
+        if (s == 128) return go(h, t, std::integral_constant<int, 128>(), parts);
+        return go(h, t, std::integral_constant<int, 64>(), parts);
+    };
+    if (part) return type == AQ_F16 ? sized(f16_t(), float(), std::true_type()) : sized(bf16_t(), float(), std::true_type());
+    if (type == AQ_F32) return sized(bf16_t(), float(), std::false_type());
+    if (type == AQ_F16) return sized(f16_t(), f16_t(), std::false_type());
+    return sized(bf16_t(), bf16_t(), std::false_type());
+}
+
+}  // namespace aq

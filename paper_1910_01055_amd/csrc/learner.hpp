@@ -51,6 +51,14 @@ aq_status launch_weight_grad(const aq_matrix& dy, const aq_ckpt8& kept, const aq
                              hipStream_t st);
 int64_t input_grad_workspace(int64_t rows, int64_t n, int64_t k);
 aq_status launch_input_grad(const aq_matrix& dy, const aq_mx4& w, const aq_matrix& dx, void* ws, uint64_t ws_bytes, hipStream_t st);
+// ---- gated.hip
+int64_t gated_forward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype);
+int64_t gated_backward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype);
+aq_status launch_gated_forward(const aq_matrix& x, const aq_matrix& wg, const aq_matrix& wu, int act, const aq_matrix& y, const aq_matrix* gate,
+                               const aq_matrix* up, void* ws, hipStream_t st);
+aq_status launch_gated_backward(const aq_matrix& dy, const aq_matrix& x, const aq_matrix& wg, const aq_matrix& wu, const aq_matrix& gate,
+                                const aq_matrix& up, int act, const aq_matrix* dx, const aq_matrix* dwg, const aq_matrix* dwu, void* ws,
+                                hipStream_t st);
 // ---- recurrence.hip
 int64_t recurrence_workspace(int64_t rows, int64_t count, int64_t cols);
 aq_status launch_recurrence_forward(const aq_matrix& z, const aq_matrix& v, const int32_t* offsets, int64_t count, const uint8_t* starts,

@@ -161,6 +161,82 @@ extern "C" aq_status aq_mx4_input_grad(const aq_matrix* dy, const aq_mx4* w, con
     return dy->rows == 0 ? AQ_OK : launch_input_grad(*dy, *w, *dx, d_workspace, workspace_bytes, as_stream(stream));
 }
 
+// ---- gated layers
+
+namespace {
+
+// a matrix of a call whose matrices have one type
+aq_status sized(const aq_matrix* m, int64_t rows, int64_t cols, int32_t dtype) {
+    AQ_TRY(matrix_ok(m));
+    return m->rows != rows || m->cols != cols || m->dtype != dtype ? AQ_ESHAPE : AQ_OK;
+}
+bool gate_ok(int32_t act) { return act >= AQ_GATE_SIGMOID && act <= AQ_GATE_RELU; }
+bool dtype_ok(int32_t dtype) { return dtype == AQ_F32 || dtype == AQ_F16 || dtype == AQ_BF16; }
+// rows, features and inputs whose products' tiles and laid-out pieces a launch's 32 bits count
+aq_status gated_sizes_ok(int64_t rows, int64_t n, int64_t k) {
+    if (rows > AQ_GATED_MAX_VALUES / (n > k ? n : k) || n > AQ_GATED_MAX_VALUES / k) return AQ_ESHAPE;
+    return AQ_OK;
+}
+
+}  // namespace
+
+extern "C" aq_status aq_gated_forward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype, uint64_t* bytes) {
+    AQ_TRY(sizes_ok(rows, n, k, bytes));
+    if (!dtype_ok(dtype)) return AQ_EINVAL;
+    AQ_TRY(gated_sizes_ok(rows, n, k));
+    *bytes = (uint64_t)gated_forward_workspace(rows, n, k, dtype);
+    return AQ_OK;
+}
+
+extern "C" aq_status aq_gated_backward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype, uint64_t* bytes) {
+    AQ_TRY(sizes_ok(rows, n, k, bytes));
+    if (!dtype_ok(dtype)) return AQ_EINVAL;
+    AQ_TRY(gated_sizes_ok(rows, n, k));
+    *bytes = (uint64_t)gated_backward_workspace(rows, n, k, dtype);
+    return AQ_OK;
+}
+
+extern "C" aq_status aq_gated_forward(const aq_matrix* x, const aq_matrix* wg, const aq_matrix* wu, int32_t act, const aq_matrix* y,
+                                      const aq_matrix* gate, const aq_matrix* up, void* d_workspace, uint64_t workspace_bytes, void* stream) {
+    AQ_TRY(matrix_ok(x));
+    AQ_TRY(matrix_ok(wg));
+    if (!gate_ok(act) || (gate != nullptr) != (up != nullptr)) return AQ_EINVAL;
+    const int64_t rows = x->rows, n = wg->rows, k = x->cols;
+    if (n < 1 || n > kMostCols) return AQ_ESHAPE;
+    AQ_TRY(sized(wg, n, k, x->dtype));
+    AQ_TRY(sized(wu, n, k, x->dtype));
+    AQ_TRY(sized(y, rows, n, x->dtype));
+    if (gate) {
+        AQ_TRY(sized(gate, rows, n, x->dtype));
+        AQ_TRY(sized(up, rows, n, x->dtype));
+    }
+    AQ_TRY(gated_sizes_ok(rows, n, k));
+    if (!workspace_ok(d_workspace, workspace_bytes, gated_forward_workspace(rows, n, k, x->dtype))) return AQ_EINVAL;
+    return rows == 0 ? AQ_OK : launch_gated_forward(*x, *wg, *wu, act, *y, gate, up, d_workspace, as_stream(stream));
+}
+
+extern "C" aq_status aq_gated_backward(const aq_matrix* dy, const aq_matrix* x, const aq_matrix* wg, const aq_matrix* wu, const aq_matrix* gate,
+                                       const aq_matrix* up, int32_t act, const aq_matrix* dx, const aq_matrix* dwg, const aq_matrix* dwu,
+                                       void* d_workspace, uint64_t workspace_bytes, void* stream) {
+    AQ_TRY(matrix_ok(dy));
+    AQ_TRY(matrix_ok(x));
+    if (!gate_ok(act) || (dwg != nullptr) != (dwu != nullptr)) return AQ_EINVAL;
+    const int64_t rows = x->rows, n = dy->cols, k = x->cols;
+    AQ_TRY(sized(dy, rows, n, x->dtype));
+    AQ_TRY(sized(wg, n, k, x->dtype));
+    AQ_TRY(sized(wu, n, k, x->dtype));
+    AQ_TRY(sized(gate, rows, n, x->dtype));
+    AQ_TRY(sized(up, rows, n, x->dtype));
+    if (dx) AQ_TRY(sized(dx, rows, k, x->dtype));
+    if (dwg) {
+        AQ_TRY(sized(dwg, n, k, x->dtype));
+        AQ_TRY(sized(dwu, n, k, x->dtype));
+    }
+    AQ_TRY(gated_sizes_ok(rows, n, k));
+    if (!workspace_ok(d_workspace, workspace_bytes, gated_backward_workspace(rows, n, k, x->dtype))) return AQ_EINVAL;
+    return launch_gated_backward(*dy, *x, *wg, *wu, *gate, *up, act, dx, dwg, dwu, d_workspace, as_stream(stream));
+}
+
 // ---- the recurrence
 
 namespace {

@@ -1,0 +1,275 @@
+"""Gated layers against their definition in 64 bits.
+
+Tolerances: U is the rounding of an fp32 operation.  A sum of k products is off by at most k U times the sum of their magnitudes, six times
+as many terms where fp32 values come in three parts (what those leave out is below 2 U of each product).  An activation of a is off by
+at most act_error(a) times its value: the exponential's argument by 1.5 |a| U (a^2 U for the normal distribution's density and, by its
+condition, function), the functions themselves by 32 U, some ten operations around them.  dgate and dup are rounded to the matrices'
+type before they are summed up, which is OUT of each."""
+import math
+
+import pytest
+import torch
+
+from paper_1910_01055_amd import binding as B
+from test_gpu_learner import DEV, OUT, SENTINEL, TINY, TYPES, U, Framed
+
+pytestmark = pytest.mark.gpu
+
+ACTS = ["sigmoid", "silu", "gelu", "relu"]
+
+
+def act_of(a, act):
+    s = torch.sigmoid(a)
+    if act == "relu":
+        return a.clamp(min=0), (a > 0).double()
+    if act == "gelu":
+        p = 0.5 * torch.special.erfc(-a / math.sqrt(2))
+        return a * p, p + a * torch.exp(-a * a / 2) / math.sqrt(2 * math.pi)
+    if act == "sigmoid":
+        return s, s * torch.sigmoid(-a)
+    return a * s, s * (1 + a * torch.sigmoid(-a))
+
+
+def act_error(a, act):
+    return torch.zeros_like(a) if act == "relu" else (64 + 3 * a.abs() + 2 * a * a) * U
+
+
+def workspace(size):
+    """Scratch that holds NaNs."""
+    return torch.full((size,), 255, dtype=torch.uint8, device=DEV) if size else None
+
+
+def within(got, want, tol, kind, what):
+    tol = tol + OUT[kind] * (want.abs() + tol) + TINY[kind]
+    off = (got.to(DEV) - want).abs()
+    assert bool((off <= tol).all()), f"{what}: {float((off - tol).max())} over at {int((off > tol).sum())} of {off.numel()}"
+
+
+def run(rows, n, k, kind, act, gap=0, at=0, keep=True, seed=0):
+    g = torch.Generator().manual_seed(seed + rows + 1000 * n + k)
+    t = TYPES[kind]
+    values = [torch.randn(rows, k, generator=g), torch.randn(n, k, generator=g) / math.sqrt(k) * 1.5, torch.randn(n, k, generator=g) / math.sqrt(k),
+              0.1 * torch.randn(rows, n, generator=g)]
+    X, WG, WU, DY = (Framed(*v.shape, t, gap, at, v.to(t).to(DEV)) for v in values)
+    Y, G, UP, DX, DWG, DWU = (Framed(*shape, t, gap, at) for shape in ((rows, n),) * 3 + ((rows, k),) + ((n, k),) * 2)
+    x, wg, wu, dy = (f.m.double() for f in (X, WG, WU, DY))
+    terms = 6 if kind == "f32" else 1
+    ws = workspace(B.gated_forward_workspace(rows, n, k, t))
+    B.gated_forward(X.m, WG.m, WU.m, act, Y.m, G.m if keep else None, UP.m if keep else None, ws)
+    gate, up = x @ wg.t(), x @ wu.t()
+    gt, ut = ((terms * k + 2) * U * (x.abs() @ w.abs().t()) for w in (wg, wu))
+    h, _ = act_of(gate, act)
+    ht = 1.13 * gt + act_error(gate, act) * h.abs()
+    within(Y.get(), h * up, ht * (up.abs() + ut) + h.abs() * ut + U * (h * up).abs(), kind, "y")
+    if not keep:
+        return
+    within(G.get(), gate, gt, kind, "gate")
+    within(UP.get(), up, ut, kind, "up")
+    ws = workspace(B.gated_backward_workspace(rows, n, k, t))
+    B.gated_backward(DY.m, X.m, WG.m, WU.m, G.m, UP.m, act, DX.m, DWG.m, DWU.m, ws)
+    gate, up = G.m.double(), UP.m.double()
+    h, slope = act_of(gate, act)
+    dg, du = dy * up * slope, dy * h
+    half = OUT["bf16" if kind == "bf16" else kind]
+    dgt = (dy * up).abs() * (act_error(gate, act) * (1 + gate.abs()) + 4 * U) + half * dg.abs() + TINY[kind]
+    dut = du.abs() * (act_error(gate, act) + 2 * U + half) + TINY[kind]
+    sums = dg.abs() @ wg.abs() + du.abs() @ wu.abs()
+    within(DX.get(), dg @ wg + du @ wu, dgt @ wg.abs() + dut @ wu.abs() + (2 * terms * n + 4) * U * sums, kind, "dx")
+    for name, M, d, dt in (("dwg", DWG, dg, dgt), ("dwu", DWU, du, dut)):
+        within(M.get(), d.t() @ x, dt.t() @ x.abs() + (terms * rows + 4) * U * (d.abs().t() @ x.abs()), kind, name)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("act", ACTS)
+def test_activations(kind, act):
+    run(70, 48, 72, kind, act)
+    run(3, 48, 72, kind, act)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,n,k", [(1, 1, 1), (1, 2, 7), (2, 3, 8), (3, 5, 513), (4, 33, 2050), (5, 1, 1), (5, 31, 9), (8, 32, 64), (33, 33, 63), (64, 64, 64),
+                                      (65, 65, 65), (129, 31, 200), (130, 257, 130), (300, 403, 1111), (1, 300, 4096), (6, 40, 4096), (2000, 17, 24)])
+def test_sizes(kind, rows, n, k):
+    run(rows, n, k, kind, "silu")
+
+
+@pytest.mark.parametrize("kind,gap,at", [("f32", 3, 1), ("f16", 1, 1), ("bf16", 5, 3), ("bf16", 8, 0), ("f16", 8, 8), ("bf16", 0, 1), ("f16", 4, 0)])
+@pytest.mark.parametrize("rows,n,k", [(2, 24, 40), (40, 24, 40), (70, 33, 41)])
+def test_rows_apart_and_odd_addresses(kind, gap, at, rows, n, k):
+    run(rows, n, k, kind, "gelu", gap, at)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 50])
+def test_without_what_is_kept(kind, rows):
+    run(rows, 40, 56, kind, "silu", keep=False)
+
+
+def whole(shape, low, high, g, t):
+    return torch.randint(low, high + 1, shape, generator=g, device=DEV).to(t)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,n,k", [(4096, 1024, 512), (16384, 2048, 64), (700, 520, 1000), (64, 64, 4096), (100, 2048, 2048), (8192, 72, 80), (30000, 24, 136),
+                                      (512, 4096, 256), (2048, 2048, 2048), (320, 1000, 1000)])
+def test_whole_numbers(kind, rows, n, k):
+    """Whole numbers whose sums are exact: every tile, slice and segment, value by value."""
+    g = torch.Generator(device=DEV).manual_seed(rows + n + k)
+    t = TYPES[kind]
+    x, wg, wu, dy = whole((rows, k), -2, 2, g, t), whole((n, k), -1, 1, g, t), whole((n, k), -1, 1, g, t), whole((rows, n), -1, 1, g, t)
+    y, gate, up = (torch.full((rows, n), SENTINEL, dtype=t, device=DEV) for _ in range(3))
+    B.gated_forward(x, wg, wu, "relu", y, gate, up, workspace(B.gated_forward_workspace(rows, n, k, t)))
+    want_g, want_u = (x.double() @ w.double().t() for w in (wg, wu))
+    assert bool((gate == want_g.to(t)).all()) and bool((up == want_u.to(t)).all())
+    assert bool((y == (want_g.clamp(min=0).float() * want_u.float()).to(t)).all())
+    gate, up = whole((rows, n), -1, 2, g, t), whole((rows, n), -2, 2, g, t)
+    dx, dwg, dwu = torch.full((rows, k), SENTINEL, dtype=t, device=DEV), torch.full((n, k), SENTINEL, dtype=t, device=DEV), torch.full((n, k), SENTINEL, dtype=t, device=DEV)
+    B.gated_backward(dy, x, wg, wu, gate, up, "relu", dx, dwg, dwu, workspace(B.gated_backward_workspace(rows, n, k, t)))
+    dg, du = dy.double() * up.double() * (gate > 0), dy.double() * gate.double().clamp(min=0)
+    for got, want in ((dx, dg @ wg.double() + du @ wu.double()), (dwg, dg.t() @ x.double()), (dwu, du.t() @ x.double())):
+        assert float(want.abs().max()) < 2 ** 24
+        assert bool((got == want.to(t)).all())
+
+
+def test_parts_of_fp32():
+    """Values that need all 24 bits, and the largest ones."""
+    rows, n, k = 64, 64, 64
+    x = torch.eye(64, device=DEV) * (1 + 2.0 ** -23)
+    wg = torch.full((n, k), 3.0, device=DEV)
+    wu = torch.full((n, k), 1 + 2.0 ** -12, device=DEV)
+    wu[5, 7] = 3.3e38 / 4
+    y, gate, up = (torch.empty(rows, n, device=DEV) for _ in range(3))
+    B.gated_forward(x, wg, wu, "sigmoid", y, gate, up, workspace(B.gated_forward_workspace(rows, n, k, torch.float32)))
+    want = x.double() @ wu.double().t()
+    assert bool(((up.double() - want).abs() <= 2 * U * want.abs()).all()) and bool(torch.isfinite(y).all())
+    x[:, 9] = torch.finfo(torch.float32).max
+    wg[:] = 0
+    wg[:, 9] = 1.0
+    B.gated_forward(x, wg, wg, "sigmoid", y, gate, up, workspace(B.gated_forward_workspace(rows, n, k, torch.float32)))
+    assert bool(((gate.double() - torch.finfo(torch.float32).max).abs() <= 2 * U * torch.finfo(torch.float32).max).all())
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows", [2, 90])
+def test_what_is_not_finite_stays_where_it_belongs(kind, rows):
+    n, k = 40, 48
+    t = TYPES[kind]
+    x, wg, wu, dy = (torch.ones(s, dtype=t, device=DEV) for s in ((rows, k), (n, k), (n, k), (rows, n)))
+    x[1, 5] = math.inf
+    y, gate, up = (torch.empty(rows, n, dtype=t, device=DEV) for _ in range(3))
+    B.gated_forward(x, wg, wu, "silu", y, gate, up, workspace(B.gated_forward_workspace(rows, n, k, t)))
+    bad = ~torch.isfinite(y)
+    assert bool(bad[1].all()) and int(bad.sum()) == n
+    if kind != "f32":
+        assert bool((y[1] == math.inf).all())
+    x[1, 5] = 1.0
+    B.gated_forward(x, wg, wu, "silu", y, gate, up, workspace(B.gated_forward_workspace(rows, n, k, t)))
+    dy[0, 3] = math.nan
+    dx, dwg, dwu = torch.empty_like(x), torch.empty_like(wg), torch.empty_like(wu)
+    B.gated_backward(dy, x, wg, wu, gate, up, "silu", dx, dwg, dwu, workspace(B.gated_backward_workspace(rows, n, k, t)))
+    bad = ~torch.isfinite(dx)
+    assert bool(bad[0].all()) and int(bad.sum()) == k
+    for d in (dwg, dwu):
+        bad = ~torch.isfinite(d)
+        assert bool(bad[3].all()) and int(bad.sum()) == k
+
+
+def test_activations_at_their_ends():
+    """Gates far from zero and infinite ones, by way of a layer of one input."""
+    inf = math.inf
+    a = torch.tensor([-inf, -3e38, -1e30, -300.0, -20.0, 0.0, 20.0, 300.0, 1e30, 3e38, inf], device=DEV)[:, None]
+    rows = a.shape[0]
+    one = torch.ones(1, 1, device=DEV)
+    for act, low, slope_low in (("sigmoid", 0.0, 0.0), ("silu", 0.0, 0.0), ("gelu", 0.0, 0.0), ("relu", 0.0, 0.0)):
+        # (backward reads gate and up as they are given)
+        up, dy = torch.ones_like(a), torch.ones_like(a)
+        dx, dwg, dwu = torch.empty_like(a), torch.empty_like(one), torch.empty_like(one)
+        zero = torch.zeros_like(one)
+        B.gated_backward(dy, up, one, zero, a, up, act, dx, None, None, workspace(B.gated_backward_workspace(rows, 1, 1, torch.float32)))
+        slope = dx[:, 0]
+        top = 0.0 if act == "sigmoid" else 1.0
+        assert bool((slope[:4].abs() < 1e-30).all()) and bool(((slope[-4:-1] - top).abs() < 1e-6).all()), (act, slope)
+        assert abs(float(slope[5]) - {"sigmoid": 0.25, "silu": 0.5, "gelu": 0.5, "relu": 0.0}[act]) < 1e-6
+    del dwg, dwu, low, slope_low
+
+
+def test_parts_of_the_backward_pass():
+    """dx alone, the weights' gradients alone: the same values as all together."""
+    rows, n, k, t = 150, 72, 88, torch.bfloat16
+    x, wg, wu, dy = (torch.randn(s, device=DEV).to(t) for s in ((rows, k), (n, k), (n, k), (rows, n)))
+    gate, up = torch.randn(rows, n, device=DEV).to(t), torch.randn(rows, n, device=DEV).to(t)
+    ws = workspace(B.gated_backward_workspace(rows, n, k, t))
+    all3 = torch.empty_like(x), torch.empty_like(wg), torch.empty_like(wu)
+    B.gated_backward(dy, x, wg, wu, gate, up, "silu", *all3, ws)
+    dx, dwg, dwu = torch.empty_like(x), torch.empty_like(wg), torch.empty_like(wu)
+    B.gated_backward(dy, x, wg, wu, gate, up, "silu", dx, None, None, ws)
+    B.gated_backward(dy, x, wg, wu, gate, up, "silu", None, dwg, dwu, ws)
+    B.gated_backward(dy, x, wg, wu, gate, up, "silu", None, None, None, ws)
+    assert all(bool((a == b).all()) for a, b in zip(all3, (dx, dwg, dwu)))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_no_rows(kind):
+    t = TYPES[kind]
+    none, no = torch.empty(0, 40, dtype=t, device=DEV), torch.empty(0, 24, dtype=t, device=DEV)
+    w = torch.ones(24, 40, dtype=t, device=DEV)
+    dwg, dwu = torch.full_like(w, SENTINEL), torch.full_like(w, SENTINEL)
+    B.gated_forward(none, w, w, "silu", no, no, no, workspace(B.gated_forward_workspace(0, 24, 40, t)))
+    B.gated_backward(no, none, w, w, no, no, "silu", none, dwg, dwu, workspace(B.gated_backward_workspace(0, 24, 40, t)))
+    assert bool((dwg == 0).all()) and bool((dwu == 0).all())
+
+
+def test_differences():
+    """The gradients against differences of the forward pass along one direction."""
+    rows, n, k, step = 40, 24, 16, 2.0 ** -6
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x, tx, wg, tg, wu, tu, dy = (torch.randn(s, generator=g, device=DEV) for s in ((rows, k),) * 2 + ((n, k),) * 4 + ((rows, n),))
+    wg, wu, tg, tu, tx = wg / 4, wu / 4, tg / 16, tu / 16, tx / 4
+    y, gate, up = (torch.empty(rows, n, device=DEV) for _ in range(3))
+    ws = workspace(max(B.gated_forward_workspace(rows, n, k, torch.float32), B.gated_backward_workspace(rows, n, k, torch.float32)))
+    for act in ("sigmoid", "silu", "gelu"):
+        def value(s):
+            B.gated_forward(x + s * tx, wg + s * tg, wu + s * tu, act, y, gate, up, ws)
+            return float((y.double() * dy.double()).sum())
+
+        ends = [value(s * step) for s in (2, 1, -1, -2)]
+        value(0.0)
+        dx, dwg, dwu = torch.empty_like(x), torch.empty_like(wg), torch.empty_like(wu)
+        B.gated_backward(dy, x, wg, wu, gate, up, act, dx, dwg, dwu, ws)
+        slope = sum(float((a.double() * b.double()).sum()) for a, b in ((dx, tx), (dwg, tg), (dwu, tu)))
+        want = (8 * (ends[1] - ends[2]) - (ends[0] - ends[3])) / (12 * step)
+        # 960 terms of size 1 off by some 100 U each over the step: < 960 * 100 * 2^-24 / 2^-6 = 0.4 at the very most
+        assert abs(slope - want) < 0.4 and abs(want) > 1.0, act
+
+
+def test_captured_and_replayed():
+    """Forward and backward passes with slices, captured; two graphs with scratch of their own between eager work."""
+    rows, n, k, t = 100, 96, 2048, torch.bfloat16
+    x, wg, wu, dy = (torch.randn(s, device=DEV).to(t) * 0.1 for s in ((rows, k), (n, k), (n, k), (rows, n)))
+    size = max(B.gated_forward_workspace(rows, n, k, t), B.gated_backward_workspace(rows, n, k, t))
+    graphs = []
+    for _ in range(2):
+        out = [torch.empty(s, dtype=t, device=DEV) for s in ((rows, n),) * 3 + ((rows, k), (n, k), (n, k))]
+        ws = workspace(size)
+
+        def work(out=out, ws=ws):
+            B.gated_forward(x, wg, wu, "silu", *out[:3], ws)
+            B.gated_backward(dy, x, wg, wu, out[1], out[2], "silu", *out[3:], ws)
+
+        work()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            work()
+        graphs.append((graph, out, work))
+    for _ in range(3):
+        x.copy_(torch.randn(rows, k, device=DEV))
+        for graph, out, work in graphs:
+            work()
+            torch.cuda.synchronize()
+            want = [o.clone() for o in out]
+            for o in out:
+                o.fill_(SENTINEL)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(bool((a == b).all()) for a, b in zip(want, out))
