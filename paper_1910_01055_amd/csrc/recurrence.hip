@@ -10,13 +10,17 @@
 // theirs begin with, without another read.  Where sequences and units are too few to fill the chip, every sequence is cut into as
 // many parts as it takes, in proportion to its length, and a launch in front of this one leaves the parts' (A, B).
 // The state and (A, B) are fp32; a start that cuts a run is kept as A = -1, which no product gives: a NaN in front of it ends there.
+#include <initializer_list>
+
 #include "learner.hpp"
 #include "learner_device.hpp"
 
 namespace aq {
 namespace {
 
-constexpr int64_t kMostParts = 256;  // of a sequence
+constexpr int64_t kManyGroups = 512;  // of 64 lanes: as many have pairs of units
+constexpr int kRows = 16;             // of a run, over a lane's units (backward: 8, see there)
+constexpr int kRowsBackward = 8;
 
 template <class T, int V>
 struct Units;  // V neighbouring values, as they lie in memory
@@ -28,7 +32,8 @@ struct Units<float, 1> {
     __device__ __forceinline__ void set(uint32_t two) { w = two; }
     __device__ __forceinline__ void load(const float* p) { w = *(const uint32_t AQ_GLOBAL*)p; }
     __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = __uint_as_float(w); }
-    static __device__ __forceinline__ void put(float* p, const float (&v)[1]) { *(float AQ_GLOBAL*)p = v[0]; }
+    static __device__ __forceinline__ Units of(const float (&v)[1]) { return {__float_as_uint(v[0])}; }
+    __device__ __forceinline__ void put(float* p) const { *(uint32_t AQ_GLOBAL*)p = w; }
 };
 template <>
 struct Units<float, 2> {
@@ -36,9 +41,8 @@ struct Units<float, 2> {
     __device__ __forceinline__ void set(uint32_t two) { w = v2u{two, two}; }
     __device__ __forceinline__ void load(const float* p) { w = *(const v2u_any AQ_GLOBAL*)p; }
     __device__ __forceinline__ void get(float (&v)[2]) const { v[0] = __uint_as_float(w[0]), v[1] = __uint_as_float(w[1]); }
-    static __device__ __forceinline__ void put(float* p, const float (&v)[2]) {
-        *(v2u_any AQ_GLOBAL*)p = v2u{__float_as_uint(v[0]), __float_as_uint(v[1])};
-    }
+    static __device__ __forceinline__ Units of(const float (&v)[2]) { return {v2u{__float_as_uint(v[0]), __float_as_uint(v[1])}}; }
+    __device__ __forceinline__ void put(float* p) const { *(v2u_any AQ_GLOBAL*)p = w; }
 };
 template <class T>
 struct Units<T, 1> {
@@ -46,7 +50,8 @@ struct Units<T, 1> {
     __device__ __forceinline__ void set(uint32_t two) { w = __builtin_bit_cast(T, (uint16_t)two); }
     __device__ __forceinline__ void load(const T* p) { w = *(const T AQ_GLOBAL*)p; }
     __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = (float)w; }
-    static __device__ __forceinline__ void put(T* p, const float (&v)[1]) { *(T AQ_GLOBAL*)p = (T)v[0]; }
+    static __device__ __forceinline__ Units of(const float (&v)[1]) { return {(T)v[0]}; }
+    __device__ __forceinline__ void put(T* p) const { *(T AQ_GLOBAL*)p = w; }
 };
 template <class T>
 struct Units<T, 2> {
@@ -63,17 +68,15 @@ struct Units<T, 2> {
             v[0] = (float)h[0], v[1] = (float)h[1];
         }
     }
-    static __device__ __forceinline__ void put(T* p, const float (&v)[2]) {
-        *(word AQ_GLOBAL*)p = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f32{v[0], v[1]}), t2));
-    }
+    static __device__ __forceinline__ Units of(const float (&v)[2]) { return {__builtin_bit_cast(uint32_t, __builtin_convertvector((v2f32{v[0], v[1]}), t2))}; }
+    __device__ __forceinline__ void put(T* p) const { *(word AQ_GLOBAL*)p = w; }
 };
 
-// sigmoid(z) and sigmoid(-z), neither as a difference from 1
+// sigmoid(z) and sigmoid(-z), neither as a difference from 1: 1 / (1 + e) and e / (1 + e), e = exp(-z) at most 2^126 (a NaN stays one)
 __device__ __forceinline__ void gates(float z, float& f, float& rest) {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(z));
-    const float large = __builtin_amdgcn_rcpf(1.0f + e), small = e * large;
-    f = z >= 0.0f ? large : small;
-    rest = z >= 0.0f ? small : large;
+    const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(-1.44269504f * z, 126.0f));
+    f = __builtin_amdgcn_rcpf(1.0f + e);
+    rest = e * f;
 }
 // the same value to the program, another one to the compiler, which else keeps every comparison with it for the second pass in registers
 __device__ __forceinline__ uint32_t anew(uint32_t v) {
@@ -82,51 +85,65 @@ __device__ __forceinline__ uint32_t anew(uint32_t v) {
 }
 __device__ __forceinline__ float apply(float a, float b, float h) { return a < 0.0f ? b : fmaf(a, h, b); }
 
+// Sequences are cut into parts of at least 2^shift rows (shorter ones are one part), and parts have slots.  Part p of sequence s has slot
+// floor(begin / 2^shift) + s + p, which no other one's is, and of which there are rows / 2^shift + count: so a slot finds its part
+// by a search among the offsets, long sequences fill as many workgroups as short ones of as many rows, and nothing is written down.
 struct Rows {
     const int32_t* offsets;
-    int64_t rows, cols, each;  // each: rows of a sequence, without offsets
-    int32_t count, across;     // sequences; lanes to one
-    int32_t parts, least;      // most parts of a sequence, and the least rows of one
+    int64_t rows, cols, each;         // each: rows of a sequence, without offsets
+    int32_t count, across, slots;     // sequences; lanes to a slot
+    int32_t parts, shift, rounds;     // parts of a sequence without offsets; with: rounds of the search (0: slots are sequences)
+    int32_t most;                     // bytes between rows of any matrix, 0: pairs do not begin at words (see Near)
 };
-// Rows of one lane's sequence that its workgroup takes.  A sequence has as many parts as its rows fill, so that short ones need no sums;
-// its parts' sums lie from slot begin / least + (its number) on, which no other one's reach.
+// a lane's part: rows of its sequence that its workgroup takes
 struct Span {
     int64_t begin, first, behind;  // of the sequence; of the part; behind the sequence
-    int n, parts;                  // rows of the part; parts of the sequence
-    int seq, unit;
-    bool active;                   // has such a part
+    int n, part, parts;            // rows of the part; which one of how many
+    int slot, seq, unit;           // slot: of the sequence's first part
+    bool active;
 };
+__device__ __forceinline__ int64_t inside(int64_t at, int64_t low, int64_t high) { return at < low ? low : at > high ? high : at; }
 template <int V>
-__device__ __forceinline__ Span span_of(const Rows& r, int part) {
+__device__ __forceinline__ Span span_of(const Rows& r) {
     Span s;
     const uint32_t q = blockIdx.x * 64 + (threadIdx.x & 63);
-    s.seq = (int)(q / (uint32_t)r.across);
-    s.active = s.seq < r.count;
-    if (!s.active) s.seq = 0;
+    const int slot = (int)(q / (uint32_t)r.across);
     s.unit = (int)(q % (uint32_t)r.across) * V;
     if (V > 1 && s.unit > (int)r.cols - V) s.unit = (int)r.cols - V;  // (units that two lanes have are the same in both)
+    s.active = slot < r.slots;
     if (r.offsets) {
-        const int64_t a = r.offsets[s.seq], b = r.offsets[s.seq + 1];
-        s.begin = a < 0 ? 0 : a > r.rows ? r.rows : a;
-        s.behind = b < s.begin ? s.begin : b > r.rows ? r.rows : b;
+        int low = s.active ? slot : 0;
+        if (r.rounds) {
+            low = 0;
+            int high = r.count - 1;
+            for (int i = 0; i < r.rounds; ++i) {
+                const int mid = (low + high + 1) >> 1;
+                const bool below = (int)(inside(r.offsets[mid], 0, r.rows) >> r.shift) + mid <= slot;
+                low = below ? mid : low;
+                high = below ? high : mid > low ? mid - 1 : low;
+            }
+        }
+        s.seq = low;
+        s.begin = inside(r.offsets[low], 0, r.rows);
+        s.behind = inside(r.offsets[low + 1], s.begin, r.rows);
+        const int len = (int)(s.behind - s.begin);
+        s.slot = r.rounds ? (int)(s.begin >> r.shift) + low : slot;
+        s.part = slot - s.slot;
+        s.parts = r.rounds && len >> r.shift > 1 ? len >> r.shift : 1;
     } else {
+        s.seq = s.active ? slot / r.parts : 0;
+        s.parts = r.parts;
+        s.slot = s.seq * r.parts;
+        s.part = slot - s.slot;
         s.begin = s.seq * r.each;
         s.behind = s.begin + r.each;
     }
-    const int len = (int)(s.behind - s.begin);
-    s.first = s.begin;
-    s.n = len;
-    s.parts = 1;
-    if (r.parts > 1) {
-        s.parts = len / r.least;
-        s.parts = s.parts < 1 ? 1 : s.parts > r.parts ? r.parts : s.parts;
-        const int each = (len + s.parts - 1) / s.parts;
-        s.active = s.active && part < s.parts;
-        s.first = s.begin + (int64_t)each * part;
-        s.n = s.first + each < s.behind ? each : (int)(s.behind - s.first);
-        if (s.n < 0) s.n = 0, s.first = s.behind;
-    }
-    if (!s.active) s.n = 0;
+    s.active = s.active && s.part >= 0 && s.part < s.parts;
+    if (!s.active) s.part = 0;
+    const int len = (int)(s.behind - s.begin), each = s.parts > 1 ? (len + s.parts - 1) / s.parts : len;
+    s.first = s.begin + (int64_t)each * s.part;
+    const int64_t left = s.behind - s.first;
+    s.n = !s.active || left < 0 ? 0 : left < each ? (int)left : each;
     return s;
 }
 __device__ __forceinline__ int longest_of(int m) {
@@ -137,6 +154,42 @@ __device__ __forceinline__ int longest_of(int m) {
     }
     return __builtin_amdgcn_readfirstlane(m);
 }
+
+// Rows from `row` on (each lane its own) of a matrix as a buffer that begins at the first lane's: a row's address is then a scalar and
+// a lane's offset, for all rows of a run the same.  `most`: the largest distance between rows in bytes of any matrix, or 0 where pairs do not begin
+// at words.
+struct Near {
+    int64_t base;
+    uint32_t behind;  // rows
+    __device__ __forceinline__ Near(int64_t row) {
+        base = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(row >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)row));
+        behind = (uint32_t)(row - base);
+    }
+    static __device__ __forceinline__ bool reaches(int64_t row, int most) {
+        const Near n(row);
+        return most && __all(row >= n.base && (row - n.base) * most < (1 << 30));
+    }
+};
+template <class T, int V>
+struct NearRows {
+    __amdgpu_buffer_rsrc_t r;
+    int at;
+    __device__ __forceinline__ NearRows(const T* m, int64_t ld, const Near& n, int unit) {
+        r = __builtin_amdgcn_make_buffer_rsrc((void*)(m + n.base * ld), 0, 0x7ffffff0, 0x00020000);
+        at = (int)((n.behind * (uint32_t)ld + (uint32_t)unit) * (uint32_t)sizeof(T));
+    }
+    __device__ __forceinline__ void load(Units<T, V>& u, int offset) const {  // offset: of a row, in bytes
+        if constexpr (V * sizeof(T) == 8) u.w = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(r, at, offset, 0));
+        else if constexpr (V * sizeof(T) == 4) u.w = __builtin_amdgcn_raw_buffer_load_b32(r, at, offset, 0);
+        else u.w = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, offset, 0));
+    }
+    __device__ __forceinline__ void store(const float (&v)[V], int offset) const {
+        const Units<T, V> u = Units<T, V>::of(v);
+        if constexpr (V * sizeof(T) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, u.w), r, at, offset, 0);
+        else if constexpr (V * sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(u.w, r, at, offset, 0);
+        else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, u.w), r, at, offset, 0);
+    }
+};
 
 // Exchange of W wavefronts' (A, B) of the same lanes: `in` gets the state in front of this wavefront's rows, `carry` that behind all.
 template <int V, int W>
@@ -176,12 +229,12 @@ struct Exchange {
 
 // where parts leave and find their (A, B): [slot][A, B][cols]
 __device__ __forceinline__ float* sum_at(float* sums, const Rows& r, int part, int which, const Span& s) {
-    return sums + ((s.begin / r.least + s.seq + part) * 2 + which) * r.cols + s.unit;
+    return sums + ((int64_t)(s.slot + part) * 2 + which) * r.cols + s.unit;
 }
-// The state in front of a part, from the sums of the parts `from`, from + step .. (`many` of them, those below `parts` of which exist): each
-// wavefront joins a run of them, four on their way at a time.
+// The state in front of a part, from the sums of `own` others in the order from, from + step .. (`many`: the most of any lane): each wavefront
+// joins a run of them, four on their way at a time.
 template <int V, int W>
-__device__ __forceinline__ void carry_of_parts(Exchange<V, W>& exchange, float* sums, const Rows& r, int from, int many, int step, const Span& s,
+__device__ __forceinline__ void carry_of_parts(Exchange<V, W>& exchange, float* sums, const Rows& r, int from, int own, int many, int step, const Span& s,
                                                int wave, int lane, float (&carry)[V]) {
     const int each = (many + W - 1) / W, first = wave * each, end = first + each < many ? first + each : many;
     float a[V], b[V], unused[V];
@@ -192,7 +245,7 @@ __device__ __forceinline__ void carry_of_parts(Exchange<V, W>& exchange, float* 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int p = from + (k + i) * step;
-            const bool there = k + i < end && p < s.parts && s.active;
+            const bool there = k + i < end && k + i < own;
 #pragma unroll
             for (int v = 0; v < V; ++v) A[i][v] = there ? sum_at(sums, r, p, 0, s)[v] : 1.0f, B[i][v] = there ? sum_at(sums, r, p, 1, s)[v] : 0.0f;
         }
@@ -240,9 +293,9 @@ __global__ void __launch_bounds__(64 * W) k_recurrence(const T* __restrict__ z, 
                                                        int64_t ldy, const uint8_t* __restrict__ starts, const float* first, float* last, Rows rows,
                                                        float* __restrict__ sums) {
     __shared__ Exchange<V, W> exchange;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = blockIdx.y;
-    const Span s = span_of<V>(rows, part);
-    const bool summed = SUMS ? s.active && s.parts > 1 && part < s.parts - 1 : s.active;  // (the last part's sums reach nothing)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Span s = span_of<V>(rows);
+    const bool summed = SUMS ? s.active && s.part < s.parts - 1 : s.active;  // (the last part's sums reach nothing)
     const int n = summed ? s.n : 0, longest = longest_of(n);
     float carry[V], whole[V];
 #pragma unroll
@@ -251,7 +304,7 @@ __global__ void __launch_bounds__(64 * W) k_recurrence(const T* __restrict__ z, 
         whole[i] = 1.0f;
     }
     if constexpr (!SUMS)
-        if (part) carry_of_parts(exchange, sums, rows, 0, part, 1, s, wave, lane, carry);
+        if (const int many = sums ? longest_of(s.part) : 0) carry_of_parts(exchange, sums, rows, 0, s.part, many, 1, s, wave, lane, carry);
     Units<T, V> rz[R], rv[R];
     Starts<R> rs;
     auto left_of = [&](int t0) __attribute__((always_inline)) { return n - t0 - R * wave < R ? n - t0 - R * wave : R; };
@@ -261,10 +314,20 @@ __global__ void __launch_bounds__(64 * W) k_recurrence(const T* __restrict__ z, 
         const int64_t row = row_of(t0, left);
         const T *pz = z + row * ldz + s.unit, *pv = v + row * ldv + s.unit;
         if (__all(left == R)) {
+            if (Near::reaches(row, rows.most)) {
+                const Near near(row);
+                const NearRows<T, V> nz(z, ldz, near, s.unit), nv(v, ldv, near, s.unit);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                rz[r].load(pz + r * ldz);
-                rv[r].load(pv + r * ldv);
+                for (int r = 0; r < R; ++r) {
+                    nz.load(rz[r], r * (int)ldz * (int)sizeof(T));
+                    nv.load(rv[r], r * (int)ldv * (int)sizeof(T));
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    rz[r].load(pz + r * ldz);
+                    rv[r].load(pv + r * ldv);
+                }
             }
         } else {
 #pragma unroll
@@ -313,21 +376,32 @@ __global__ void __launch_bounds__(64 * W) k_recurrence(const T* __restrict__ z, 
         if constexpr (SUMS) {
             exchange.extend(turn, lane, a, whole);
         } else {
-            T* const py = y + row_of(t0, left) * ldy + s.unit;
-            const int stored = full ? R : (int)anew(left);
+            const int64_t row = row_of(t0, left);
+            auto pass = [&](auto&& put) __attribute__((always_inline)) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
+                for (int r = 0; r < R; ++r) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) h[i] = STARTS && (cuts >> r & 1) ? u[r][i] : fmaf(f[r][i], h[i], u[r][i]);
-                if (r < stored) Units<T, V>::put(py + r * ldy, h);
+                    for (int i = 0; i < V; ++i) h[i] = STARTS && (cuts >> r & 1) ? u[r][i] : fmaf(f[r][i], h[i], u[r][i]);
+                    put(r);
+                }
+            };
+            if (full && Near::reaches(row, rows.most)) {
+                const NearRows<T, V> ny(y, ldy, Near(row), s.unit);
+                pass([&](int r) __attribute__((always_inline)) { ny.store(h, r * (int)ldy * (int)sizeof(T)); });
+            } else {
+                T* const py = y + row * ldy + s.unit;
+                const int stored = (int)anew(left);
+                pass([&](int r) __attribute__((always_inline)) {
+                    if (r < stored) Units<T, V>::of(h).put(py + r * ldy);
+                });
             }
         }
     }
     if (wave != 0 || !summed) return;
     if constexpr (SUMS) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum_at(sums, rows, part, 0, s)[i] = whole[i], sum_at(sums, rows, part, 1, s)[i] = carry[i];
-    } else if (last && part == s.parts - 1) {
+        for (int i = 0; i < V; ++i) sum_at(sums, rows, s.part, 0, s)[i] = whole[i], sum_at(sums, rows, s.part, 1, s)[i] = carry[i];
+    } else if (last && s.part == s.parts - 1) {
 #pragma unroll
         for (int i = 0; i < V; ++i) last[s.seq * rows.cols + s.unit + i] = carry[i];
     }
@@ -341,9 +415,9 @@ __global__ void __launch_bounds__(64 * W)
                           const float* dlast, T* __restrict__ dz, int64_t lddz, T* __restrict__ dv, int64_t lddv, float* dfirst, Rows rows,
                           float* __restrict__ sums) {
     __shared__ Exchange<V, W> exchange;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = blockIdx.y;
-    const Span s = span_of<V>(rows, part);
-    const bool summed = SUMS ? s.active && part > 0 : s.active;  // (the first part's sums reach nothing)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Span s = span_of<V>(rows);
+    const bool summed = SUMS ? s.active && s.part > 0 : s.active;  // (the first part's sums reach nothing)
     const int n = summed ? s.n : 0, longest = longest_of(n);
     float carry[V], whole[V], before[V];
 #pragma unroll
@@ -353,8 +427,8 @@ __global__ void __launch_bounds__(64 * W)
         whole[i] = 1.0f;
     }
     if constexpr (!SUMS) {
-        const int behind = longest_of(s.active ? s.parts - 1 - part : 0);
-        if (behind) carry_of_parts(exchange, sums, rows, part + behind, behind, -1, s, wave, lane, carry);
+        const int own = s.active ? s.parts - 1 - s.part : 0;
+        if (const int many = sums ? longest_of(own) : 0) carry_of_parts(exchange, sums, rows, s.parts - 1, own, many, -1, s, wave, lane, carry);
     }
     Units<T, V> rz[R], rd[R], rv[SUMS ? 1 : R], ry[SUMS ? 1 : R];
     Starts<R> rs;
@@ -368,10 +442,20 @@ __global__ void __launch_bounds__(64 * W)
         const int64_t top = top_of(t0, left);
         const T *pz = z + top * ldz + s.unit, *pd = dy + top * lddy + s.unit;
         if (full_of(top, left)) {
+            if (Near::reaches(top - (R - 1), rows.most)) {
+                const Near near(top - (R - 1));
+                const NearRows<T, V> nz(z, ldz, near, s.unit), nd(dy, lddy, near, s.unit);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                rz[r].load(pz - r * ldz);
-                rd[r].load(pd - r * lddy);
+                for (int r = 0; r < R; ++r) {
+                    nz.load(rz[r], (R - 1 - r) * (int)ldz * (int)sizeof(T));
+                    nd.load(rd[r], (R - 1 - r) * (int)lddy * (int)sizeof(T));
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    rz[r].load(pz - r * ldz);
+                    rd[r].load(pd - r * lddy);
+                }
             }
         } else {
 #pragma unroll
@@ -388,10 +472,19 @@ __global__ void __launch_bounds__(64 * W)
         const int64_t top = top_of(t0, left);
         const T *pv = v + top * ldv + s.unit, *py = y + top * ldy + s.unit;
         if (full_of(top, left)) {
+            if (Near::reaches(top - R, rows.most)) {
+                const NearRows<T, V> nv(v, ldv, Near(top - (R - 1)), s.unit), ny(y, ldy, Near(top - R), s.unit);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                rv[r].load(pv - r * ldv);
-                ry[r].load(py - (r + 1) * ldy);
+                for (int r = 0; r < R; ++r) {
+                    nv.load(rv[r], (R - 1 - r) * (int)ldv * (int)sizeof(T));
+                    ny.load(ry[r], (R - 1 - r) * (int)ldy * (int)sizeof(T));
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    rv[r].load(pv - r * ldv);
+                    ry[r].load(py - (r + 1) * ldy);
+                }
             }
         } else {
 #pragma unroll
@@ -443,26 +536,42 @@ __global__ void __launch_bounds__(64 * W)
         if constexpr (SUMS) {
             exchange.extend(turn, lane, a, whole);
         } else {
-            T *const pdz = dz + top * lddz + s.unit, *const pdv = dv + top * lddv + s.unit;
-            const int stored = full ? R : (int)anew(left), inside = full ? R : (int)(top - s.begin < R ? top - s.begin : R);
+            const int inside = full ? R : (int)(top - s.begin < R ? top - s.begin : R);  // rows with one in front of them
+            float oz[V], ov[V];
+            auto pass = [&](auto&& put) __attribute__((always_inline)) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float x[V], h[V], oz[V], ov[V];
-                rv[r].get(x);
-                ry[r].get(h);
-                const bool cut = STARTS && (cuts >> (R - 1 - r) & 1), has = r < inside;
+                for (int r = 0; r < R; ++r) {
+                    float x[V], h[V];
+                    rv[r].get(x);
+                    ry[r].get(h);
+                    const bool cut = STARTS && (cuts >> (R - 1 - r) & 1), has = r < inside;
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float hb = cut ? 0.0f : has ? h[i] : before[i];
-                    const float g = d[r][i] + G[i];
-                    ov[i] = g * rest[r][i];
-                    oz[i] = ov[i] * f[r][i] * (hb - x[i]);
-                    G[i] = cut ? 0.0f : f[r][i] * g;
+                    for (int i = 0; i < V; ++i) {
+                        const float hb = cut ? 0.0f : has ? h[i] : before[i];
+                        const float g = d[r][i] + G[i];
+                        ov[i] = g * rest[r][i];
+                        oz[i] = ov[i] * f[r][i] * (hb - x[i]);
+                        G[i] = cut ? 0.0f : f[r][i] * g;
+                    }
+                    put(r);
                 }
-                if (r < stored) {
-                    Units<T, V>::put(pdv - r * lddv, ov);
-                    Units<T, V>::put(pdz - r * lddz, oz);
-                }
+            };
+            if (full && Near::reaches(top - (R - 1), rows.most)) {
+                const Near near(top - (R - 1));
+                const NearRows<T, V> nz(dz, lddz, near, s.unit), nv(dv, lddv, near, s.unit);
+                pass([&](int r) __attribute__((always_inline)) {
+                    nv.store(ov, (R - 1 - r) * (int)lddv * (int)sizeof(T));
+                    nz.store(oz, (R - 1 - r) * (int)lddz * (int)sizeof(T));
+                });
+            } else {
+                T *const pdz = dz + top * lddz + s.unit, *const pdv = dv + top * lddv + s.unit;
+                const int stored = (int)anew(left);
+                pass([&](int r) __attribute__((always_inline)) {
+                    if (r < stored) {
+                        Units<T, V>::of(ov).put(pdv - r * lddv);
+                        Units<T, V>::of(oz).put(pdz - r * lddz);
+                    }
+                });
             }
             if (t0 + R * W < longest) load_second(t0 + R * W);
         }
@@ -470,8 +579,8 @@ __global__ void __launch_bounds__(64 * W)
     if (wave != 0 || !summed) return;
     if constexpr (SUMS) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum_at(sums, rows, part, 0, s)[i] = whole[i], sum_at(sums, rows, part, 1, s)[i] = carry[i];
-    } else if (dfirst && part == 0) {
+        for (int i = 0; i < V; ++i) sum_at(sums, rows, s.part, 0, s)[i] = whole[i], sum_at(sums, rows, s.part, 1, s)[i] = carry[i];
+    } else if (dfirst && s.part == 0) {
 #pragma unroll
         for (int i = 0; i < V; ++i) dfirst[s.seq * rows.cols + s.unit + i] = carry[i];
     }
@@ -511,62 +620,87 @@ __global__ void __launch_bounds__(256) k_recurrence_step(const T* __restrict__ z
     }
 }
 
-// How sequences are cut: into parts of at least `least` rows.
-struct Cut {
-    int64_t parts, least;
+// How a pass runs: units of a lane, and the parts that sequences are cut into, of at least 2^shift rows (0: not at all).
+//
+// Parts: a launch of their own sums them up, which reads z and v (dy) once more, so a chip that is full without them does better without
+// (128 x 512 x 1024 bfloat16 forward 87 us, in halves 130; ragged 139 and 161); there only sequences of 16 times the mean
+// length and more are cut.  Where it is not, parts shorten what one workgroup does one after the other (2 x 65536 x 256: 83 us; in one part 900).
+// Units: pairs take fewer instructions a value, single units half the time of one workgroup: 37 x 203 x 512 binary16, ragged, 32 us
+// with pairs, 27 without; 128 x 512 x 1024 bfloat16 87 and 91, ragged 162 and 139.
+struct Plan {
+    int units, shift;
+    int64_t across;
 };
-Cut cut_of(int64_t rows, int64_t count, int64_t cols) {
-    const int64_t across = cols > 1 ? (cols + 1) / 2 : 1, groups = (count * across + 63) / 64, mean = rows / count;
-    const int64_t want = 1024 / groups;  // parts of each sequence that fill the chip
-    int64_t least = mean < 1024 ? (mean < 256 ? 1024 : 4 * mean) : want > 1 ? mean / want : 4 * mean;
-    if (least < 256) least = 256;
-    int64_t parts = 8192 / groups;
-    if (parts > kMostParts) parts = kMostParts;
-    if (parts > rows / least) parts = rows / least;
-    return {parts < 1 ? 1 : parts, least};
+Plan plan_of(int64_t rows, int64_t count, int64_t cols, bool ragged) {
+    const int64_t pairs = (cols + 1) / 2, mean = rows / count;
+    int shift = 7;
+    if ((count * pairs + 63) / 64 >= kManyGroups) {
+        while (mean * 8 >> shift) ++shift;
+    } else {
+        while ((rows * pairs >> shift) > 64 * kManyGroups * 2) ++shift;
+    }
+    if (mean < 64 || rows >> shift < 2) shift = 0;  // (sequences of several times as many rows still take less than another launch)
+    const int64_t groups = (((shift ? rows >> shift : 0) + count) * pairs + 63) / 64;
+    const int units = cols > 1 && groups >= kManyGroups * (ragged ? 8 : 1) ? 2 : 1;
+    return {units, shift, units > 1 ? pairs : cols};
 }
 int waves_of(int64_t steps, int rows) { return steps <= rows ? 1 : steps <= 2 * rows ? 2 : steps <= 4 * rows ? 4 : 8; }
 template <int N>
 using Int = std::integral_constant<int, N>;
 // calls go(units of a lane, wavefronts of a workgroup)
 template <class Go>
-aq_status with_form(int64_t cols, int waves, Go&& go) {
-    auto by = [&](auto units) { return waves == 1 ? go(units, Int<1>()) : waves == 2 ? go(units, Int<2>()) : waves == 4 ? go(units, Int<4>()) : go(units, Int<8>()); };
-    return cols > 1 ? by(Int<2>()) : by(Int<1>());
+aq_status with_form(int units, int waves, Go&& go) {
+    auto by = [&](auto u) { return waves == 1 ? go(u, Int<1>()) : waves == 2 ? go(u, Int<2>()) : waves == 4 ? go(u, Int<4>()) : go(u, Int<8>()); };
+    return units > 1 ? by(Int<2>()) : by(Int<1>());
 }
 aq_status launched() { return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK; }
-Rows rows_of(const int32_t* offsets, int64_t rows, int64_t count, int64_t cols) {
-    const Cut cut = cut_of(rows, count, cols);
-    const int64_t each = rows / count, parts = offsets || cut.parts * cut.least <= each ? cut.parts : each / cut.least;
-    return {offsets, rows, cols, each, (int32_t)count, (int32_t)(cols > 1 ? (cols + 1) / 2 : 1), (int32_t)(parts < 1 ? 1 : parts), (int32_t)cut.least};
+Rows rows_of(const Plan& plan, const int32_t* offsets, int64_t count, std::initializer_list<const aq_matrix*> all) {
+    const aq_matrix& z = **all.begin();
+    const int64_t rows = z.rows, cols = z.cols, bytes = (int64_t)dtype_bytes(z.dtype);
+    int64_t most = 0;
+    bool words = true;
+    for (const aq_matrix* m : all) {
+        if (m->ld * bytes > most) most = m->ld * bytes;
+        if (plan.units > 1 && (((uintptr_t)m->d & 3) || (m->ld * bytes & 3) || (cols & 1))) words = false;
+    }
+    const int64_t each = rows / count, parts = !offsets && plan.shift && each >> plan.shift > 1 ? each >> plan.shift : 1;
+    const bool search = offsets && plan.shift;
+    int rounds = 0;
+    while (search && ((int64_t)1 << rounds) < count) ++rounds;
+    return {offsets, rows, cols, each, (int32_t)count, (int32_t)plan.across, (int32_t)(search ? (rows >> plan.shift) + count : count * parts),
+            (int32_t)parts, plan.shift, search && rounds == 0 ? 1 : rounds, words ? (int32_t)most : 0};
 }
-dim3 grid_of(const Rows& r) { return dim3((uint32_t)(((int64_t)r.count * r.across + 63) / 64), r.parts); }
+// whether sequences are in parts
+bool in_parts(const Rows& r) { return r.parts > 1 || r.rounds; }
+int64_t steps_of(const Rows& r) { return in_parts(r) && r.each > 1 << r.shift ? 1 << r.shift : r.each; }
+int64_t grid_of(const Rows& r) { return ((int64_t)r.slots * r.across + 63) / 64; }
 
 }  // namespace
 
 int64_t recurrence_workspace(int64_t rows, int64_t count, int64_t cols) {
     if (count < 1) return 0;
-    const Cut cut = cut_of(rows, count, cols);
-    return cut.parts < 2 ? 0 : (rows / cut.least + count + 1) * 2 * cols * (int64_t)sizeof(float);
+    const Plan plan = plan_of(rows, count, cols, false);
+    return plan.shift ? ((rows >> plan.shift) + count) * 2 * cols * (int64_t)sizeof(float) : 0;
 }
 
 aq_status launch_recurrence_forward(const aq_matrix& z, const aq_matrix& v, const int32_t* offsets, int64_t count, const uint8_t* starts,
                                     const float* first, const aq_matrix& y, float* last, float* ws, hipStream_t st) {
-    constexpr int R = 16;
-    const Rows rows = rows_of(offsets, z.rows, count, z.cols);
-    const int64_t steps = rows.parts > 1 && rows.least < rows.each ? rows.least : rows.each;
+    const Plan plan = plan_of(z.rows, count, z.cols, offsets != nullptr);
+    const Rows rows = rows_of(plan, offsets, count, {&z, &v, &y});
+    if (!grid_ok(grid_of(rows), 64 * 8)) return AQ_ESHAPE;
     return with_dtype(z.dtype, [&](auto t) {
         using T = decltype(t);
-        return with_form(z.cols, waves_of(steps, R), [&](auto units, auto waves) {
-            constexpr int V = decltype(units)::value, W = decltype(waves)::value;
+        return with_form(plan.units, waves_of(steps_of(rows), kRows / plan.units), [&](auto units, auto waves) {
+            constexpr int V = decltype(units)::value, R = kRows / V, W = decltype(waves)::value;
             auto run = [&](auto kernel) {
-                kernel<<<grid_of(rows), 64 * W, 0, st>>>((const T*)z.d, z.ld, (const T*)v.d, v.ld, (T*)y.d, y.ld, starts, first, last, rows, ws);
+                kernel<<<(unsigned)grid_of(rows), 64 * W, 0, st>>>((const T*)z.d, z.ld, (const T*)v.d, v.ld, (T*)y.d, y.ld, starts, first, last, rows,
+                                                         in_parts(rows) ? ws : nullptr);
             };
             if (starts) {
-                if (rows.parts > 1) run(k_recurrence<T, V, R, W, true, true>);
+                if (in_parts(rows)) run(k_recurrence<T, V, R, W, true, true>);
                 run(k_recurrence<T, V, R, W, false, true>);
             } else {
-                if (rows.parts > 1) run(k_recurrence<T, V, R, W, true, false>);
+                if (in_parts(rows)) run(k_recurrence<T, V, R, W, true, false>);
                 run(k_recurrence<T, V, R, W, false, false>);
             }
             return launched();
@@ -577,22 +711,23 @@ aq_status launch_recurrence_forward(const aq_matrix& z, const aq_matrix& v, cons
 aq_status launch_recurrence_backward(const aq_matrix& dy, const float* dlast, const aq_matrix& z, const aq_matrix& v, const aq_matrix& y,
                                      const int32_t* offsets, int64_t count, const uint8_t* starts, const float* first, const aq_matrix& dz,
                                      const aq_matrix& dv, float* dfirst, float* ws, hipStream_t st) {
-    constexpr int R = 8;
-    const Rows rows = rows_of(offsets, z.rows, count, z.cols);
-    const int64_t steps = rows.parts > 1 && rows.least < rows.each ? rows.least : rows.each;
+    const Plan plan = plan_of(z.rows, count, z.cols, offsets != nullptr);
+    const Rows rows = rows_of(plan, offsets, count, {&z, &dy, &v, &y, &dz, &dv});
+    if (!grid_ok(grid_of(rows), 64 * 8)) return AQ_ESHAPE;
     return with_dtype(z.dtype, [&](auto t) {
         using T = decltype(t);
-        return with_form(z.cols, waves_of(steps, R), [&](auto units, auto waves) {
-            constexpr int V = decltype(units)::value, W = decltype(waves)::value;
+        return with_form(plan.units, waves_of(steps_of(rows), kRowsBackward), [&](auto units, auto waves) {
+            constexpr int V = decltype(units)::value, R = kRowsBackward, W = decltype(waves)::value;
             auto run = [&](auto kernel) {
-                kernel<<<grid_of(rows), 64 * W, 0, st>>>((const T*)dy.d, dy.ld, (const T*)z.d, z.ld, (const T*)v.d, v.ld, (const T*)y.d, y.ld, starts, first,
-                                                         dlast, (T*)dz.d, dz.ld, (T*)dv.d, dv.ld, dfirst, rows, ws);
+                kernel<<<(unsigned)grid_of(rows), 64 * W, 0, st>>>((const T*)dy.d, dy.ld, (const T*)z.d, z.ld, (const T*)v.d, v.ld, (const T*)y.d, y.ld, starts, first,
+                                                         dlast, (T*)dz.d, dz.ld, (T*)dv.d, dv.ld, dfirst, rows,
+                                                         in_parts(rows) ? ws : nullptr);
             };
             if (starts) {
-                if (rows.parts > 1) run(k_recurrence_backward<T, V, R, W, true, true>);
+                if (in_parts(rows)) run(k_recurrence_backward<T, V, R, W, true, true>);
                 run(k_recurrence_backward<T, V, R, W, false, true>);
             } else {
-                if (rows.parts > 1) run(k_recurrence_backward<T, V, R, W, true, false>);
+                if (in_parts(rows)) run(k_recurrence_backward<T, V, R, W, true, false>);
                 run(k_recurrence_backward<T, V, R, W, false, false>);
             }
             return launched();
