@@ -143,7 +143,10 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
     const int first = (int)at.z * p.chunks, end = first + p.chunks < p.all ? first + p.chunks : p.all;
     int segment = first / p.each, ahead = first;  // what is loaded next
     int64_t t0 = (int64_t)(first - segment * p.each) * kChunk;
-    auto fetch = [&](int buf) __attribute__((always_inline)) {
+    // what the next chunk's loads need, in scalar registers, then the loads themselves
+    Window wa, wb, wb2;
+    bool there_a = true, there_b = true;
+    auto aim = [&]() __attribute__((always_inline)) {
         const int code = (int)(p.segments >> (5 * (segment < 12 ? segment : 0))) & 31;
         const int64_t which = F == kWeightGrad ? second : code >> 4;
         const bool more = ahead < end;
@@ -151,23 +154,25 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
         const int64_t tb = kAcrossB ? c0 * p.b.ld + t0 * 2 : t0 * p.b.ld + c0 * 2;
         const uint8_t* const pa = p.a.base + (code & 3) * p.a.plane + which * p.a.other;
         const uint8_t* const pb = p.b.base + (code >> 2 & 3) * p.b.plane + (F == kInputGrad ? which * p.b.other : 0);
-        Window wa, wb, wb2;
         wa.set(pa, ta, more ? p.a.bytes : 0);
         wb.set(pb, tb, more ? p.b.bytes : 0);
         if constexpr (F == kForward) wb2.set(pb + p.b.other, tb, more ? p.b.bytes : 0);
         const int left = p.t - t0 < kChunk ? (int)(p.t - t0) : kChunk;
-        const bool there_a = !kAcrossA || 8 * TA::piece(tid) < left, there_b = !kAcrossB || 8 * TB::piece(tid) < left;
-        uint8_t* const to = lds + buf * kBuf + wave * 1024;
-#pragma unroll
-        for (int j = 0; j < J; ++j) load_to_lds(wa, there_a ? off_a[j] : Window::kOutside, to + NT * j * 16);
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const bool up = F == kForward && ((wave * 64 + NT * j) >> 3 & 32);
-            load_to_lds(up ? wb2 : wb, there_b ? off_b[j] : Window::kOutside, to + kSide + NT * j * 16);
-        }
+        there_a = !kAcrossA || 8 * TA::piece(tid) < left;
+        there_b = !kAcrossB || 8 * TB::piece(tid) < left;
         ++ahead;
         t0 += kChunk;
         if (t0 >= p.t) t0 = 0, ++segment;
+    };
+    auto pull = [&](int unit, int buf) __attribute__((always_inline)) {  // units 0 .. J - 1: of a, behind them of b
+        uint8_t* const to = lds + buf * kBuf + wave * 1024;
+        if (unit < J) {
+            load_to_lds(wa, there_a ? off_a[unit] : Window::kOutside, to + NT * unit * 16);
+        } else {
+            const int j = unit - J;
+            const bool up = F == kForward && ((wave * 64 + NT * j) >> 3 & 32);
+            load_to_lds(up ? wb2 : wb, there_b ? off_b[j] : Window::kOutside, to + kSide + NT * j * 16);
+        }
     };
     // ---- products
     v16f32 acc[2][TM];
@@ -185,21 +190,29 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
 #pragma unroll
         for (int i = 0; i < 2; ++i) ob[Q & 1][i] = TB::read(from + kSide, wc + 32 * i, Q, lane);
     };
-    auto products = [&](auto turn) __attribute__((always_inline)) {
+    auto products = [&](auto turn, auto&& between) __attribute__((always_inline)) {
         constexpr int Q = decltype(turn)::value;
         __builtin_amdgcn_sched_barrier(0);  // (the order stays: operands are requested a turn ahead)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < TM; ++j) acc[i][j] = mfma16<H>(ob[Q & 1][i], oa[Q & 1][j], acc[i][j]);
+            for (int j = 0; j < TM; ++j) {
+                acc[i][j] = mfma16<H>(ob[Q & 1][i], oa[Q & 1][j], acc[i][j]);
+                between(i * TM + j);
+            }
         __builtin_amdgcn_sched_barrier(0);
     };
+    auto nothing = [](int) __attribute__((always_inline)) {};
     constexpr std::integral_constant<int, 0> q0{};
     constexpr std::integral_constant<int, 1> q1{};
     constexpr std::integral_constant<int, 2> q2{};
     constexpr std::integral_constant<int, 3> q3{};
 #pragma unroll
-    for (int b = 0; b < kBufs; ++b) fetch(b);
+    for (int b = 0; b < kBufs; ++b) {
+        aim();
+#pragma unroll
+        for (int u = 0; u < 2 * J; ++u) pull(u, b);
+    }
     wait_loads<(kBufs - 1) * 2 * J>();
     lds_barrier();
     int buf = 0;
@@ -208,16 +221,21 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
         const uint8_t* const now = lds + buf * kBuf;
         const int next = buf + 1 == kBufs ? 0 : buf + 1;
         read(q1, now);
-        products(q0);
+        products(q0, nothing);
         read(q2, now);
-        products(q1);
+        aim();
+        products(q1, nothing);
         read(q3, now);
-        products(q2);
+        products(q2, nothing);
         wait_loads<(kBufs - 2) * 2 * J>();  // the next chunk is there,
         lds_barrier();                      // and all of this one in registers
-        fetch(buf);
         read(q0, lds + next * kBuf);
-        products(q3);
+        products(q3, [&](int k) __attribute__((always_inline)) {
+            constexpr int kEach = 2 * J / (2 * TM);
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) pull(k * kEach + u, buf);
+            __builtin_amdgcn_sched_barrier(0);
+        });
         buf = next;
     }
     wait_loads<0>();  // (chunks behind the last one, which arrive as zeros)
