@@ -71,6 +71,20 @@ __device__ __forceinline__ float gate_act(float a, int act, float& slope) {
     return s == 0.0f ? 0.0f : a * s;
 }
 
+// A buffer of `size` bytes, in scalar registers.
+__device__ __forceinline__ v4i scalar_window(const uint8_t* at, int size) {
+    const uint64_t a = (uint64_t)at;
+    return v4i{__builtin_amdgcn_readfirstlane((int)(uint32_t)a), __builtin_amdgcn_readfirstlane((int)(a >> 32) & 0xffff), __builtin_amdgcn_readfirstlane(size),
+               0x00020000};
+}
+// load_to_lds() behind the compiler's back, which else waits for every load that is on its way to LDS in front of a transposing read of
+// LDS, wherever either lies.  `to`: the same for the whole wavefront, a multiple of 16.  (No register receives anything; nothing
+// else here uses M0.)
+__device__ __forceinline__ void pull_to_lds(v4i r, int at, uint8_t* to) {
+    const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m0), "v"(at), "s"(r) : "memory");
+}
+
 template <class H>
 __device__ __forceinline__ v16f32 mfma16(v4u a, v4u b, v16f32 c) {
     if constexpr (std::is_same<H, bf16_t>::value)
@@ -141,37 +155,49 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
         }
     }
     const int first = (int)at.z * p.chunks, end = first + p.chunks < p.all ? first + p.chunks : p.all;
-    int segment = first / p.each, ahead = first;  // what is loaded next
-    int64_t t0 = (int64_t)(first - segment * p.each) * kChunk;
-    // what the next chunk's loads need, in scalar registers, then the loads themselves
-    Window wa, wb, wb2;
-    bool there_a = true, there_b = true;
-    auto aim = [&]() __attribute__((always_inline)) {
+    // What is loaded next: the chunk's first value of both operands, and how many t of its segment are left.  From chunk to chunk addresses
+    // move on; from segment to segment they are formed anew.
+    int segment = first / p.each, ahead = first;
+    int64_t left = p.t - (int64_t)(first - segment * p.each) * kChunk;
+    const uint8_t *from_a, *from_b;
+    auto begin = [&]() __attribute__((always_inline)) {
         const int code = (int)(p.segments >> (5 * (segment < 12 ? segment : 0))) & 31;
-        const int64_t which = F == kWeightGrad ? second : code >> 4;
-        const bool more = ahead < end;
-        const int64_t ta = kAcrossA ? m0 * p.a.ld + t0 * 2 : t0 * p.a.ld + m0 * 2;
-        const int64_t tb = kAcrossB ? c0 * p.b.ld + t0 * 2 : t0 * p.b.ld + c0 * 2;
-        const uint8_t* const pa = p.a.base + (code & 3) * p.a.plane + which * p.a.other;
-        const uint8_t* const pb = p.b.base + (code >> 2 & 3) * p.b.plane + (F == kInputGrad ? which * p.b.other : 0);
-        wa.set(pa, ta, more ? p.a.bytes : 0);
-        wb.set(pb, tb, more ? p.b.bytes : 0);
-        if constexpr (F == kForward) wb2.set(pb + p.b.other, tb, more ? p.b.bytes : 0);
-        const int left = p.t - t0 < kChunk ? (int)(p.t - t0) : kChunk;
-        there_a = !kAcrossA || 8 * TA::piece(tid) < left;
-        there_b = !kAcrossB || 8 * TB::piece(tid) < left;
+        const int64_t which = F == kWeightGrad ? second : code >> 4, t0 = p.t - left;
+        from_a = p.a.base + (code & 3) * p.a.plane + which * p.a.other + (kAcrossA ? m0 * p.a.ld + t0 * 2 : t0 * p.a.ld + m0 * 2);
+        from_b = p.b.base + (code >> 2 & 3) * p.b.plane + (F == kInputGrad ? which * p.b.other : 0) +
+                 (kAcrossB ? c0 * p.b.ld + t0 * 2 : t0 * p.b.ld + c0 * 2);
+    };
+    begin();
+    // rows and bytes of a row that a tile has (a row's last piece is whole)
+    auto most = [](int64_t n, int m) __attribute__((always_inline)) { return n < m ? (int)(n > 0 ? n : 0) : m; };
+    const int rows_a = most(p.m - m0, S), rows_b = most(p.c - c0, F == kForward ? S / 2 : S);
+    const int wide_a = (rows_a + 7 & ~7) * 2, wide_b = (rows_b + 7 & ~7) * 2;
+    v4i wa, wb, wb2;
+    bool there = true;
+    auto aim = [&]() __attribute__((always_inline)) {  // at the next chunk, in scalar registers
+        const int now = ahead < end ? most(left, kChunk) : 0, bytes = (now + 7 & ~7) * 2;
+        wa = scalar_window(from_a, kAcrossA ? (rows_a - 1) * p.a.ld + bytes : now > 0 ? (now - 1) * p.a.ld + wide_a : 0);
+        wb = scalar_window(from_b, kAcrossB ? (rows_b - 1) * p.b.ld + bytes : now > 0 ? (now - 1) * p.b.ld + wide_b : 0);
+        if constexpr (F == kForward) wb2 = scalar_window(from_b + p.b.other, (rows_b - 1) * p.b.ld + bytes);
+        there = 8 * TA::piece(tid) < now;
+        from_a += kAcrossA ? kChunk * 2 : kChunk * (int64_t)p.a.ld;
+        from_b += kAcrossB ? kChunk * 2 : kChunk * (int64_t)p.b.ld;
         ++ahead;
-        t0 += kChunk;
-        if (t0 >= p.t) t0 = 0, ++segment;
+        left -= kChunk;
+        if (left <= 0) {
+            left = p.t;
+            ++segment;
+            begin();
+        }
     };
     auto pull = [&](int unit, int buf) __attribute__((always_inline)) {  // units 0 .. J - 1: of a, behind them of b
         uint8_t* const to = lds + buf * kBuf + wave * 1024;
         if (unit < J) {
-            load_to_lds(wa, there_a ? off_a[unit] : Window::kOutside, to + NT * unit * 16);
+            pull_to_lds(wa, !kAcrossA || there ? off_a[unit] : Window::kOutside, to + NT * unit * 16);
         } else {
             const int j = unit - J;
             const bool up = F == kForward && ((wave * 64 + NT * j) >> 3 & 32);
-            load_to_lds(up ? wb2 : wb, there_b ? off_b[j] : Window::kOutside, to + kSide + NT * j * 16);
+            pull_to_lds(up ? wb2 : wb, !kAcrossB || there ? off_b[j] : Window::kOutside, to + kSide + NT * j * 16);
         }
     };
     // ---- products
