@@ -61,7 +61,7 @@ __device__ __forceinline__ float gate_act(float a, int act, float& slope) {
         if (fabsf(a) > 3.0e18f) slope = p;  // (a^2 infinite)
         return p == 0.0f ? 0.0f : a * p;
     }
-    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(a)), large = 1.0f / (1.0f + e), small = e * large;
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(a)), large = __builtin_amdgcn_rcpf(1.0f + e), small = e * large;
     const float s = a >= 0.0f ? large : small, rest = a >= 0.0f ? small : large;
     if (act == AQ_GATE_SIGMOID) {
         slope = s * rest;
@@ -133,7 +133,8 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
     constexpr bool kAcrossA = F != kWeightGrad, kAcrossB = F == kForward;
     using TA = Tile<S, kAcrossA>;
     using TB = Tile<S, kAcrossB>;
-    constexpr int TM = S / 64, NT = 2 * S, kBufs = gated_buffers(S), kSide = S * 128, kBuf = 2 * kSide, J = 4;
+    // a wavefront's tiles of 32: TM by NC.  (Forward, NC = 4: its features' outputs are whole lines; 551 -> 530 us at 16384 x 4096 x 2048.)
+    constexpr int NC = F == kForward && S == 256 ? 4 : 2, TM = S / 32 / NC, kWavesDown = S / 32 / TM, NT = 2 * S, kBufs = gated_buffers(S), kSide = S * 128, kBuf = 2 * kSide, J = 4;
     static_assert(NT / 64 * 32 * kOutRow<float, 2> <= kBufs * kBuf, "results leave through the buffers");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31;
@@ -141,7 +142,7 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
     const int second = F == kWeightGrad && at.m >= (uint32_t)p.tiles_m;  // which of two outputs
     if (second) at.m -= p.tiles_m;
     const int64_t m0 = (int64_t)at.m * S, c0 = (int64_t)at.c * (F == kForward ? S / 2 : S);
-    const int wm = (wave & 1) * (S / 2), wc = (wave >> 1) * 64;
+    const int wm = wave % kWavesDown * (32 * TM), wc = wave / kWavesDown * (32 * NC);
     // ---- loads
     int off_a[J], off_b[J];
 #pragma unroll
@@ -201,26 +202,26 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
         }
     };
     // ---- products
-    v16f32 acc[2][TM];
+    v16f32 acc[NC][TM];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NC; ++i)
 #pragma unroll
         for (int j = 0; j < TM; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    v4u oa[2][TM], ob[2][2];
+    v4u oa[2][TM], ob[2][NC];
     auto read = [&](auto turn, const uint8_t* from) __attribute__((always_inline)) {
         constexpr int Q = decltype(turn)::value;
 #pragma unroll
         for (int j = 0; j < TM; ++j) oa[Q & 1][j] = TA::read(from, wm + 32 * j, Q, lane);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) ob[Q & 1][i] = TB::read(from + kSide, wc + 32 * i, Q, lane);
+        for (int i = 0; i < NC; ++i) ob[Q & 1][i] = TB::read(from + kSide, wc + 32 * i, Q, lane);
     };
     auto products = [&](auto turn, auto&& between) __attribute__((always_inline)) {
         constexpr int Q = decltype(turn)::value;
         __builtin_amdgcn_sched_barrier(0);  // (the order stays: operands are requested a turn ahead)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < NC; ++i)
 #pragma unroll
             for (int j = 0; j < TM; ++j) {
                 acc[i][j] = mfma16<H>(ob[Q & 1][i], oa[Q & 1][j], acc[i][j]);
@@ -257,7 +258,7 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
         lds_barrier();                      // and all of this one in registers
         read(q0, lds + next * kBuf);
         products(q3, [&](int k) __attribute__((always_inline)) {
-            constexpr int kEach = 2 * J / (2 * TM);
+            constexpr int kEach = 2 * J / (NC * TM);
 #pragma unroll
             for (int u = 0; u < kEach; ++u) pull(k * kEach + u, buf);
             __builtin_amdgcn_sched_barrier(0);
@@ -272,21 +273,22 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
     for (int j = 0; j < TM; ++j) {
         const int64_t row = m0 + wm + 32 * j, rows = p.m - row;
         if constexpr (F == kForward) {
-            const int64_t f = c0 + (wave >> 1) * 32, cols = p.c - f;
+            constexpr int NF = NC / 2;  // blocks of 32 features: 2 i of gate, 2 i + 1 of up
+            const int64_t f = c0 + wc / 2, cols = p.c - f;
+            auto gate = [&](int i, int q, int e) __attribute__((always_inline)) { return acc[2 * i][j][4 * q + e]; };
+            auto up = [&](int i, int q, int e) __attribute__((always_inline)) { return acc[2 * i + 1][j][4 * q + e]; };
             if constexpr (PART) {
                 float* const to = out.part + at.z * out.part_stride + row * out.ld_part + f;
-                store_rows<float, 1>(place, lane, to, out.ld_part, rows, cols, [&](int, int q, int e) { return acc[0][j][4 * q + e]; });
-                store_rows<float, 1>(place, lane, to + out.part_second, out.ld_part, rows, cols, [&](int, int q, int e) { return acc[1][j][4 * q + e]; });
+                store_rows<float, NF>(place, lane, to, out.ld_part, rows, cols, gate);
+                store_rows<float, NF>(place, lane, to + out.part_second, out.ld_part, rows, cols, up);
             } else {
-                store_rows<T, 1>(place, lane, (T*)out.first + row * out.ld_first + f, out.ld_first, rows, cols, [&](int, int q, int e) {
+                store_rows<T, NF>(place, lane, (T*)out.first + row * out.ld_first + f, out.ld_first, rows, cols, [&](int i, int q, int e) {
                     float slope;
-                    return gate_act(acc[0][j][4 * q + e], act, slope) * acc[1][j][4 * q + e];
+                    return gate_act(gate(i, q, e), act, slope) * up(i, q, e);
                 });
                 if (out.second) {
-                    store_rows<T, 1>(place, lane, (T*)out.second + row * out.ld_second + f, out.ld_second, rows, cols,
-                                     [&](int, int q, int e) { return acc[0][j][4 * q + e]; });
-                    store_rows<T, 1>(place, lane, (T*)out.third + row * out.ld_third + f, out.ld_third, rows, cols,
-                                     [&](int, int q, int e) { return acc[1][j][4 * q + e]; });
+                    store_rows<T, NF>(place, lane, (T*)out.second + row * out.ld_second + f, out.ld_second, rows, cols, gate);
+                    store_rows<T, NF>(place, lane, (T*)out.third + row * out.ld_third + f, out.ld_third, rows, cols, up);
                 }
             }
         } else {
