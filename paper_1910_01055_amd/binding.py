@@ -450,13 +450,13 @@ def quantize_tensor(w, rows, cols, wscheme, qdenom, codes, scale, zp, workspace)
 # Python otherwise (`_lib or load()`).
 
 _DTYPES = {}
-_F32 = None
+_F32 = _U8 = _I32 = None
 
 
 def _learn_dtypes():
-    global _F32
+    global _F32, _U8, _I32
     import torch
-    _F32 = torch.float32
+    _F32, _U8, _I32 = torch.float32, torch.uint8, torch.int32
     _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
 
 
@@ -709,6 +709,8 @@ def _here(*tensors):
             if t.is_cuda:
                 raise ValueError(f"a tensor lies on device {t.get_device()}, and {device} is the current one")
             _reachable(t)
+    if _F32 is None:
+        _learn_dtypes()
 
 
 def _plain(t, dtype, n, what):
@@ -760,22 +762,21 @@ def recurrence_workspace(rows, count, cols):
     return _size("aq_recurrence_workspace", rows, count, cols)
 
 
-def _sequences(z, offsets, starts, state, what):
+def _sequences(z, offsets, starts, state):
     """Pointers to offsets, starts and the states of the sequences, and how many these are (as many as `state` has rows, if there are no
     offsets; one without either)."""
-    import torch
     rows, cols = z.shape
     count = offsets.numel() - 1 if offsets is not None else 1 if state is None else state.shape[0]
     if count < 0:
         raise ValueError("offsets holds one value more than there are sequences")
-    return (_plain(offsets, torch.int32, count + 1, "offsets"), count, _plain(starts, torch.uint8, rows, "starts"))
+    return _plain(offsets, _I32, count + 1, "offsets"), count, _plain(starts, _U8, rows, "starts")
 
 
 def recurrence_forward(z, v, first, y, last=None, offsets=None, starts=None, workspace=None):
     """y = h, h_t = f_t h_{t-1} + (1 - f_t) v_t, f = sigmoid(z).  Sequence s has the rows offsets[s] .. offsets[s + 1] (int32), or, without
     offsets, an equal part of all rows: as many sequences as `first` or `last` has rows.  starts: uint8, not 0 where an episode begins."""
     _here(z, v, first, y, last, offsets, starts, workspace)
-    where, count, begin = _sequences(z, offsets, starts, last if first is None else first, "states")
+    where, count, begin = _sequences(z, offsets, starts, last if first is None else first)
     n = count * z.shape[1]
     status = (_lib or load()).aq_recurrence_forward(_matrix(z), _matrix(v), where, count, begin, _vector(first, n, "first"), _matrix(y),
                                                     _vector(last, n, "last"), _ptr(workspace), _bytes(workspace), _stream())
@@ -786,7 +787,7 @@ def recurrence_forward(z, v, first, y, last=None, offsets=None, starts=None, wor
 def recurrence_backward(dy, dlast, z, v, y, first, dz, dv, dfirst=None, offsets=None, starts=None, workspace=None):
     """The gradients of recurrence_forward, from those of y and (None: zeros) of last."""
     _here(dy, dlast, z, v, y, first, dz, dv, dfirst, offsets, starts, workspace)
-    where, count, begin = _sequences(z, offsets, starts, next((t for t in (first, dlast, dfirst) if t is not None), None), "states")
+    where, count, begin = _sequences(z, offsets, starts, next((t for t in (first, dlast, dfirst) if t is not None), None))
     n = count * z.shape[1]
     status = (_lib or load()).aq_recurrence_backward(_matrix(dy), _vector(dlast, n, "dlast"), _matrix(z), _matrix(v), _matrix(y), where, count,
                                                      begin, _vector(first, n, "first"), _matrix(dz), _matrix(dv), _vector(dfirst, n, "dfirst"),
@@ -797,10 +798,9 @@ def recurrence_backward(dy, dlast, z, v, y, first, dz, dv, dfirst=None, offsets=
 
 def recurrence_step(z, v, state, y=None, starts=None):
     """One step of the memories of all rows: `state` (fp32) in place, y the same rounded."""
-    import torch
     _here(z, v, state, y, starts)
     rows, cols = z.shape
-    status = (_lib or load()).aq_recurrence_step(_matrix(z), _matrix(v), _plain(starts, torch.uint8, rows, "starts"),
+    status = (_lib or load()).aq_recurrence_step(_matrix(z), _matrix(v), _plain(starts, _U8, rows, "starts"),
                                                  _vector(state, rows * cols, "state"), None if y is None else _matrix(y), _stream())
     if status:
         raise AqError(status, "aq_recurrence_step")

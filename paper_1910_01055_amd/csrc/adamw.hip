@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(1024) k_grad_norm(const double* __restrict__ i
 }
 
 int64_t chunks_of(int64_t n) { return (n + kValues - 1) / kValues; }
-constexpr int64_t kMostSums = 2048;  // workgroups of a launch for the norm
+uint32_t sums_of(uint32_t chunks) { return chunks < 2048 ? chunks : 2048; }  // workgroups of a launch for the norm
 
 // calls go(tensors, chunks, the indices of the tensors) for every N that hold values
 template <int N, class Go>
@@ -326,7 +326,7 @@ aq_status in_groups(const aq_learned* t, int64_t count, Go&& go) {
 int64_t grad_norm_workspace(const aq_learned* t, int64_t count) {
     int64_t sums = 0;
     in_groups<kTensors>(t, count, [&](const Tensors<kTensors>&, uint32_t chunks, const int64_t*) {
-        sums += chunks < kMostSums ? chunks : kMostSums;
+        sums += sums_of(chunks);
         return AQ_OK;
     });
     return sums * (int64_t)sizeof(double);
@@ -335,7 +335,7 @@ int64_t grad_norm_workspace(const aq_learned* t, int64_t count) {
 aq_status launch_grad_norm(const aq_learned* t, int64_t count, float* norm, void* ws, hipStream_t st) {
     int64_t sums = 0;
     const aq_status done = in_groups<kTensors>(t, count, [&](const Tensors<kTensors>& all, uint32_t chunks, const int64_t*) {
-        const uint32_t grid = chunks < kMostSums ? chunks : (uint32_t)kMostSums;
+        const uint32_t grid = sums_of(chunks);
         k_grad_squares<<<grid, kThreads, 0, st>>>(all, chunks, (double*)ws + sums);
         sums += grid;
         return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;

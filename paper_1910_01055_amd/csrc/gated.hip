@@ -193,18 +193,24 @@ struct Plan {
     int s, slices, chunks;  // tile, slices of so many chunks
 };
 // The tile and the slices by an estimate in us: a launch, the chunks of a workgroup one after the other, each as long as `alone` while few
-// workgroups are about and `full` while as many as fit are, and the join's launch and bytes.
+// workgroups are about and `full` while as many as fit are, and the join's launch and bytes.  Fitted to every tile in one slice, us on
+// tiles of 64 / 128 / 256, bfloat16 (forward, input gradient, both weight gradients):
+//   2048 x 2048 x 2048  69 / 53 / 57,  66 / 44 / 87,  59 / 46 / 51      1024 x 1024 x 1024  16 / 17 / 33,  18 / 23 / 48,  13 / 16 / 28
+//   64 x 2048 x 2048    18 / 24 / 50,  30 / 41 / 85,  14 / 11 / 10      16384 x 512 x 512   52 / 46 / 28,  37 / 26 / 28,  95 / 150 / 324
+// (in eight slices the last weight gradient takes 41 / 32 / 55).
 Plan plan_of(Form form, int64_t m, int64_t c, int64_t t, int segments) {
     struct Kind {
         int s, at_once;
-        float launch, alone, full;
+        float launch, alone, full, more = 0.0f;  // more: for each turn behind the first
     };
-    constexpr Kind kinds[] = {{64, 768, 3.0f, 0.35f, 0.90f}, {128, 256, 3.5f, 0.60f, 0.75f}, {256, 256, 5.0f, 1.10f, 1.80f}};
+    constexpr Kind kinds[3][3] = {{{64, 768, 4.0f, 0.43f, 0.68f, 2.0f}, {128, 512, 4.0f, 0.64f, 1.50f, 2.0f}, {256, 256, 6.0f, 1.45f, 2.05f, 4.0f}},
+                                  {{64, 768, 3.0f, 0.43f, 0.60f}, {128, 256, 3.2f, 0.60f, 0.63f}, {256, 256, 5.0f, 1.28f, 1.72f}},
+                                  {{64, 768, 3.0f, 0.42f, 0.58f}, {128, 256, 3.2f, 0.60f, 0.67f}, {256, 256, 5.0f, 1.30f, 1.70f}}};
     const int64_t outputs = form == kWeightGrad ? 2 : 1, each = t > 0 ? (t + kChunk - 1) / kChunk : 1, all = each * segments;
     Plan best{64, 1, (int)all};
     float least = 3.0e38f;
-    for (const Kind& k : kinds) {
-        const int64_t tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + (form == kForward ? k.s / 2 : k.s) - 1) / (form == kForward ? k.s / 2 : k.s)) * outputs;
+    for (const Kind& k : kinds[form]) {
+        const int64_t wide = form == kForward ? k.s / 2 : k.s, tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + wide - 1) / wide) * outputs;
         for (int64_t want = 1; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
             const int64_t chunks = (all + want - 1) / want, z = (all + chunks - 1) / chunks, wgs = tiles * z;
             const int64_t values = z * m * c * (form == kInputGrad ? 1 : 2);
@@ -214,7 +220,7 @@ Plan plan_of(Form form, int64_t m, int64_t c, int64_t t, int segments) {
             const float share = (float)busy / (float)k.at_once;
             const float chunk = turns > 1 ? k.full * (float)turns : k.alone + (k.full - k.alone) * share * share;
             const float join = z > 1 ? 3.0f + (float)values * 4.0f * (1.0f / 3.5e6f) : 0.0f;
-            const float us = k.launch + join + (float)chunks * chunk;
+            const float us = k.launch + join + (float)chunks * chunk + (float)(turns - 1) * k.more;
             if (us < least) {
                 least = us;
                 best = {k.s, (int)z, (int)chunks};

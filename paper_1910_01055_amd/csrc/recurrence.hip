@@ -89,7 +89,7 @@ __device__ __forceinline__ float apply(float a, float b, float h) { return a < 0
 // floor(begin / 2^shift) + s + p, which no other one's is, and of which there are rows / 2^shift + count: so a slot finds its part
 // by a search among the offsets, long sequences fill as many workgroups as short ones of as many rows, and nothing is written down.
 struct Rows {
-    const int32_t* offsets;
+    const int32_t *offsets, *order;   // order: the sequences, the longest first (NULL: as they are numbered)
     int64_t rows, cols, each;         // each: rows of a sequence, without offsets
     int32_t count, across, slots;     // sequences; lanes to a slot
     int32_t parts, shift, rounds;     // parts of a sequence without offsets; with: rounds of the search (0: slots are sequences)
@@ -112,7 +112,7 @@ __device__ __forceinline__ Span span_of(const Rows& r) {
     if (V > 1 && s.unit > (int)r.cols - V) s.unit = (int)r.cols - V;  // (units that two lanes have are the same in both)
     s.active = slot < r.slots;
     if (r.offsets) {
-        int low = s.active ? slot : 0;
+        int low = !s.active ? 0 : r.order ? r.order[slot] : slot;
         if (r.rounds) {
             low = 0;
             int high = r.count - 1;
@@ -586,6 +586,23 @@ __global__ void __launch_bounds__(64 * W)
     }
 }
 
+// The sequences' numbers, the longest first: those that take longest begin first where not all run at once.
+constexpr int kMostOrdered = 1024;
+__global__ void __launch_bounds__(kMostOrdered) k_recurrence_order(const int32_t* __restrict__ offsets, int64_t rows, int count, int32_t* __restrict__ order) {
+    __shared__ int length[kMostOrdered];
+    const int i = threadIdx.x;
+    int own = 0;
+    if (i < count) {
+        const int64_t a = inside(offsets[i], 0, rows);
+        length[i] = own = (int)(inside(offsets[i + 1], a, rows) - a);
+    }
+    __syncthreads();
+    if (i >= count) return;
+    int before = 0;
+    for (int j = 0; j < count; ++j) before += length[j] > own || (length[j] == own && j < i);
+    order[before] = i;
+}
+
 // One step of `rows` memories: eight units to a thread.
 template <class T>
 __global__ void __launch_bounds__(256) k_recurrence_step(const T* __restrict__ z, int64_t ldz, const T* __restrict__ v, int64_t ldv,
@@ -620,29 +637,28 @@ __global__ void __launch_bounds__(256) k_recurrence_step(const T* __restrict__ z
     }
 }
 
-// How a pass runs: units of a lane, and the parts that sequences are cut into, of at least 2^shift rows (0: not at all).
+// How a pass runs: units of a lane, and either the parts that sequences are cut into, of at least 2^shift rows (0: not at all), or, where
+// sequences are as many as fill the chip, their order.
 //
-// Parts: a launch of their own sums them up, which reads z and v (dy) once more, so a chip that is full without them does better without
-// (128 x 512 x 1024 bfloat16 forward 87 us, in halves 130; ragged 139 and 161); there only sequences of 16 times the mean
-// length and more are cut.  Where it is not, parts shorten what one workgroup does one after the other (2 x 65536 x 256: 83 us; in one part 900).
+// Parts: a launch of their own sums them up, which reads z and v (dy) once more; they shorten what one workgroup does one after the
+// other (2 x 65536 x 256 bfloat16 forward: 82 us; in one part 900) and lose on a chip that is full without them (128 x 512 x 1024: 87 us, in
+// halves 130; ragged 139 and 161).
 // Units: pairs take fewer instructions a value, single units half the time of one workgroup: 37 x 203 x 512 binary16, ragged, 32 us
 // with pairs, 27 without; 128 x 512 x 1024 bfloat16 87 and 91, ragged 162 and 139.
 struct Plan {
     int units, shift;
     int64_t across;
+    bool ordered;
 };
 Plan plan_of(int64_t rows, int64_t count, int64_t cols, bool ragged) {
     const int64_t pairs = (cols + 1) / 2, mean = rows / count;
+    const bool full = (count * pairs + 63) / 64 >= kManyGroups;
     int shift = 7;
-    if ((count * pairs + 63) / 64 >= kManyGroups) {
-        while (mean * 8 >> shift) ++shift;
-    } else {
-        while ((rows * pairs >> shift) > 64 * kManyGroups * 2) ++shift;
-    }
-    if (mean < 64 || rows >> shift < 2) shift = 0;  // (sequences of several times as many rows still take less than another launch)
+    while ((rows * pairs >> shift) > 64 * kManyGroups * 2) ++shift;
+    if (full || mean < 64 || rows >> shift < 2) shift = 0;  // (sequences of several times as many rows still take less than another launch)
     const int64_t groups = (((shift ? rows >> shift : 0) + count) * pairs + 63) / 64;
     const int units = cols > 1 && groups >= kManyGroups * (ragged ? 8 : 1) ? 2 : 1;
-    return {units, shift, units > 1 ? pairs : cols};
+    return {units, shift, units > 1 ? pairs : cols, full && mean >= 64 && count > 1 && count <= kMostOrdered};
 }
 int waves_of(int64_t steps, int rows) { return steps <= rows ? 1 : steps <= 2 * rows ? 2 : steps <= 4 * rows ? 4 : 8; }
 template <int N>
@@ -653,7 +669,6 @@ aq_status with_form(int units, int waves, Go&& go) {
     auto by = [&](auto u) { return waves == 1 ? go(u, Int<1>()) : waves == 2 ? go(u, Int<2>()) : waves == 4 ? go(u, Int<4>()) : go(u, Int<8>()); };
     return units > 1 ? by(Int<2>()) : by(Int<1>());
 }
-aq_status launched() { return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK; }
 Rows rows_of(const Plan& plan, const int32_t* offsets, int64_t count, std::initializer_list<const aq_matrix*> all) {
     const aq_matrix& z = **all.begin();
     const int64_t rows = z.rows, cols = z.cols, bytes = (int64_t)dtype_bytes(z.dtype);
@@ -667,8 +682,15 @@ Rows rows_of(const Plan& plan, const int32_t* offsets, int64_t count, std::initi
     const bool search = offsets && plan.shift;
     int rounds = 0;
     while (search && ((int64_t)1 << rounds) < count) ++rounds;
-    return {offsets, rows, cols, each, (int32_t)count, (int32_t)plan.across, (int32_t)(search ? (rows >> plan.shift) + count : count * parts),
+    return {offsets, nullptr, rows, cols, each, (int32_t)count, (int32_t)plan.across, (int32_t)(search ? (rows >> plan.shift) + count : count * parts),
             (int32_t)parts, plan.shift, search && rounds == 0 ? 1 : rounds, words ? (int32_t)most : 0};
+}
+aq_status launched() { return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK; }
+aq_status order_of(const Plan& plan, Rows& rows, float* ws, hipStream_t st) {
+    if (!rows.offsets || !plan.ordered) return AQ_OK;
+    k_recurrence_order<<<1, kMostOrdered, 0, st>>>(rows.offsets, rows.rows, rows.count, (int32_t*)ws);
+    rows.order = (const int32_t*)ws;
+    return launched();
 }
 // whether sequences are in parts
 bool in_parts(const Rows& r) { return r.parts > 1 || r.rounds; }
@@ -680,14 +702,16 @@ int64_t grid_of(const Rows& r) { return ((int64_t)r.slots * r.across + 63) / 64;
 int64_t recurrence_workspace(int64_t rows, int64_t count, int64_t cols) {
     if (count < 1) return 0;
     const Plan plan = plan_of(rows, count, cols, false);
+    if (plan.ordered) return count * (int64_t)sizeof(int32_t);
     return plan.shift ? ((rows >> plan.shift) + count) * 2 * cols * (int64_t)sizeof(float) : 0;
 }
 
 aq_status launch_recurrence_forward(const aq_matrix& z, const aq_matrix& v, const int32_t* offsets, int64_t count, const uint8_t* starts,
                                     const float* first, const aq_matrix& y, float* last, float* ws, hipStream_t st) {
     const Plan plan = plan_of(z.rows, count, z.cols, offsets != nullptr);
-    const Rows rows = rows_of(plan, offsets, count, {&z, &v, &y});
+    Rows rows = rows_of(plan, offsets, count, {&z, &v, &y});
     if (!grid_ok(grid_of(rows), 64 * 8)) return AQ_ESHAPE;
+    if (const aq_status s = order_of(plan, rows, ws, st); s != AQ_OK) return s;
     return with_dtype(z.dtype, [&](auto t) {
         using T = decltype(t);
         return with_form(plan.units, waves_of(steps_of(rows), kRows / plan.units), [&](auto units, auto waves) {
@@ -712,8 +736,9 @@ aq_status launch_recurrence_backward(const aq_matrix& dy, const float* dlast, co
                                      const int32_t* offsets, int64_t count, const uint8_t* starts, const float* first, const aq_matrix& dz,
                                      const aq_matrix& dv, float* dfirst, float* ws, hipStream_t st) {
     const Plan plan = plan_of(z.rows, count, z.cols, offsets != nullptr);
-    const Rows rows = rows_of(plan, offsets, count, {&z, &dy, &v, &y, &dz, &dv});
+    Rows rows = rows_of(plan, offsets, count, {&z, &dy, &v, &y, &dz, &dv});
     if (!grid_ok(grid_of(rows), 64 * 8)) return AQ_ESHAPE;
+    if (const aq_status s = order_of(plan, rows, ws, st); s != AQ_OK) return s;
     return with_dtype(z.dtype, [&](auto t) {
         using T = decltype(t);
         return with_form(plan.units, waves_of(steps_of(rows), kRowsBackward), [&](auto units, auto waves) {
