@@ -10,6 +10,7 @@ import math
 import pytest
 import torch
 
+import gated_shapes as shapes
 from paper_1910_01055_amd import binding as B
 from test_gpu_learner import DEV, OUT, SENTINEL, TINY, TYPES, U, Framed
 
@@ -110,8 +111,7 @@ def whole(shape, low, high, g, t):
 
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("rows,n,k", [(4096, 1024, 512), (16384, 2048, 64), (700, 520, 1000), (64, 64, 4096), (100, 2048, 2048), (8192, 72, 80), (30000, 24, 136),
-                                      (512, 4096, 256), (2048, 2048, 2048), (320, 1000, 1000)])
+@pytest.mark.parametrize("rows,n,k", shapes.GATED)
 def test_whole_numbers(kind, rows, n, k):
     """Whole numbers whose sums are exact: every tile, slice and segment, value by value."""
     g = torch.Generator(device=DEV).manual_seed(rows + n + k)

@@ -8,6 +8,7 @@ b_t = f b_{t-1} + (E + 4 U) a_t.  What is rounded to a type has half a step of t
 import pytest
 import torch
 
+import gated_shapes as shapes
 from paper_1910_01055_amd import binding as B
 from test_gpu_learner import DEV, OUT, SENTINEL, TINY, TYPES, U, Framed
 
@@ -109,10 +110,28 @@ def test_ragged(kind, c):
     run(offsets, offsets[-1] + 5, c, kind, seed=c)
 
 
-@pytest.mark.parametrize("kind", ["f32", "bf16"])
-@pytest.mark.parametrize("length", [1, 8, 9, 16, 31, 32, 64, 65, 127, 128, 129, 300])
-def test_equal_lengths(kind, length):
-    run([length * i for i in range(6)], 5 * length, 34, kind, seed=length, uniform=True)
+def lengths_of(count, mean, ragged):
+    """As many rows in all; ragged ones from none to some times the mean, in no order."""
+    if not ragged:
+        return [mean] * count
+    g = torch.Generator().manual_seed(count + mean)
+    cuts = torch.randint(0, count * mean + 1, (count - 1,), generator=g).sort()[0].tolist()
+    ends = [0] + cuts + [count * mean]
+    return [b - a for a, b in zip(ends, ends[1:])]
+
+
+@pytest.mark.parametrize("form", shapes.RECURRENCE, ids=lambda f: "x".join(map(str, f[0])))
+def test_every_form(form):
+    """Every number of units and wavefronts, sequences as they are, in parts and in order."""
+    (count, mean, c, ragged), units = form[:2]
+    offsets = [0]
+    for n in lengths_of(count, mean, ragged):
+        offsets.append(offsets[-1] + n)
+    small = offsets[-1] * c < 1 << 21
+    for kind in ("f32", "f16", "bf16") if small else ("bf16",):
+        run(offsets, offsets[-1], c, kind, seed=mean, uniform=not ragged, starts_share=0.03)
+    if small and units > 1:
+        run(offsets, offsets[-1], c, "bf16", seed=mean, uniform=not ragged, starts_share=0.0, gap=1, at=1)
 
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
