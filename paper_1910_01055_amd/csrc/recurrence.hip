@@ -75,7 +75,9 @@ struct Units<T, 2> {
 // sigmoid(z) and sigmoid(-z), neither as a difference from 1: 1 / (1 + e) and e / (1 + e), e = exp(-z) at most 2^126 (a NaN stays one)
 __device__ __forceinline__ void gates(float z, float& f, float& rest) {
     const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(-1.44269504f * z, 126.0f));
-    f = __builtin_amdgcn_rcpf(1.0f + e);
+    // (the reciprocal's last bit, which a unit that remembers for long multiplies by itself, set right by one step of Newton's)
+    const float d = 1.0f + e, r = __builtin_amdgcn_rcpf(d);
+    f = fmaf(fmaf(-d, r, 1.0f), r, r);
     rest = e * f;
 }
 // the same value to the program, another one to the compiler, which else keeps every comparison with it for the second pass in registers
