@@ -1,0 +1,143 @@
+"""A policy with a memory learns from replayed sequences, then acts step by step: `python examples/recurrent_learner.py` on a GPU.
+
+The policy: a gated layer on the observation, a gated linear recurrence over the steps, linear actions.  Behaviour cloning on seeded
+sequences of unequal lengths in which episodes begin anew: the actions to copy are running means of an episode's observations so far, which
+only a memory gives.  A training step runs on the library's operators:
+
+  forward   h = act(x wg^T) * (x wu^T);  z = h wz^T + bz, v = h wv^T;  y_t = f_t y_{t-1} + (1 - f_t) v_t, f = sigmoid(z);  a = y wo^T
+  backward  the recurrence's gradients, then the gated layer's, for all steps of all sequences at once
+  update    AdamW over all tensors in one call, the large ones' moments in 8 bits, gradients limited by the norm of all of them, and the
+            16-bit copies that the next forward pass reads in the same pass
+
+The plain products (wz, wv, wo) are torch's.  Acting takes one step of the recurrence at a time, from the state that the actor keeps.
+"""
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_1910_01055_amd import binding as aq  # noqa: E402
+
+DEV = "cuda:0"
+
+
+class RecurrentPolicy:
+    def __init__(self, inputs=16, width=128, units=96, actions=4, dtype=torch.bfloat16, bits=8, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        shapes = {"wg": (width, inputs), "wu": (width, inputs), "wz": (units, width), "wv": (units, width), "wo": (actions, units), "bz": (units,)}
+        self.dtype, self.units, self.width = dtype, units, width
+        self.master, self.grad, self.w, learned = {}, {}, {}, []
+        for name, shape in shapes.items():
+            w = torch.linspace(0.0, 6.0, units) if name == "bz" else torch.randn(shape, generator=g) / shape[1] ** 0.5
+            self.master[name] = w.to(DEV)
+            n = w.numel()
+            low = dtype != torch.float32 and name != "bz"
+            self.w[name] = self.master[name].to(dtype) if low else self.master[name]
+            self.grad[name] = torch.zeros(shape, dtype=self.w[name].dtype, device=DEV)
+            eight = bits == 8 and name != "bz"
+            m, v = ((aq.moment8_zeros(n, DEV) if eight else torch.zeros(n, device=DEV)) for _ in range(2))
+            learned.append(aq.Learned(self.master[name], self.grad[name], m, v, self.w[name] if low else None, decay=name != "bz"))
+        self.learned = aq.LearnedSet(learned)
+        self.norm = torch.empty(1, device=DEV)
+        self.norm_ws = torch.empty(aq.grad_norm_workspace(self.learned), dtype=torch.uint8, device=DEV)
+        self.steps = 0
+
+    def new(self, *shape, dtype=None):
+        return torch.empty(shape, dtype=dtype or self.dtype, device=DEV)
+
+    def scratch(self, size):
+        return self.new(size, dtype=torch.uint8) if size else None
+
+    def gates(self, h):
+        w = self.w
+        return (h @ w["wz"].t() + w["bz"].to(h.dtype)).contiguous(), (h @ w["wv"].t()).contiguous()
+
+    def forward(self, x, offsets, starts, first):
+        """The actions of all steps; what backward needs is kept."""
+        rows, w = x.shape[0], self.w
+        s = {"x": x, "offsets": offsets, "starts": starts, "first": first}
+        s["h"], s["gate"], s["up"] = (self.new(rows, self.width) for _ in range(3))
+        aq.gated_forward(x, w["wg"], w["wu"], "silu", s["h"], s["gate"], s["up"], self.scratch(aq.gated_forward_workspace(rows, self.width, x.shape[1], self.dtype)))
+        s["z"], s["v"] = self.gates(s["h"])
+        s["y"], s["last"] = self.new(rows, self.units), self.new(*first.shape, dtype=torch.float32)
+        s["ws"] = self.scratch(aq.recurrence_workspace(rows, first.shape[0], self.units))
+        aq.recurrence_forward(s["z"], s["v"], first, s["y"], s["last"], offsets, starts, s["ws"])
+        self.kept = s
+        return s["y"] @ w["wo"].t()
+
+    def backward(self, da):
+        """The weights' gradients from those of the actions; returns the first states'."""
+        s, w, g = self.kept, self.w, self.grad
+        rows = da.shape[0]
+        g["wo"].copy_(da.t() @ s["y"])
+        dy = (da @ w["wo"]).contiguous()
+        dz, dv, dfirst = torch.empty_like(s["z"]), torch.empty_like(s["v"]), torch.empty_like(s["first"])
+        aq.recurrence_backward(dy, None, s["z"], s["v"], s["y"], s["first"], dz, dv, dfirst, s["offsets"], s["starts"], s["ws"])
+        g["wz"].copy_(dz.t() @ s["h"])
+        g["wv"].copy_(dv.t() @ s["h"])
+        g["bz"].copy_(dz.float().sum(0))
+        dh = (dz @ w["wz"] + dv @ w["wv"]).contiguous()
+        aq.gated_backward(dh, s["x"], w["wg"], w["wu"], s["gate"], s["up"], "silu", None, g["wg"], g["wu"],
+                          self.scratch(aq.gated_backward_workspace(rows, self.width, s["x"].shape[1], self.dtype)))
+        return dfirst
+
+    def update(self, lr=3e-3, weight_decay=1e-3, max_norm=1.0):
+        self.steps += 1
+        aq.grad_norm(self.learned, self.norm, self.norm_ws)
+        aq.adamw_step(self.learned, lr, 0.9, 0.99, 1e-8, weight_decay, self.steps, self.norm, max_norm)
+
+    def act(self, x, state, starts=None):
+        """One step of as many environments as x has rows: their actions; `state` moves on."""
+        rows, w = x.shape[0], self.w
+        h = self.new(rows, self.width)
+        aq.gated_forward(x, w["wg"], w["wu"], "silu", h, workspace=self.scratch(aq.gated_forward_workspace(rows, self.width, x.shape[1], self.dtype)))
+        z, v = self.gates(h)
+        y = self.new(rows, self.units)
+        aq.recurrence_step(z, v, state, y, starts)
+        return y @ w["wo"].t()
+
+
+def replayed(count, most, inputs, actions, seed):
+    """Sequences of unequal lengths behind each other: observations, offsets, where episodes begin, and the actions to copy."""
+    g = torch.Generator().manual_seed(seed)
+    lengths = torch.randint(0, most + 1, (count,), generator=g)
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64), lengths.cumsum(0)])
+    rows = int(offsets[-1])
+    x = torch.randn(rows, inputs, generator=g)
+    starts = torch.rand(rows, generator=g) < 0.03
+    begins = starts.clone()
+    begins[offsets[:-1][lengths > 0]] = True
+    episode = begins.cumsum(0) - 1
+    seen = torch.arange(rows) - torch.nonzero(begins)[:, 0][episode] + 1
+    total = x[:, :actions].cumsum(0)
+    before = torch.cat([torch.zeros(1, actions), total])[torch.nonzero(begins)[:, 0]][episode]
+    return x, offsets.to(torch.int32), starts.to(torch.uint8), (total - before) / seen[:, None]
+
+
+def run(steps=300, count=64, most=120, dtype=torch.bfloat16, bits=8, tell=print):
+    """The policy and its losses."""
+    policy = RecurrentPolicy(dtype=dtype, bits=bits)
+    first = torch.zeros(count, policy.units, device=DEV)
+    losses = []
+    for i in range(steps):
+        x, offsets, starts, want = (t.to(DEV) for t in replayed(count, most, 16, 4, seed=i))
+        error = policy.forward(x.to(dtype), offsets, starts, first).float() - want
+        losses.append((error * error).mean())
+        policy.backward((2.0 / error.numel() * error).to(dtype))
+        policy.update()
+        if i % 50 == 0 or i == steps - 1:
+            tell(f"step {i}: loss {float(losses[-1]):.5f}")
+    return policy, torch.stack(losses).cpu()
+
+
+def act_one_by_one(policy, x, starts):
+    """The actions of one sequence, one step after the other."""
+    state = torch.zeros(1, policy.units, device=DEV)
+    return torch.cat([policy.act(x[t:t + 1], state, starts[t:t + 1]) for t in range(x.shape[0])])
+
+
+if __name__ == "__main__":
+    trained, _ = run()
+    obs, _, begins, wanted = (t.to(DEV) for t in replayed(1, 200, 16, 4, seed=10_000))
+    print(f"error of one sequence, step by step: {float(((act_one_by_one(trained, obs.to(trained.dtype), begins).float() - wanted) ** 2).mean()):.5f}")
