@@ -248,9 +248,9 @@ struct Layer {
     Lays lays{};
     int jobs = 0;
     int32_t dtype;
-    Operand operand(const aq_matrix& m) {
+    Operand operand(const aq_matrix& m, bool where_it_lies) {
         Operand o{};
-        if (in_place(m)) {
+        if (where_it_lies) {
             o.base = (const uint8_t*)m.d;
             o.ld = (int32_t)(m.ld * 2);
         } else {
@@ -262,6 +262,14 @@ struct Layer {
             ws += laid_bytes(m.rows, m.cols, m.dtype);
         }
         o.bytes = m.rows > 0 ? (m.rows - 1) * o.ld + up8(m.cols) * 2 : 0;
+        return o;
+    }
+    Operand operand(const aq_matrix& m) { return operand(m, in_place(m)); }
+    // two matrices of the same sizes whose rows lie equally far apart
+    Operand pair(const aq_matrix& a, const aq_matrix& b) {
+        const bool where_they_lie = in_place(a) && in_place(b) && a.ld == b.ld;
+        Operand o = operand(a, where_they_lie);
+        o.other = operand(b, where_they_lie).base - o.base;
         return o;
     }
     aq_status run(hipStream_t st) {
@@ -343,10 +351,7 @@ aq_status launch_gated_forward(const aq_matrix& x, const aq_matrix& wg, const aq
     Layer lay{(uint8_t*)ws};
     lay.dtype = x.dtype;
     const Operand a = lay.operand(x);
-    Operand b = lay.operand(wg);
-    const Operand b2 = lay.operand(wu);
-    if (b.ld != b2.ld || b.plane != b2.plane) return AQ_ESHAPE;
-    b.other = b2.base - b.base;
+    const Operand b = lay.pair(wg, wu);
     const aq_status s = lay.run(st);
     if (s != AQ_OK) return s;
     Outputs out{};
@@ -363,12 +368,7 @@ aq_status launch_gated_backward(const aq_matrix& dy, const aq_matrix& x, const a
     lay.dtype = x.dtype;
     Operand ox{}, ow{}, d{};
     if (dwg) ox = lay.operand(x);
-    if (dx && m > 0) {
-        ow = lay.operand(wg);
-        const Operand second = lay.operand(wu);
-        if (ow.ld != second.ld || ow.plane != second.plane) return AQ_ESHAPE;
-        ow.other = second.base - ow.base;
-    }
+    if (dx && m > 0) ow = lay.pair(wg, wu);
     aq_status s = lay.run(st);
     if (s != AQ_OK) return s;
     d.base = lay.ws;

@@ -100,6 +100,21 @@ def test_rows_apart_and_odd_addresses(kind, gap, at, rows, n, k):
     run(rows, n, k, kind, "gelu", gap, at)
 
 
+@pytest.mark.parametrize("rows", [2, 90])
+@pytest.mark.parametrize("wg_at,wg_gap,wu_at,wu_gap", [(0, 0, 0, 8), (0, 8, 1, 0), (3, 0, 0, 0), (0, 1, 8, 0)])
+def test_weights_that_lie_differently(rows, wg_at, wg_gap, wu_at, wu_gap):
+    """The same values, whatever the addresses and the distances between rows of the two weight matrices."""
+    n, k, t = 40, 56, torch.bfloat16
+    x, wg, wu, dy = (torch.randn(s, device=DEV).to(t) for s in ((rows, k), (n, k), (n, k), (rows, n)))
+    out = []
+    for a, b in ((Framed(n, k, t, 0, 0, wg), Framed(n, k, t, 0, 0, wu)), (Framed(n, k, t, wg_gap, wg_at, wg), Framed(n, k, t, wu_gap, wu_at, wu))):
+        y, gate, up, dx, dwg, dwu = (torch.empty(s, dtype=t, device=DEV) for s in ((rows, n),) * 3 + ((rows, k), (n, k), (n, k)))
+        B.gated_forward(x, a.m, b.m, "silu", y, gate, up, workspace(B.gated_forward_workspace(rows, n, k, t)))
+        B.gated_backward(dy, x, a.m, b.m, gate, up, "silu", dx, dwg, dwu, workspace(B.gated_backward_workspace(rows, n, k, t)))
+        out.append((y, gate, up, dx, dwg, dwu))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [1, 50])
 def test_without_what_is_kept(kind, rows):
