@@ -111,13 +111,16 @@ struct Lay {
 struct Lays {
     Lay job[3];
 };
-// rows of whole pieces, zeros behind their ends
+// rows of whole pieces, zeros behind their ends: piece i of all
 template <class T>
-__global__ void __launch_bounds__(kThreads) k_lay_out(Lays all) {
-    int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    int which = 0;
-    while (which < 2 && i >= all.job[which].pieces) i -= all.job[which++].pieces;
-    const Lay& job = all.job[which];
+__device__ __forceinline__ void lay_out(const Lays& all, int64_t i) {
+    Lay job = all.job[0];  // (picked without an index, which would send the jobs through scratch memory)
+#pragma unroll
+    for (int k = 1; k < 3; ++k)
+        if (i >= job.pieces && all.job[k].pieces) {
+            i -= job.pieces;
+            job = all.job[k];
+        }
     if (i >= job.pieces) return;
     const int64_t across = job.pitch / 8, row = i / across;
     const int at = (int)(i - row * across) * 8;
@@ -127,13 +130,22 @@ __global__ void __launch_bounds__(kThreads) k_lay_out(Lays all) {
     p.get(v);
     put_planes<T>(v, (Half<T>*)job.to + row * job.pitch + at, job.rows * job.pitch);
 }
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_lay_out(Lays all) {
+    lay_out<T>(all, (int64_t)blockIdx.x * kThreads + threadIdx.x);
+}
 
-// dgate and dup, [rows][pitch], zeros behind their ends
+// dgate and dup, [rows][pitch], zeros behind their ends; in front of them `laid` pieces that are laid out
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_gated_slopes(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ gate, int64_t ldgate,
                                                            const T* __restrict__ up, int64_t ldup, int act, Half<T>* __restrict__ dgate,
-                                                           Half<T>* __restrict__ dup, int64_t rows, int cols, int pitch) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, across = pitch / 8, row = i / across;
+                                                           Half<T>* __restrict__ dup, int64_t rows, int cols, int pitch, Lays lays, int64_t laid) {
+    const int64_t of_all = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (of_all < laid) {
+        lay_out<T>(lays, of_all);
+        return;
+    }
+    const int64_t i = of_all - laid, across = pitch / 8, row = i / across;
     if (row >= rows) return;
     const int at = (int)(i - row * across) * 8, left = cols - at;
     Piece<T> pd, pg, pu;
@@ -197,8 +209,10 @@ struct Plan {
 // tiles of 64 / 128 / 256, bfloat16 (forward, input gradient, both weight gradients):
 //   2048 x 2048 x 2048  69 / 53 / 57,  66 / 44 / 87,  59 / 46 / 51      1024 x 1024 x 1024  16 / 17 / 33,  18 / 23 / 48,  13 / 16 / 28
 //   64 x 2048 x 2048    18 / 24 / 50,  30 / 41 / 85,  14 / 11 / 10      16384 x 512 x 512   52 / 46 / 28,  37 / 26 / 28,  95 / 150 / 324
-// (in eight slices the last weight gradient takes 41 / 32 / 55).
-Plan plan_of(Form form, int64_t m, int64_t c, int64_t t, int segments) {
+// (in eight slices the last weight gradient takes 41 / 32 / 55), and fp32 ones on tiles of 64 / 128, chunks of half the length:
+//   4096 x 2048 x 2048  561 / 390,  526 / 355,  511 / 345      300 x 403 x 1111  32 / 60,  25 / 44,  17 / 23
+// (in slices 22 / 21 and 21 / 21 the first two).
+Plan plan_of(Form form, int64_t m, int64_t c, int64_t t, int planes) {
     struct Kind {
         int s, at_once;
         float launch, alone, full, more = 0.0f;  // more: for each turn behind the first
@@ -206,10 +220,15 @@ Plan plan_of(Form form, int64_t m, int64_t c, int64_t t, int segments) {
     constexpr Kind kinds[3][3] = {{{64, 768, 4.0f, 0.43f, 0.68f, 2.0f}, {128, 512, 4.0f, 0.64f, 1.50f, 2.0f}, {256, 256, 6.0f, 1.45f, 2.05f, 4.0f}},
                                   {{64, 768, 3.0f, 0.43f, 0.60f}, {128, 256, 3.2f, 0.60f, 0.63f}, {256, 256, 5.0f, 1.28f, 1.72f}},
                                   {{64, 768, 3.0f, 0.42f, 0.58f}, {128, 256, 3.2f, 0.60f, 0.67f}, {256, 256, 5.0f, 1.30f, 1.70f}}};
-    const int64_t outputs = form == kWeightGrad ? 2 : 1, each = t > 0 ? (t + kChunk - 1) / kChunk : 1, all = each * segments;
+    constexpr Kind kinds3[3][2] = {{{64, 512, 4.0f, 0.68f, 1.05f, 2.0f}, {128, 256, 4.5f, 1.15f, 1.44f, 2.0f}},
+                                   {{64, 512, 3.0f, 0.70f, 1.02f}, {128, 256, 3.5f, 1.15f, 1.38f}},
+                                   {{64, 512, 3.0f, 0.65f, 1.00f}, {128, 256, 3.5f, 1.15f, 1.35f}}};
+    const int64_t chunk = chunk_of(planes), outputs = form == kWeightGrad ? 2 : 1, each = t > 0 ? (t + chunk - 1) / chunk : 1;
+    const int64_t all = each * (form == kInputGrad ? 2 : 1);
     Plan best{64, 1, (int)all};
     float least = 3.0e38f;
-    for (const Kind& k : kinds[form]) {
+    for (int i = 0; i < (planes == 1 ? 3 : 2); ++i) {
+        const Kind& k = planes == 1 ? kinds[form][i] : kinds3[form][i];
         const int64_t wide = form == kForward ? k.s / 2 : k.s, tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + wide - 1) / wide) * outputs;
         for (int64_t want = 1; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
             const int64_t chunks = (all + want - 1) / want, z = (all + chunks - 1) / chunks, wgs = tiles * z;
@@ -218,9 +237,9 @@ Plan plan_of(Form form, int64_t m, int64_t c, int64_t t, int segments) {
             const int64_t busy = wgs <= 256 ? wgs : (wgs + 255) / 256 * 256;
             const int64_t turns = (busy + k.at_once - 1) / k.at_once;
             const float share = (float)busy / (float)k.at_once;
-            const float chunk = turns > 1 ? k.full * (float)turns : k.alone + (k.full - k.alone) * share * share;
+            const float one = turns > 1 ? k.full * (float)turns : k.alone + (k.full - k.alone) * share * share;
             const float join = z > 1 ? 3.0f + (float)values * 4.0f * (1.0f / 3.5e6f) : 0.0f;
-            const float us = k.launch + join + (float)chunks * chunk + (float)(turns - 1) * k.more;
+            const float us = k.launch + join + (float)chunks * one + (float)(turns - 1) * k.more;
             if (us < least) {
                 least = us;
                 best = {k.s, (int)z, (int)chunks};
@@ -230,12 +249,11 @@ Plan plan_of(Form form, int64_t m, int64_t c, int64_t t, int segments) {
     return best;
 }
 int planes_of(int32_t dtype) { return dtype == AQ_F32 ? 3 : 1; }
-int segments_count(Form form, int32_t dtype) { return (dtype == AQ_F32 ? 6 : 1) * (form == kInputGrad ? 2 : 1); }
 int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
 int64_t up256(int64_t n) { return (n + 255) & ~(int64_t)255; }
 int64_t laid_bytes(int64_t rows, int64_t cols, int32_t dtype) { return up256(rows * up8(cols) * 2 * planes_of(dtype)); }
 int64_t part_bytes(Form form, int64_t m, int64_t c, int64_t t, int32_t dtype) {
-    const Plan p = plan_of(form, m, c, t, segments_count(form, dtype));
+    const Plan p = plan_of(form, m, c, t, planes_of(dtype));
     return p.slices > 1 ? up256((int64_t)p.slices * m * c * (form == kInputGrad ? 1 : 2) * 4) : 0;
 }
 constexpr int64_t kFewRows = 4;
@@ -272,9 +290,13 @@ struct Layer {
         o.other = operand(b, where_they_lie).base - o.base;
         return o;
     }
-    aq_status run(hipStream_t st) {
+    int64_t pieces_of_all() const {
         int64_t pieces = 0;
         for (int i = 0; i < jobs; ++i) pieces += lays.job[i].pieces;
+        return pieces;
+    }
+    aq_status run(hipStream_t st) {
+        const int64_t pieces = pieces_of_all();
         if (pieces == 0) return AQ_OK;
         if (!grid_ok((pieces + kThreads - 1) / kThreads, kThreads)) return AQ_ESHAPE;
         return with_dtype(dtype, [&](auto t) {
@@ -285,15 +307,14 @@ struct Layer {
 };
 // a product's sums: planned, run, joined
 aq_status run_product(Form form, int32_t dtype, Operand a, Operand b, int64_t m, int64_t c, int64_t t, Outputs out, int act, uint8_t* ws, hipStream_t st) {
-    int count;
     Product p{};
-    p.segments = segments_of(dtype == AQ_F32, form == kInputGrad ? 2 : 1, count);
-    const Plan plan = plan_of(form, m, c, t, count);
+    const int chunk = chunk_of(planes_of(dtype));
+    const Plan plan = plan_of(form, m, c, t, planes_of(dtype));
     p.a = a;
     p.b = b;
     p.m = m, p.c = c, p.t = t;
-    p.each = t > 0 ? (int32_t)((t + kChunk - 1) / kChunk) : 1;
-    p.all = p.each * count;
+    p.each = t > 0 ? (int32_t)((t + chunk - 1) / chunk) : 1;
+    p.all = p.each * (form == kInputGrad ? 2 : 1);
     p.chunks = plan.chunks;
     p.tiles_m = (int32_t)((m + plan.s - 1) / plan.s);
     const int features = form == kForward ? plan.s / 2 : plan.s;
@@ -369,7 +390,7 @@ aq_status launch_gated_backward(const aq_matrix& dy, const aq_matrix& x, const a
     Operand ox{}, ow{}, d{};
     if (dwg) ox = lay.operand(x);
     if (dx && m > 0) ow = lay.pair(wg, wu);
-    aq_status s = lay.run(st);
+    aq_status s = m == 0 ? lay.run(st) : AQ_OK;
     if (s != AQ_OK) return s;
     d.base = lay.ws;
     d.ld = (int32_t)(pitch * 2);
@@ -378,13 +399,13 @@ aq_status launch_gated_backward(const aq_matrix& dy, const aq_matrix& x, const a
     d.bytes = m * pitch * 2;
     lay.ws += 2 * d.other;
     if (m > 0) {
-        const int64_t pieces = m * (pitch / 8);
+        const int64_t laid = lay.pieces_of_all(), pieces = laid + m * (pitch / 8);
         if (!grid_ok((pieces + kThreads - 1) / kThreads, kThreads)) return AQ_ESHAPE;
         s = with_dtype(x.dtype, [&](auto t) {
             using T = decltype(t);
             k_gated_slopes<T><<<(unsigned)((pieces + kThreads - 1) / kThreads), kThreads, 0, st>>>(
                 (const T*)dy.d, dy.ld, (const T*)gate.d, gate.ld, (const T*)up.d, up.ld, act, (Half<T>*)d.base, (Half<T>*)(d.base + d.other), m, (int)n,
-                (int)pitch);
+                (int)pitch, lay.lays, laid);
             return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
         });
         if (s != AQ_OK) return s;

@@ -2,7 +2,7 @@
 // that have t along their rows or along their columns.
 //
 // Values are 16 bits wide.  fp32 matrices come as three bf16 planes, whose sum they are, and their products as the six pairs of planes
-// that reach 2^-24 of them: pairs, like the two halves of dx = dgate wg + dup wu, are segments of one long sum over t.
+// that reach 2^-24 of them.  The two halves of dx = dgate wg + dup wu are segments of one long sum over t.
 #pragma once
 #include "learner.hpp"
 #include "product_device.hpp"
@@ -12,7 +12,7 @@ namespace aq {
 typedef f16_t v8f16 __attribute__((ext_vector_type(8)));
 typedef short v4s16 __attribute__((ext_vector_type(4)));
 
-constexpr int kChunk = 64;  // t at a time
+constexpr int chunk_of(int planes) { return planes == 1 ? 64 : 32; }  // t at a time
 
 struct Operand {
     const uint8_t* base;
@@ -23,7 +23,6 @@ struct Operand {
 struct Product {
     Operand a, b;
     int64_t m, c, t;      // of one output; t: of a segment
-    uint64_t segments;    // five bits each: plane of a, plane of b, which matrices
     int32_t each, chunks;  // chunks of a segment, of a slice
     int32_t all;          // of all segments
     int32_t tiles_m, tiles_c;  // of one output, in tiles (gated: of S / 2 features)
@@ -36,18 +35,8 @@ struct Outputs {
 };
 enum Form { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
 
-// what three planes or one hold: pairs in the order of their size, the smallest first
-constexpr int kPlanes3[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
-inline uint64_t segments_of(bool planes, int halves, int& count) {
-    uint64_t s = 0;
-    count = 0;
-    for (int p = 0; p < (planes ? 6 : 1); ++p)
-        for (int h = 0; h < halves; ++h) {
-            const uint64_t code = planes ? kPlanes3[p][0] | kPlanes3[p][1] << 2 | h << 4 : h << 4;
-            s |= code << (5 * count++);
-        }
-    return s;
-}
+// the pairs of planes, the smallest products first
+constexpr int kPairs[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
 
 __device__ __forceinline__ float gate_act(float a, int act, float& slope) {
     if (act == AQ_GATE_RELU) {
@@ -92,26 +81,28 @@ __device__ __forceinline__ v16f32 mfma16(v4u a, v4u b, v16f32 c) {
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8f16, a), __builtin_bit_cast(v8f16, b), c, 0, 0, 0);
 }
 
-// A chunk of an operand in LDS.  t along the rows of memory's matrix (kAcross): S rows of 64 t, 128 bytes each, 16-byte piece s of row r in
-// place s ^ (r / 2 mod 8).  t along its columns: 64 rows of S values, 32-byte piece p of row t in place p ^ 2 (t mod 4); the read
-// transposes four rows of 16 columns at once.  Either way the rows (pieces) that a read takes at once lie in different banks, and either way
-// pieces lie so that a wavefront's loads to LDS fill 1 KB in a row: what is permuted is which piece of memory a lane asks for.
-template <int S, bool kAcross>
+// A chunk of an operand in LDS.  t along the rows of memory's matrix (kAcross): S rows of C t, whose 16-byte piece s of row r lies in
+// place s ^ (r / 2 mod 8) (C = 32: s ^ (r / 4 mod 4)).  t along its columns: C rows of S values, 32-byte piece p of row t in place
+// p ^ 2 (t mod 4); the read transposes four rows of 16 columns at once.  Either way the rows (pieces) that a read takes at once lie in different
+// banks, and either way pieces lie so that a wavefront's loads to LDS fill 1 KB in a row: what is permuted is which piece of memory a lane asks
+// for.
+template <int S, bool kAcross, int C>
 struct Tile {
-    static constexpr int NT = 2 * S, J = 4;
+    static constexpr int NT = 2 * S, kRow = C / 8, J = C / 16;  // threads; pieces of a row; units of a thread
     // byte offset in memory of this thread's unit j, from the tile's first value of the chunk
     static __device__ __forceinline__ int offset(int tid, int j, int ld) {
         const int u = tid + NT * j;
-        if constexpr (kAcross) return (u >> 3) * ld + piece(tid) * 16;
+        if constexpr (kAcross) return (u / kRow) * ld + piece(tid) * 16;
         const int t = u / (S / 8), s = u % (S / 8);
         return t * ld + ((((s >> 1) ^ ((t & 3) << 1 & (S / 16 - 1))) << 4) + ((s & 1) << 3)) * 2;
     }
-    static __device__ __forceinline__ int piece(int tid) { return (tid & 7) ^ ((tid >> 4) & 7); }
+    static __device__ __forceinline__ int place_of(int row) { return C == 64 ? row >> 1 & 7 : row >> 2 & 3; }
+    static __device__ __forceinline__ int piece(int tid) { return (tid % kRow) ^ place_of(tid / kRow); }
     // 32 rows (columns) from `at` on, 16 t from 16 Q on, as an MFMA operand: lane l has row l mod 32, t = 8 (l / 32) .. + 7
     static __device__ __forceinline__ v4u read(const uint8_t* tile, int at, int q, int lane) {
         if constexpr (kAcross) {
             const int r = lane & 31;
-            return *(const v4u*)(tile + (at + r) * 128 + (((2 * q + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4));
+            return *(const v4u*)(tile + (at + r) * (2 * C) + (((2 * q + (lane >> 5)) ^ place_of(r)) << 4));
         } else {
             typedef __attribute__((address_space(3))) v4s16* lds_ptr;
             const int i = lane & 15, t = 16 * q + 8 * (lane >> 5) + (i >> 2), col = at + (lane & 16);
@@ -124,19 +115,22 @@ struct Tile {
 };
 // Two buffers where a third would keep another workgroup from a CU that it would fill (forward, tiles of 128: while one writes its
 // results, the other's products run; 4096 x 1024 x 256 bfloat16 21.8 -> 15.9 us), three where loads are what is waited for.
-constexpr int gated_buffers(int s, Form f) { return s == 256 || (s == 128 && f == kForward) ? 2 : 3; }
-constexpr int gated_lds(int s, Form f) { return gated_buffers(s, f) * 2 * s * 128; }
+constexpr int gated_buffers(int s, Form f, int planes) { return planes == 1 && (s == 256 || (s == 128 && f == kForward)) ? 2 : 3; }
+constexpr int gated_lds(int s, Form f, int planes) { return gated_buffers(s, f, planes) * planes * 2 * s * chunk_of(planes) * 2; }
 
 // C tile of S x S (gated: S rows of S / 2 features, gate and up in blocks of 32 columns in turn), a wavefront 32 TM rows of 64 columns.
 // A chunk's products come in four turns of 16 t, whose operands are read a turn ahead; behind the third all of a chunk is in registers, and
-// the barrier there hands its buffer to the chunk kBufs ahead.
-template <class H, class T, int S, Form F, bool PART>
+// the barrier there hands its buffer to the chunk kBufs ahead.  (P = 3: three planes of both operands, whose six pairs are formed of what is
+// read once; a chunk has two turns.)
+template <class H, class T, int S, Form F, bool PART, int P>
 __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs out, int act) {
     constexpr bool kAcrossA = F != kWeightGrad, kAcrossB = F == kForward;
-    using TA = Tile<S, kAcrossA>;
-    using TB = Tile<S, kAcrossB>;
+    constexpr int C = chunk_of(P);
+    using TA = Tile<S, kAcrossA, C>;
+    using TB = Tile<S, kAcrossB, C>;
     // a wavefront's tiles of 32: TM by NC.  (Forward, NC = 4: its features' outputs are whole lines; 551 -> 530 us at 16384 x 4096 x 2048.)
-    constexpr int NC = F == kForward && S == 256 ? 4 : 2, TM = S / 32 / NC, kWavesDown = S / 32 / TM, NT = 2 * S, kBufs = gated_buffers(S, F), kSide = S * 128, kBuf = 2 * kSide, J = 4;
+    constexpr int NC = F == kForward && S == 256 ? 4 : 2, TM = S / 32 / NC, kWavesDown = S / 32 / TM, NT = 2 * S;
+    constexpr int kBufs = gated_buffers(S, F, P), kPlane = S * C * 2, kSide = P * kPlane, kBuf = 2 * kSide, J = TA::J, kUnits = 2 * P * J;
     static_assert(NT / 64 * 32 * kOutRow<float, 2> <= kBufs * kBuf, "results leave through the buffers");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31;
@@ -151,7 +145,7 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
     for (int j = 0; j < J; ++j) {
         off_a[j] = TA::offset(tid, j, p.a.ld);
         if constexpr (F == kForward) {  // rows 64 i .. of the tile: 32 of wg and 32 of wu from feature 32 i on
-            const int row = (tid + NT * j) >> 3;
+            const int row = (tid + NT * j) / TB::kRow;
             off_b[j] = ((row >> 6 << 5) + (row & 31)) * p.b.ld + TB::piece(tid) * 16;
         } else {
             off_b[j] = TB::offset(tid, j, p.b.ld);
@@ -161,46 +155,47 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
     // What is loaded next: the chunk's first value of both operands, and how many t of its segment are left.  From chunk to chunk addresses
     // move on; from segment to segment they are formed anew.
     int segment = first / p.each, ahead = first;
-    int64_t left = p.t - (int64_t)(first - segment * p.each) * kChunk;
+    int64_t left = p.t - (int64_t)(first - segment * p.each) * C;
     const uint8_t *from_a, *from_b;
     auto begin = [&]() __attribute__((always_inline)) {
-        const int code = (int)(p.segments >> (5 * (segment < 12 ? segment : 0))) & 31;
-        const int64_t which = F == kWeightGrad ? second : code >> 4, t0 = p.t - left;
-        from_a = p.a.base + (code & 3) * p.a.plane + which * p.a.other + (kAcrossA ? m0 * p.a.ld + t0 * 2 : t0 * p.a.ld + m0 * 2);
-        from_b = p.b.base + (code >> 2 & 3) * p.b.plane + (F == kInputGrad ? which * p.b.other : 0) +
-                 (kAcrossB ? c0 * p.b.ld + t0 * 2 : t0 * p.b.ld + c0 * 2);
+        const int64_t which = F == kWeightGrad ? second : F == kInputGrad ? segment & 1 : 0, t0 = p.t - left;
+        from_a = p.a.base + which * p.a.other + (kAcrossA ? m0 * p.a.ld + t0 * 2 : t0 * p.a.ld + m0 * 2);
+        from_b = p.b.base + (F == kInputGrad ? which * p.b.other : 0) + (kAcrossB ? c0 * p.b.ld + t0 * 2 : t0 * p.b.ld + c0 * 2);
     };
     begin();
     // rows and bytes of a row that a tile has (a row's last piece is whole)
     auto most = [](int64_t n, int m) __attribute__((always_inline)) { return n < m ? (int)(n > 0 ? n : 0) : m; };
     const int rows_a = most(p.m - m0, S), rows_b = most(p.c - c0, F == kForward ? S / 2 : S);
     const int wide_a = (rows_a + 7 & ~7) * 2, wide_b = (rows_b + 7 & ~7) * 2;
-    v4i wa, wb, wb2;
+    v4i wa[P], wb[P], wb2[P];
     bool there = true;
     auto aim = [&]() __attribute__((always_inline)) {  // at the next chunk, in scalar registers
-        const int now = ahead < end ? most(left, kChunk) : 0, bytes = (now + 7 & ~7) * 2;
-        wa = scalar_window(from_a, kAcrossA ? (rows_a - 1) * p.a.ld + bytes : now > 0 ? (now - 1) * p.a.ld + wide_a : 0);
-        wb = scalar_window(from_b, kAcrossB ? (rows_b - 1) * p.b.ld + bytes : now > 0 ? (now - 1) * p.b.ld + wide_b : 0);
-        if constexpr (F == kForward) wb2 = scalar_window(from_b + p.b.other, (rows_b - 1) * p.b.ld + bytes);
+        const int now = ahead < end ? most(left, C) : 0, bytes = (now + 7 & ~7) * 2;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            wa[k] = scalar_window(from_a + k * p.a.plane, kAcrossA ? (rows_a - 1) * p.a.ld + bytes : now > 0 ? (now - 1) * p.a.ld + wide_a : 0);
+            wb[k] = scalar_window(from_b + k * p.b.plane, kAcrossB ? (rows_b - 1) * p.b.ld + bytes : now > 0 ? (now - 1) * p.b.ld + wide_b : 0);
+            if constexpr (F == kForward) wb2[k] = scalar_window(from_b + k * p.b.plane + p.b.other, (rows_b - 1) * p.b.ld + bytes);
+        }
         there = 8 * TA::piece(tid) < now;
-        from_a += kAcrossA ? kChunk * 2 : kChunk * (int64_t)p.a.ld;
-        from_b += kAcrossB ? kChunk * 2 : kChunk * (int64_t)p.b.ld;
+        from_a += kAcrossA ? C * 2 : C * (int64_t)p.a.ld;
+        from_b += kAcrossB ? C * 2 : C * (int64_t)p.b.ld;
         ++ahead;
-        left -= kChunk;
+        left -= C;
         if (left <= 0) {
             left = p.t;
             ++segment;
             begin();
         }
     };
-    auto pull = [&](int unit, int buf) __attribute__((always_inline)) {  // units 0 .. J - 1: of a, behind them of b
-        uint8_t* const to = lds + buf * kBuf + wave * 1024;
-        if (unit < J) {
-            pull_to_lds(wa, !kAcrossA || there ? off_a[unit] : Window::kOutside, to + NT * unit * 16);
+    auto pull = [&](int unit, int buf) __attribute__((always_inline)) {  // units 0 .. P J - 1: planes of a, behind them of b
+        const int k = unit / J % P, j = unit % J;
+        uint8_t* const to = lds + buf * kBuf + wave * 1024 + k * kPlane + NT * j * 16;
+        if (unit < P * J) {
+            pull_to_lds(wa[k], !kAcrossA || there ? off_a[j] : Window::kOutside, to);
         } else {
-            const int j = unit - J;
-            const bool up = F == kForward && ((wave * 64 + NT * j) >> 3 & 32);
-            pull_to_lds(up ? wb2 : wb, !kAcrossB || there ? off_b[j] : Window::kOutside, to + kSide + NT * j * 16);
+            const bool up = F == kForward && ((wave * 64 + NT * j) / TB::kRow & 32);
+            pull_to_lds(up ? wb2[k] : wb[k], !kAcrossB || there ? off_b[j] : Window::kOutside, to + kSide);
         }
     };
     // ---- products
@@ -211,38 +206,44 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
         for (int j = 0; j < TM; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    v4u oa[2][TM], ob[2][NC];
+    v4u oa[2][P][TM], ob[2][P][NC];
     auto read = [&](auto turn, const uint8_t* from) __attribute__((always_inline)) {
         constexpr int Q = decltype(turn)::value;
 #pragma unroll
-        for (int j = 0; j < TM; ++j) oa[Q & 1][j] = TA::read(from, wm + 32 * j, Q, lane);
+        for (int k = 0; k < P; ++k) {
 #pragma unroll
-        for (int i = 0; i < NC; ++i) ob[Q & 1][i] = TB::read(from + kSide, wc + 32 * i, Q, lane);
+            for (int j = 0; j < TM; ++j) oa[Q & 1][k][j] = TA::read(from + k * kPlane, wm + 32 * j, Q, lane);
+#pragma unroll
+            for (int i = 0; i < NC; ++i) ob[Q & 1][k][i] = TB::read(from + kSide + k * kPlane, wc + 32 * i, Q, lane);
+        }
     };
+    constexpr int kProducts = (P == 1 ? 1 : 6) * NC * TM;  // of a turn
     auto products = [&](auto turn, auto&& between) __attribute__((always_inline)) {
         constexpr int Q = decltype(turn)::value;
         __builtin_amdgcn_sched_barrier(0);  // (the order stays: operands are requested a turn ahead)
 #pragma unroll
-        for (int i = 0; i < NC; ++i)
+        for (int k = 0; k < (P == 1 ? 1 : 6); ++k)
 #pragma unroll
-            for (int j = 0; j < TM; ++j) {
-                acc[i][j] = mfma16<H>(ob[Q & 1][i], oa[Q & 1][j], acc[i][j]);
-                between(i * TM + j);
-            }
+            for (int i = 0; i < NC; ++i)
+#pragma unroll
+                for (int j = 0; j < TM; ++j) {
+                    acc[i][j] = mfma16<H>(ob[Q & 1][P == 1 ? 0 : kPairs[k][1]][i], oa[Q & 1][P == 1 ? 0 : kPairs[k][0]][j], acc[i][j]);
+                    between((k * NC + i) * TM + j);
+                }
         __builtin_amdgcn_sched_barrier(0);
     };
     auto nothing = [](int) __attribute__((always_inline)) {};
     constexpr std::integral_constant<int, 0> q0{};
     constexpr std::integral_constant<int, 1> q1{};
     constexpr std::integral_constant<int, 2> q2{};
-    constexpr std::integral_constant<int, 3> q3{};
+    constexpr std::integral_constant<int, C / 16 - 1> last{};
 #pragma unroll
     for (int b = 0; b < kBufs; ++b) {
         aim();
 #pragma unroll
-        for (int u = 0; u < 2 * J; ++u) pull(u, b);
+        for (int u = 0; u < kUnits; ++u) pull(u, b);
     }
-    wait_loads<(kBufs - 1) * 2 * J>();
+    wait_loads<(kBufs - 1) * kUnits>();
     lds_barrier();
     int buf = 0;
     read(q0, lds);
@@ -250,19 +251,24 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
         const uint8_t* const now = lds + buf * kBuf;
         const int next = buf + 1 == kBufs ? 0 : buf + 1;
         read(q1, now);
-        products(q0, nothing);
-        read(q2, now);
-        aim();
-        products(q1, nothing);
-        read(q3, now);
-        products(q2, nothing);
-        wait_loads<(kBufs - 2) * 2 * J>();  // the next chunk is there,
-        lds_barrier();                      // and all of this one in registers
+        if constexpr (C == 64) {
+            products(q0, nothing);
+            read(q2, now);
+            aim();
+            products(q1, nothing);
+            read(last, now);
+            products(q2, nothing);
+        } else {
+            aim();
+            products(q0, nothing);
+        }
+        wait_loads<(kBufs - 2) * kUnits>();  // the next chunk is there,
+        lds_barrier();                       // and all of this one in registers
         read(q0, lds + next * kBuf);
-        products(q3, [&](int k) __attribute__((always_inline)) {
-            constexpr int kEach = 2 * J / (NC * TM);
+        products(last, [&](int k) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < kEach; ++u) pull(k * kEach + u, buf);
+            for (int u = 0; u < kUnits; ++u)
+                if (u * kProducts / kUnits == k) pull(u, buf);
             __builtin_amdgcn_sched_barrier(0);
         });
         buf = next;
@@ -314,24 +320,31 @@ aq_status launch_gated_weight_product(int type, int s, bool part, const Product&
 
 template <Form F>
 aq_status launch_gated_product(int type, int s, bool part, const Product& p, const Outputs& out, int act, int slices, hipStream_t st) {
-    auto go = [&](auto h, auto t, auto size, auto parts) {
+    auto go = [&](auto h, auto t, auto size, auto parts, auto planes) {
         using H = decltype(h);
         using T = decltype(t);
-        constexpr int S = decltype(size)::value;
-        auto* const k = k_gated_product<H, T, S, F, decltype(parts)::value>;
+        constexpr int S = decltype(size)::value, P = decltype(planes)::value, kLds = gated_lds(S, F, P);
+        static_assert(kLds <= kMostLds, "");
+        auto* const k = k_gated_product<H, T, S, F, decltype(parts)::value, P>;
         const int64_t grid = (int64_t)p.tiles_m * (F == kWeightGrad ? 2 : 1) * p.tiles_c * slices;
         if (!grid_ok(grid, 2 * S)) return AQ_ESHAPE;
-        if (!allow_lds<H, T, decltype(size), decltype(parts), std::integral_constant<int, F>>((const void*)k, gated_lds(S, F))) return AQ_EHIP;
-        k<<<(unsigned)grid, 2 * S, gated_lds(S, F), st>>>(p, out, act);
+        if (!allow_lds<H, T, decltype(size), decltype(parts), decltype(planes), std::integral_constant<int, F>>((const void*)k, kLds)) return AQ_EHIP;
+        k<<<(unsigned)grid, 2 * S, kLds, st>>>(p, out, act);
         return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
     };
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 3> three{};
     auto sized = [&](auto h, auto t, auto parts) {
-        if (s == 256) return go(h, t, std::integral_constant<int, 256>(), parts);
-        if (s == 128) return go(h, t, std::integral_constant<int, 128>(), parts);
-        return go(h, t, std::integral_constant<int, 64>(), parts);
+        if (s == 256) return go(h, t, std::integral_constant<int, 256>(), parts, one);
+        if (s == 128) return go(h, t, std::integral_constant<int, 128>(), parts, one);
+        return go(h, t, std::integral_constant<int, 64>(), parts, one);
     };
+    auto sized3 = [&](auto parts) {
+        if (s == 128) return go(bf16_t(), float(), std::integral_constant<int, 128>(), parts, three);
+        return go(bf16_t(), float(), std::integral_constant<int, 64>(), parts, three);
+    };
+    if (type == AQ_F32) return part ? sized3(std::true_type()) : sized3(std::false_type());
     if (part) return type == AQ_F16 ? sized(f16_t(), float(), std::true_type()) : sized(bf16_t(), float(), std::true_type());
-    if (type == AQ_F32) return sized(bf16_t(), float(), std::false_type());
     if (type == AQ_F16) return sized(f16_t(), f16_t(), std::false_type());
     return sized(bf16_t(), bf16_t(), std::false_type());
 }

@@ -2,7 +2,7 @@
 test_gpu_recurrence.py) and those that look at the launches (test_memory_routes.py) read the same lists."""
 
 # gated layers, rows, n, k: together every tile of every product, in one slice and in several
-GATED = [(8, 8, 8), (2192, 9, 1716), (72, 1758, 3266), (5724, 917, 110), (28632, 64, 392), (886, 3553, 3172), (410, 381, 4277), (10374, 1404, 139)]
+GATED = [(8, 8, 8), (5, 709, 2173), (2192, 9, 1716), (72, 1758, 3266), (5724, 917, 110), (28632, 64, 392), (886, 3553, 3172), (410, 381, 4277), (10374, 1404, 139)]
 
 # the recurrence: sequences, their mean rows, units, whether they are ragged; then units of a lane, wavefronts forward and backward, and how
 # sequences are taken ("each", "parts", "ordered")
