@@ -169,41 +169,89 @@ __global__ void __launch_bounds__(kThreads) k_gated_slopes(const T* __restrict__
 }
 
 // ---- the slices' sums, in their order
-template <class T, bool GATED>
-__global__ void __launch_bounds__(kThreads) k_gated_join(const float* __restrict__ part, int slices, int64_t stride, int64_t m, int64_t c, Outputs out,
-                                                         int outputs, int act) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    auto total = [slices, stride](const float* p) __attribute__((always_inline)) {
-        float s = 0.0f;
-        int k = 0;
-        for (; k + 4 <= slices; k += 4) {
-            const float a = p[k * stride], b = p[(k + 1) * stride], d = p[(k + 2) * stride], e = p[(k + 3) * stride];
-            s = s + a + b + d + e;
-        }
-        for (; k < slices; ++k) s += p[k * stride];
-        return s;
-    };
-    const int64_t which = i / (m * c), row = (i - which * m * c) / c, col = i - which * m * c - row * c;
-    if (which >= (GATED ? 1 : outputs)) return;
-    if constexpr (GATED) {
-        const float g = total(part + row * out.ld_part + col), u = total(part + out.part_second + row * out.ld_part + col);
-        float slope;
-        ((T*)out.first)[row * out.ld_first + col] = (T)(gate_act(g, act, slope) * u);
-        if (out.second) {
-            ((T*)out.second)[row * out.ld_second + col] = (T)g;
-            ((T*)out.third)[row * out.ld_third + col] = (T)u;
-        }
-    } else {
-        const float s = total(part + which * out.part_second + row * out.ld_part + col);
-        if (which) ((T*)out.second)[row * out.ld_second + col] = (T)s;
-        else ((T*)out.first)[row * out.ld_first + col] = (T)s;
+struct Slices {
+    const float* part;
+    int64_t stride, n;  // values of a slice; results that are joined
+    int32_t slices;
+};
+__device__ __forceinline__ float joined(const float* __restrict__ p, const Slices& of) {
+    float s = 0.0f;
+    int k = 0;
+    for (; k + 4 <= of.slices; k += 4) {
+        const float a = p[k * of.stride], b = p[(k + 1) * of.stride], d = p[(k + 2) * of.stride], e = p[(k + 3) * of.stride];
+        s = s + a + b + d + e;
     }
+    for (; k < of.slices; ++k) s += p[k * of.stride];
+    return s;
+}
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_gated_join(Slices of, int64_t c, Outputs out, int act) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = i / c, col = i - row * c;
+    if (i >= of.n) return;
+    const float* const p = of.part + row * out.ld_part + col;
+    const float g = joined(p, of), u = joined(p + out.part_second, of);
+    float slope;
+    ((T*)out.first)[row * out.ld_first + col] = (T)(gate_act(g, act, slope) * u);
+    if (out.second) {
+        ((T*)out.second)[row * out.ld_second + col] = (T)g;
+        ((T*)out.third)[row * out.ld_third + col] = (T)u;
+    }
+}
+// dx, behind it dwg and dwu (either may have none)
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_gated_join_gradients(Slices dx, int64_t c_dx, Outputs out_dx, Slices dw, int64_t m_dw, int64_t c_dw, Outputs out_dw) {
+    int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i < dx.n) {
+        const int64_t row = i / c_dx;
+        ((T*)out_dx.first)[row * out_dx.ld_first + i - row * c_dx] = (T)joined(dx.part + i, dx);
+        return;
+    }
+    i -= dx.n;
+    if (i >= dw.n) return;
+    const float s = joined(dw.part + i, dw);
+    int64_t row = i / c_dw;
+    const int64_t col = i - row * c_dw;
+    if (row >= m_dw) ((T*)out_dw.second)[(row - m_dw) * out_dw.ld_second + col] = (T)s;
+    else ((T*)out_dw.first)[row * out_dw.ld_first + col] = (T)s;
 }
 
 // ---- plans
+int64_t up256(int64_t n) { return (n + 255) & ~(int64_t)255; }
 struct Plan {
     int s, slices, chunks;  // tile, slices of so many chunks
+    float us;
 };
+struct Kind {
+    int s, at_once;
+    float launch, alone, full, more = 0.0f;  // more: for each turn behind the first
+};
+constexpr Kind kKinds[3][3] = {{{64, 768, 4.0f, 0.43f, 0.68f, 2.0f}, {128, 512, 4.0f, 0.64f, 1.50f, 2.0f}, {256, 256, 6.0f, 1.45f, 2.05f, 4.0f}},
+                               {{64, 768, 3.0f, 0.43f, 0.60f}, {128, 256, 3.2f, 0.60f, 0.63f}, {256, 256, 5.0f, 1.28f, 1.72f}},
+                               {{64, 768, 3.0f, 0.42f, 0.58f}, {128, 256, 3.2f, 0.60f, 0.67f}, {256, 256, 5.0f, 1.30f, 1.70f}}};
+constexpr Kind kKinds3[3][2] = {{{64, 512, 4.0f, 0.68f, 1.05f, 2.0f}, {128, 256, 4.5f, 1.15f, 1.44f, 2.0f}},
+                                {{64, 512, 3.0f, 0.70f, 1.02f}, {128, 256, 3.5f, 1.15f, 1.38f}},
+                                {{64, 512, 3.0f, 0.65f, 1.00f}, {128, 256, 3.5f, 1.15f, 1.35f}}};
+// one product's shape
+struct Shape {
+    Form form;
+    int64_t m, c, t;
+    int planes;
+    int64_t outputs() const { return form == kInputGrad ? 1 : 2; }  // as they are summed
+    int64_t all() const {
+        const int64_t chunk = chunk_of(planes), each = t > 0 ? (t + chunk - 1) / chunk : 1;
+        return each * (form == kInputGrad ? 2 : 1);
+    }
+    int64_t tiles(int s) const {
+        const int64_t wide = form == kForward ? s / 2 : s;
+        return ((m < 1 ? 1 : m) + s - 1) / s * ((c + wide - 1) / wide) * (form == kWeightGrad ? 2 : 1);
+    }
+    int64_t values(int64_t slices) const { return slices > 1 ? slices * m * c * outputs() : 0; }
+    bool fits(int s, int64_t slices) const {
+        return grid_ok(tiles(s) * slices, 2 * s) && (slices == 1 || (grid_ok((m * c * outputs() + kThreads - 1) / kThreads, kThreads) && values(slices) * 4 <= (1LL << 30)));
+    }
+    int64_t bytes(int64_t slices) const { return up256(values(slices) * 4); }
+};
+float join_us(int64_t values) { return values > 0 ? 3.0f + (float)values * 4.0f * (1.0f / 3.5e6f) : 0.0f; }
 // The tile and the slices by an estimate in us: a launch, the chunks of a workgroup one after the other, each as long as `alone` while few
 // workgroups are about and `full` while as many as fit are, and the join's launch and bytes.  Fitted to every tile in one slice, us on
 // tiles of 64 / 128 / 256, bfloat16 (forward, input gradient, both weight gradients):
@@ -212,37 +260,53 @@ struct Plan {
 // (in eight slices the last weight gradient takes 41 / 32 / 55), and fp32 ones on tiles of 64 / 128, chunks of half the length:
 //   4096 x 2048 x 2048  561 / 390,  526 / 355,  511 / 345      300 x 403 x 1111  32 / 60,  25 / 44,  17 / 23
 // (in slices 22 / 21 and 21 / 21 the first two).
-Plan plan_of(Form form, int64_t m, int64_t c, int64_t t, int planes) {
-    struct Kind {
-        int s, at_once;
-        float launch, alone, full, more = 0.0f;  // more: for each turn behind the first
-    };
-    constexpr Kind kinds[3][3] = {{{64, 768, 4.0f, 0.43f, 0.68f, 2.0f}, {128, 512, 4.0f, 0.64f, 1.50f, 2.0f}, {256, 256, 6.0f, 1.45f, 2.05f, 4.0f}},
-                                  {{64, 768, 3.0f, 0.43f, 0.60f}, {128, 256, 3.2f, 0.60f, 0.63f}, {256, 256, 5.0f, 1.28f, 1.72f}},
-                                  {{64, 768, 3.0f, 0.42f, 0.58f}, {128, 256, 3.2f, 0.60f, 0.67f}, {256, 256, 5.0f, 1.30f, 1.70f}}};
-    constexpr Kind kinds3[3][2] = {{{64, 512, 4.0f, 0.68f, 1.05f, 2.0f}, {128, 256, 4.5f, 1.15f, 1.44f, 2.0f}},
-                                   {{64, 512, 3.0f, 0.70f, 1.02f}, {128, 256, 3.5f, 1.15f, 1.38f}},
-                                   {{64, 512, 3.0f, 0.65f, 1.00f}, {128, 256, 3.5f, 1.15f, 1.35f}}};
-    const int64_t chunk = chunk_of(planes), outputs = form == kWeightGrad ? 2 : 1, each = t > 0 ? (t + chunk - 1) / chunk : 1;
-    const int64_t all = each * (form == kInputGrad ? 2 : 1);
-    Plan best{64, 1, (int)all};
-    float least = 3.0e38f;
-    for (int i = 0; i < (planes == 1 ? 3 : 2); ++i) {
-        const Kind& k = planes == 1 ? kinds[form][i] : kinds3[form][i];
-        const int64_t wide = form == kForward ? k.s / 2 : k.s, tiles = ((m < 1 ? 1 : m) + k.s - 1) / k.s * ((c + wide - 1) / wide) * outputs;
+Plan plan_of(const Shape& of) {
+    const int64_t all = of.all();
+    Plan best{64, 1, (int)all, 3.0e38f};
+    for (int i = 0; i < (of.planes == 1 ? 3 : 2); ++i) {
+        const Kind& k = of.planes == 1 ? kKinds[of.form][i] : kKinds3[of.form][i];
         for (int64_t want = 1; want <= 64 && (want == 1 || 2 * want <= all); want *= 2) {
-            const int64_t chunks = (all + want - 1) / want, z = (all + chunks - 1) / chunks, wgs = tiles * z;
-            const int64_t values = z * m * c * (form == kInputGrad ? 1 : 2);
-            if (!grid_ok(wgs, 2 * k.s) || (z > 1 && (!grid_ok((m * c * outputs + kThreads - 1) / kThreads, kThreads) || values * 4 > (1LL << 30)))) continue;
+            const int64_t chunks = (all + want - 1) / want, z = (all + chunks - 1) / chunks, wgs = of.tiles(k.s) * z;
+            if (!of.fits(k.s, z)) continue;
             const int64_t busy = wgs <= 256 ? wgs : (wgs + 255) / 256 * 256;
             const int64_t turns = (busy + k.at_once - 1) / k.at_once;
             const float share = (float)busy / (float)k.at_once;
             const float one = turns > 1 ? k.full * (float)turns : k.alone + (k.full - k.alone) * share * share;
-            const float join = z > 1 ? 3.0f + (float)values * 4.0f * (1.0f / 3.5e6f) : 0.0f;
-            const float us = k.launch + join + (float)chunks * one + (float)(turns - 1) * k.more;
+            const float us = k.launch + join_us(of.values(z)) + (float)chunks * one + (float)(turns - 1) * k.more;
+            if (us < best.us) best = {k.s, (int)z, (int)chunks, us};
+        }
+    }
+    return best;
+}
+// Both gradients: one behind the other, each on its tiles, or in one launch on tiles of one size, in slices that are about as long.
+// Estimated as above, with a fifth of a workgroup's chunks for the end, when the chip empties.  One launch against two, with what is
+// around them, us: 300 x 403 x 1111 fp32 28 / 34, 4096 x 1024 x 256 fp16 35 / 46, 16 x 512 x 512 bf16 9 / 13, 2048 x 1024 x 512 bf16 26 / 43;
+// 2048 x 2048 x 2048 bf16 98 / 101, 16384 x 4096 x 2048 (two: tiles of 256) 1300 and more / 1020.
+struct Pair {
+    Plan dx, dw;
+    bool together;
+};
+Pair pair_of(const Shape& dx, const Shape& dw) {
+    Pair best{plan_of(dx), plan_of(dw), false};
+    float least = best.dx.us + best.dw.us;
+    const int64_t all_dx = dx.all(), all_dw = dw.all(), longest = all_dx > all_dw ? all_dx : all_dw;
+    for (int i = 0; i < 2; ++i) {
+        const Kind& k = dx.planes == 1 ? kKinds[kInputGrad][i] : kKinds3[kInputGrad][i];
+        for (int64_t want = 1; want <= 64 && (want == 1 || 2 * want <= longest); want *= 2) {
+            const int64_t most = (longest + want - 1) / want, z_dx = (all_dx + most - 1) / most, z_dw = (all_dw + most - 1) / most;
+            const int64_t chunks_dx = (all_dx + z_dx - 1) / z_dx, chunks_dw = (all_dw + z_dw - 1) / z_dw;
+            const int64_t slices_dx = (all_dx + chunks_dx - 1) / chunks_dx, slices_dw = (all_dw + chunks_dw - 1) / chunks_dw;
+            const int64_t wgs_dx = dx.tiles(k.s) * slices_dx, wgs_dw = dw.tiles(k.s) * slices_dw;
+            const int64_t results = (slices_dx > 1 ? dx.m * dx.c : 0) + (slices_dw > 1 ? 2 * dw.m * dw.c : 0);
+            if (!dx.fits(k.s, slices_dx) || !dw.fits(k.s, slices_dw) || !grid_ok(wgs_dx + wgs_dw, 2 * k.s) || !grid_ok((results + kThreads - 1) / kThreads, kThreads))
+                continue;
+            const float chunks = (float)(chunks_dx > chunks_dw ? chunks_dx : chunks_dw);
+            const float share = (float)(wgs_dx * chunks_dx + wgs_dw * chunks_dw) / (chunks * (float)k.at_once);
+            const float one = wgs_dx + wgs_dw > k.at_once ? k.full * (share + 0.2f) : k.alone + (k.full - k.alone) * share * share;
+            const float us = k.launch + join_us(dx.values(slices_dx) + dw.values(slices_dw)) + chunks * one;
             if (us < least) {
                 least = us;
-                best = {k.s, (int)z, (int)chunks};
+                best = {{k.s, (int)slices_dx, (int)chunks_dx, us}, {k.s, (int)slices_dw, (int)chunks_dw, us}, true};
             }
         }
     }
@@ -250,12 +314,7 @@ Plan plan_of(Form form, int64_t m, int64_t c, int64_t t, int planes) {
 }
 int planes_of(int32_t dtype) { return dtype == AQ_F32 ? 3 : 1; }
 int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
-int64_t up256(int64_t n) { return (n + 255) & ~(int64_t)255; }
 int64_t laid_bytes(int64_t rows, int64_t cols, int32_t dtype) { return up256(rows * up8(cols) * 2 * planes_of(dtype)); }
-int64_t part_bytes(Form form, int64_t m, int64_t c, int64_t t, int32_t dtype) {
-    const Plan p = plan_of(form, m, c, t, planes_of(dtype));
-    return p.slices > 1 ? up256((int64_t)p.slices * m * c * (form == kInputGrad ? 1 : 2) * 4) : 0;
-}
 constexpr int64_t kFewRows = 4;
 
 bool in_place(const aq_matrix& m) { return m.dtype != AQ_F32 && ((uintptr_t)m.d & 15) == 0 && m.ld % 8 == 0 && m.cols % 8 == 0; }
@@ -305,51 +364,44 @@ struct Layer {
         });
     }
 };
-// a product's sums: planned, run, joined
-aq_status run_product(Form form, int32_t dtype, Operand a, Operand b, int64_t m, int64_t c, int64_t t, Outputs out, int act, uint8_t* ws, hipStream_t st) {
+// a product as planned, its slices' sums from `ws` on
+Product product_of(const Shape& of, const Plan& plan, const Operand& a, const Operand& b, Outputs& out, uint8_t* ws) {
     Product p{};
-    const int chunk = chunk_of(planes_of(dtype));
-    const Plan plan = plan_of(form, m, c, t, planes_of(dtype));
     p.a = a;
     p.b = b;
-    p.m = m, p.c = c, p.t = t;
-    p.each = t > 0 ? (int32_t)((t + chunk - 1) / chunk) : 1;
-    p.all = p.each * (form == kInputGrad ? 2 : 1);
+    p.m = of.m, p.c = of.c, p.t = of.t;
+    p.all = (int32_t)of.all();
+    p.each = of.form == kInputGrad ? p.all / 2 : p.all;
     p.chunks = plan.chunks;
-    p.tiles_m = (int32_t)((m + plan.s - 1) / plan.s);
-    const int features = form == kForward ? plan.s / 2 : plan.s;
-    p.tiles_c = (int32_t)((c + features - 1) / features);
-    const bool part = plan.slices > 1;
-    const int64_t outputs = form == kInputGrad ? 1 : 2;
-    if (part) {
+    p.tiles_m = (int32_t)((of.m + plan.s - 1) / plan.s);
+    const int features = of.form == kForward ? plan.s / 2 : plan.s;
+    p.tiles_c = (int32_t)((of.c + features - 1) / features);
+    if (plan.slices > 1) {
         out.part = (float*)ws;
-        out.ld_part = form == kForward ? 2 * c : c;
-        out.part_second = form == kForward ? c : m * c;
-        out.part_stride = outputs * m * c;
+        out.ld_part = of.form == kForward ? 2 * of.c : of.c;
+        out.part_second = of.form == kForward ? of.c : of.m * of.c;
+        out.part_stride = of.outputs() * of.m * of.c;
     }
-    const aq_status s = form == kForward      ? launch_gated_forward_product(dtype, plan.s, part, p, out, act, plan.slices, st)
-                        : form == kInputGrad ? launch_gated_input_product(dtype, plan.s, part, p, out, plan.slices, st)
-                                             : launch_gated_weight_product(dtype, plan.s, part, p, out, plan.slices, st);
-    if (s != AQ_OK || !part) return s;
-    const int64_t values = m * c * (form == kWeightGrad ? 2 : 1);
-    return with_dtype(dtype, [&](auto type) {
-        using T = decltype(type);
-        const unsigned grid = (unsigned)((values + kThreads - 1) / kThreads);
-        if (form == kForward) k_gated_join<T, true><<<grid, kThreads, 0, st>>>(out.part, plan.slices, out.part_stride, m, c, out, 1, act);
-        else k_gated_join<T, false><<<grid, kThreads, 0, st>>>(out.part, plan.slices, out.part_stride, m, c, out, (int)(values / (m * c)), act);
-        return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
-    });
+    return p;
 }
+Slices slices_of(const Shape& of, const Plan& plan, const Outputs& out) {
+    return {out.part, out.part_stride, plan.slices > 1 ? of.m * of.c * (of.form == kWeightGrad ? 2 : 1) : 0, plan.slices};
+}
+unsigned join_grid(int64_t n) { return (unsigned)((n + kThreads - 1) / kThreads); }
 
 }  // namespace
 
 int64_t gated_forward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype) {
     if (rows <= kFewRows) return 0;
-    return laid_bytes(rows, k, dtype) + 2 * laid_bytes(n, k, dtype) + part_bytes(kForward, rows, n, k, dtype);
+    const Shape of{kForward, rows, n, k, planes_of(dtype)};
+    return laid_bytes(rows, k, dtype) + 2 * laid_bytes(n, k, dtype) + of.bytes(plan_of(of).slices);
 }
 int64_t gated_backward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype) {
-    const int64_t dx = part_bytes(kInputGrad, rows, k, n, dtype), dw = part_bytes(kWeightGrad, n, k, rows, dtype);
-    return laid_bytes(rows, k, dtype) + 2 * laid_bytes(n, k, dtype) + 2 * laid_bytes(rows, n, dtype) + (dx > dw ? dx : dw);
+    const Shape dx{kInputGrad, rows, k, n, planes_of(dtype)}, dw{kWeightGrad, n, k, rows, planes_of(dtype)};
+    const Pair both = pair_of(dx, dw);
+    const int64_t one = dx.bytes(plan_of(dx).slices), other = dw.bytes(plan_of(dw).slices), most = one > other ? one : other;
+    const int64_t pair = both.together ? dx.bytes(both.dx.slices) + dw.bytes(both.dw.slices) : 0;
+    return laid_bytes(rows, k, dtype) + 2 * laid_bytes(n, k, dtype) + 2 * laid_bytes(rows, n, dtype) + (pair > most ? pair : most);
 }
 
 aq_status launch_gated_forward(const aq_matrix& x, const aq_matrix& wg, const aq_matrix& wu, int act, const aq_matrix& y, const aq_matrix* gate,
@@ -373,12 +425,21 @@ aq_status launch_gated_forward(const aq_matrix& x, const aq_matrix& wg, const aq
     lay.dtype = x.dtype;
     const Operand a = lay.operand(x);
     const Operand b = lay.pair(wg, wu);
-    const aq_status s = lay.run(st);
+    aq_status s = lay.run(st);
     if (s != AQ_OK) return s;
     Outputs out{};
     out.first = y.d, out.ld_first = y.ld;
     if (gate) out.second = gate->d, out.ld_second = gate->ld, out.third = up->d, out.ld_third = up->ld;
-    return run_product(kForward, x.dtype, a, b, x.rows, n, k, out, act, lay.ws, st);
+    const Shape of{kForward, x.rows, n, k, planes_of(x.dtype)};
+    const Plan plan = plan_of(of);
+    const Product p = product_of(of, plan, a, b, out, lay.ws);
+    s = launch_gated_forward_product(x.dtype, plan.s, plan.slices > 1, p, out, act, plan.slices, st);
+    if (s != AQ_OK || plan.slices == 1) return s;
+    const Slices sums = slices_of(of, plan, out);
+    return with_dtype(x.dtype, [&](auto t) {
+        k_gated_join<decltype(t)><<<join_grid(sums.n), kThreads, 0, st>>>(sums, n, out, act);
+        return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+    });
 }
 
 aq_status launch_gated_backward(const aq_matrix& dy, const aq_matrix& x, const aq_matrix& wg, const aq_matrix& wu, const aq_matrix& gate,
@@ -410,16 +471,44 @@ aq_status launch_gated_backward(const aq_matrix& dy, const aq_matrix& x, const a
         });
         if (s != AQ_OK) return s;
     }
-    if (dx && m > 0) {
-        Outputs out{};
-        out.first = dx->d, out.ld_first = dx->ld;
-        s = run_product(kInputGrad, x.dtype, d, ow, m, k, n, out, act, lay.ws, st);
-        if (s != AQ_OK) return s;
+    const Shape of_dx{kInputGrad, m, k, n, planes_of(x.dtype)}, of_dw{kWeightGrad, n, k, m, planes_of(x.dtype)};
+    const bool inputs = dx && m > 0, weights = dwg != nullptr;
+    // products without a plan have no workgroups
+    auto run = [&](const Plan* plan_dx, const Plan* plan_dw) {
+        Outputs out_dx{}, out_dw{};
+        Product p_dx{}, p_dw{};
+        Slices sums_dx{}, sums_dw{};
+        uint8_t* at = lay.ws;
+        if (plan_dx) {
+            out_dx.first = dx->d, out_dx.ld_first = dx->ld;
+            p_dx = product_of(of_dx, *plan_dx, d, ow, out_dx, at);
+            sums_dx = slices_of(of_dx, *plan_dx, out_dx);
+            at += of_dx.bytes(plan_dx->slices);
+        }
+        if (plan_dw) {
+            out_dw.first = dwg->d, out_dw.ld_first = dwg->ld, out_dw.second = dwu->d, out_dw.ld_second = dwu->ld;
+            p_dw = product_of(of_dw, *plan_dw, d, ox, out_dw, at);
+            sums_dw = slices_of(of_dw, *plan_dw, out_dw);
+        }
+        const int size = plan_dx ? plan_dx->s : plan_dw->s;
+        const aq_status r = size < 256 ? launch_gated_gradients(x.dtype, size, p_dx, out_dx, plan_dx ? plan_dx->slices : 0, p_dw, out_dw, plan_dw ? plan_dw->slices : 0, st)
+                            : plan_dx  ? launch_gated_input_product(x.dtype, sums_dx.n > 0, p_dx, out_dx, plan_dx->slices, st)
+                                       : launch_gated_weight_product(x.dtype, sums_dw.n > 0, p_dw, out_dw, plan_dw->slices, st);
+        if (r != AQ_OK || sums_dx.n + sums_dw.n == 0) return r;
+        return with_dtype(x.dtype, [&](auto t) {
+            k_gated_join_gradients<decltype(t)><<<join_grid(sums_dx.n + sums_dw.n), kThreads, 0, st>>>(sums_dx, k, out_dx, sums_dw, n, k, out_dw);
+            return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+        });
+    };
+    if (inputs && weights) {
+        const Pair both = pair_of(of_dx, of_dw);
+        if (both.together) return run(&both.dx, &both.dw);
+        s = run(&both.dx, nullptr);
+        return s != AQ_OK ? s : run(nullptr, &both.dw);
     }
-    if (!dwg) return AQ_OK;
-    Outputs out{};
-    out.first = dwg->d, out.ld_first = dwg->ld, out.second = dwu->d, out.ld_second = dwu->ld;
-    return run_product(kWeightGrad, x.dtype, d, ox, n, k, m, out, act, lay.ws, st);
+    if (!inputs && !weights) return AQ_OK;
+    const Plan alone = plan_of(inputs ? of_dx : of_dw);
+    return inputs ? run(&alone, nullptr) : run(nullptr, &alone);
 }
 
 }  // namespace aq

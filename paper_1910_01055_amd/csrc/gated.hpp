@@ -44,9 +44,18 @@ __device__ __forceinline__ float gate_act(float a, int act, float& slope) {
         return a > 0.0f ? a : a != a ? a : 0.0f;
     }
     if (act == AQ_GATE_GELU) {
-        // a Phi(a), Phi(a) = erfc(-a / sqrt 2) / 2: without a difference from 1 for negative a
-        const float p = 0.5f * erfcf(-0.70710678f * a);
-        slope = p + a * __builtin_amdgcn_exp2f(-0.72134752f * a * a) * 0.39894228f;
+        // a Phi(a), Phi(-|a|) = exp(-a^2 / 2) t P(t), t = 1 / (1 + |a| / 4): without a difference from 1 for negative a.  P is fitted in
+        // the least maximum of its relative error, 3.4e-8, over all t.  (16384 x 4096 x 2048
+        // bfloat16 541 us; with erfcf 590.)
+        constexpr float kP[10] = {0.0997355655f, 0.0997364298f, 0.0934663564f, 0.0816031098f, 0.0589751527f,
+                                  0.0636991262f, -0.031717591f, 0.0955972001f, -0.0808774009f, 0.019782036542892456f};
+        const float t = __builtin_amdgcn_rcpf(1.0f + 0.25f * fabsf(a)), density = __builtin_amdgcn_exp2f(-0.72134752f * a * a);
+        float q = kP[9];
+#pragma unroll
+        for (int i = 8; i >= 0; --i) q = fmaf(q, t, kP[i]);
+        q *= t * density;
+        const float p = a < 0.0f ? q : 1.0f - q;
+        slope = p + a * density * 0.39894228f;
         if (fabsf(a) > 3.0e18f) slope = p;  // (a^2 infinite)
         return p == 0.0f ? 0.0f : a * p;
     }
@@ -122,8 +131,9 @@ constexpr int gated_lds(int s, Form f, int planes) { return gated_buffers(s, f, 
 // A chunk's products come in four turns of 16 t, whose operands are read a turn ahead; behind the third all of a chunk is in registers, and
 // the barrier there hands its buffer to the chunk kBufs ahead.  (P = 3: three planes of both operands, whose six pairs are formed of what is
 // read once; a chunk has two turns.)
-template <class H, class T, int S, Form F, bool PART, int P>
-__global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs out, int act) {
+// Workgroup `block` of the product's `blocks`; `part`: a slice's sums instead of the results.
+template <class H, class T, int S, Form F, int P>
+__device__ __forceinline__ void gated_product(const Product& p, const Outputs& out, int act, bool part, uint32_t block, uint32_t blocks) {
     constexpr bool kAcrossA = F != kWeightGrad, kAcrossB = F == kForward;
     constexpr int C = chunk_of(P);
     using TA = Tile<S, kAcrossA, C>;
@@ -134,7 +144,7 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
     static_assert(NT / 64 * 32 * kOutRow<float, 2> <= kBufs * kBuf, "results leave through the buffers");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31;
-    Place at = place_of_workgroup((uint32_t)(F == kWeightGrad ? 2 * p.tiles_m : p.tiles_m), (uint32_t)p.tiles_c);
+    Place at = place_of_workgroup((uint32_t)(F == kWeightGrad ? 2 * p.tiles_m : p.tiles_m), (uint32_t)p.tiles_c, block, blocks);
     const int second = F == kWeightGrad && at.m >= (uint32_t)p.tiles_m;  // which of two outputs
     if (second) at.m -= p.tiles_m;
     const int64_t m0 = (int64_t)at.m * S, c0 = (int64_t)at.c * (F == kForward ? S / 2 : S);
@@ -285,7 +295,7 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
             const int64_t f = c0 + wc / 2, cols = p.c - f;
             auto gate = [&](int i, int q, int e) __attribute__((always_inline)) { return acc[2 * i][j][4 * q + e]; };
             auto up = [&](int i, int q, int e) __attribute__((always_inline)) { return acc[2 * i + 1][j][4 * q + e]; };
-            if constexpr (PART) {
+            if (part) {
                 float* const to = out.part + at.z * out.part_stride + row * out.ld_part + f;
                 store_rows<float, NF>(place, lane, to, out.ld_part, rows, cols, gate);
                 store_rows<float, NF>(place, lane, to + out.part_second, out.ld_part, rows, cols, up);
@@ -301,7 +311,7 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
             }
         } else {
             const int64_t col = c0 + wc, cols = p.c - col;
-            if constexpr (PART) {
+            if (part) {
                 store_rows<float, 2>(place, lane, out.part + at.z * out.part_stride + second * out.part_second + row * out.ld_part + col, out.ld_part, rows, cols,
                                      [&](int i, int q, int e) { return acc[i][j][4 * q + e]; });
             } else {
@@ -313,40 +323,48 @@ __global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs o
     }
 }
 
-// one product as planned; `type`: of its matrices (AQ_F32: three planes of bf16)
-aq_status launch_gated_forward_product(int type, int s, bool part, const Product& p, const Outputs& out, int act, int slices, hipStream_t st);
-aq_status launch_gated_input_product(int type, int s, bool part, const Product& p, const Outputs& out, int slices, hipStream_t st);
-aq_status launch_gated_weight_product(int type, int s, bool part, const Product& p, const Outputs& out, int slices, hipStream_t st);
+template <class H, class T, int S, Form F, bool PART, int P>
+__global__ void __launch_bounds__(2 * S, 1) k_gated_product(Product p, Outputs out, int act) {
+    gated_product<H, T, S, F, P>(p, out, act, PART, blockIdx.x, gridDim.x);
+}
+// Both gradients' products beside each other, the one with the longer sums first (either may have no workgroups): one launch, and one
+// product's workgroups fill what the other one's leave.
+template <class H, class T, int S, int P>
+__global__ void __launch_bounds__(2 * S, 1) k_gated_gradients(Product dx, Outputs out_dx, Product dw, Outputs out_dw, uint32_t split, bool weights_first) {
+    const uint32_t rest = gridDim.x - split;
+    const bool ahead = blockIdx.x < split;
+    const uint32_t block = ahead ? blockIdx.x : blockIdx.x - split, blocks = ahead ? split : rest;
+    if (ahead == weights_first) gated_product<H, T, S, kWeightGrad, P>(dw, out_dw, 0, out_dw.part != nullptr, block, blocks);
+    else gated_product<H, T, S, kInputGrad, P>(dx, out_dx, 0, out_dx.part != nullptr, block, blocks);
+}
 
+// one product as planned; `type`: of its matrices (AQ_F32: three planes of bf16).  Gradients on tiles of 256 have a launch each.
+aq_status launch_gated_forward_product(int type, int s, bool part, const Product& p, const Outputs& out, int act, int slices, hipStream_t st);
+aq_status launch_gated_input_product(int type, bool part, const Product& p, const Outputs& out, int slices, hipStream_t st);
+aq_status launch_gated_weight_product(int type, bool part, const Product& p, const Outputs& out, int slices, hipStream_t st);
+// slices of 0: without this one
+aq_status launch_gated_gradients(int type, int s, const Product& dx, const Outputs& out_dx, int slices_dx, const Product& dw, const Outputs& out_dw, int slices_dw,
+                                 hipStream_t st);
+
+template <class H, class T, int S, Form F, bool PART, int P>
+aq_status launch_gated_product(const Product& p, const Outputs& out, int act, int slices, hipStream_t st) {
+    constexpr int kLds = gated_lds(S, F, P);
+    static_assert(kLds <= kMostLds, "");
+    auto* const k = k_gated_product<H, T, S, F, PART, P>;
+    const int64_t grid = (int64_t)p.tiles_m * (F == kWeightGrad ? 2 : 1) * p.tiles_c * slices;
+    if (!grid_ok(grid, 2 * S)) return AQ_ESHAPE;
+    if (!allow_lds<H, T, std::integral_constant<int, S>, std::integral_constant<bool, PART>, std::integral_constant<int, P>, std::integral_constant<int, F>>((const void*)k, kLds))
+        return AQ_EHIP;
+    k<<<(unsigned)grid, 2 * S, kLds, st>>>(p, out, act);
+    return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
+}
 template <Form F>
-aq_status launch_gated_product(int type, int s, bool part, const Product& p, const Outputs& out, int act, int slices, hipStream_t st) {
-    auto go = [&](auto h, auto t, auto size, auto parts, auto planes) {
-        using H = decltype(h);
-        using T = decltype(t);
-        constexpr int S = decltype(size)::value, P = decltype(planes)::value, kLds = gated_lds(S, F, P);
-        static_assert(kLds <= kMostLds, "");
-        auto* const k = k_gated_product<H, T, S, F, decltype(parts)::value, P>;
-        const int64_t grid = (int64_t)p.tiles_m * (F == kWeightGrad ? 2 : 1) * p.tiles_c * slices;
-        if (!grid_ok(grid, 2 * S)) return AQ_ESHAPE;
-        if (!allow_lds<H, T, decltype(size), decltype(parts), decltype(planes), std::integral_constant<int, F>>((const void*)k, kLds)) return AQ_EHIP;
-        k<<<(unsigned)grid, 2 * S, kLds, st>>>(p, out, act);
-        return hip_failed(hipGetLastError()) ? AQ_EHIP : AQ_OK;
-    };
-    constexpr std::integral_constant<int, 1> one{};
-    constexpr std::integral_constant<int, 3> three{};
-    auto sized = [&](auto h, auto t, auto parts) {
-        if (s == 256) return go(h, t, std::integral_constant<int, 256>(), parts, one);
-        if (s == 128) return go(h, t, std::integral_constant<int, 128>(), parts, one);
-        return go(h, t, std::integral_constant<int, 64>(), parts, one);
-    };
-    auto sized3 = [&](auto parts) {
-        if (s == 128) return go(bf16_t(), float(), std::integral_constant<int, 128>(), parts, three);
-        return go(bf16_t(), float(), std::integral_constant<int, 64>(), parts, three);
-    };
-    if (type == AQ_F32) return part ? sized3(std::true_type()) : sized3(std::false_type());
-    if (part) return type == AQ_F16 ? sized(f16_t(), float(), std::true_type()) : sized(bf16_t(), float(), std::true_type());
-    if (type == AQ_F16) return sized(f16_t(), f16_t(), std::false_type());
-    return sized(bf16_t(), bf16_t(), std::false_type());
+aq_status launch_gated_large(int type, bool part, const Product& p, const Outputs& out, int act, int slices, hipStream_t st) {
+    if (part)
+        return type == AQ_F16 ? launch_gated_product<f16_t, float, 256, F, true, 1>(p, out, act, slices, st)
+                              : launch_gated_product<bf16_t, float, 256, F, true, 1>(p, out, act, slices, st);
+    return type == AQ_F16 ? launch_gated_product<f16_t, f16_t, 256, F, false, 1>(p, out, act, slices, st)
+                          : launch_gated_product<bf16_t, bf16_t, 256, F, false, 1>(p, out, act, slices, st);
 }
 
 }  // namespace aq

@@ -1,10 +1,10 @@
-// The gated layer's products: the gradients of its weights.
+// The gated layer's products: the gradients of its weights, on tiles of 256.
 #include "gated.hpp"
 
 namespace aq {
 
-aq_status launch_gated_weight_product(int type, int s, bool part, const Product& p, const Outputs& out, int slices, hipStream_t st) {
-    return launch_gated_product<kWeightGrad>(type, s, part, p, out, 0, slices, st);
+aq_status launch_gated_weight_product(int type, bool part, const Product& p, const Outputs& out, int slices, hipStream_t st) {
+    return launch_gated_large<kWeightGrad>(type, part, p, out, 0, slices, st);
 }
 
 }  // namespace aq

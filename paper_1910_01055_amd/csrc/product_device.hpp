@@ -43,13 +43,14 @@ __device__ __forceinline__ void wait_loads() {
 struct Place {
     uint32_t m, c, z;
 };
-__device__ __forceinline__ Place place_of_workgroup(uint32_t gm, uint32_t gc) {
-    const uint32_t all = gridDim.x, xcd = blockIdx.x % 8, each = all / 8, more = all % 8;
-    const uint32_t p = xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8;
+__device__ __forceinline__ Place place_of_workgroup(uint32_t gm, uint32_t gc, uint32_t at, uint32_t all) {
+    const uint32_t xcd = at % 8, each = all / 8, more = all % 8;
+    const uint32_t p = xcd * each + (xcd < more ? xcd : more) + at / 8;
     const uint32_t z = p / (gm * gc), tile = p % (gm * gc), strip = tile / (4 * gc), in = tile % (4 * gc);
     const uint32_t high = gm - 4 * strip < 4 ? gm - 4 * strip : 4;
     return {4 * strip + in % high, in / high, z};
 }
+__device__ __forceinline__ Place place_of_workgroup(uint32_t gm, uint32_t gc) { return place_of_workgroup(gm, gc, blockIdx.x, gridDim.x); }
 
 // 32 rows and 32 C columns of sums in the layout of a 32x32 MFMA (lane l: row l mod 32 here, columns 32 i + 8 q + 4 (l / 32) + e),
 // rounded and stored as whole lines through 32 kOutRow<T, C> bytes of LDS of the wavefront's own.  get(i, q, e): the sums.  Of the

@@ -1,8 +1,9 @@
 """Sizes at which gated layers and the recurrence are tested, and what they are to reach there: the tests that run them (test_gpu_gated.py,
 test_gpu_recurrence.py) and those that look at the launches (test_memory_routes.py) read the same lists."""
 
-# gated layers, rows, n, k: together every tile of every product, in one slice and in several
-GATED = [(8, 8, 8), (5, 709, 2173), (2192, 9, 1716), (72, 1758, 3266), (5724, 917, 110), (28632, 64, 392), (886, 3553, 3172), (410, 381, 4277), (10374, 1404, 139)]
+# gated layers, rows, n, k: together every tile of every product, in one slice and in several, and both gradients in one launch
+GATED = [(8, 8, 8), (5, 8, 11), (5, 396, 799), (5, 709, 2173), (325, 4099, 8), (29024, 206, 10), (70, 1733, 3042), (13474, 76, 70), (3125, 481, 75), (546, 225, 2950),
+         (12422, 10, 2492), (442, 3504, 4404), (5579, 392, 2527)]
 
 # the recurrence: sequences, their mean rows, units, whether they are ragged; then units of a lane, wavefronts forward and backward, and how
 # sequences are taken ("each", "parts", "ordered")

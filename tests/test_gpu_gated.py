@@ -67,7 +67,6 @@ def run(rows, n, k, kind, act, gap=0, at=0, keep=True, seed=0):
     within(G.get(), gate, gt, kind, "gate")
     within(UP.get(), up, ut, kind, "up")
     ws = workspace(B.gated_backward_workspace(rows, n, k, t))
-    B.gated_backward(DY.m, X.m, WG.m, WU.m, G.m, UP.m, act, DX.m, DWG.m, DWU.m, ws)
     gate, up = G.m.double(), UP.m.double()
     h, slope = act_of(gate, act)
     dg, du = dy * up * slope, dy * h
@@ -75,9 +74,17 @@ def run(rows, n, k, kind, act, gap=0, at=0, keep=True, seed=0):
     dgt = (dy * up).abs() * (act_error(gate, act) * (1 + gate.abs()) + 4 * U) + half * dg.abs() + TINY[kind]
     dut = du.abs() * (act_error(gate, act) + 2 * U + half) + TINY[kind]
     sums = dg.abs() @ wg.abs() + du.abs() @ wu.abs()
-    within(DX.get(), dg @ wg + du @ wu, dgt @ wg.abs() + dut @ wu.abs() + (2 * terms * n + 4) * U * sums, kind, "dx")
-    for name, M, d, dt in (("dwg", DWG, dg, dgt), ("dwu", DWU, du, dut)):
-        within(M.get(), d.t() @ x, dt.t() @ x.abs() + (terms * rows + 4) * U * (d.abs().t() @ x.abs()), kind, name)
+    dx, dxt = dg @ wg + du @ wu, dgt @ wg.abs() + dut @ wu.abs() + (2 * terms * n + 4) * U * sums
+    dws = [(d.t() @ x, dt.t() @ x.abs() + (terms * rows + 4) * U * (d.abs().t() @ x.abs())) for d, dt in ((dg, dgt), (du, dut))]
+    for asked in ("all", "dx", "dw"):  # (both gradients in one launch, each by itself)
+        for f in (DX, DWG, DWU):
+            f.m.fill_(SENTINEL)
+        B.gated_backward(DY.m, X.m, WG.m, WU.m, G.m, UP.m, act, DX.m if asked != "dw" else None, *((DWG.m, DWU.m) if asked != "dx" else (None, None)), ws)
+        if asked != "dw":
+            within(DX.get(), dx, dxt, kind, "dx of " + asked)
+        if asked != "dx":
+            within(DWG.get(), *dws[0], kind, "dwg of " + asked)
+            within(DWU.get(), *dws[1], kind, "dwu of " + asked)
 
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])

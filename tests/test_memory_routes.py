@@ -40,22 +40,42 @@ class Memory(Learner):
 
 
 PRODUCT = re.compile(rb"k_gated_productI.*?Li(\d+)ELNS_4FormE(\d)ELb(\d)E")
+GRADIENTS = re.compile(rb"k_gated_gradientsI.*?Li(\d+)ELi\dE")
+
+
+def reached_by(kind, sizes, launches):
+    """The products of a call's launches: type, tile, form (0 forward, 1 input, 2 weights, 3 both gradients in one launch), then what is joined:
+    0 nothing, 1 the product (the input's gradient), 2 the weights' gradients, 3 all."""
+    rows, n, k = sizes
+    _, names, grids = launches
+    for i, name in enumerate(names):
+        follows = names[i + 1] if i + 1 < len(names) else b""
+        found, pair = PRODUCT.search(name), GRADIENTS.search(name)
+        if found:
+            assert (b"k_gated_join" in follows) == (found[3] == b"1"), names
+            yield (kind, *map(int, found.groups()))
+        elif pair:
+            size, blocks = int(pair[1]), lambda v: -(-v // 256)
+            joins = {0: 0, blocks(rows * k): 1, blocks(2 * n * k): 2, blocks(rows * k + 2 * n * k): 3}
+            alone = [b"k_gated_gradients" in m or b"k_gated_productI" in m for m in names].count(True) > 1
+            form = 3 if not alone else 1 if b"slopes" in names[i - 1] else 2
+            joined = joins[grids[i + 1]] if b"k_gated_join" in follows else 0
+            yield (kind, size, form, joined)
 
 
 def gated_products(h):
-    """The sizes of the tests reach every tile of every product, in one slice and in several, for every type; few rows have a kernel of
-    their own, and rows that are no whole pieces are laid out first."""
+    """The sizes of the tests reach every tile of every product, in one slice and in several, for every type, alone and with both gradients
+    in one launch; few rows have a kernel of their own, and rows that are no whole pieces are laid out first."""
     reached = set()
     for sizes in shapes.GATED:
         for kind in TYPES:
-            for status, names, _ in h.gated(*sizes, kind):
-                assert status == h.aq.OK
-                for name in names:
-                    found = PRODUCT.search(name)
-                    if found:
-                        reached.add((kind, *map(int, found.groups())))
-                        assert (b"k_gated_join" in names[names.index(name) + 1] if found[3] == b"1" else True)
-    assert reached == {(k, s, f, p) for k in TYPES for s in ((64, 128) if k == "f32" else (64, 128, 256)) for f in (0, 1, 2) for p in (0, 1)}
+            for launches in h.gated(*sizes, kind):
+                assert launches[0] == h.aq.OK
+                reached |= set(reached_by(kind, sizes, launches))
+    wanted = {(k, s, 0, p) for k in TYPES for s in ((64, 128) if k == "f32" else (64, 128, 256)) for p in (0, 1)}
+    wanted |= {(k, 256, f, p) for k in ("f16", "bf16") for f in (1, 2) for p in (0, 1)}
+    wanted |= {(k, s, 3, p) for k in TYPES for s in (64, 128) for p in (0, 1, 2, 3)}
+    assert wanted <= reached, sorted(wanted - reached)
     for kind in TYPES:
         for rows in (1, 2, 3, 4):
             _, names, _ = h.gated(rows, 40, 77, kind)[0]
@@ -71,7 +91,7 @@ def gated_sizes(h):
     for rows, n, k in (((1 << 31) - (1 << 20), 1, 4), (1 << 27, 64, 8), (5, 1 << 20, 1), (1, 1 << 20, 8192), (0, 5, 7), (100, 8192, 1 << 20)):
         for kind in TYPES:
             for status, names, _ in h.gated(rows, n, k, kind):
-                assert status == h.aq.OK and bool(names) == (rows > 0 or b"k_gated_product" in b"".join(names)), (rows, n, k, kind, status)
+                assert status == h.aq.OK and bool(names) == (rows > 0 or b"k_gated_gradients" in b"".join(names)), (rows, n, k, kind, status)
     size = C.c_uint64()
     for rows, n, k in ((1 << 27, 65, 8), (1 << 27, 8, 65), (8, 1 << 20, 8193)):
         assert h.lib.aq_gated_forward_workspace(rows, n, k, 2, C.byref(size)) == h.aq.ESHAPE
