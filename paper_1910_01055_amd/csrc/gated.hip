@@ -281,7 +281,7 @@ Plan plan_of(const Shape& of) {
 // Both gradients: one behind the other, each on its tiles, or in one launch on tiles of one size, in slices that are about as long.
 // Estimated as above, with a fifth of a workgroup's chunks for the end, when the chip empties.  One launch against two, with what is
 // around them, us: 300 x 403 x 1111 fp32 28 / 34, 4096 x 1024 x 256 fp16 35 / 46, 16 x 512 x 512 bf16 9 / 13, 2048 x 1024 x 512 bf16 26 / 43;
-// 2048 x 2048 x 2048 bf16 98 / 101, 16384 x 4096 x 2048 (two: tiles of 256) 1300 and more / 1020.
+// 2048 x 2048 x 2048 bf16 98 / 101, 16384 x 4096 x 2048 bf16 1490 / 1080 (two: tiles of 256).
 struct Pair {
     Plan dx, dw;
     bool together;
