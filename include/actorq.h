@@ -487,7 +487,8 @@ aq_status aq_mx4_input_grad(const aq_matrix* dy, const aq_mx4* w, const aq_matri
  * All matrices of a call have one type.  The products' sums are fp32; those of fp32 matrices are formed of three bfloat16 parts of
  * each value (all but 2^-24 of a product), and what depends on a value of theirs that is not finite is not finite, NaN or infinity.
  * `gate` and `up` may be NULL, both or neither: they receive what the backward pass reads.  dgate and dup are rounded to the
- * matrices' type in front of its products.  dx may be NULL; dwg and dwu may be NULL, both or neither. */
+ * matrices' type in front of its products.  dx may be NULL; dwg and dwu may be NULL, both or neither (which of them are asked for may
+ * change the order of their sums). */
 typedef enum { AQ_GATE_SIGMOID = 0, AQ_GATE_SILU = 1, AQ_GATE_GELU = 2, AQ_GATE_RELU = 3 } aq_gate; /* silu: a sigmoid(a); gelu: a times the normal distribution's function of a */
 #define AQ_GATED_MAX_VALUES (1LL << 33) /* rows * n, rows * k and n * k */
 aq_status aq_gated_forward_workspace(int64_t rows, int64_t n, int64_t k, int32_t dtype, uint64_t* bytes);

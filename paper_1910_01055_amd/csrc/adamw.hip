@@ -194,6 +194,9 @@ __device__ __forceinline__ double power(double b, int64_t t) {
     return p;
 }
 
+// Every tensor once, all of a thread's loads on their way before it computes.  Memory: 100 M weights with bfloat16 gradients and a bfloat16
+// copy 519 us (5.4 TB/s), 8.6 M with moments in 8 bits 31 (4.5 TB/s), the 0.2 M of a control policy 5.7 (the launch, the search for the
+// tensor and one trip to memory).
 __global__ void __launch_bounds__(kThreads) k_adamw(Tensors<kTensors> all, Step s) {
     float scale = 1.0f;
     if (s.d_norm) {
@@ -247,7 +250,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(Tensors<kTensors> all, Step 
     store_moments(t, at, left, m, v, r, (uint32_t)s.step * kTurn, false);
 }
 
-// moments from one form into another
+// moments from one form into another: memory, 8.6 M weights from 8 bits to 32 in 18.6 us (4.6 TB/s)
 __global__ void __launch_bounds__(kThreads) k_moments(Tensors<kTensors / 2> from, Tensors<kTensors / 2> to) {
     const int i = tensor_of(from, blockIdx.x);
     const int64_t at = (int64_t)(blockIdx.x - from.first[i]) * kValues + 8 * (int)threadIdx.x;
@@ -261,7 +264,8 @@ __global__ void __launch_bounds__(kThreads) k_moments(Tensors<kTensors / 2> from
     store_moments(to.t[i], at, left, m, v, r, 0, true);
 }
 
-// ---- the norm: each workgroup's sum of squares, in 64 bits, then one workgroup that adds them in their order
+// ---- the norm: each workgroup's sum of squares, in 64 bits, then one workgroup that adds them in their order: two launches, 9.5 + 3 us for
+// 8.6 M bfloat16 gradients (17 MB, 3.5 us at a copy's rate), 3.8 + 2.1 for 0.2 M.  (Four chunks of a thread on their way at a time: the same.)
 __device__ __forceinline__ double sum_of_workgroup(double s, double* shared) {
 #pragma unroll
     for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);

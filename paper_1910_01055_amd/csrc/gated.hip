@@ -15,7 +15,8 @@ namespace {
 constexpr int kThreads = 256;
 
 // ---- layers of few rows: bound by the weights' way from memory
-// A workgroup takes FEATURES features, each of its four wavefronts a quarter of k: 512 k at a time, eight to a lane.
+// A workgroup takes kFeatures features, each of its four wavefronts a quarter of k: 512 k at a time, eight to a lane.  (1 x 2048 x 2048
+// bfloat16, 16.8 MB of weights: 4.8 us, 3.5 TB/s.  For more rows matrix instructions read the weights once for all of them.)
 constexpr int kFeatures = 2;
 template <class T, int M>
 __global__ void __launch_bounds__(kThreads) k_gated_rows(const T* __restrict__ x, int64_t ldx, const T* __restrict__ wg, int64_t ldg,
@@ -111,7 +112,7 @@ struct Lay {
 struct Lays {
     Lay job[3];
 };
-// rows of whole pieces, zeros behind their ends: piece i of all
+// rows of whole pieces, zeros behind their ends: piece i of all (a launch in front of the forward pass: 300 x 1111 and twice 403 x 1111 fp32 4 us)
 template <class T>
 __device__ __forceinline__ void lay_out(const Lays& all, int64_t i) {
     Lay job = all.job[0];  // (picked without an index, which would send the jobs through scratch memory)
@@ -135,7 +136,9 @@ __global__ void __launch_bounds__(kThreads) k_lay_out(Lays all) {
     lay_out<T>(all, (int64_t)blockIdx.x * kThreads + threadIdx.x);
 }
 
-// dgate and dup, [rows][pitch], zeros behind their ends; in front of them `laid` pieces that are laid out
+// dgate and dup, [rows][pitch], zeros behind their ends; in front of them `laid` pieces that are laid out.  Memory: 16384 x 4096 bfloat16 121 us
+// (5.5 TB/s), 4096 x 1024 fp16 8.  (Formed in both products instead they would be read from three matrices in place of one, each tile's
+// row of them as often as there are tiles across, and their activations formed as often.)
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_gated_slopes(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ gate, int64_t ldgate,
                                                            const T* __restrict__ up, int64_t ldup, int act, Half<T>* __restrict__ dgate,
@@ -168,7 +171,7 @@ __global__ void __launch_bounds__(kThreads) k_gated_slopes(const T* __restrict__
     put_planes<T>(u, dup + row * pitch + at, plane);
 }
 
-// ---- the slices' sums, in their order
+// ---- the slices' sums, in their order: they come from behind the L2s, and the launch is most of it (2 MB in 4 us, 20 in 6)
 struct Slices {
     const float* part;
     int64_t stride, n;  // values of a slice; results that are joined

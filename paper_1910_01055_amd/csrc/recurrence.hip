@@ -9,6 +9,8 @@
 // at a time in registers; W wavefronts take R rows each, exchange (A, B) through LDS and go over their rows once more, from the state that
 // theirs begin with, without another read.  Where sequences and units are too few to fill the chip, every sequence is cut into as
 // many parts as it takes, in proportion to its length, and a launch in front of this one leaves the parts' (A, B).
+// Measured, bfloat16, forward and backward: 128 sequences of 512 x 1024 89 and 168 us (4.5 and 4.8 TB/s); of unequal lengths 107 and 196,
+// whose longest end last; 2 x 65536 x 256 in parts 83 and 126; 64 x 80 x 256 fp32 7.4 and 9.7, a launch and two trips to memory.
 // The state and (A, B) are fp32; a start that cuts a run is kept as A = -1, which no product gives: a NaN in front of it ends there.
 #include <initializer_list>
 
@@ -624,7 +626,7 @@ __global__ void __launch_bounds__(kMostOrdered) k_recurrence_order(const int32_t
     order[before] = i;
 }
 
-// One step of `rows` memories: eight units to a thread.
+// One step of `rows` memories: eight units to a thread.  (16 x 256 fp32 2.5 us, the launch and one trip to memory.)
 template <class T>
 __global__ void __launch_bounds__(256) k_recurrence_step(const T* __restrict__ z, int64_t ldz, const T* __restrict__ v, int64_t ldv,
                                                          const uint8_t* __restrict__ starts, float* __restrict__ state, T* __restrict__ y, int64_t ldy,
