@@ -21,8 +21,8 @@ namespace aq {
 namespace {
 
 constexpr int64_t kManyGroups = 512;  // of 64 lanes: as many have pairs of units
-constexpr int kRows = 16;             // of a run, over a lane's units (backward: 8, see there)
-constexpr int kRowsBackward = 8;
+constexpr int kRows = 16;             // of a run, over a lane's units
+constexpr int kRowsBackward = 8;      // (of which it keeps four values each, and has the next run's four on their way)
 
 template <class T, int V>
 struct Units;  // V neighbouring values, as they lie in memory
