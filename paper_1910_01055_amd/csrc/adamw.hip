@@ -36,7 +36,7 @@ struct Tensors {
 static_assert(sizeof(Tensors<kTensors>) <= 3600, "kernel arguments");
 
 struct Step {
-    float b1, c1, b2, c2, lr, rate, decay, root, eps, max_norm;  // rate = lr / (1 - b1^t), decay = 1 - lr wd, root = 1 / sqrt(1 - b2^t)
+    float b1, c1, b2, c2, rate, decay, root, eps, max_norm;  // rate = lr / (1 - b1^t), decay = 1 - lr wd, root = 1 / sqrt(1 - b2^t)
     double beta1, beta2, weight_decay, host_lr;
     int64_t step;
     const float *d_lr, *d_norm;

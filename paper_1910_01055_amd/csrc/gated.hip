@@ -341,7 +341,6 @@ struct Layer {
             o.plane = m.rows * pitch * 2;
             ws += laid_bytes(m.rows, m.cols, m.dtype);
         }
-        o.bytes = m.rows > 0 ? (m.rows - 1) * o.ld + up8(m.cols) * 2 : 0;
         return o;
     }
     Operand operand(const aq_matrix& m) { return operand(m, in_place(m)); }
@@ -460,7 +459,6 @@ aq_status launch_gated_backward(const aq_matrix& dy, const aq_matrix& x, const a
     d.ld = (int32_t)(pitch * 2);
     d.plane = m * pitch * 2;
     d.other = laid_bytes(m, n, x.dtype);
-    d.bytes = m * pitch * 2;
     lay.ws += 2 * d.other;
     if (m > 0) {
         const int64_t laid = lay.pieces_of_all(), pieces = laid + m * (pitch / 8);

@@ -17,7 +17,6 @@ constexpr int chunk_of(int planes) { return planes == 1 ? 64 : 32; }  // t at a 
 struct Operand {
     const uint8_t* base;
     int64_t plane, other;  // bytes from a plane to the next one, and from the first of two matrices to the second
-    int64_t bytes;         // of a plane, from its first value to its last
     int32_t ld;            // bytes of a row
 };
 struct Product {
