@@ -667,7 +667,9 @@ __global__ void __launch_bounds__(256) k_recurrence_step(const T* __restrict__ z
 // other (2 x 65536 x 256 bfloat16 forward: 82 us; in one part 900) and lose on a chip that is full without them (128 x 512 x 1024: 87 us, in
 // halves 130; ragged 139 and 161).
 // Units: pairs take fewer instructions a value, single units half the time of one workgroup: 37 x 203 x 512 binary16, ragged, 32 us
-// with pairs, 27 without; 128 x 512 x 1024 bfloat16 87 and 91, ragged 162 and 139.
+// with pairs, 27 without; 128 x 512 x 1024 bfloat16 87 and 91.  Where lengths differ and groups are few the longest sequences' time counts
+// (forward and backward: 256 x 512 x 1024 bfloat16 241 and 432 with pairs, 206 and 362 without), and less so where the mean is short
+// (300 x 100 x 1024 61 and 105, 79 and 111).
 struct Plan {
     int units, shift;
     int64_t across;
@@ -680,10 +682,9 @@ Plan plan_of(int64_t rows, int64_t count, int64_t cols, bool ragged, bool forwar
     while ((rows * pairs >> shift) > 64 * kManyGroups * 2) ++shift;
     if (full || mean < 64 || rows >> shift < 2) shift = 0;  // (sequences of several times as many rows still take less than another launch)
     const int64_t groups = (((shift ? rows >> shift : 0) + count) * pairs + 63) / 64;
-    const int units = cols > 1 && groups >= kManyGroups * (ragged ? 8 : 1) ? 2 : 1;
+    const int units = cols > 1 && groups >= kManyGroups * (!ragged ? 1 : mean < 128 ? 4 : 8) ? 2 : 1;
     return {units, shift, units > 1 ? pairs : cols, full && mean >= 64 && count > 1 && count <= kMostOrdered};
 }
-int waves_of(int64_t steps, int rows) { return steps <= rows ? 1 : steps <= 2 * rows ? 2 : steps <= 4 * rows ? 4 : 8; }
 template <int N>
 using Int = std::integral_constant<int, N>;
 // calls go(units of a lane, wavefronts of a workgroup)
@@ -718,6 +719,14 @@ aq_status order_of(const Plan& plan, Rows& rows, float* ws, hipStream_t st) {
 // whether sequences are in parts
 bool in_parts(const Rows& r) { return r.parts > 1 || r.rounds; }
 int64_t steps_of(const Rows& r) { return in_parts(r) && r.each > 1 << r.shift ? 1 << r.shift : r.each; }
+// Wavefronts of a workgroup: as many as the mean length gives rows, up to eight; half of them where many groups of unequal lengths wait
+// for their turn, and wavefronts that find no rows keep others away (ragged, 900 x 80 x 1024 bfloat16 135 and 229 us, without 153 and 272;
+// 2000 x 200 x 512 binary16 287 and 553, without 297 and 717; one in place of two loses: 3000 x 10 x 512 fp32 43 and 80 with two, 45 and 86).
+int waves_of(const Rows& r, const Plan& plan, int rows) {
+    const int64_t steps = steps_of(r);
+    const int waves = steps <= rows ? 1 : steps <= 2 * rows ? 2 : steps <= 4 * rows ? 4 : 8;
+    return r.offsets && plan.units > 1 && waves >= 4 ? waves / 2 : waves;
+}
 int64_t grid_of(const Rows& r) { return ((int64_t)r.slots * r.across + 63) / 64; }
 
 }  // namespace
@@ -737,7 +746,7 @@ aq_status launch_recurrence_forward(const aq_matrix& z, const aq_matrix& v, cons
     if (const aq_status s = order_of(plan, rows, ws, st); s != AQ_OK) return s;
     return with_dtype(z.dtype, [&](auto t) {
         using T = decltype(t);
-        return with_form(plan.units, waves_of(steps_of(rows), kRows / plan.units), [&](auto units, auto waves) {
+        return with_form(plan.units, waves_of(rows, plan, kRows / plan.units), [&](auto units, auto waves) {
             constexpr int V = decltype(units)::value, R = kRows / V, W = decltype(waves)::value;
             auto run = [&](auto kernel) {
                 kernel<<<(unsigned)grid_of(rows), 64 * W, 0, st>>>((const T*)z.d, z.ld, (const T*)v.d, v.ld, (T*)y.d, y.ld, starts, first, last, rows,
@@ -764,7 +773,7 @@ aq_status launch_recurrence_backward(const aq_matrix& dy, const float* dlast, co
     if (const aq_status s = order_of(plan, rows, ws, st); s != AQ_OK) return s;
     return with_dtype(z.dtype, [&](auto t) {
         using T = decltype(t);
-        return with_form(plan.units, waves_of(steps_of(rows), kRowsBackward), [&](auto units, auto waves) {
+        return with_form(plan.units, waves_of(rows, plan, kRowsBackward), [&](auto units, auto waves) {
             constexpr int V = decltype(units)::value, R = kRowsBackward, W = decltype(waves)::value;
             auto run = [&](auto kernel) {
                 kernel<<<(unsigned)grid_of(rows), 64 * W, 0, st>>>((const T*)dy.d, dy.ld, (const T*)z.d, z.ld, (const T*)v.d, v.ld, (const T*)y.d, y.ld, starts, first,

@@ -13,5 +13,6 @@ RECURRENCE = [
     ((5, 300, 35, True), 1, 4, 8, "parts"), ((1, 2100, 66, True), 1, 4, 8, "parts"),
     ((64, 1, 1024, False), 2, 1, 1, "each"), ((64, 9, 1025, False), 2, 2, 2, "each"), ((64, 30, 1024, False), 2, 4, 4, "each"),
     ((64, 70, 1026, False), 2, 8, 8, "each"), ((64, 66, 1023, True), 1, 8, 8, "ordered"), ((600, 5, 1000, True), 2, 1, 1, "each"),
-    ((8, 1500, 1024, False), 2, 8, 8, "parts"), ((520, 64, 1024, True), 2, 8, 8, "ordered"),
+    ((8, 1500, 1024, False), 2, 8, 8, "parts"), ((520, 64, 1024, True), 2, 4, 4, "ordered"),
+    ((600, 30, 1000, True), 2, 2, 2, "each"), ((260, 100, 1024, True), 2, 4, 4, "ordered"), ((260, 128, 1024, True), 1, 8, 8, "ordered"),
 ]
